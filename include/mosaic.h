@@ -429,6 +429,125 @@ int mosaic_gram_accumulate(const void *X, int64_t tokens, int64_t cols, int64_t 
                            int64_t ldg, int flags, int *status_dev, void *stream);
 
 /* ---------------------------------------------------------------------------
+ * Recovery of a pruned model (Section 3.3, Post-Pruning Optimizer: the pruned
+ * model is trained to restore its quality).  The calls below run its compacted
+ * dense projections forward and backward, keep the top logits of the foundation
+ * model's answer, and give the distillation loss against them with its gradient.
+ * Unlike the matrices of the pruning path, theirs may have any leading dimension
+ * and any base aligned to their element (a compacted matrix of odd width, logits
+ * over an odd vocabulary); rows on 16-byte boundaries are faster.
+ * ------------------------------------------------------------------------- */
+typedef enum mosaic_act {
+    MOSAIC_ACT_NONE = 0,
+    MOSAIC_ACT_RELU = 1,
+    MOSAIC_ACT_GELU = 2, /* z/2 (1 + erf(z / sqrt 2)) */
+    MOSAIC_ACT_SILU = 3  /* z / (1 + exp(-z))         */
+} mosaic_act;
+
+/* ---------------------------------------------------------------------------
+ * mosaic_linear - a projection's matrix product with its epilogue:
+ *     Z[t,o] = sum_i X[t,i] W[o,i] + bias[o],     Y[t,o] = act(Z[t,o]) + residual[t,o]
+ *   X         device, [tokens, in_features], ld ldx
+ *   W         device, [out_features, in_features], ld ldw
+ *   dtype     MOSAIC_BF16 for every matrix and the bias (bf16 products are exact in
+ *             fp32; MOSAIC_F32 -> MOSAIC_ERR_BAD_DTYPE)
+ *   bias      device, [out_features], or NULL
+ *   residual  device, [tokens, out_features], ld ldr, or NULL; may be Y itself
+ *             (same ld): added in place
+ *   Y         device, [tokens, out_features], ld ldy
+ *   Z         device, [tokens, out_features], ld ldz, or NULL: the value before the
+ *             activation, for the backward call
+ *   status_dev  as in mosaic_gram_accumulate, or NULL
+ *   ws        device scratch, >= mosaic_linear_workspace_bytes() for the same
+ *             arguments: 0 when X and W have 16-byte aligned bases and leading
+ *             dimensions (ws may then be NULL), else room for an aligned copy of each
+ *             that has not
+ * Sums in fp32 on the tensor cores; bias, activation and residual in fp32 on the
+ * sum; one rounding to bf16 for Y and one for Z.  tokens = 0 is legal.  Outputs
+ * must not overlap the inputs (Y and residual excepted) or each other.
+ * Results do not depend on anything but the arguments.
+ * ------------------------------------------------------------------------- */
+size_t mosaic_linear_workspace_bytes(const void *X, int64_t ldx, const void *W, int64_t ldw, int64_t tokens,
+                                     int64_t out_features, int64_t in_features);
+int mosaic_linear(const void *X, int64_t ldx, const void *W, int64_t ldw, int64_t tokens, int64_t out_features,
+                  int64_t in_features, int dtype, const void *bias, const void *residual, int64_t ldr, int act, void *Y,
+                  int64_t ldy, void *Z, int64_t ldz, int *status_dev, void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * mosaic_linear_backward - the gradients of mosaic_linear:
+ *     dZ = dY * act'(Z),   dX = dZ W,   dW = dZ^T X,   dbias[o] = sum_t dZ[t,o]
+ * (the residual's gradient is dY itself).
+ *   dY        device, [tokens, out_features], ld lddy
+ *   Z         device, [tokens, out_features], ld ldz: what the forward call stored;
+ *             ignored for MOSAIC_ACT_NONE
+ *   dX, dW, dbias   device outputs, [tokens, in_features] ld lddx, [out_features,
+ *             in_features] ld lddw, [out_features]; each may be NULL (not wanted;
+ *             W is needed for dX only, X for dW only)
+ *   ws        device scratch, >= the query for the same arguments
+ * dZ is rounded once to bf16 before the two products (the tensor cores' input
+ * type); dbias sums the unrounded values in fp32 in a fixed order.  With tokens = 0
+ * dW and dbias are zero.
+ * ------------------------------------------------------------------------- */
+size_t mosaic_linear_backward_workspace_bytes(const void *dY, int64_t lddy, const void *X, int64_t ldx, const void *W,
+                                              int64_t ldw, int64_t tokens, int64_t out_features, int64_t in_features,
+                                              int act, int want_dx, int want_dw, int want_dbias);
+int mosaic_linear_backward(const void *dY, int64_t lddy, const void *X, int64_t ldx, const void *W, int64_t ldw,
+                           const void *Z, int64_t ldz, int64_t tokens, int64_t out_features, int64_t in_features,
+                           int dtype, int act, void *dX, int64_t lddx, void *dW, int64_t lddw, void *dbias,
+                           int *status_dev, void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * mosaic_top_logits - the `top` largest entries of every row of logits, in order
+ * (value descending, ties by ascending index), and the row's log-sum-exp:
+ *     lse[r] = log sum_j exp(L[r,j] / temperature)     over the whole row
+ * which is all distillation needs of a teacher's answer.
+ *   L         device, [rows, vocab], ld ldl, fp32 or bf16; vocab < 2^31 - 256
+ *   top       1 .. min(vocab, 1024)
+ *   values    device, [rows, top] fp32, dense: the logits themselves
+ *   indices   device, [rows, top] int32, dense
+ *   lse       device, [rows] fp32, or NULL
+ * -0 and +0 are equal; a NaN orders above +inf (its row's lse is NaN).  Entries of
+ * -inf are masked: they come last, lowest index first.  A row of -inf has lse -inf.
+ * ------------------------------------------------------------------------- */
+int mosaic_top_logits(const void *L, int64_t rows, int64_t vocab, int64_t ldl, int dtype, int64_t top,
+                      float temperature, float *values, int32_t *indices, float *lse, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * mosaic_distill_loss / _grad / _loss_grad - distillation from a teacher's top
+ * logits.  Per row, T = temperature, x = S / T, q = softmax(x) over the vocabulary,
+ *     p_i   = exp(t_i / T - t_lse)                (t_lse given: the teacher's own
+ *                                                  probabilities, P = sum p_i <= 1)
+ *           = softmax over the kept t_i / T       (t_lse NULL: renormalised, P = 1)
+ *     loss  = w T^2 sum_i p_i (log p_i - log q_{j_i}),   lse = log sum_j exp(x_j)
+ *     dS_j  = grad_scale g w T (P q_j - sum_{i: j_i = j} p_i)
+ *   S          device, [rows, vocab], ld lds, fp32 or bf16: the student's logits
+ *   t_values, t_indices   device, [rows, top] fp32 / int32, dense, top 1 .. 1024: the
+ *              teacher's logits t_i and their places j_i, in any order.  An index
+ *              outside [0, vocab) is an absent entry, a logit of -inf has p = 0, an
+ *              index that occurs twice counts twice
+ *   t_lse      device, [rows] fp32 at the same temperature, or NULL
+ *   row_weight device, [rows] fp32 w, or NULL (1); a row of weight 0, and a row
+ *              without teacher mass (P = 0), has loss 0 and gradient 0 whatever it holds
+ *   grad_rows  device, [rows] fp32 g, or NULL (1): the gradient of each row's loss
+ *   loss, lse  device, [rows] fp32 (lse may be NULL in the loss calls; _grad reads it)
+ *   dS         device, [rows, vocab], ld ldd, S's dtype; may be S itself (same ld)
+ * _loss_grad does both in one pass over S.  With top = 1 and t_lse NULL the loss is
+ * the cross entropy of a label.  Sums in fp32 over the vocabulary and fp64 over the
+ * kept entries; the gradient is rounded once.
+ * ------------------------------------------------------------------------- */
+int mosaic_distill_loss(const void *S, int64_t rows, int64_t vocab, int64_t lds, int dtype, const float *t_values,
+                        const int32_t *t_indices, int64_t top, const float *t_lse, const float *row_weight,
+                        float temperature, float *loss, float *lse, void *stream);
+int mosaic_distill_grad(const void *S, int64_t rows, int64_t vocab, int64_t lds, int dtype, const float *t_values,
+                        const int32_t *t_indices, int64_t top, const float *t_lse, const float *row_weight,
+                        float temperature, const float *lse, const float *grad_rows, float grad_scale, void *dS,
+                        int64_t ldd, void *stream);
+int mosaic_distill_loss_grad(const void *S, int64_t rows, int64_t vocab, int64_t lds, int dtype, const float *t_values,
+                             const int32_t *t_indices, int64_t top, const float *t_lse, const float *row_weight,
+                             float temperature, float *loss, float *lse, const float *grad_rows, float grad_scale,
+                             void *dS, int64_t ldd, void *stream);
+
+/* ---------------------------------------------------------------------------
  * mosaic_bounded_wait_selftest - a diagnostic with no counterpart in the paper.
  * The tensor-core kernel of mosaic_gram_accumulate synchronises its roles
  * through mbarriers, and every such wait carries a cycle budget so that a

@@ -25,6 +25,8 @@ WEIGHTED_MEAN = 2        # flag, or-ed into the mode
 REDISTRIBUTE = 4         # flag, or-ed into the mode: clamp and redistribute
 ROWS_GIVEN, COLS_GIVEN, RANK_ONLY, SCORES_ONLY, SCORES_ACCUM = 1, 2, 4, 8, 16
 OK, ERR_INFEASIBLE = 0, -9
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+_ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "silu": ACT_SILU}
 
 # every symbol include/mosaic.h declares
 SYMBOLS = (
@@ -41,7 +43,12 @@ SYMBOLS = (
     "mosaic_rank_units", "mosaic_sum_unit_scores",
     "mosaic_unit_scores_batch_workspace_bytes", "mosaic_unit_scores_batch", "mosaic_add_unit_scores_batch",
     "mosaic_rank_units_batch", "mosaic_compact_batch",
-    "mosaic_gram_accumulate", "mosaic_bounded_wait_selftest",
+    "mosaic_gram_accumulate",
+    "mosaic_linear_workspace_bytes", "mosaic_linear",
+    "mosaic_linear_backward_workspace_bytes", "mosaic_linear_backward",
+    "mosaic_top_logits",
+    "mosaic_distill_loss", "mosaic_distill_grad", "mosaic_distill_loss_grad",
+    "mosaic_bounded_wait_selftest",
 )
 
 
@@ -122,6 +129,24 @@ def lib() -> C.CDLL:
         L.mosaic_rank_units_batch.argtypes = [vp, i64, vp]
         L.mosaic_compact_batch.restype = ci
         L.mosaic_compact_batch.argtypes = [vp, i64, ci, vp]
+        L.mosaic_linear_workspace_bytes.restype = sz
+        L.mosaic_linear_workspace_bytes.argtypes = [vp, i64, vp, i64, i64, i64, i64]
+        L.mosaic_linear.restype = ci
+        L.mosaic_linear.argtypes = [vp, i64, vp, i64, i64, i64, i64, ci, vp, vp, i64, ci, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.mosaic_linear_backward_workspace_bytes.restype = sz
+        L.mosaic_linear_backward_workspace_bytes.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, ci, ci, ci, ci]
+        L.mosaic_linear_backward.restype = ci
+        L.mosaic_linear_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, ci, ci, vp, i64, vp, i64, vp,
+                                             vp, vp, sz, vp]
+        L.mosaic_top_logits.restype = ci
+        L.mosaic_top_logits.argtypes = [vp, i64, i64, i64, ci, i64, flt, vp, vp, vp, vp]
+        teacher = [vp, i64, i64, i64, ci, vp, vp, i64, vp, vp, flt]
+        L.mosaic_distill_loss.restype = ci
+        L.mosaic_distill_loss.argtypes = teacher + [vp, vp, vp]
+        L.mosaic_distill_grad.restype = ci
+        L.mosaic_distill_grad.argtypes = teacher + [vp, vp, flt, vp, i64, vp]
+        L.mosaic_distill_loss_grad.restype = ci
+        L.mosaic_distill_loss_grad.argtypes = teacher + [vp, vp, vp, flt, vp, i64, vp]
         _lib = L
     return _lib
 
@@ -655,3 +680,177 @@ def mosaic_compact_batch(jobs, stream=None) -> None:
     col_units_keep, col_group, W_out) in one launch."""
     if jobs:
         CompactBatch(jobs).run(stream)
+
+
+# ------------------------------------------------------------------ recovery of a pruned model
+def _act_code(act) -> int:
+    """An activation by its name or its code."""
+    if isinstance(act, str):
+        if act not in _ACTS:
+            raise ValueError(f"unknown activation {act!r}: one of {sorted(_ACTS)}")
+        return _ACTS[act]
+    return int(act)
+
+
+def _mat_of(t, name: str, rows: int, cols: int, dtype):
+    """(pointer, leading dimension) of an optional [rows, cols] matrix."""
+    if t is None:
+        return None, max(cols, 1)
+    _dev(t, name, dtype, 2)
+    if t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must be row-major (unit stride along columns)")
+    return t.data_ptr(), (t.stride(0) if rows > 1 else max(t.stride(0), cols))
+
+
+def _vec_of(t, name: str, n: int, dtype):
+    """Pointer of an optional contiguous vector of n entries."""
+    if t is None:
+        return None
+    _dev(t, name, dtype, 1)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with {n} entries")
+    return t.data_ptr()
+
+
+def _same_device(first: torch.Tensor, *others) -> None:
+    """All tensors of a call live on one device (that of the stream it runs on)."""
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors of one call on different devices: {first.device} and {t.device}")
+
+
+def mosaic_linear(X, W, Y, bias=None, residual=None, act=ACT_NONE, Z=None, status: torch.Tensor | None = None,
+                  ws: Workspace | None = None, stream=None) -> None:
+    """Y = act(X W^T + bias) + residual for bf16 X [tokens, in], W [out, in], Y / residual / Z [tokens, out]
+    and bias [out]; Z, if given, receives the value before the activation.  `act` is one of the ACT_*
+    codes or "none" / "relu" / "gelu" / "silu"; `residual` may be Y (added in place).  `status` (int32, one
+    word) as in mosaic_gram_accumulate."""
+    _dev(X, "X", torch.bfloat16, 2)
+    _dev(W, "W", torch.bfloat16, 2)
+    tokens, n_in = X.shape
+    n_out = W.shape[0]
+    xp, ldx = _mat_of(X, "X", tokens, n_in, torch.bfloat16)
+    wp, ldw = _mat_of(W, "W", n_out, n_in, torch.bfloat16)
+    if Y is None:
+        raise TypeError("Y must be a CUDA tensor")
+    yp, ldy = _mat_of(Y, "Y", tokens, n_out, torch.bfloat16)
+    rp, ldr = _mat_of(residual, "residual", tokens, n_out, torch.bfloat16)
+    zp, ldz = _mat_of(Z, "Z", tokens, n_out, torch.bfloat16)
+    bp = _vec_of(bias, "bias", n_out, torch.bfloat16)
+    sp = _vec_of(status, "status", 1, torch.int32)
+    _same_device(X, W, Y, bias, residual, Z, status)
+    L = lib()
+    need = L.mosaic_linear_workspace_bytes(xp, ldx, wp, ldw, tokens, n_out, n_in)
+    sc, sn = _ws(ws, X.device).get(need) if need else (None, 0)
+    _check(L.mosaic_linear(xp, ldx, wp, ldw, tokens, n_out, n_in, BF16, bp, rp, ldr, _act_code(act), yp, ldy, zp, ldz, sp, sc, sn,
+                           _stream(stream)), "mosaic_linear")
+
+
+def mosaic_linear_backward(dY, X, W, Z=None, act=ACT_NONE, dX=None, dW=None, dbias=None, status: torch.Tensor | None = None,
+                           ws: Workspace | None = None, stream=None) -> None:
+    """Gradients of mosaic_linear: dX [tokens, in], dW [out, in], dbias [out] (each optional, all bf16) from dY
+    [tokens, out], the inputs X and W, and - unless the activation is none - the stored Z."""
+    _dev(dY, "dY", torch.bfloat16, 2)
+    tokens, n_out = dY.shape
+    if X is None and W is None:
+        raise TypeError("X or W must be given")
+    n_in = (X if X is not None else W).shape[1]
+    if (dW is not None and X is None) or (dX is not None and W is None):
+        raise ValueError("dW needs X and dX needs W")
+    act = _act_code(act)
+    if act != ACT_NONE and Z is None:
+        raise ValueError("the backward pass of an activation needs the stored Z")
+    dyp, lddy = _mat_of(dY, "dY", tokens, n_out, torch.bfloat16)
+    xp, ldx = _mat_of(X, "X", tokens, n_in, torch.bfloat16)
+    wp, ldw = _mat_of(W, "W", n_out, n_in, torch.bfloat16)
+    zp, ldz = _mat_of(Z, "Z", tokens, n_out, torch.bfloat16)
+    dxp, lddx = _mat_of(dX, "dX", tokens, n_in, torch.bfloat16)
+    dwp, lddw = _mat_of(dW, "dW", n_out, n_in, torch.bfloat16)
+    dbp = _vec_of(dbias, "dbias", n_out, torch.bfloat16)
+    sp = _vec_of(status, "status", 1, torch.int32)
+    _same_device(dY, X, W, Z, dX, dW, dbias, status)
+    L = lib()
+    need = L.mosaic_linear_backward_workspace_bytes(dyp, lddy, xp, ldx, wp, ldw, tokens, n_out, n_in, act, dxp is not None, dwp is not None,
+                                                    dbp is not None)
+    sc, sn = _ws(ws, dY.device).get(need) if need else (None, 0)
+    _check(L.mosaic_linear_backward(dyp, lddy, xp, ldx, wp, ldw, zp, ldz, tokens, n_out, n_in, BF16, act, dxp, lddx, dwp, lddw, dbp, sp, sc, sn,
+                                    _stream(stream)), "mosaic_linear_backward")
+
+
+def _logits_of(t, name: str):
+    _dev(t, name, ndim=2)
+    p, ld = _mat_of(t, name, t.shape[0], t.shape[1], t.dtype)
+    return p, t.shape[0], t.shape[1], ld, _dtype_code(t)
+
+
+def mosaic_top_logits(L, values, indices, lse=None, temperature: float = 1.0, stream=None) -> None:
+    """The values.shape[1] largest logits of every row of L [rows, vocab] (fp32 or bf16), in order (value
+    descending, ties by index): `values` fp32 and `indices` int32 [rows, top]; `lse`, fp32 [rows], receives
+    log sum exp(L / temperature) over the whole row."""
+    lp, rows, vocab, ldl, code = _logits_of(L, "L")
+    _dev(values, "values", torch.float32, 2)
+    _dev(indices, "indices", torch.int32, 2)
+    top = values.shape[1]
+    for t, nm in ((values, "values"), (indices, "indices")):
+        if tuple(t.shape) != (rows, top) or not t.is_contiguous():
+            raise ValueError(f"{nm} must be contiguous [{rows}, {top}]")
+    sp = _vec_of(lse, "lse", rows, torch.float32)
+    _same_device(L, values, indices, lse)
+    _check(lib().mosaic_top_logits(lp, rows, vocab, ldl, code, top, float(temperature), values.data_ptr(), indices.data_ptr(), sp,
+                                   _stream(stream)), "mosaic_top_logits")
+
+
+def _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature):
+    sp, rows, vocab, lds, code = _logits_of(S, "S")
+    _dev(t_values, "t_values", torch.float32, 2)
+    _dev(t_indices, "t_indices", torch.int32, 2)
+    top = t_values.shape[1]
+    for t, nm in ((t_values, "t_values"), (t_indices, "t_indices")):
+        if tuple(t.shape) != (rows, top) or not t.is_contiguous():
+            raise ValueError(f"{nm} must be contiguous [{rows}, {top}]")
+    tl = _vec_of(t_lse, "t_lse", rows, torch.float32)
+    rw = _vec_of(row_weight, "row_weight", rows, torch.float32)
+    _same_device(S, t_values, t_indices, t_lse, row_weight)
+    return (sp, rows, vocab, lds, code, t_values.data_ptr(), t_indices.data_ptr(), top, tl, rw, float(temperature)), rows, vocab
+
+
+def _distill_dS(S, dS, rows, vocab):
+    if dS is None:
+        raise TypeError("dS must be a CUDA tensor")
+    p, ld = _mat_of(dS, "dS", rows, vocab, S.dtype)
+    _same_device(S, dS)
+    return p, ld
+
+
+def mosaic_distill_loss(S, t_values, t_indices, loss, lse=None, t_lse=None, row_weight=None, temperature: float = 1.0, stream=None) -> None:
+    """Distillation loss of every row of the student's logits S [rows, vocab] (fp32 or bf16) against a teacher's
+    kept logits (t_values fp32, t_indices int32 [rows, top]); `loss` and `lse` (optional) are fp32 [rows]."""
+    args, rows, _ = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
+    lo, ls = _vec_of(loss, "loss", rows, torch.float32), _vec_of(lse, "lse", rows, torch.float32)
+    _same_device(S, loss, lse)
+    _check(lib().mosaic_distill_loss(*args, lo, ls, _stream(stream)), "mosaic_distill_loss")
+
+
+def mosaic_distill_grad(S, t_values, t_indices, lse, dS, t_lse=None, row_weight=None, grad_rows=None, grad_scale: float = 1.0,
+                        temperature: float = 1.0, stream=None) -> None:
+    """Gradient of mosaic_distill_loss with respect to S, from the lse that call stored; `grad_rows` (fp32 [rows]) times
+    `grad_scale` is the gradient of each row's loss.  dS may be S."""
+    args, rows, vocab = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
+    ls, gr = _vec_of(lse, "lse", rows, torch.float32), _vec_of(grad_rows, "grad_rows", rows, torch.float32)
+    dp, ldd = _distill_dS(S, dS, rows, vocab)
+    _same_device(S, lse, grad_rows)
+    _check(lib().mosaic_distill_grad(*args, ls, gr, float(grad_scale), dp, ldd, _stream(stream)), "mosaic_distill_grad")
+
+
+def mosaic_distill_loss_grad(S, t_values, t_indices, loss, lse, dS, t_lse=None, row_weight=None, grad_rows=None, grad_scale: float = 1.0,
+                             temperature: float = 1.0, stream=None) -> None:
+    """mosaic_distill_loss and mosaic_distill_grad in one pass over S (the training step, where the gradient of each row's
+    loss is known beforehand).  `lse` may be None; dS may be S."""
+    args, rows, vocab = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
+    lo, ls = _vec_of(loss, "loss", rows, torch.float32), _vec_of(lse, "lse", rows, torch.float32)
+    gr = _vec_of(grad_rows, "grad_rows", rows, torch.float32)
+    dp, ldd = _distill_dS(S, dS, rows, vocab)
+    _same_device(S, loss, lse, grad_rows)
+    _check(lib().mosaic_distill_loss_grad(*args, lo, ls, gr, float(grad_scale), dp, ldd, _stream(stream)), "mosaic_distill_loss_grad")

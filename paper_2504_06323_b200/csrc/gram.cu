@@ -19,9 +19,7 @@
 // A block is accumulated by one CTA in token order, so results do not depend on the grid.
 // Every wait on an mbarrier is bounded; a wait that runs out sets the kernel's error word, all
 // roles leave their loops, loads in flight are awaited (bounded), tensor memory is freed.
-#include <cuda.h>   // CUtensorMap and its enums; the encoder itself is looked up at run time
-
-#include "common.cuh"
+#include "umma.cuh"
 
 namespace mosaic {
 namespace {
@@ -37,101 +35,8 @@ constexpr int kGEpiWarps = 8;                                            // two 
 constexpr int kGThreads = 64 + 32 * kGEpiWarps;
 constexpr uint32_t kGTmemCols = 512;
 constexpr size_t kGSmemBytes = (size_t)kGStages * kGStageBytes + 1024 /* alignment */ + 256 /* barriers */;
-constexpr long long kGWaitCycles = 4000000000ll;                         // about two seconds
 
-// Instruction descriptor of tcgen05.mma kind::f16: fp32 accumulator (bits 4-5 = 1), A and B bf16
-// (bits 7-9 and 10-12 = 1), A and B MN-major (bits 15, 16), N / 8 at bit 17, M / 16 at bit 24.
-constexpr uint32_t kGInstrDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((256u >> 3) << 17) | ((128u >> 4) << 24);
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t"
-        ".reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t"
-        "}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0u;
-}
-// Waits for the phase of the given parity to complete.  False if it gave up: after kGWaitCycles
-// (then it raises *err) or because another role raised *err.
-__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* err, long long budget = kGWaitCycles) {
-    const long long t0 = clock64();
-    while (!mbar_try_wait(bar, parity)) {
-        if (*err != 0) return false;
-        if (clock64() - t0 > budget) {
-            *err = 1;
-            return false;
-        }
-    }
-    return true;
-}
-
-__device__ __forceinline__ void tma_load_box(void* dst, const CUtensorMap* map, uint64_t* bar, int col, int token) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
-                     smem_u32(dst)),
-                 "l"(map), "r"(smem_u32(bar)), "r"(col), "r"(token)
-                 : "memory");
-}
-
-// Shared-memory operand descriptor, MN-major with the 128-byte swizzle: 64 columns of a token are
-// contiguous (one swizzle row), the rows of 8 consecutive tokens lie 128 bytes apart, groups of 8
-// tokens 1024 bytes apart (stride offset), the next 64 columns one TMA box further (leading offset).
-__device__ __forceinline__ uint64_t operand_desc(uint32_t smem_addr) {
-    uint64_t d = (uint64_t)((smem_addr >> 4) & 0x3FFFu);
-    d |= (uint64_t)((kGBoxBytes >> 4) & 0x3FFFu) << 16;
-    d |= (uint64_t)((1024u >> 4) & 0x3FFFu) << 32;
-    d |= (uint64_t)1 << 46;   // descriptor version of this architecture
-    d |= (uint64_t)2 << 61;   // 128-byte swizzle
-    return d;
-}
-
-__device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t"
-        ".reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %6, %7, %8}, p;\n\t"
-        "}"
-        :
-        : "r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(kGInstrDesc), "r"(accumulate), "r"(0u), "r"(0u), "r"(0u), "r"(0u)
-        : "memory");
-}
-// The barrier gets one arrival when every MMA issued so far by this thread has completed.
-__device__ __forceinline__ void umma_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-// 16 consecutive accumulator columns of this thread's lane of tensor memory.
-__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
-    uint32_t r[16];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(addr)
-        : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
+constexpr uint32_t kGInstrDesc = instr_desc(true, true, 128u, 256u);
 
 // Block (bi, bj), bi <= bj, number `tile` in the row-by-row list of the blocks on or above the diagonal.
 __device__ __forceinline__ void block_of_tile(int tile, int n_blk, int* bi, int* bj) {
@@ -230,11 +135,11 @@ __global__ void __launch_bounds__(kGThreads, 1) gram_kernel(const __grid_constan
 #pragma unroll
                     for (int kk = 0; kk < kGTok / 16; ++kk) {
                         // 16 tokens further = 16 swizzle rows = 2048 bytes
-                        const uint64_t db = operand_desc(b_base + (uint32_t)kk * 2048u);
+                        const uint64_t db = operand_desc(b_base + (uint32_t)kk * 2048u, kGBoxBytes);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const uint64_t da = operand_desc(a_base + (uint32_t)h * 2u * kGBoxBytes + (uint32_t)kk * 2048u);
-                            umma_bf16(tmem_base + (uint32_t)h * 256u, da, db, (k > 0 || kk > 0) ? 1u : 0u);
+                            const uint64_t da = operand_desc(a_base + (uint32_t)h * 2u * kGBoxBytes + (uint32_t)kk * 2048u, kGBoxBytes);
+                            umma_bf16(tmem_base + (uint32_t)h * 256u, da, db, kGInstrDesc, (k > 0 || kk > 0) ? 1u : 0u);
                         }
                     }
                     umma_commit(&empty[s]);
@@ -318,7 +223,7 @@ __global__ void __launch_bounds__(kGThreads, 1) gram_kernel(const __grid_constan
         for (uint32_t back = 1; back <= (uint32_t)kGStages && back <= issued; ++back) {
             const uint32_t j = issued - back, s = j % kGStages, ph = (j / kGStages) & 1u;
             const long long t0 = clock64();
-            while (!mbar_try_wait(&full[s], ph) && clock64() - t0 < kGWaitCycles) {
+            while (!mbar_try_wait(&full[s], ph) && clock64() - t0 < kWaitCycles) {
             }
         }
         if (status != nullptr) atomicExch(status, 1);
@@ -337,26 +242,6 @@ __global__ void bounded_wait_selftest_kernel(long long budget, int* status) {
         const bool completed = mbar_wait(&bar, 0u, &err, budget);
         *status = completed ? 2 : (err != 0 ? 1 : 3);   // 1: gave up after the budget and raised the error word
     }
-}
-
-using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's tensor-map encoder (a host-side function of the process, not of a device).
-EncodeTiledFn encode_tiled() {
-    static std::atomic<void*> cached{nullptr};
-    void* fn = cached.load(std::memory_order_acquire);
-    if (fn == nullptr) {
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            return nullptr;
-        }
-        cached.store(fn, std::memory_order_release);
-    }
-    return reinterpret_cast<EncodeTiledFn>(fn);
 }
 
 }  // namespace
@@ -390,16 +275,8 @@ extern "C" int mosaic_gram_accumulate(const void* X, int64_t tokens, int64_t col
         if (reset) MOSAIC_CUDA_TRY(cudaMemset2DAsync(G, (size_t)ldg * 4u, 0, (size_t)cols * 4u, (size_t)cols, st));
         return MOSAIC_OK;
     }
-    EncodeTiledFn encode = encode_tiled();
-    if (encode == nullptr) return MOSAIC_ERR_CUDA;
     CUtensorMap map;
-    const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)tokens};
-    const cuuint64_t gstride[1] = {(cuuint64_t)ldx * 2u};
-    const cuuint32_t box[2] = {(cuuint32_t)kGBoxCols, (cuuint32_t)kGTok};
-    const cuuint32_t estride[2] = {1u, 1u};
-    if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2u, const_cast<void*>(X), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return MOSAIC_ERR_CUDA;
+    if (!encode_bf16(&map, X, tokens, cols, ldx, kGTok, kGBoxCols)) return MOSAIC_ERR_CUDA;
     static DeviceCache opted;   // the shared-memory opt-in belongs to one device's copy of the kernel
     const int ok = opted.get([&]() -> int {
         if (cudaFuncSetAttribute(gram_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGSmemBytes) != cudaSuccess) {

@@ -1,0 +1,478 @@
+// mosaic_linear / mosaic_linear_backward: a projection's matrix product with its bias, activation and residual
+// in the epilogue, and the three products of its gradient - all on the tensor cores (bf16 in, fp32 sums).
+//
+//     forward    Z = X W^T + b,  Y = act(Z) + R          [tokens, out]
+//     backward   dZ = dY * act'(Z);  dX = dZ W  [tokens, in],  dW = dZ^T X  [out, in],  db = sum over tokens of dZ
+//
+// One kernel computes all of them as   out[j, i] = sum_c A[i, c] B[j, c]:  the matrix instruction's 128 rows run
+// along the CONTIGUOUS dimension of the output, its columns along the rows of the output.  The accumulator of a
+// fixed column is then a run of adjacent output elements across the lanes of a warp: the epilogue reads and writes
+// 64 adjacent bytes per instruction whatever the alignment, the bias is one register per lane, and few tokens mean
+// a narrow instruction instead of one mostly filled with nothing.
+//     forward    A = W  (contraction contiguous)   B = X   (contraction contiguous)
+//     dX         A = W  (contraction = rows)       B = dZ  (contraction contiguous)
+//     dW         A = X  (contraction = rows)       B = dZ  (contraction = rows)
+// "Contraction = rows" operands are MN-major for tcgen05.mma; nothing is transposed.
+#include <cooperative_groups.h>
+
+#include "linear.cuh"
+#include "umma.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace mosaic {
+namespace {
+
+constexpr int kMI = 128;               // rows of the matrix instruction: adjacent output elements
+constexpr int kMC = 64;                // contraction steps per stage (128 bytes: one swizzle row)
+constexpr int kMThreads = 192;         // loader, MMA issue, four epilogue warps (one per quarter of tensor memory)
+constexpr int kMMaxSplit = 8;          // CTAs (one cluster) that share one tile's contraction
+constexpr uint32_t kMBox = 64 * 64 * 2;   // an MN-major box: 64 elements x 64 contraction steps
+
+struct MmArgs {
+    int64_t n_i, n_j, n_c;             // extents
+    int tiles_i, tiles_j, stages;
+    uint16_t* out;
+    int64_t ld_out;
+    const uint16_t* bias;              // [n_i] or null
+    const uint16_t* resid;             // [n_j, n_i] or null
+    int64_t ld_resid;
+    uint16_t* z;                       // [n_j, n_i] or null: the value before the activation
+    int64_t ld_z;
+    int act;
+    int* status;
+};
+
+__device__ __forceinline__ float finish(const MmArgs& a, float v, float bias, int64_t i, int64_t j, float resid) {
+    v = __fadd_rn(v, bias);
+    if (a.z != nullptr) a.z[j * a.ld_z + i] = f32_to_bf16(v);
+    return __fadd_rn(activate(v, a.act), resid);
+}
+
+// One output tile of kMI x BN per cluster; its contraction is split over the cluster's CTAs, whose partial
+// tiles meet in shared memory and are added in the CTAs' order.
+template <bool A_MN, bool B_MN, int BN>
+__global__ void __launch_bounds__(kMThreads) mm_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+                                                       const __grid_constant__ MmArgs a) {
+    constexpr uint32_t kABytes = kMI * kMC * 2, kBBytes = BN * kMC * 2, kStage = kABytes + kBBytes;
+    constexpr uint32_t kCols = BN < 32 ? 32 : BN;
+    constexpr uint32_t kDesc = instr_desc(A_MN, B_MN, kMI, BN);
+    extern __shared__ unsigned char mm_smem_raw[];
+    __shared__ uint64_t full[8], empty[8], acc_full;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int err_word;
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(mm_smem_raw) + 1023u) & ~(uintptr_t)1023u);
+    volatile int* err = &err_word;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tile = (int)(blockIdx.x / (unsigned)split);
+    const int64_t i0 = (int64_t)(tile % a.tiles_i) * kMI, j0 = (int64_t)(tile / a.tiles_i) * BN;
+    const int64_t steps = (a.n_c + kMC - 1) / kMC;
+    const int s0 = (int)(steps * rank / split), s1 = (int)(steps * (rank + 1) / split);   // split <= steps: never empty
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < a.stages; ++s) {
+            mbar_init(&full[s], 1u);
+            mbar_init(&empty[s], 1u);
+        }
+        mbar_init(&acc_full, 1u);
+        *err = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(kCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    uint32_t issued = 0;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            for (int s = s0; s < s1; ++s) {
+                const uint32_t it = (uint32_t)(s - s0), slot = it % (uint32_t)a.stages, ph = (it / (uint32_t)a.stages) & 1u;
+                if (!mbar_wait(&empty[slot], ph ^ 1u, err)) break;
+                unsigned char* sa = ring + (size_t)slot * kStage;
+                unsigned char* sb = sa + kABytes;
+                mbar_expect_tx(&full[slot], kStage);
+                if (A_MN) {
+#pragma unroll
+                    for (int b = 0; b < kMI / 64; ++b) tma_load_box(sa + (size_t)b * kMBox, &a_map, &full[slot], (int)i0 + b * 64, s * kMC);
+                } else {
+                    tma_load_box(sa, &a_map, &full[slot], s * kMC, (int)i0);
+                }
+                if (B_MN) {
+#pragma unroll
+                    for (int b = 0; b < BN / 64; ++b) tma_load_box(sb + (size_t)b * kMBox, &b_map, &full[slot], (int)j0 + b * 64, s * kMC);
+                } else {
+                    tma_load_box(sb, &b_map, &full[slot], s * kMC, (int)j0);
+                }
+                issued = it + 1u;
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            bool ok = true;
+            for (int s = s0; s < s1; ++s) {
+                const uint32_t it = (uint32_t)(s - s0), slot = it % (uint32_t)a.stages, ph = (it / (uint32_t)a.stages) & 1u;
+                if (!mbar_wait(&full[slot], ph, err)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t sa = smem_u32(ring + (size_t)slot * kStage), sb = sa + kABytes;
+#pragma unroll
+                for (int kk = 0; kk < kMC / 16; ++kk) {
+                    // 16 contraction steps further: 16 swizzle rows (MN-major) or 32 bytes along one (K-major)
+                    const uint64_t da = operand_desc(sa + (uint32_t)kk * (A_MN ? 2048u : 32u), A_MN ? kMBox : 16u);
+                    const uint64_t db = operand_desc(sb + (uint32_t)kk * (B_MN ? 2048u : 32u), B_MN ? kMBox : 16u);
+                    umma_bf16(tmem, da, db, kDesc, (it > 0 || kk > 0) ? 1u : 0u);
+                }
+                umma_commit(&empty[slot]);
+            }
+            if (ok) umma_commit(&acc_full);
+        }
+    }
+    __syncwarp();
+    const bool done = warp >= 2 && mbar_wait(&acc_full, 0u, err);
+    tc_fence_after();
+    const int q = warp & 3;
+    const int64_t i = i0 + q * 32 + lane;
+    const int n_cols = (int)(a.n_j - j0 < BN ? a.n_j - j0 : BN);
+    float* part = reinterpret_cast<float*>(ring);   // [BN][kMI]: every load has been consumed once the accumulator is complete
+    if (done) {
+        const float bias = a.bias != nullptr && i < a.n_i ? bf16_to_f32(a.bias[i]) : 0.0f;
+#pragma unroll 1
+        for (int c0 = 0; c0 < n_cols; c0 += 16) {
+            float v[16];
+            tmem_load16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c0, v);
+            if (split > 1) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) part[(c0 + e) * kMI + q * 32 + lane] = v[e];
+            } else if (i < a.n_i) {
+                float r[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    r[e] = a.resid != nullptr && c0 + e < n_cols ? bf16_to_f32(a.resid[(j0 + c0 + e) * a.ld_resid + i]) : 0.0f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (c0 + e < n_cols) a.out[(j0 + c0 + e) * a.ld_out + i] = f32_to_bf16(finish(a, v[e], bias, i, j0 + c0 + e, r[e]));
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {   // tensor memory goes back before the cluster's CTAs wait for one another
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
+    }
+    if (threadIdx.x == 0 && *err != 0) {
+        // a role gave up: let the loads of the last stages land before shared memory is reused or left (bounded)
+        for (uint32_t back = 1; back <= (uint32_t)a.stages && back <= issued; ++back) {
+            const uint32_t it = issued - back, slot = it % (uint32_t)a.stages, ph = (it / (uint32_t)a.stages) & 1u;
+            const long long t0 = clock64();
+            while (!mbar_try_wait(&full[slot], ph) && clock64() - t0 < kWaitCycles) {
+            }
+        }
+        if (a.status != nullptr) atomicExch(a.status, 1);
+    }
+    if (split > 1) {
+        cluster.sync();
+        const int all = n_cols * kMI, per = (all + split - 1) / split;
+        const int e1 = (rank + 1) * per < all ? (rank + 1) * per : all;
+        for (int e = rank * per + (int)threadIdx.x; e < e1; e += kMThreads) {
+            float v[kMMaxSplit];
+#pragma unroll
+            for (int p = 0; p < kMMaxSplit; ++p) v[p] = p < split ? *cluster.map_shared_rank(part + e, p) : 0.0f;
+            float sum = v[0];
+#pragma unroll
+            for (int p = 1; p < kMMaxSplit; ++p)
+                if (p < split) sum = __fadd_rn(sum, v[p]);
+            const int64_t oi = i0 + e % kMI, oj = j0 + e / kMI;
+            if (oi < a.n_i) {
+                const float bias = a.bias != nullptr ? bf16_to_f32(a.bias[oi]) : 0.0f;
+                const float r = a.resid != nullptr ? bf16_to_f32(a.resid[oj * a.ld_resid + oi]) : 0.0f;
+                a.out[oj * a.ld_out + oi] = f32_to_bf16(finish(a, sum, bias, oi, oj, r));
+            }
+        }
+        cluster.sync();   // nobody leaves while its partial tile is being read
+    }
+}
+
+// ---------------------------------------------------------------- elementwise passes
+// dst[r, c] = src[r, c] * act'(z[r, c]) (z null: a plain copy), dst with rows on 16-byte boundaries; column sums of
+// the unrounded values over the rows of this CTA's band into partial[band, c] if wanted.  A thread owns a column.
+constexpr int kBandCols = 128;
+__global__ void __launch_bounds__(kBandCols) slope_kernel(const uint16_t* __restrict__ src, int64_t ld_src, const uint16_t* __restrict__ z,
+                                                          int64_t ld_z, int act, uint16_t* __restrict__ dst, int64_t ld_dst, int64_t rows,
+                                                          int64_t cols, int64_t band, float* __restrict__ partial) {
+    const int64_t c = (int64_t)blockIdx.x * kBandCols + threadIdx.x;
+    if (c >= cols) return;
+    const int64_t r0 = (int64_t)blockIdx.y * band, r1 = r0 + band < rows ? r0 + band : rows;
+    float sum = 0.0f;
+    for (int64_t r = r0; r < r1; ++r) {
+        const uint16_t raw = src[r * ld_src + c];
+        float v = bf16_to_f32(raw);
+        if (z != nullptr) v = __fmul_rn(v, activate_slope(bf16_to_f32(z[r * ld_z + c]), act));
+        // dZ is rounded to bf16 here because the tensor cores take bf16; the column sums are not
+        if (dst != nullptr) dst[r * ld_dst + c] = z != nullptr ? f32_to_bf16(v) : raw;
+        sum = __fadd_rn(sum, v);
+    }
+    if (partial != nullptr) partial[(int64_t)blockIdx.y * cols + c] = sum;
+}
+__global__ void __launch_bounds__(kBandCols) column_sum_kernel(const float* __restrict__ partial, int64_t bands, int64_t cols, uint16_t* __restrict__ out) {
+    const int64_t c = (int64_t)blockIdx.x * kBandCols + threadIdx.x;
+    if (c >= cols) return;
+    float sum = 0.0f;
+    for (int64_t b = 0; b < bands; ++b) sum = __fadd_rn(sum, partial[b * cols + c]);
+    out[c] = f32_to_bf16(sum);
+}
+
+// ---------------------------------------------------------------- host side
+struct Matrix {
+    const void* p;
+    int64_t rows, cols, ld;
+    size_t bytes() const { return rows > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * 2u : 0u; }
+    bool tma_ok() const { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || ld % 8 == 0); }
+    int64_t padded_ld() const { return (cols + 7) / 8 * 8; }
+    size_t padded_bytes() const { return align_up((size_t)rows * (size_t)padded_ld() * 2u, 256); }
+};
+
+int64_t band_rows(int64_t rows) { return rows <= 64 ? rows : (rows + 63) / 64 < 32 ? 32 : (rows + 63) / 64; }
+int64_t bands_of(int64_t rows) { return rows > 0 ? (rows + band_rows(rows) - 1) / band_rows(rows) : 0; }
+
+int run_slope(const Matrix& src, const void* z, int64_t ld_z, int act, void* dst, int64_t ld_dst, float* partial, void* db, cudaStream_t st) {
+    const int64_t bands = bands_of(src.rows);
+    if (bands > 0) {
+        const dim3 grid((unsigned)((src.cols + kBandCols - 1) / kBandCols), (unsigned)bands);
+        slope_kernel<<<grid, kBandCols, 0, st>>>(static_cast<const uint16_t*>(src.p), src.ld, static_cast<const uint16_t*>(z), ld_z, act,
+                                                 static_cast<uint16_t*>(dst), ld_dst, src.rows, src.cols, band_rows(src.rows), partial);
+        MOSAIC_LAUNCH_CHECK();
+    }
+    if (db != nullptr) {
+        column_sum_kernel<<<(unsigned)((src.cols + kBandCols - 1) / kBandCols), kBandCols, 0, st>>>(partial, bands, src.cols, static_cast<uint16_t*>(db));
+        MOSAIC_LAUNCH_CHECK();
+    }
+    return MOSAIC_OK;
+}
+
+// A matrix TMA can read: itself, or a copy at *ws (advanced) with rows on 16-byte boundaries.
+int readable(Matrix& m, char** ws, cudaStream_t st) {
+    if (m.rows == 0 || m.tma_ok()) return MOSAIC_OK;
+    const int rc = run_slope(m, nullptr, 0, MOSAIC_ACT_NONE, *ws, m.padded_ld(), nullptr, nullptr, st);
+    if (rc != MOSAIC_OK) return rc;
+    m.p = *ws;
+    m.ld = m.padded_ld();
+    *ws += m.padded_bytes();
+    return MOSAIC_OK;
+}
+
+template <bool A_MN, bool B_MN, int BN>
+int launch_mm(const Matrix& A, const Matrix& B, MmArgs a, cudaStream_t st) {
+    constexpr size_t kStage = (size_t)(kMI + BN) * kMC * 2;
+    CUtensorMap a_map, b_map;
+    if (!(A_MN ? encode_bf16(&a_map, A.p, A.rows, A.cols, A.ld, kMC, 64) : encode_bf16(&a_map, A.p, A.rows, A.cols, A.ld, kMI, kMC))) return MOSAIC_ERR_CUDA;
+    if (!(B_MN ? encode_bf16(&b_map, B.p, B.rows, B.cols, B.ld, kMC, 64) : encode_bf16(&b_map, B.p, B.rows, B.cols, B.ld, BN, kMC))) return MOSAIC_ERR_CUDA;
+    a.tiles_i = (int)((a.n_i + kMI - 1) / kMI);
+    a.tiles_j = (int)((a.n_j + BN - 1) / BN);
+    const int64_t tiles = (int64_t)a.tiles_i * a.tiles_j, steps = (a.n_c + kMC - 1) / kMC;
+    int split = 1;   // share a tile's contraction while SMs would stay idle and each share keeps four stages
+    while (split < kMMaxSplit && tiles * split * 2 <= 2 * sm_count() && steps >= 8 * split) split *= 2;
+    if (tiles * split > 0x7FFFFFFF) return MOSAIC_ERR_INVALID_ARG;
+    // two CTAs an SM (100 KB of stages each): one's epilogue under the other's products
+    a.stages = (int)(100 * 1024 / kStage);
+    if (a.stages > 8) a.stages = 8;
+    size_t smem = a.stages * kStage;
+    if (split > 1 && smem < (size_t)BN * kMI * 4u) smem = (size_t)BN * kMI * 4u;
+    smem += 1024;
+    static DeviceCache opted;
+    const int ok = opted.get([&]() -> int {
+        if (cudaFuncSetAttribute(mm_kernel<A_MN, B_MN, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, 110 * 1024) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return -1;
+        }
+        return 1;
+    });
+    if (ok < 0) return MOSAIC_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * split));
+    cfg.blockDim = dim3(kMThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)split;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, mm_kernel<A_MN, B_MN, BN>, a_map, b_map, a));
+    return MOSAIC_OK;
+}
+
+// out[j, i] = sum_c A B; A: [n_i, n_c] (or [n_c, n_i] if A_MN), B likewise.
+template <bool A_MN, bool B_MN> int run_mm(const Matrix& A, const Matrix& B, const MmArgs& a, cudaStream_t st) {
+    if constexpr (!B_MN) {   // narrow instructions for few output rows
+        if (a.n_j <= 16) return launch_mm<A_MN, B_MN, 16>(A, B, a, st);
+        if (a.n_j <= 32) return launch_mm<A_MN, B_MN, 32>(A, B, a, st);
+    }
+    if (a.n_j <= 64) return launch_mm<A_MN, B_MN, 64>(A, B, a, st);
+    return launch_mm<A_MN, B_MN, 128>(A, B, a, st);
+}
+
+bool overlap(const Matrix& a, const Matrix& b) {
+    const char *x = static_cast<const char*>(a.p), *y = static_cast<const char*>(b.p);
+    return x != nullptr && y != nullptr && a.bytes() > 0 && b.bytes() > 0 && x < y + b.bytes() && y < x + a.bytes();
+}
+
+// null / element alignment / leading dimension of a matrix that is there (rows > 0)
+int check_bf16(const Matrix& m) {
+    if (m.ld < m.cols) return MOSAIC_ERR_INVALID_ARG;
+    if (m.rows > 0 && m.p == nullptr) return MOSAIC_ERR_NULL_PTR;
+    if ((reinterpret_cast<uintptr_t>(m.p) & 1u) != 0) return MOSAIC_ERR_MISALIGNED;
+    return MOSAIC_OK;
+}
+constexpr int64_t kMostExtent = 0x7FFFFFFF - 1024;
+bool extents_ok(int64_t m, int64_t n, int64_t k) { return m >= 0 && n > 0 && k > 0 && m <= kMostExtent && n <= kMostExtent && k <= kMostExtent; }
+bool act_ok(int act) { return act >= MOSAIC_ACT_NONE && act <= MOSAIC_ACT_SILU; }
+
+int check_workspace(const void* ws, size_t ws_bytes, size_t need) {
+    if (need == 0) return MOSAIC_OK;
+    if (ws == nullptr) return MOSAIC_ERR_NULL_PTR;
+    if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return MOSAIC_ERR_MISALIGNED;
+    return ws_bytes < need ? MOSAIC_ERR_WORKSPACE_TOO_SMALL : MOSAIC_OK;
+}
+
+size_t backward_workspace(const Matrix& dY, const Matrix& X, const Matrix& W, int act, bool want_dx, bool want_dw, bool want_db) {
+    size_t need = 0;
+    if (want_dx || want_dw) {
+        if (act != MOSAIC_ACT_NONE || !dY.tma_ok()) need += dY.padded_bytes();
+        if (want_dw && !X.tma_ok()) need += X.padded_bytes();
+        if (want_dx && !W.tma_ok()) need += W.padded_bytes();
+    }
+    if (want_db) need += align_up((size_t)bands_of(dY.rows) * (size_t)dY.cols * 4u, 256);
+    return need;
+}
+
+}  // namespace
+}  // namespace mosaic
+
+using namespace mosaic;
+
+extern "C" size_t mosaic_linear_workspace_bytes(const void* X, int64_t ldx, const void* W, int64_t ldw, int64_t tokens, int64_t out_features,
+                                                int64_t in_features) {
+    if (!extents_ok(tokens, out_features, in_features)) return 0;
+    const Matrix x{X, tokens, in_features, ldx}, w{W, out_features, in_features, ldw};
+    return (x.tma_ok() ? 0 : x.padded_bytes()) + (w.tma_ok() ? 0 : w.padded_bytes());
+}
+
+extern "C" int mosaic_linear(const void* X, int64_t ldx, const void* W, int64_t ldw, int64_t tokens, int64_t out_features, int64_t in_features,
+                             int dtype, const void* bias, const void* residual, int64_t ldr, int act, void* Y, int64_t ldy, void* Z, int64_t ldz,
+                             int* status_dev, void* ws, size_t ws_bytes, void* stream) {
+    if (dtype != MOSAIC_BF16) return MOSAIC_ERR_BAD_DTYPE;   // bf16 products are exact in fp32; fp32 ones are not
+    if (!extents_ok(tokens, out_features, in_features) || !act_ok(act)) return MOSAIC_ERR_INVALID_ARG;
+    Matrix x{X, tokens, in_features, ldx}, w{W, out_features, in_features, ldw};
+    const Matrix y{Y, tokens, out_features, ldy}, z{Z, tokens, out_features, ldz}, r{residual, tokens, out_features, ldr};
+    const Matrix b{bias, 1, out_features, out_features};
+    int rc;
+    if ((rc = check_bf16(x)) != MOSAIC_OK || (rc = check_bf16(w)) != MOSAIC_OK || (rc = check_bf16(y)) != MOSAIC_OK) return rc;
+    if (Z != nullptr && (rc = check_bf16(z)) != MOSAIC_OK) return rc;
+    if (residual != nullptr && (rc = check_bf16(r)) != MOSAIC_OK) return rc;
+    if (bias != nullptr && (rc = check_bf16(b)) != MOSAIC_OK) return rc;
+    if ((reinterpret_cast<uintptr_t>(status_dev) & 3u) != 0) return MOSAIC_ERR_MISALIGNED;
+    // the residual may be the output itself (added in place), with the same leading dimension
+    if (overlap(y, x) || overlap(y, w) || overlap(y, b) || overlap(y, z) || overlap(z, x) || overlap(z, w) || overlap(z, b) || overlap(z, r))
+        return MOSAIC_ERR_ALIASING;
+    if (overlap(y, r) && !(residual == Y && ldr == ldy)) return MOSAIC_ERR_ALIASING;
+    if ((rc = check_workspace(ws, ws_bytes, mosaic_linear_workspace_bytes(X, ldx, W, ldw, tokens, out_features, in_features))) != MOSAIC_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (status_dev != nullptr) MOSAIC_CUDA_TRY(cudaMemsetAsync(status_dev, 0, sizeof(int), st));
+    if (tokens == 0) return MOSAIC_OK;
+    char* scratch = static_cast<char*>(ws);
+    if ((rc = readable(x, &scratch, st)) != MOSAIC_OK || (rc = readable(w, &scratch, st)) != MOSAIC_OK) return rc;
+    MmArgs a = {};
+    a.n_i = out_features; a.n_j = tokens; a.n_c = in_features;
+    a.out = static_cast<uint16_t*>(Y); a.ld_out = ldy;
+    a.bias = static_cast<const uint16_t*>(bias);
+    a.resid = static_cast<const uint16_t*>(residual); a.ld_resid = ldr;
+    a.z = static_cast<uint16_t*>(Z); a.ld_z = ldz;
+    a.act = act; a.status = status_dev;
+    return run_mm<false, false>(w, x, a, st);
+}
+
+extern "C" size_t mosaic_linear_backward_workspace_bytes(const void* dY, int64_t lddy, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                                                         int64_t tokens, int64_t out_features, int64_t in_features, int act, int want_dx,
+                                                         int want_dw, int want_dbias) {
+    if (!extents_ok(tokens, out_features, in_features)) return 0;
+    return backward_workspace({dY, tokens, out_features, lddy}, {X, tokens, in_features, ldx}, {W, out_features, in_features, ldw}, act, want_dx != 0,
+                              want_dw != 0, want_dbias != 0);
+}
+
+extern "C" int mosaic_linear_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* Z, int64_t ldz,
+                                      int64_t tokens, int64_t out_features, int64_t in_features, int dtype, int act, void* dX, int64_t lddx, void* dW,
+                                      int64_t lddw, void* dbias, int* status_dev, void* ws, size_t ws_bytes, void* stream) {
+    if (dtype != MOSAIC_BF16) return MOSAIC_ERR_BAD_DTYPE;
+    if (!extents_ok(tokens, out_features, in_features) || !act_ok(act)) return MOSAIC_ERR_INVALID_ARG;
+    Matrix dy{dY, tokens, out_features, lddy}, x{X, tokens, in_features, ldx}, w{W, out_features, in_features, ldw};
+    const Matrix z{Z, tokens, out_features, ldz}, dx{dX, tokens, in_features, lddx}, dw{dW, out_features, in_features, lddw}, db{dbias, 1, out_features, out_features};
+    int rc;
+    if ((rc = check_bf16(dy)) != MOSAIC_OK) return rc;
+    if (dW != nullptr && ((rc = check_bf16(x)) != MOSAIC_OK || (rc = check_bf16(dw)) != MOSAIC_OK)) return rc;
+    if (dX != nullptr && ((rc = check_bf16(w)) != MOSAIC_OK || (rc = check_bf16(dx)) != MOSAIC_OK)) return rc;
+    if (act != MOSAIC_ACT_NONE && (rc = check_bf16(z)) != MOSAIC_OK) return rc;
+    if (dbias != nullptr && (rc = check_bf16(db)) != MOSAIC_OK) return rc;
+    if ((reinterpret_cast<uintptr_t>(status_dev) & 3u) != 0) return MOSAIC_ERR_MISALIGNED;
+    {   // outputs overlap neither inputs nor one another
+        const Matrix in[4] = {dy, dW != nullptr ? x : Matrix{}, dX != nullptr ? w : Matrix{}, act != MOSAIC_ACT_NONE ? z : Matrix{}};
+        const Matrix out[3] = {dx, dw, db};
+        for (int o = 0; o < 3; ++o) {
+            for (int i = 0; i < 4; ++i)
+                if (overlap(out[o], in[i])) return MOSAIC_ERR_ALIASING;
+            for (int i = o + 1; i < 3; ++i)
+                if (overlap(out[o], out[i])) return MOSAIC_ERR_ALIASING;
+        }
+    }
+    if ((rc = check_workspace(ws, ws_bytes, backward_workspace(dy, x, w, act, dX != nullptr, dW != nullptr, dbias != nullptr))) != MOSAIC_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (status_dev != nullptr) MOSAIC_CUDA_TRY(cudaMemsetAsync(status_dev, 0, sizeof(int), st));
+    char* scratch = static_cast<char*>(ws);
+    float* partial = nullptr;
+    if (dbias != nullptr) {
+        partial = reinterpret_cast<float*>(scratch);
+        scratch += align_up((size_t)bands_of(tokens) * (size_t)out_features * 4u, 256);
+    }
+    const bool products = dX != nullptr || dW != nullptr;
+    const bool copy = products && tokens > 0 && (act != MOSAIC_ACT_NONE || !dy.tma_ok());
+    if (copy || dbias != nullptr) {
+        if ((rc = run_slope(dy, act != MOSAIC_ACT_NONE ? Z : nullptr, ldz, act, copy ? scratch : nullptr, dy.padded_ld(), partial, dbias, st)) != MOSAIC_OK) return rc;
+        if (copy) {
+            dy.p = scratch;
+            dy.ld = dy.padded_ld();
+            scratch += dy.padded_bytes();
+        }
+    }
+    if (tokens == 0) {   // an empty sum
+        if (dW != nullptr) MOSAIC_CUDA_TRY(cudaMemset2DAsync(dW, (size_t)lddw * 2u, 0, (size_t)in_features * 2u, (size_t)out_features, st));
+        return MOSAIC_OK;
+    }
+    if (dX != nullptr) {
+        if ((rc = readable(w, &scratch, st)) != MOSAIC_OK) return rc;
+        MmArgs a = {};
+        a.n_i = in_features; a.n_j = tokens; a.n_c = out_features;
+        a.out = static_cast<uint16_t*>(dX); a.ld_out = lddx; a.status = status_dev;
+        if ((rc = run_mm<true, false>(w, dy, a, st)) != MOSAIC_OK) return rc;
+    }
+    if (dW != nullptr) {
+        if ((rc = readable(x, &scratch, st)) != MOSAIC_OK) return rc;
+        MmArgs a = {};
+        a.n_i = in_features; a.n_j = out_features; a.n_c = tokens;
+        a.out = static_cast<uint16_t*>(dW); a.ld_out = lddw; a.status = status_dev;
+        if ((rc = run_mm<true, true>(x, dy, a, st)) != MOSAIC_OK) return rc;
+    }
+    return MOSAIC_OK;
+}
