@@ -17,7 +17,7 @@ namespace cg = cooperative_groups;
 namespace mosaic {
 namespace {
 
-struct DistillArgs {
+struct DistillArgs {   // (rows and leading dimensions in elements)
     const void* S;
     void* dS;
     int64_t rows, vocab, lds, ldd;
@@ -28,33 +28,34 @@ struct DistillArgs {
     const float* row_weight;
     const float* grad_rows;
     float grad_scale;
-    double inv_t, t;
-    float c;          // log2(e) / T
+    double inv_t;
+    float t, c;       // T, log2(e) / T
+    int slots;        // of the table of kept places: a power of two, at least 2 * top
     float* loss;
     float* lse;
 };
 
 constexpr int kWantLoss = 1, kWantGrad = 2;
 
-__device__ __forceinline__ double warp_max(double v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-    return v;
-}
+// A kept logit's probability under the teacher's own log-sum-exp.
+__device__ __forceinline__ float teacher_p(float t, float t_lse, double inv_t) { return expf((float)((double)t * inv_t - (double)t_lse)); }
 
 // One row by a cluster of CTAs.  MODE: what is wanted; with kWantGrad alone the saved log-sum-exp is an input.
+// Every thread takes its share of the kept entries (loads in flight beside the row's), so that the row's and the
+// teacher's statistics meet in one barrier.
 template <int DT, int MODE>
-__global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const __grid_constant__ DistillArgs a) {
+__global__ void __launch_bounds__(kRowThreads, kRowCtasPerSm) distill_kernel(const __grid_constant__ DistillArgs a) {
     using RV = RowVec<DT>;
     using Elem = typename RV::Elem;
     __shared__ SoftStat warp_stat[kRowWarps];
     __shared__ SoftStat cta_stat[kMaxCluster];   // written by the CTAs of the cluster
-    __shared__ float mass_s;                     // P
+    __shared__ SoftStat kept_stat[kRowWarps];    // renormalised: softmax statistics of the kept entries; else the sum of their p in .s
+    __shared__ double warp_loss[kRowWarps];
     __shared__ int doubled;                      // some vocabulary entry is kept twice
     extern __shared__ unsigned char dyn[];
-    int32_t* k_idx = reinterpret_cast<int32_t*>(dyn);          // [top] -1: absent
-    float* k_p = reinterpret_cast<float*>(k_idx + a.top);      // [top]
-    float* k_x = k_p + a.top;                                  // [top] the student's logit there
+    int32_t* k_idx = reinterpret_cast<int32_t*>(dyn);             // [top] -1: absent
+    float* k_t = reinterpret_cast<float*>(k_idx + a.top);         // [top] the teacher's logit, later its probability
+    float* k_x = k_t + a.top;                                     // [top] the student's logit there
     uint32_t* table = reinterpret_cast<uint32_t*>(k_x + a.top);   // [slots] entries seen, to find doubled ones
 
     cg::cluster_group cluster = cg::this_cluster();
@@ -66,66 +67,62 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const __grid_co
     const bool held = part.v_hi - part.v_lo <= kRowThreads * kRowVecs;   // the CTA's part stays in registers between the passes
     const float weight = a.row_weight != nullptr ? a.row_weight[r] : 1.0f;
     const bool reads = (MODE & kWantLoss) != 0 || weight != 0.0f;   // a dropped row's gradient is zero whatever it holds
-    int slots = 64;
-    while (slots < 2 * a.top) slots *= 2;
+    const bool given = a.t_lse != nullptr;
+    const int lone = part.single();
 
     uint4 raw[kRowVecs];
     if (reads) part.load_pass(part.v_lo, raw);
-
+    const float lone_x = reads && lone >= 0 ? part.at(lone) : -INFINITY;
     cg::cluster_group::arrival_token started = cluster.barrier_arrive();   // waited for before the first write to another CTA
 
-    // ---- the kept entries: one warp, while the row is on its way
-    if (threadIdx.x == 32) doubled = 0;
-    if (MODE & kWantGrad)
-        for (int i = threadIdx.x; i < slots; i += kRowThreads) table[i] = 0xFFFFFFFFu;
-    const float* tv = a.t_values + r * a.top;
-    double norm = 0.0;   // warp 0: log of what the kept entries' exponentials are divided by
-    if (warp == 0) {
+    // ---- the kept entries, while the row is on its way
+    const float t_lse = given ? a.t_lse[r] : 0.0f;
+    {
+        const float* tv = a.t_values + r * a.top;
         const int32_t* ti = a.t_indices + r * a.top;
-        double top_u = -INFINITY;
-        for (int i = lane; i < a.top; i += 32) {
+        SoftStat kst = {-INFINITY, 0.0f};
+        for (int i = threadIdx.x; i < a.top; i += kRowThreads) {
             const int32_t j = ti[i];
             const bool there = j >= 0 && j < vocab;
+            const float t = there ? tv[i] : -INFINITY;
             k_idx[i] = there ? j : -1;
             // gathered before any gradient is written (dS may be S); without the loss only the own part's are used
             k_x[i] = there && reads && ((MODE & kWantLoss) || part.owns(j)) ? part.at(j) : 0.0f;
-            if (there) top_u = fmax(top_u, (double)tv[i] * a.inv_t);
+            k_t[i] = t;
+            if (given) kst.s = __fadd_rn(kst.s, teacher_p(t, t_lse, a.inv_t));
+            else kst = soft_merge(kst, soft_one(t, a.c), a.c);
         }
-        if (a.t_lse != nullptr) {
-            norm = (double)a.t_lse[r];
+        if (given) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) kst.s = __fadd_rn(kst.s, __shfl_xor_sync(0xFFFFFFFFu, kst.s, o));
         } else {
-            top_u = warp_max(top_u);
-            if (!(fabs(top_u) <= 1.7e308)) top_u = 0.0;   // no finite entry
-            double s = 0.0;
-            for (int i = lane; i < a.top; i += 32)
-                if (k_idx[i] >= 0) s += exp((double)tv[i] * a.inv_t - top_u);
-            norm = top_u + log(warp_sum(s));
+            kst = soft_warp(kst, a.c);
         }
-        double mass = 0.0;
-        for (int i = lane; i < a.top; i += 32) {
-            double p = 0.0;
-            const double u = (double)tv[i] * a.inv_t;
-            if (k_idx[i] >= 0 && u != -INFINITY) p = exp(u - norm);
-            k_p[i] = (float)p;
-            mass += p;
+        if (lane == 0) kept_stat[warp] = kst;
+        if (MODE & kWantGrad) {
+            if (threadIdx.x == 0) doubled = 0;
+            for (int i = threadIdx.x; i < a.slots; i += kRowThreads) table[i] = 0xFFFFFFFFu;
         }
-        mass = warp_sum(mass);
-        if (lane == 0) mass_s = (float)mass;
     }
 
     // ---- softmax statistics of the row
     SoftStat st = {-INFINITY, 0.0f};
     if (MODE & kWantLoss) {
-        soft_pass<DT>(raw, a.c, st);
-        for (int b = part.v_lo + kRowThreads * kRowVecs; b < part.v_hi; b += kRowThreads * kRowVecs) {
-            part.load_pass(b, raw);
-            soft_pass<DT>(raw, a.c, st);
-        }
-        st = soft_warp(st, a.c);
+        st = soft_warp(soft_part<DT>(part, raw, lone_x, a.c), a.c);
         if (lane == 0) warp_stat[warp] = st;
     }
     cluster.barrier_wait(std::move(started));
     __syncthreads();
+    SoftStat kst = {0.0f, 0.0f};
+    float mass;   // P
+    if (given) {
+        mass = lane < kRowWarps ? kept_stat[lane].s : 0.0f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mass = __fadd_rn(mass, __shfl_xor_sync(0xFFFFFFFFu, mass, o));
+    } else {
+        kst = soft_all(kept_stat, kRowWarps, a.c);
+        mass = kst.s == 0.0f ? 0.0f : __fdiv_rn(kst.s, kst.s);   // 1; NaN stays NaN
+    }
     if (MODE & kWantLoss) {
         st = soft_all(warp_stat, kRowWarps, a.c);
         if (n_ctas > 1) {
@@ -133,105 +130,114 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const __grid_co
             cluster.sync();   // also: every CTA has gathered its kept entries' logits
             st = soft_all(cta_stat, n_ctas, a.c);
         }
-        if (rank == 0 && warp == 0) {
-            const double lse = soft_lse(st, a.inv_t);
-            double sum = 0.0;
-            for (int i = lane; i < a.top; i += 32) {
-                const double p = (double)k_p[i];
-                if (p != 0.0) sum += p * (((double)tv[i] * a.inv_t - norm) - ((double)k_x[i] * a.inv_t - lse));
-            }
-            sum = warp_sum(sum);
-            if (lane == 0) {
-                a.loss[r] = weight != 0.0f ? (float)((double)weight * a.t * a.t * sum) : 0.0f;
-                if (a.lse != nullptr) a.lse[r] = (float)lse;
-            }
+    }
+
+    // ---- the kept entries' probabilities, and the loss in fp64: differences of logarithms that nearly cancel
+    const float kept_inv = __frcp_rn(kst.s), kept_ref = soft_ref(kst.m);
+    double sum = 0.0;
+    if ((int)threadIdx.x < a.top) {
+        double lse = 0.0, norm = 0.0;
+        if ((MODE & kWantLoss) && rank == 0) {
+            lse = soft_lse(st, a.inv_t);
+            norm = given ? (double)t_lse : soft_lse(kst, a.inv_t);
+            if (threadIdx.x == 0 && a.lse != nullptr) a.lse[r] = (float)lse;
+        }
+        for (int i = threadIdx.x; i < a.top; i += kRowThreads) {
+            const float t = k_t[i];
+            float p = given ? teacher_p(t, t_lse, a.inv_t) : __fmul_rn(exp2_fast(__fmul_rn(__fsub_rn(t, kept_ref), a.c)), kept_inv);
+            if (t == -INFINITY) p = 0.0f;
+            k_t[i] = p;
+            if ((MODE & kWantLoss) && rank == 0 && p != 0.0f)
+                sum += (double)p * (((double)t * a.inv_t - norm) - ((double)k_x[i] * a.inv_t - lse));
         }
     }
-    if (!(MODE & kWantGrad)) return;
-
-    // ---- gradient
-    const float mass = mass_s;
+    if ((MODE & kWantLoss) && rank == 0) {
+        if (warp * 32 < a.top) sum = warp_sum(sum);
+        if (lane == 0) warp_loss[warp] = sum;
+    }
     const bool zero = weight == 0.0f || mass == 0.0f;
-    const float coef = (float)((a.grad_rows != nullptr ? (double)a.grad_rows[r] : 1.0) * (double)a.grad_scale * (double)weight * a.t);
-    // q_j = 2^((x_j - ref) c) * scale;  from a saved log-sum-exp L: ref = L T and scale = 1
-    float ref, scale;
-    if (MODE & kWantLoss) {
-        ref = soft_ref(st.m);
-        scale = (float)(1.0 / (double)st.s);
-    } else {
-        ref = 0.0f;
-        scale = 1.0f;
-    }
-    const float inv_t = (float)a.inv_t;
-    const float minus_lse = (MODE & kWantLoss) || zero ? 0.0f : -a.lse[r];
-    const float dense = __fmul_rn(__fmul_rn(coef, mass), scale);
-    auto q_of = [&](float x) -> float {   // without `scale`
-        if (MODE & kWantLoss) return exp2_fast(__fmul_rn(__fsub_rn(x, ref), a.c));
-        return exp2_fast(__fmul_rn(__fmaf_rn(x, inv_t, minus_lse), 1.4426950408889634f));
-    };
-    Elem* out = reinterpret_cast<Elem*>(a.dS) + r * a.ldd;
-    const bool aligned = (((reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(part.row)) & 15u) == 0);
-    for (int b = part.v_lo; b < part.v_hi; b += kRowThreads * kRowVecs) {
-        if (!held && !zero) part.load_pass(b, raw);
-        keep_packed(raw);
-#pragma unroll
-        for (int i = 0; i < kRowVecs; ++i) {
-            const int v = b + (int)threadIdx.x + i * kRowThreads;
-            if (v < part.v_hi) {
-                float f[RV::kElems];
-#pragma unroll
-                for (int e = 0; e < RV::kElems; ++e) f[e] = zero ? 0.0f : __fmul_rn(q_of(RV::get(raw[i], e)), dense);
-                const int j = part.first(v);
-                if (aligned && part.whole(v)) {
-                    st_stream16(out + j, RV::pack(f));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < RV::kElems; ++e)
-                        if (j + e >= 0 && j + e < vocab) out[j + e] = RV::narrow(f[e]);
-                }
-            }
-        }
-    }
-    if (zero) return;
 
-    // ---- the kept entries' correction: their whole value, from the gathered logit
-    for (int i = threadIdx.x; i < a.top; i += kRowThreads) {
-        const int32_t j = k_idx[i];
-        if (j >= 0) {   // open addressing; a second entry for the same place is noted
-            uint32_t h = ((uint32_t)j * 2654435761u) & (uint32_t)(slots - 1);
-            for (;;) {
-                const uint32_t old = atomicCAS(&table[h], 0xFFFFFFFFu, (uint32_t)j);
-                if (old == 0xFFFFFFFFu) break;
-                if (old == (uint32_t)j) {
-                    doubled = 1;
-                    break;
+    if (MODE & kWantGrad) {
+        const float coef = __fmul_rn(__fmul_rn(__fmul_rn(a.grad_rows != nullptr ? a.grad_rows[r] : 1.0f, a.grad_scale), weight), a.t);
+        // P q_j coef = 2^((x_j - ref) c) * dense;  from a saved log-sum-exp L: 2^((x_j / T - L) log2 e) * dense
+        const float ref = soft_ref(st.m), inv_t = (float)a.inv_t;
+        const float minus_lse = (MODE & kWantLoss) || zero ? 0.0f : -a.lse[r];
+        const float dense = (MODE & kWantLoss) ? __fmul_rn(__fmul_rn(coef, mass), __frcp_rn(st.s)) : __fmul_rn(coef, mass);
+        auto dense_of = [&](float x) -> float {
+            if (MODE & kWantLoss) return __fmul_rn(exp2_fast(__fmul_rn(__fsub_rn(x, ref), a.c)), dense);
+            return __fmul_rn(exp2_fast(__fmul_rn(__fmaf_rn(x, inv_t, minus_lse), 1.4426950408889634f)), dense);
+        };
+        Elem* out = reinterpret_cast<Elem*>(a.dS) + r * a.ldd;
+        const bool aligned = (reinterpret_cast<uintptr_t>(out + part.head) & 15u) == 0;
+        if (lone >= 0) out[lone] = RV::narrow(zero ? 0.0f : dense_of(lone_x));
+        for (int b = part.v_lo; b < part.v_hi; b += kRowThreads * kRowVecs) {
+            if (!held && !zero) part.load_pass(b, raw);
+            keep_packed(raw);
+#pragma unroll
+            for (int i = 0; i < kRowVecs; ++i) {
+                const int v = b + (int)threadIdx.x + i * kRowThreads;
+                if (v < part.v_hi) {
+                    float f[RV::kElems];
+#pragma unroll
+                    for (int e = 0; e < RV::kElems; ++e) f[e] = zero ? 0.0f : dense_of(RV::get(raw[i], e));
+                    Elem* o = out + part.first(v);
+                    if (aligned) {
+                        st_stream16(o, RV::pack(f));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < RV::kElems; ++e) o[e] = RV::narrow(f[e]);
+                    }
                 }
-                h = (h + 1u) & (uint32_t)(slots - 1);
             }
         }
-    }
-    __syncthreads();   // the dense values of this CTA's part are written, the table is complete
-    for (int i = threadIdx.x; i < a.top; i += kRowThreads) {
-        const int32_t j = k_idx[i];
-        if (j < 0 || !part.owns(j)) continue;
-        float p = k_p[i];
-        if (doubled) {   // every copy of the entry writes the same sum
-            p = 0.0f;
-            for (int o = 0; o < a.top; ++o)
-                if (k_idx[o] == j) p = __fadd_rn(p, k_p[o]);
+        if (!zero) {
+            for (int i = threadIdx.x; i < a.top; i += kRowThreads) {
+                const int32_t j = k_idx[i];
+                if (j >= 0) {   // open addressing; a second entry for the same place is noted
+                    uint32_t h = ((uint32_t)j * 2654435761u) & (uint32_t)(a.slots - 1);
+                    for (;;) {
+                        const uint32_t old = atomicCAS(&table[h], 0xFFFFFFFFu, (uint32_t)j);
+                        if (old == 0xFFFFFFFFu) break;
+                        if (old == (uint32_t)j) {
+                            doubled = 1;
+                            break;
+                        }
+                        h = (h + 1u) & (uint32_t)(a.slots - 1);
+                    }
+                }
+            }
         }
-        out[j] = RV::narrow(__fsub_rn(__fmul_rn(q_of(k_x[i]), dense), __fmul_rn(coef, p)));
+        __syncthreads();   // the dense values of this CTA's part are written, the table and the losses are complete
+        // the kept entries' places: their whole value, from the gathered logit
+        if (!zero) {
+            for (int i = threadIdx.x; i < a.top; i += kRowThreads) {
+                const int32_t j = k_idx[i];
+                if (j < 0 || !part.owns(j)) continue;
+                float p = k_t[i];
+                if (doubled) {   // every copy of the entry writes the same sum
+                    p = 0.0f;
+                    for (int o = 0; o < a.top; ++o)
+                        if (k_idx[o] == j) p = __fadd_rn(p, k_t[o]);
+                }
+                out[j] = RV::narrow(__fsub_rn(dense_of(k_x[i]), __fmul_rn(coef, p)));
+            }
+        }
+    } else {
+        __syncthreads();
+    }
+    if ((MODE & kWantLoss) && rank == 0 && threadIdx.x == 0) {
+        double total = 0.0;
+        for (int w = 0; w < kRowWarps; ++w) total += warp_loss[w];
+        a.loss[r] = zero ? 0.0f : (float)((double)weight * (double)a.t * (double)a.t * total);
     }
 }
 
 template <int DT, int MODE> int launch_distill(const DistillArgs& a, cudaStream_t st) {
     const int c = row_cluster(a.rows, row_vectors(a.vocab, DT));
-    int slots = 64;
-    while (slots < 2 * a.top) slots *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.rows * c));
     cfg.blockDim = dim3(kRowThreads);
-    cfg.dynamicSmemBytes = (size_t)a.top * 12u + (size_t)slots * 4u;   // at most 20 KB
+    cfg.dynamicSmemBytes = (size_t)a.top * 12u + (size_t)a.slots * 4u;   // at most 20 KB
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -281,7 +287,9 @@ template <int MODE> int distill(DistillArgs a, int64_t top, float temperature, i
         for (int i = o + 1; i < 3; ++i)
             if (overlap(out[o], out_n[o], out[i], out_n[i])) return MOSAIC_ERR_ALIASING;
     }
-    a.t = (double)temperature;
+    a.t = temperature;
+    a.slots = 64;
+    while (a.slots < 2 * a.top) a.slots *= 2;
     a.inv_t = 1.0 / (double)temperature;
     a.c = (float)(1.4426950408889634 / (double)temperature);
     cudaStream_t st = static_cast<cudaStream_t>(stream);

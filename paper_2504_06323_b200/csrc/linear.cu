@@ -43,10 +43,36 @@ struct MmArgs {
     int* status;
 };
 
-__device__ __forceinline__ float finish(const MmArgs& a, float v, float bias, int64_t i, int64_t j, float resid) {
-    v = __fadd_rn(v, bias);
-    if (a.z != nullptr) a.z[j * a.ld_z + i] = f32_to_bf16(v);
-    return __fadd_rn(activate(v, a.act), resid);
+// Sixteen accumulator columns of a lane into the output: v[e] belongs to element (i, j + e), e < n.
+__device__ __forceinline__ void epilogue16(const MmArgs& a, float (&v)[16], float bias, int64_t i, int64_t j, int n) {
+    float r[16];
+    if (a.resid != nullptr) {
+        const uint16_t* p = a.resid + j * a.ld_resid + i;
+#pragma unroll
+        for (int e = 0; e < 16; ++e, p += a.ld_resid) r[e] = e < n ? bf16_to_f32(*p) : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = __fadd_rn(v[e], bias);
+    if (a.z != nullptr) {
+        uint16_t* p = a.z + j * a.ld_z + i;
+#pragma unroll
+        for (int e = 0; e < 16; ++e, p += a.ld_z)
+            if (e < n) *p = f32_to_bf16(v[e]);
+    }
+    if (a.act != MOSAIC_ACT_NONE) activate_all(v, a.act);
+    if (a.resid != nullptr) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = __fadd_rn(v[e], r[e]);
+    }
+    uint16_t* p = a.out + j * a.ld_out + i;
+    if (n == 16) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e, p += a.ld_out) *p = f32_to_bf16(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e, p += a.ld_out)
+            if (e < n) *p = f32_to_bf16(v[e]);
+    }
 }
 
 // One output tile of kMI x BN per cluster; its contraction is split over the cluster's CTAs, whose partial
@@ -154,13 +180,7 @@ __global__ void __launch_bounds__(kMThreads) mm_kernel(const __grid_constant__ C
 #pragma unroll
                 for (int e = 0; e < 16; ++e) part[(c0 + e) * kMI + q * 32 + lane] = v[e];
             } else if (i < a.n_i) {
-                float r[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    r[e] = a.resid != nullptr && c0 + e < n_cols ? bf16_to_f32(a.resid[(j0 + c0 + e) * a.ld_resid + i]) : 0.0f;
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (c0 + e < n_cols) a.out[(j0 + c0 + e) * a.ld_out + i] = f32_to_bf16(finish(a, v[e], bias, i, j0 + c0 + e, r[e]));
+                epilogue16(a, v, bias, i, j0 + c0, n_cols - c0 < 16 ? n_cols - c0 : 16);
             }
         }
     }
@@ -197,11 +217,179 @@ __global__ void __launch_bounds__(kMThreads) mm_kernel(const __grid_constant__ C
             if (oi < a.n_i) {
                 const float bias = a.bias != nullptr ? bf16_to_f32(a.bias[oi]) : 0.0f;
                 const float r = a.resid != nullptr ? bf16_to_f32(a.resid[oj * a.ld_resid + oi]) : 0.0f;
-                a.out[oj * a.ld_out + oi] = f32_to_bf16(finish(a, sum, bias, oi, oj, r));
+                sum = __fadd_rn(sum, bias);
+                if (a.z != nullptr) a.z[oj * a.ld_z + oi] = f32_to_bf16(sum);
+                a.out[oj * a.ld_out + oi] = f32_to_bf16(__fadd_rn(activate(sum, a.act), r));
             }
         }
         cluster.sync();   // nobody leaves while its partial tile is being read
     }
+}
+
+// ---------------------------------------------------------------- large products
+// Two CTAs (a cluster, two SMs) share each matrix instruction: 256 x 256 output elements, each CTA holding its half
+// of both operands in shared memory (32 KB a stage for 256 x 256 x 64 products: half of what a CTA alone would have
+// to load for the same work) and 128 x 256 of the accumulator in its tensor memory, twice: the epilogue of a tile
+// runs under the products of the next.  Persistent: a pair takes tile after tile.  The tiles go band by band
+// (kPBand tiles of output rows), so that the tiles in flight share operands in L2.
+constexpr int kPTile = 256, kPHalf = 128;
+constexpr int kPStages = 6;
+constexpr uint32_t kPOperand = kPHalf * kMC * 2, kPStage = 2 * kPOperand;
+constexpr int kPEpiWarps = 8;
+constexpr int kPThreads = 64 + 32 * kPEpiWarps;
+constexpr int kPBand = 8;
+constexpr size_t kPSmem = (size_t)kPStages * kPStage + 1024;
+
+__device__ __forceinline__ void pair_tile(int tile, int tiles_i, int tiles_j, int* ti, int* tj) {
+    const int band = tile / (kPBand * tiles_i), in = tile - band * kPBand * tiles_i;
+    const int width = tiles_j - band * kPBand < kPBand ? tiles_j - band * kPBand : kPBand;
+    *ti = in / width;
+    *tj = band * kPBand + in % width;
+}
+
+template <bool A_MN, bool B_MN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
+    mm_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ MmArgs a, int tiles) {
+    constexpr uint32_t kDesc = instr_desc(A_MN, B_MN, kPTile, kPTile);
+    extern __shared__ unsigned char pair_smem_raw[];
+    __shared__ uint64_t full[kPStages], empty[kPStages], acc_full[2], acc_empty[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int err_word;
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pair_smem_raw) + 1023u) & ~(uintptr_t)1023u);
+    volatile int* err = &err_word;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
+    const int steps = (int)((a.n_c + kMC - 1) / kMC);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kPStages; ++s) {
+            mbar_init(&full[s], 1u);    // first CTA's: both CTAs' loads of a stage have landed
+            mbar_init(&empty[s], 1u);   // the products reading a stage have completed
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&acc_full[b], 1u);
+            mbar_init(&acc_empty[b], 2u * kPEpiWarps);   // first CTA's: both epilogues have read the accumulator
+        }
+        *err = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    cluster.sync();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    uint32_t issued = 0;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (int tile = pair; tile < tiles && ok; tile += pairs) {
+                int ti, tj;
+                pair_tile(tile, a.tiles_i, a.tiles_j, &ti, &tj);
+                const int i0 = ti * kPTile + rank * kPHalf, j0 = tj * kPTile + rank * kPHalf;
+                for (int s = 0; s < steps; ++s, ++it) {
+                    const uint32_t slot = it % kPStages, ph = (it / kPStages) & 1u;
+                    if (!mbar_wait(&empty[slot], ph ^ 1u, err)) {
+                        ok = false;
+                        break;
+                    }
+                    unsigned char* sa = ring + (size_t)slot * kPStage;
+                    unsigned char* sb = sa + kPOperand;
+                    if (rank == 0) mbar_expect_tx(&full[slot], 2u * kPStage);
+                    const uint32_t bar = cluster_addr(&full[slot], 0u);
+                    if (A_MN) {
+                        tma_load_box_pair(sa, &a_map, bar, i0, s * kMC);
+                        tma_load_box_pair(sa + kMBox, &a_map, bar, i0 + 64, s * kMC);
+                    } else {
+                        tma_load_box_pair(sa, &a_map, bar, s * kMC, i0);
+                    }
+                    if (B_MN) {
+                        tma_load_box_pair(sb, &b_map, bar, j0, s * kMC);
+                        tma_load_box_pair(sb + kMBox, &b_map, bar, j0 + 64, s * kMC);
+                    } else {
+                        tma_load_box_pair(sb, &b_map, bar, s * kMC, j0);
+                    }
+                }
+            }
+            issued = it;
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            uint32_t it = 0, n = 0;
+            bool ok = true;
+            for (int tile = pair; tile < tiles && ok; tile += pairs, ++n) {
+                const uint32_t buf = n & 1u;
+                if (!mbar_wait_cluster(&acc_empty[buf], ((n >> 1) & 1u) ^ 1u, err)) break;
+                tc_fence_after();
+                for (int s = 0; s < steps; ++s, ++it) {
+                    const uint32_t slot = it % kPStages, ph = (it / kPStages) & 1u;
+                    if (!mbar_wait_cluster(&full[slot], ph, err)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(ring + (size_t)slot * kPStage), sb = sa + kPOperand;
+#pragma unroll
+                    for (int kk = 0; kk < kMC / 16; ++kk) {
+                        const uint64_t da = operand_desc(sa + (uint32_t)kk * (A_MN ? 2048u : 32u), A_MN ? kMBox : 16u);
+                        const uint64_t db = operand_desc(sb + (uint32_t)kk * (B_MN ? 2048u : 32u), B_MN ? kMBox : 16u);
+                        umma_bf16_pair(tmem + buf * 256u, da, db, kDesc, (s > 0 || kk > 0) ? 1u : 0u);
+                    }
+                    umma_commit_pair(&empty[slot]);
+                }
+                if (ok) umma_commit_pair(&acc_full[buf]);
+            }
+        }
+    } else {
+        const int q = warp & 3, half = (warp - 2) >> 2;   // quarter of the lanes, half of the columns
+        uint32_t n = 0;
+        for (int tile = pair; tile < tiles; tile += pairs, ++n) {
+            int ti, tj;
+            pair_tile(tile, a.tiles_i, a.tiles_j, &ti, &tj);
+            const uint32_t buf = n & 1u;
+            const int64_t i = (int64_t)ti * kPTile + rank * kPHalf + q * 32 + lane, j0 = (int64_t)tj * kPTile;
+            const int n_cols = (int)(a.n_j - j0 < kPTile ? a.n_j - j0 : kPTile);
+            const float bias = a.bias != nullptr && i < a.n_i ? bf16_to_f32(a.bias[i]) : 0.0f;
+            if (!mbar_wait(&acc_full[buf], (n >> 1) & 1u, err)) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c0 = half * 128; c0 < half * 128 + 128 && c0 < n_cols; c0 += 16) {
+                float v[16];
+                tmem_load16(tmem + ((uint32_t)(q * 32) << 16) + buf * 256u + (uint32_t)c0, v);
+                if (i < a.n_i) epilogue16(a, v, bias, i, j0 + c0, n_cols - c0 < 16 ? n_cols - c0 : 16);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(cluster_addr(&acc_empty[buf], 0u));
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    cluster.sync();   // all products and reads of both CTAs are done, or a wait ran out and every role has left
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+    if (threadIdx.x == 0) {
+        const bool failed = *err != 0 || *cluster.map_shared_rank(&err_word, rank ^ 1) != 0;
+        if (failed && rank == 0) {   // let both CTAs' last loads land before shared memory is left (bounded)
+            for (uint32_t back = 1; back <= (uint32_t)kPStages && back <= issued; ++back) {
+                const uint32_t it = issued - back, slot = it % kPStages, ph = (it / kPStages) & 1u;
+                const long long t0 = clock64();
+                while (!mbar_try_wait(&full[slot], ph) && clock64() - t0 < kWaitCycles) {
+                }
+            }
+        }
+        if (failed && a.status != nullptr) atomicExch(a.status, 1);
+    }
+    cluster.sync();   // the error words have been read, the loads have landed
 }
 
 // ---------------------------------------------------------------- elementwise passes
@@ -315,6 +503,29 @@ int launch_mm(const Matrix& A, const Matrix& B, MmArgs a, cudaStream_t st) {
     return MOSAIC_OK;
 }
 
+template <bool A_MN, bool B_MN> int launch_pair(const Matrix& A, const Matrix& B, MmArgs a, cudaStream_t st) {
+    CUtensorMap a_map, b_map;
+    if (!(A_MN ? encode_bf16(&a_map, A.p, A.rows, A.cols, A.ld, kMC, 64) : encode_bf16(&a_map, A.p, A.rows, A.cols, A.ld, kPHalf, kMC))) return MOSAIC_ERR_CUDA;
+    if (!(B_MN ? encode_bf16(&b_map, B.p, B.rows, B.cols, B.ld, kMC, 64) : encode_bf16(&b_map, B.p, B.rows, B.cols, B.ld, kPHalf, kMC))) return MOSAIC_ERR_CUDA;
+    a.tiles_i = (int)((a.n_i + kPTile - 1) / kPTile);
+    a.tiles_j = (int)((a.n_j + kPTile - 1) / kPTile);
+    const int64_t tiles = (int64_t)a.tiles_i * a.tiles_j;
+    if (tiles > 0x3FFFFFFF) return MOSAIC_ERR_INVALID_ARG;
+    static DeviceCache opted;
+    const int ok = opted.get([&]() -> int {
+        if (cudaFuncSetAttribute(mm_pair_kernel<A_MN, B_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPSmem) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return -1;
+        }
+        return 1;
+    });
+    if (ok < 0) return MOSAIC_ERR_CUDA;
+    const int64_t pairs = sm_count() / 2;
+    mm_pair_kernel<A_MN, B_MN><<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), kPThreads, kPSmem, st>>>(a_map, b_map, a, (int)tiles);
+    MOSAIC_LAUNCH_CHECK();
+    return MOSAIC_OK;
+}
+
 // out[j, i] = sum_c A B; A: [n_i, n_c] (or [n_c, n_i] if A_MN), B likewise.
 template <bool A_MN, bool B_MN> int run_mm(const Matrix& A, const Matrix& B, const MmArgs& a, cudaStream_t st) {
     if constexpr (!B_MN) {   // narrow instructions for few output rows
@@ -322,6 +533,8 @@ template <bool A_MN, bool B_MN> int run_mm(const Matrix& A, const Matrix& B, con
         if (a.n_j <= 32) return launch_mm<A_MN, B_MN, 32>(A, B, a, st);
     }
     if (a.n_j <= 64) return launch_mm<A_MN, B_MN, 64>(A, B, a, st);
+    const int64_t tiles = ((a.n_i + kPTile - 1) / kPTile) * ((a.n_j + kPTile - 1) / kPTile);
+    if (tiles >= sm_count() / 2) return launch_pair<A_MN, B_MN>(A, B, a, st);
     return launch_mm<A_MN, B_MN, 128>(A, B, a, st);
 }
 

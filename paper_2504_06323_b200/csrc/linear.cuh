@@ -22,6 +22,19 @@ __device__ __forceinline__ float activate(float z, int act) {
         default: return z;
     }
 }
+// The same for a lane's run of values: one branch, then straight code.
+template <int N> __device__ __forceinline__ void activate_all(float (&v)[N], int act) {
+    if (act == MOSAIC_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = activate(v[e], MOSAIC_ACT_RELU);
+    } else if (act == MOSAIC_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = activate(v[e], MOSAIC_ACT_SILU);
+    } else if (act == MOSAIC_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = activate(v[e], MOSAIC_ACT_GELU);
+    }
+}
 // d activate(z) / dz
 __device__ __forceinline__ float activate_slope(float z, int act) {
     switch (act) {

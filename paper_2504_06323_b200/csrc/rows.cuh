@@ -2,10 +2,9 @@
 // distillation) read a row of any length, alignment and leading dimension, and the running maximum
 // and sum of a softmax over it.
 //
-// A row is cut into 16-byte vectors that start on 16-byte boundaries; the first and the last may hold
-// fewer than a whole vector's elements (an odd vocabulary, a dense matrix whose rows start anywhere).
-// Whole vectors are one 16-byte load, the two ragged ones are read element by element, and the places
-// outside the row are filled with -inf: nothing outside the row is read.
+// A row is its whole 16-byte vectors on 16-byte boundaries, one 16-byte load each, and at most a vector's
+// worth of single elements on either side of them (an odd vocabulary, a dense matrix whose rows start
+// anywhere), which the first threads of the row's first CTA take one each.  Nothing outside the row is read.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -16,6 +15,7 @@ namespace mosaic {
 
 constexpr int kRowThreads = 512;   // threads of a CTA
 constexpr int kRowVecs = 8;        // vectors a thread holds in registers (128 bytes: 64 KB of a row per CTA)
+constexpr int kRowCtasPerSm = 2;
 constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kMaxTop = 1024;      // kept logits per row
 constexpr int64_t kMaxRow = 0x7FFFFF00;   // elements of a row: column and vector numbers fit 32 bits with room to spare
@@ -31,11 +31,8 @@ inline int row_cluster(int64_t rows, int64_t vectors) {
     while (c < kMaxCluster && rows * c < sm_count() && vectors >= (int64_t)2 * c * kRowThreads) c *= 2;
     return c;
 }
-// Most vectors a row of `cols` elements can be cut into, whatever its alignment.
-inline int64_t row_vectors(int64_t cols, int dtype) {
-    const int64_t per = 16 / (int64_t)elem_size(dtype);
-    return (cols + 2 * per - 2) / per;
-}
+// Vectors of a row (at most; one fewer if it starts off a boundary).
+inline int64_t row_vectors(int64_t cols, int dtype) { return cols * (int64_t)elem_size(dtype) / 16; }
 
 #ifdef __CUDACC__
 // 2^x by the hardware's approximation (relative error about 2^-22, results below 2^-126 become 0).
@@ -65,10 +62,6 @@ template <> struct RowVec<MOSAIC_BF16> {
     __device__ static __forceinline__ uint4 pack(const float (&f)[8]) {
         return make_uint4(pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7]));
     }
-    __device__ static __forceinline__ void put(uint4& v, int e, Elem b) {
-        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-        w[e >> 1] = (e & 1) ? ((w[e >> 1] & 0xFFFFu) | ((uint32_t)b << 16)) : ((w[e >> 1] & 0xFFFF0000u) | b);
-    }
 };
 template <> struct RowVec<MOSAIC_F32> {
     static constexpr int kElems = 4;
@@ -82,51 +75,49 @@ template <> struct RowVec<MOSAIC_F32> {
     __device__ static __forceinline__ uint4 pack(const float (&f)[4]) {
         return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
     }
-    __device__ static __forceinline__ void put(uint4& v, int e, Elem b) { reinterpret_cast<uint32_t*>(&v)[e] = b; }
 };
 
-// One row and the part of its vectors that this CTA of the row's cluster owns.
+// One row and the part of it that this CTA of the row's cluster owns.
 template <int DT> struct RowPart {
     using RV = RowVec<DT>;
     using Elem = typename RV::Elem;
     const Elem* row;
     int cols;
-    int off;              // elements between the first vector's boundary and the row's first element
-    int v_lo, v_hi;   // this CTA's vectors
+    int head, tail;       // single elements before and after the whole vectors
+    int v_lo, v_hi;       // this CTA's vectors
+    bool first_cta;
 
     __device__ __forceinline__ RowPart(const void* base, int64_t r, int64_t ld, int cols_, int rank, int n_ctas) : cols(cols_) {
         row = reinterpret_cast<const Elem*>(base) + r * ld;
-        off = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(Elem));
-        const int nv = (cols + off + RV::kElems - 1) / RV::kElems;
+        const int mis = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(Elem));
+        head = mis == 0 ? 0 : (RV::kElems - mis < cols ? RV::kElems - mis : cols);
+        const int nv = (cols - head) / RV::kElems;
+        tail = cols - head - nv * RV::kElems;
         const int per = (nv + n_ctas - 1) / n_ctas;
         v_lo = rank * per < nv ? rank * per : nv;
         v_hi = v_lo + per < nv ? v_lo + per : nv;
+        first_cta = rank == 0;
     }
-    __device__ __forceinline__ int first(int vec) const { return vec * RV::kElems - off; }   // column of its element 0
-    __device__ __forceinline__ bool whole(int vec) const {
-        const int j = first(vec);
-        return j >= 0 && j + RV::kElems <= cols;
+    __device__ __forceinline__ int first(int vec) const { return head + vec * RV::kElems; }   // column of its element 0
+    // The column of the single element this thread takes, or -1.
+    __device__ __forceinline__ int single() const {
+        const int t = (int)threadIdx.x;
+        return first_cta && t < head + tail ? (t < head ? t : cols - tail + (t - head)) : -1;
     }
     __device__ __forceinline__ bool owns(int col) const {
-        const int v = (col + off) / RV::kElems;
+        if (col < head || col >= cols - tail) return first_cta;
+        const int v = (col - head) / RV::kElems;
         return v >= v_lo && v < v_hi;
     }
     __device__ __forceinline__ float at(int col) const { return RV::widen(row[col]); }
-    __device__ __forceinline__ uint4 load(int vec) const {
-        const int j = first(vec);
-        if (j >= 0 && j + RV::kElems <= cols) return ld_stream16(row + j);
-        uint4 v = make_uint4(RV::kFill, RV::kFill, RV::kFill, RV::kFill);
-#pragma unroll
-        for (int e = 0; e < RV::kElems; ++e)
-            if (j + e >= 0 && j + e < cols) RV::put(v, e, row[j + e]);
-        return v;
-    }
-    // The thread's vectors of one pass, all loads issued before the first is used.
+    // The thread's vectors of one pass, all loads issued before the first is used; -inf where there is none.
     __device__ __forceinline__ void load_pass(int base, uint4 (&raw)[kRowVecs]) const {
+        const Elem* p = row + head;
 #pragma unroll
         for (int i = 0; i < kRowVecs; ++i) {
             const int v = base + (int)threadIdx.x + i * kRowThreads;
-            raw[i] = v < v_hi ? load(v) : make_uint4(RV::kFill, RV::kFill, RV::kFill, RV::kFill);
+            raw[i] = make_uint4(RV::kFill, RV::kFill, RV::kFill, RV::kFill);
+            if (v < v_hi) raw[i] = ld_stream16(p + (int64_t)v * RV::kElems);
         }
     }
 };
@@ -148,14 +139,33 @@ __device__ __forceinline__ void keep_packed(uint4 (&raw)[kRowVecs]) {
 #pragma unroll
     for (int i = 0; i < kRowVecs; ++i) asm volatile("" : "+r"(raw[i].x), "+r"(raw[i].y), "+r"(raw[i].z), "+r"(raw[i].w));
 }
+// The largest of a thread's entries (NaN aside).
+template <int DT> __device__ __forceinline__ float pass_max(const uint4 (&raw)[kRowVecs]) {
+    using RV = RowVec<DT>;
+    if constexpr (DT == MOSAIC_BF16) {   // two entries an instruction
+        uint32_t m = raw[0].x;
+#pragma unroll
+        for (int i = 0; i < kRowVecs; ++i) {
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[e]));
+        }
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+    } else {
+        float m = RV::get(raw[0], 0);
+#pragma unroll
+        for (int i = 0; i < kRowVecs; ++i)
+#pragma unroll
+            for (int e = 0; e < RV::kElems; ++e) m = fmaxf(m, RV::get(raw[i], e));
+        return m;
+    }
+}
+// One entry's statistics.
+__device__ __forceinline__ SoftStat soft_one(float x, float c) { return {x, exp2_fast(__fmul_rn(__fsub_rn(x, soft_ref(x)), c))}; }
 // The thread's statistics of the vectors of one pass, merged into `st`.
 template <int DT> __device__ __forceinline__ void soft_pass(uint4 (&raw)[kRowVecs], float c, SoftStat& st) {
     using RV = RowVec<DT>;
-    float m = st.m;
-#pragma unroll
-    for (int i = 0; i < kRowVecs; ++i)
-#pragma unroll
-        for (int e = 0; e < RV::kElems; ++e) m = fmaxf(m, RV::get(raw[i], e));
+    const float m = fmaxf(st.m, pass_max<DT>(raw));
     keep_packed(raw);
     // (x - m) first, then the factor: near the maximum the difference is exact, so the factor's rounding
     // costs next to nothing there; folded into one multiply-add, m * c would shift every term alike.
@@ -171,6 +181,17 @@ template <int DT> __device__ __forceinline__ void soft_pass(uint4 (&raw)[kRowVec
     st.m = m;
     st.s = s;
 }
+// A whole part: its vectors (the first pass's are already in `raw`) and the thread's single element x (-inf: none).
+template <int DT>
+__device__ __forceinline__ SoftStat soft_part(const RowPart<DT>& part, uint4 (&raw)[kRowVecs], float x, float c) {
+    SoftStat st = {-INFINITY, 0.0f};
+    soft_pass<DT>(raw, c, st);
+    for (int b = part.v_lo + kRowThreads * kRowVecs; b < part.v_hi; b += kRowThreads * kRowVecs) {
+        part.load_pass(b, raw);
+        soft_pass<DT>(raw, c, st);
+    }
+    return part.single() >= 0 ? soft_merge(st, soft_one(x, c), c) : st;
+}
 // The warp's statistics in every lane.
 __device__ __forceinline__ SoftStat soft_warp(SoftStat st, float c) {
     float m = st.m;
@@ -181,13 +202,11 @@ __device__ __forceinline__ SoftStat soft_warp(SoftStat st, float c) {
     for (int o = 16; o > 0; o >>= 1) s = __fadd_rn(s, __shfl_xor_sync(0xFFFFFFFFu, s, o));
     return {m, s};
 }
-// Merges n statistics in their order; every thread that calls it gets the same value.
+// The merged statistics of n <= 32 parts, by a whole warp, in every lane.
 __device__ __forceinline__ SoftStat soft_all(const SoftStat* part, int n, float c) {
-    SoftStat a = part[0];
-    for (int i = 1; i < n; ++i) a.m = fmaxf(a.m, part[i].m);
-    a.s = 0.0f;
-    for (int i = 0; i < n; ++i) a.s = __fadd_rn(a.s, __fmul_rn(part[i].s, soft_scale(part[i].m, a.m, c)));
-    return a;
+    SoftStat st = {-INFINITY, 0.0f};
+    if ((int)(threadIdx.x & 31) < n) st = part[threadIdx.x & 31];
+    return soft_warp(st, c);
 }
 // log sum exp(x / T) of a row, from its statistics (c = log2(e) / T).
 __device__ __forceinline__ double soft_lse(SoftStat st, double inv_t) { return (double)soft_ref(st.m) * inv_t + log((double)st.s); }

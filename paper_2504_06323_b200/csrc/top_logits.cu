@@ -112,7 +112,7 @@ template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, To
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kRowThreads, 2) top_logits_kernel(const __grid_constant__ TopArgs a) {
+__global__ void __launch_bounds__(kRowThreads, kRowCtasPerSm) top_logits_kernel(const __grid_constant__ TopArgs a) {
     using RV = RowVec<DT>;
     __shared__ TopShared sh;
     cg::cluster_group cluster = cg::this_cluster();
@@ -128,14 +128,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) top_logits_kernel(const __grid
     if (threadIdx.x == 0) sh.count = 0u;
     cg::cluster_group::arrival_token started = cluster.barrier_arrive();
 
-    SoftStat st = {-INFINITY, 0.0f};
-    soft_pass<DT>(raw, a.c, st);
-    for (int b = part.v_lo + kRowThreads * kRowVecs; b < part.v_hi; b += kRowThreads * kRowVecs) {
-        part.load_pass(b, raw);
-        soft_pass<DT>(raw, a.c, st);
-    }
+    const int lone = part.single();
+    const float lone_x = lone >= 0 ? part.at(lone) : -INFINITY;
+    SoftStat st = soft_part<DT>(part, raw, lone_x, a.c);
     // the thread's largest entry, as a 16-bit pattern rounded down (a NaN makes the sum NaN: above all)
-    const uint32_t mine = part.v_lo + (int)threadIdx.x < part.v_hi ? (st.s != st.s ? 0xFFFFu : order_key(st.m) >> 16) : 0u;
+    const bool any = part.v_lo + (int)threadIdx.x < part.v_hi || lone >= 0;
+    const uint32_t mine = any ? (st.s != st.s ? 0xFFFFu : order_key(st.m) >> 16) : 0u;
 
     // the largest pattern that at least `top` of the threads' maxima reach (0: all entries are candidates)
     uint32_t floor_key = 0u;
@@ -168,6 +166,11 @@ __global__ void __launch_bounds__(kRowThreads, 2) top_logits_kernel(const __grid
         uint32_t* count = cluster.map_shared_rank(&sh.count, 0);
         uint64_t* list = cluster.map_shared_rank(sh.list, 0);
         const float least = floor_key == 0u ? -INFINITY : key_value(floor_key << 16);
+        auto take = [&](float x, int j) {
+            const uint32_t at = atomicAdd(count, 1u);
+            if (at < kListCap) list[at] = entry_of(order_key(x), j);
+        };
+        if (lone >= 0 && !(lone_x < least)) take(lone_x, lone);
         for (int b = part.v_lo; b < part.v_hi; b += kRowThreads * kRowVecs) {
             if (!held) part.load_pass(b, raw);
             keep_packed(raw);
@@ -178,13 +181,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) top_logits_kernel(const __grid
 #pragma unroll
                 for (int e = 0; e < RV::kElems; ++e) {
                     const float x = RV::get(raw[i], e);
-                    if (!(x < least)) {
-                        const int j = part.first(v) + e;
-                        if (v < part.v_hi && j >= 0 && j < vocab) {
-                            const uint32_t at = atomicAdd(count, 1u);
-                            if (at < kListCap) list[at] = entry_of(order_key(x), j);
-                        }
-                    }
+                    if (!(x < least) && v < part.v_hi) take(x, part.first(v) + e);
                 }
             }
         }
