@@ -1,10 +1,12 @@
-// Rows of logits in registers: how the kernels over a model's output distribution (top logits,
-// distillation) read a row of any length, alignment and leading dimension, and the running maximum
-// and sum of a softmax over it.
+// Rows of logits: how the kernels over a model's output distribution (top logits, distillation) read a row of
+// any length, alignment and leading dimension, and the running maximum and sum of a softmax over it.
 //
 // A row is its whole 16-byte vectors on 16-byte boundaries, one 16-byte load each, and at most a vector's
 // worth of single elements on either side of them (an odd vocabulary, a dense matrix whose rows start
 // anywhere), which the first threads of the row's first CTA take one each.  Nothing outside the row is read.
+// A thread streams over its vectors, kBatch loads in flight, and holds none: few registers, so that three
+// CTAs of 512 threads share an SM and one's loads run under another's exponentials and barriers (rows held
+// in registers, 64 KB per CTA and two CTAs an SM: 115 us instead of 75 for the top logits of 4096 x 32000).
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -13,26 +15,29 @@
 
 namespace mosaic {
 
-constexpr int kRowThreads = 512;   // threads of a CTA
-constexpr int kRowVecs = 8;        // vectors a thread holds in registers (128 bytes: 64 KB of a row per CTA)
-constexpr int kRowCtasPerSm = 2;
-constexpr int kRowWarps = kRowThreads / 32;
+constexpr int kThreads = 512;                // threads of a CTA
+constexpr int kWarps = kThreads / 32;
+constexpr int kBatch = 4;                    // vectors a thread has in flight
+constexpr int kRowCtas = 3;                  // CTAs an SM holds
+constexpr int kPartVecs = 4096;              // vectors of a row that a CTA takes before the row is shared by more
 constexpr int kMaxTop = 1024;      // kept logits per row
 constexpr int64_t kMaxRow = 0x7FFFFF00;   // elements of a row: column and vector numbers fit 32 bits with room to spare
 constexpr int kMaxCluster = 8;     // CTAs that share one row (the portable cluster size)
 
 // ---------------------------------------------------------------- host side
-// CTAs per row.  A CTA holds kRowThreads * kRowVecs vectors of a row in registers (read once); a longer
-// row is shared by a cluster, and where the rows alone would leave SMs idle a row is spread further, as
-// long as every thread keeps a vector.
+// CTAs per row: one for every kPartVecs vectors (64 KB), and where the rows alone would leave SMs idle a row is
+// spread further, as long as every thread keeps a vector.
 inline int row_cluster(int64_t rows, int64_t vectors) {
     int c = 1;
-    while (c < kMaxCluster && vectors > (int64_t)c * kRowThreads * kRowVecs) c *= 2;
-    while (c < kMaxCluster && rows * c < sm_count() && vectors >= (int64_t)2 * c * kRowThreads) c *= 2;
+    while (c < kMaxCluster && vectors > (int64_t)c * kPartVecs) c *= 2;
+    while (c < kMaxCluster && rows * c < sm_count() && vectors >= (int64_t)2 * c * kThreads) c *= 2;
     return c;
 }
 // Vectors of a row (at most; one fewer if it starts off a boundary).
 inline int64_t row_vectors(int64_t cols, int dtype) { return cols * (int64_t)elem_size(dtype) / 16; }
+
+// How many rows further a CTA asks L2 for while it works on its own: those that the CTAs after the resident ones take.
+inline int rows_ahead(int cluster) { return sm_count() * kRowCtas / cluster; }
 
 #ifdef __CUDACC__
 // 2^x by the hardware's approximation (relative error about 2^-22, results below 2^-126 become 0).
@@ -40,6 +45,39 @@ __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// The two halves of a barrier over the cluster's CTAs.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// Two fp32 values an instruction.
+struct Pair {
+    uint64_t v;
+};
+__device__ __forceinline__ Pair pair_of(float lo, float hi) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ void split(Pair p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p.v)); }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+// 2^((x - ref) c) of both.  (x - ref) first, then the factor: near the maximum the difference is exact, so the
+// factor's rounding costs next to nothing there; folded into one multiply-add, ref * c would shift every term
+// alike, and overflow for logits near the type's ends.
+__device__ __forceinline__ Pair soft_pair(float x0, float x1, Pair minus_ref, Pair c) {
+    float y0, y1;
+    split(mul2(add2(pair_of(x0, x1), minus_ref), c), y0, y1);
+    return pair_of(exp2_fast(y0), exp2_fast(y1));
 }
 
 template <int DT> struct RowVec;
@@ -51,6 +89,14 @@ template <> struct RowVec<MOSAIC_BF16> {
     __device__ static __forceinline__ float get(const uint4& v, int e) {
         const uint32_t w = (e >> 1) == 0 ? v.x : (e >> 1) == 1 ? v.y : (e >> 1) == 2 ? v.z : v.w;
         return __uint_as_float((e & 1) ? (w & 0xFFFF0000u) : (w << 16));
+    }
+    __device__ static __forceinline__ float any(const uint4& v, int e) {   // e not known at compile time
+        const uint32_t a = (e & 4) ? v.z : v.x, b = (e & 4) ? v.w : v.y, w = (e & 2) ? b : a;
+        return __uint_as_float((e & 1) ? (w & 0xFFFF0000u) : (w << 16));
+    }
+    __device__ static __forceinline__ Elem bits(const uint4& v, int e) {
+        const uint32_t w = (e >> 1) == 0 ? v.x : (e >> 1) == 1 ? v.y : (e >> 1) == 2 ? v.z : v.w;
+        return (Elem)((e & 1) ? w >> 16 : w & 0xFFFFu);
     }
     __device__ static __forceinline__ Elem narrow(float f) {   // one rounding to nearest, ties to even
         return __bfloat16_as_ushort(__float2bfloat16_rn(f));
@@ -71,6 +117,11 @@ template <> struct RowVec<MOSAIC_F32> {
     __device__ static __forceinline__ float get(const uint4& v, int e) {
         return __uint_as_float(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w);
     }
+    __device__ static __forceinline__ float any(const uint4& v, int e) {
+        const uint32_t a = (e & 2) ? v.z : v.x, b = (e & 2) ? v.w : v.y;
+        return __uint_as_float((e & 1) ? b : a);
+    }
+    __device__ static __forceinline__ Elem bits(const uint4& v, int e) { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; }
     __device__ static __forceinline__ Elem narrow(float f) { return __float_as_uint(f); }
     __device__ static __forceinline__ uint4 pack(const float (&f)[4]) {
         return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
@@ -110,14 +161,20 @@ template <int DT> struct RowPart {
         return v >= v_lo && v < v_hi;
     }
     __device__ __forceinline__ float at(int col) const { return RV::widen(row[col]); }
-    // The thread's vectors of one pass, all loads issued before the first is used; -inf where there is none.
-    __device__ __forceinline__ void load_pass(int base, uint4 (&raw)[kRowVecs]) const {
-        const Elem* p = row + head;
+    // The same part of another row of the matrix (`rows` further down) on its way into L2, by one thread.
+    __device__ __forceinline__ void prefetch(int64_t rows_times_ld) const {
+        const Elem* next = row + rows_times_ld;
+        const uintptr_t lo = (reinterpret_cast<uintptr_t>(next + head + (int64_t)v_lo * RV::kElems) + 15u) & ~(uintptr_t)15u;
+        const uintptr_t hi = reinterpret_cast<uintptr_t>(next + head + (int64_t)v_hi * RV::kElems) & ~(uintptr_t)15u;
+        if (lo < hi) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(__cvta_generic_to_global((const void*)lo)), "r"((uint32_t)(hi - lo)) : "memory");
+    }
+    __device__ __forceinline__ const Elem* vec(int v) const { return row + head + (int64_t)v * RV::kElems; }
+    // kBatch vectors from v on, a block's stride apart, all loads issued before the first is used; -inf where there is none.
+    __device__ __forceinline__ void load(int v, uint4 (&raw)[kBatch]) const {
 #pragma unroll
-        for (int i = 0; i < kRowVecs; ++i) {
-            const int v = base + (int)threadIdx.x + i * kRowThreads;
+        for (int i = 0; i < kBatch; ++i) {
             raw[i] = make_uint4(RV::kFill, RV::kFill, RV::kFill, RV::kFill);
-            if (v < v_hi) raw[i] = ld_stream16(p + (int64_t)v * RV::kElems);
+            if (v + i * kThreads < v_hi) raw[i] = ld_stream16(vec(v + i * kThreads));
         }
     }
 };
@@ -133,19 +190,21 @@ __device__ __forceinline__ SoftStat soft_merge(SoftStat a, SoftStat b, float c) 
     const float m = fmaxf(a.m, b.m);
     return {m, __fadd_rn(__fmul_rn(a.s, soft_scale(a.m, m, c)), __fmul_rn(b.s, soft_scale(b.m, m, c)))};
 }
-// Between two passes over the registers: the compiler may not carry widened copies of the 64 entries across
-// (they do not fit beside the vectors and were spilled).
-__device__ __forceinline__ void keep_packed(uint4 (&raw)[kRowVecs]) {
+// Bit e: entry e of the vector is not below `least` (NaN included).
+template <int DT> __device__ __forceinline__ uint32_t reach_mask(const uint4& v, float least) {
+    using RV = RowVec<DT>;
+    uint32_t mask = 0u;
 #pragma unroll
-    for (int i = 0; i < kRowVecs; ++i) asm volatile("" : "+r"(raw[i].x), "+r"(raw[i].y), "+r"(raw[i].z), "+r"(raw[i].w));
+    for (int e = 0; e < RV::kElems; ++e) mask |= !(RV::get(v, e) < least) ? 1u << e : 0u;
+    return mask;
 }
-// The largest of a thread's entries (NaN aside).
-template <int DT> __device__ __forceinline__ float pass_max(const uint4 (&raw)[kRowVecs]) {
+// The largest entry of a batch (NaN aside).
+template <int DT> __device__ __forceinline__ float batch_max(const uint4 (&raw)[kBatch]) {
     using RV = RowVec<DT>;
     if constexpr (DT == MOSAIC_BF16) {   // two entries an instruction
         uint32_t m = raw[0].x;
 #pragma unroll
-        for (int i = 0; i < kRowVecs; ++i) {
+        for (int i = 0; i < kBatch; ++i) {
             const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[e]));
@@ -154,7 +213,7 @@ template <int DT> __device__ __forceinline__ float pass_max(const uint4 (&raw)[k
     } else {
         float m = RV::get(raw[0], 0);
 #pragma unroll
-        for (int i = 0; i < kRowVecs; ++i)
+        for (int i = 0; i < kBatch; ++i)
 #pragma unroll
             for (int e = 0; e < RV::kElems; ++e) m = fmaxf(m, RV::get(raw[i], e));
         return m;
@@ -162,35 +221,21 @@ template <int DT> __device__ __forceinline__ float pass_max(const uint4 (&raw)[k
 }
 // One entry's statistics.
 __device__ __forceinline__ SoftStat soft_one(float x, float c) { return {x, exp2_fast(__fmul_rn(__fsub_rn(x, soft_ref(x)), c))}; }
-// The thread's statistics of the vectors of one pass, merged into `st`.
-template <int DT> __device__ __forceinline__ void soft_pass(uint4 (&raw)[kRowVecs], float c, SoftStat& st) {
+// A batch's statistics merged into the thread's.
+template <int DT> __device__ __forceinline__ void soft_batch(const uint4 (&raw)[kBatch], float c, SoftStat& st) {
     using RV = RowVec<DT>;
-    const float m = fmaxf(st.m, pass_max<DT>(raw));
-    keep_packed(raw);
-    // (x - m) first, then the factor: near the maximum the difference is exact, so the factor's rounding
-    // costs next to nothing there; folded into one multiply-add, m * c would shift every term alike.
+    const float m = fmaxf(st.m, batch_max<DT>(raw));
     const float ref = soft_ref(m);
-    float s = __fmul_rn(st.s, soft_scale(st.m, m, c));
+    const Pair minus_ref = pair_of(-ref, -ref), cc = pair_of(c, c);
+    Pair sum = pair_of(0.0f, 0.0f);   // the batch's sum first: fewer roundings at the size of the total
 #pragma unroll
-    for (int i = 0; i < kRowVecs; ++i) {
-        float t = 0.0f;   // a vector's sum first: fewer roundings at the size of the total
+    for (int i = 0; i < kBatch; ++i)
 #pragma unroll
-        for (int e = 0; e < RV::kElems; ++e) t = __fadd_rn(t, exp2_fast(__fmul_rn(__fsub_rn(RV::get(raw[i], e), ref), c)));
-        s = __fadd_rn(s, t);
-    }
+        for (int e = 0; e < RV::kElems; e += 2) sum = add2(sum, soft_pair(RV::get(raw[i], e), RV::get(raw[i], e + 1), minus_ref, cc));
+    float s0, s1;
+    split(sum, s0, s1);
+    st.s = __fadd_rn(__fmul_rn(st.s, soft_scale(st.m, m, c)), __fadd_rn(s0, s1));
     st.m = m;
-    st.s = s;
-}
-// A whole part: its vectors (the first pass's are already in `raw`) and the thread's single element x (-inf: none).
-template <int DT>
-__device__ __forceinline__ SoftStat soft_part(const RowPart<DT>& part, uint4 (&raw)[kRowVecs], float x, float c) {
-    SoftStat st = {-INFINITY, 0.0f};
-    soft_pass<DT>(raw, c, st);
-    for (int b = part.v_lo + kRowThreads * kRowVecs; b < part.v_hi; b += kRowThreads * kRowVecs) {
-        part.load_pass(b, raw);
-        soft_pass<DT>(raw, c, st);
-    }
-    return part.single() >= 0 ? soft_merge(st, soft_one(x, c), c) : st;
 }
 // The warp's statistics in every lane.
 __device__ __forceinline__ SoftStat soft_warp(SoftStat st, float c) {

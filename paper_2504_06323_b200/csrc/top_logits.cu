@@ -1,7 +1,7 @@
 // mosaic_top_logits: the k largest logits of every row, in order (value descending, index ascending), and
 // the log-sum-exp of the whole row - what is kept of a teacher's answer for distillation.
 //
-// The row is read once into registers (rows.cuh).  Every thread knows the largest of its ~64 entries; the
+// One pass over the row (rows.cuh).  Every thread knows the largest of its entries (64 of 32000); the
 // k-th largest of those maxima is a value that at least k entries reach, and on rows in no particular order
 // only a few more than k do.  It is found by bisection over the maxima's order-preserving bit patterns, one
 // vote of the block a step.  The entries that reach it are collected and ranked exactly, under (value,
@@ -17,6 +17,7 @@ namespace mosaic {
 namespace {
 
 constexpr int kListCap = 2048;   // entries collected per row
+constexpr int kSlack = 8;        // candidates too many that are not worth another vote
 constexpr int kRankMost = 256;   // up to here a list is ranked by counting, above it by a bitonic sort
 
 struct TopArgs {
@@ -28,6 +29,7 @@ struct TopArgs {
     float* lse;
     double inv_t;
     float c;
+    int ahead;   // rows between a row and the one it prefetches
 };
 
 // Order-preserving pattern: larger value <=> larger key; -0 and +0 are equal, every NaN is above +inf.
@@ -42,11 +44,13 @@ __device__ __forceinline__ uint64_t entry_of(uint32_t key, int col) { return ((u
 
 struct TopShared {
     uint64_t list[kListCap];
-    SoftStat warp_stat[kRowWarps];
+    SoftStat warp_stat[kWarps];
     SoftStat cta_stat[kMaxCluster];
     uint32_t cta_floor[kMaxCluster];
     uint32_t hist[256];
-    uint32_t warp_count[kRowWarps];
+    uint32_t warp_count[kWarps];
+    uint16_t owner[kThreads];
+    uint32_t kept;
     uint32_t count;
     uint32_t digit, rest;
 };
@@ -56,9 +60,9 @@ template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, To
     const int cols = row.cols, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t prefix = 0u, mask = 0u, want = (uint32_t)top;   // the want-th largest among the keys that share the prefix
     for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = threadIdx.x; i < 256; i += kRowThreads) sh.hist[i] = 0u;
+        for (int i = threadIdx.x; i < 256; i += kThreads) sh.hist[i] = 0u;
         __syncthreads();
-        for (int j0 = 0; j0 < cols; j0 += kRowThreads) {
+        for (int j0 = 0; j0 < cols; j0 += kThreads) {
             const int j = j0 + (int)threadIdx.x;
             const uint32_t key = j < cols ? order_key(row.at(j)) : 0u;
             const bool in = j < cols && (key & mask) == prefix;
@@ -92,7 +96,7 @@ template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, To
     if (threadIdx.x == 0) sh.count = 0u;
     __syncthreads();
     uint32_t equal_before = 0u;
-    for (int j0 = 0; j0 < cols; j0 += kRowThreads) {
+    for (int j0 = 0; j0 < cols; j0 += kThreads) {
         const int j = j0 + (int)threadIdx.x;
         const uint32_t key = j < cols ? order_key(row.at(j)) : 0u;
         const bool equal = j < cols && key == prefix;
@@ -101,7 +105,7 @@ template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, To
         __syncthreads();
         uint32_t before = equal_before + (uint32_t)__popc(votes & ((1u << lane) - 1u));
         uint32_t total = 0u;
-        for (int w = 0; w < kRowWarps; ++w) {
+        for (int w = 0; w < kWarps; ++w) {
             if (w < warp) before += sh.warp_count[w];
             total += sh.warp_count[w];
         }
@@ -112,44 +116,51 @@ template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, To
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kRowThreads, kRowCtasPerSm) top_logits_kernel(const __grid_constant__ TopArgs a) {
+__global__ void __launch_bounds__(kThreads, kRowCtas) top_logits_kernel(const __grid_constant__ TopArgs a) {
     using RV = RowVec<DT>;
     __shared__ TopShared sh;
     cg::cluster_group cluster = cg::this_cluster();
     const int n_ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int64_t r = blockIdx.x / n_ctas;
+    const int64_t r = blockIdx.x >> (__ffs(n_ctas) - 1);   // a power of two
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int vocab = (int)a.vocab;
     const RowPart<DT> part(a.L, r, a.ldl, vocab, rank, n_ctas);
-    const bool held = part.v_hi - part.v_lo <= kRowThreads * kRowVecs;
-
-    uint4 raw[kRowVecs];
-    part.load_pass(part.v_lo, raw);
-    if (threadIdx.x == 0) sh.count = 0u;
-    cg::cluster_group::arrival_token started = cluster.barrier_arrive();
-
     const int lone = part.single();
     const float lone_x = lone >= 0 ? part.at(lone) : -INFINITY;
-    SoftStat st = soft_part<DT>(part, raw, lone_x, a.c);
+    if (threadIdx.x == 0) {
+        sh.count = 0u;
+        sh.kept = 0u;
+        if (r + a.ahead < a.rows) part.prefetch((int64_t)a.ahead * a.ldl);
+    }
+    if (n_ctas > 1) cluster_arrive();   // waited for before the first write to another CTA
+
+    SoftStat st = {-INFINITY, 0.0f};
+    for (int v = part.v_lo + (int)threadIdx.x; v < part.v_hi; v += kBatch * kThreads) {
+        uint4 raw[kBatch];
+        part.load(v, raw);
+        soft_batch<DT>(raw, a.c, st);
+    }
+    if (lone >= 0) st = soft_merge(st, soft_one(lone_x, a.c), a.c);
     // the thread's largest entry, as a 16-bit pattern rounded down (a NaN makes the sum NaN: above all)
     const bool any = part.v_lo + (int)threadIdx.x < part.v_hi || lone >= 0;
     const uint32_t mine = any ? (st.s != st.s ? 0xFFFFu : order_key(st.m) >> 16) : 0u;
 
-    // the largest pattern that at least `top` of the threads' maxima reach (0: all entries are candidates)
+    // a pattern that at least `top` of the threads' maxima reach, the largest or one that few more do (0: all entries
+    // are candidates)
     uint32_t floor_key = 0u;
     for (int bit = 15; bit >= 0; --bit) {
         const uint32_t trial = floor_key | (1u << bit);
         const int n = __syncthreads_count(mine >= trial);
         if (n >= a.top) {
             floor_key = trial;
-            if (n == a.top) break;
+            if (n <= a.top + kSlack) break;
         }
     }
     st = soft_warp(st, a.c);
     if (lane == 0) sh.warp_stat[warp] = st;
-    cluster.barrier_wait(std::move(started));
+    if (n_ctas > 1) cluster_wait();
     __syncthreads();
-    st = soft_all(sh.warp_stat, kRowWarps, a.c);
+    st = soft_all(sh.warp_stat, kWarps, a.c);
     if (n_ctas > 1) {   // a part's floor holds for the row: the highest of them serves all
         if (threadIdx.x < n_ctas) {
             *cluster.map_shared_rank(&sh.cta_stat[rank], threadIdx.x) = st;
@@ -171,18 +182,21 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtasPerSm) top_logits_kernel(
             if (at < kListCap) list[at] = entry_of(order_key(x), j);
         };
         if (lone >= 0 && !(lone_x < least)) take(lone_x, lone);
-        for (int b = part.v_lo; b < part.v_hi; b += kRowThreads * kRowVecs) {
-            if (!held) part.load_pass(b, raw);
-            keep_packed(raw);
-            if (held && mine < floor_key) break;
-#pragma unroll
-            for (int i = 0; i < kRowVecs; ++i) {
-                const int v = b + (int)threadIdx.x + i * kRowThreads;
-#pragma unroll
-                for (int e = 0; e < RV::kElems; ++e) {
-                    const float x = RV::get(raw[i], e);
-                    if (!(x < least) && v < part.v_hi) take(x, part.first(v) + e);
-                }
+        // Few threads (about `top` of them) hold a candidate.  The whole block goes through their vectors, a vector or
+        // two per thread, from L2.
+        if (mine >= floor_key && part.v_lo + (int)threadIdx.x < part.v_hi) sh.owner[atomicAdd(&sh.kept, 1u)] = (uint16_t)threadIdx.x;
+        __syncthreads();
+        const int kept = (int)sh.kept;
+        const int rounds = (part.v_hi - part.v_lo + kThreads - 1) / kThreads;
+        for (int u = (int)threadIdx.x; u < kept * rounds; u += kThreads) {
+            const int v = part.v_lo + sh.owner[u % kept] + (u / kept) * kThreads;
+            if (v >= part.v_hi) continue;
+            const uint4 w = ld_stream16(part.vec(v));
+            uint32_t mask = reach_mask<DT>(w, least);
+            while (mask != 0u) {
+                const int e = __ffs(mask) - 1;
+                mask &= mask - 1u;
+                take(RV::any(w, e), part.first(v) + e);
             }
         }
     }
@@ -202,14 +216,16 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtasPerSm) top_logits_kernel(
     int32_t* indices = a.indices + r * a.top;
     auto emit = [&](uint32_t place, uint64_t entry) {
         const int j = (int)~(uint32_t)entry;
-        values[place] = part.at(j);   // the logit's own bits (its key has lost the sign of zero and a NaN's payload)
+        const uint32_t key = (uint32_t)(entry >> 32);
+        // the logit's own bits: the key has lost the sign of zero and a NaN's payload
+        values[place] = key == 0x80000000u || key == 0xFFFFFFFFu ? part.at(j) : key_value(key);
         indices[place] = j;
     };
     if (n <= kRankMost) {
         // a group of `share` threads counts the larger entries of one candidate
         uint32_t share = 2u;
-        while (share < 32u && n * share * 2u <= kRowThreads) share *= 2u;
-        for (uint32_t i0 = 0; i0 < n; i0 += kRowThreads / share) {
+        while (share < 32u && n * share * 2u <= kThreads) share *= 2u;
+        for (uint32_t i0 = 0; i0 < n; i0 += kThreads / share) {
             const uint32_t i = i0 + threadIdx.x / share;
             const uint64_t me = i < n ? sh.list[i] : 0ull;
             uint32_t above = 0u;
@@ -221,11 +237,11 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtasPerSm) top_logits_kernel(
     }
     uint32_t size = kRankMost * 2;
     while (size < n) size *= 2u;
-    for (uint32_t i = n + threadIdx.x; i < size; i += kRowThreads) sh.list[i] = 0ull;   // below every entry (a column's complement is not 0)
+    for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) sh.list[i] = 0ull;   // below every entry (a column's complement is not 0)
     __syncthreads();
     for (uint32_t k = 2u; k <= size; k <<= 1) {
         for (uint32_t d = k >> 1; d > 0u; d >>= 1) {
-            for (uint32_t p = threadIdx.x; p < size / 2u; p += kRowThreads) {
+            for (uint32_t p = threadIdx.x; p < size / 2u; p += kThreads) {
                 const uint32_t lo = 2u * d * (p / d) + (p % d), hi = lo + d;
                 const uint64_t x = sh.list[lo], y = sh.list[hi];
                 if ((x < y) == ((lo & k) == 0u)) {
@@ -236,14 +252,15 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtasPerSm) top_logits_kernel(
             __syncthreads();
         }
     }
-    for (uint32_t i = threadIdx.x; i < (uint32_t)a.top; i += kRowThreads) emit(i, sh.list[i]);
+    for (uint32_t i = threadIdx.x; i < (uint32_t)a.top; i += kThreads) emit(i, sh.list[i]);
 }
 
-template <int DT> int launch_top(const TopArgs& a, cudaStream_t st) {
+template <int DT> int launch_top(TopArgs a, cudaStream_t st) {
     const int c = row_cluster(a.rows, row_vectors(a.vocab, DT));
+    a.ahead = rows_ahead(c);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.rows * c));
-    cfg.blockDim = dim3(kRowThreads);
+    cfg.blockDim = dim3(kThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
