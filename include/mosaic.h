@@ -531,21 +531,23 @@ int mosaic_top_logits(const void *L, int64_t rows, int64_t vocab, int64_t ldl, i
  *   grad_rows  device, [rows] fp32 g, or NULL (1): the gradient of each row's loss
  *   loss, lse  device, [rows] fp32 (lse may be NULL in the loss calls; _grad reads it)
  *   dS         device, [rows, vocab], ld ldd, S's dtype; may be S itself (same ld)
+ *   ws         device scratch, >= mosaic_distill_workspace_bytes(rows, top)
  * _loss_grad does both in one pass over S.  With top = 1 and t_lse NULL the loss is
  * the cross entropy of a label.  Sums in fp32 over the vocabulary and fp64 over the
  * kept entries; the gradient is rounded once.
  * ------------------------------------------------------------------------- */
+size_t mosaic_distill_workspace_bytes(int64_t rows, int64_t top);
 int mosaic_distill_loss(const void *S, int64_t rows, int64_t vocab, int64_t lds, int dtype, const float *t_values,
                         const int32_t *t_indices, int64_t top, const float *t_lse, const float *row_weight,
-                        float temperature, float *loss, float *lse, void *stream);
+                        float temperature, float *loss, float *lse, void *ws, size_t ws_bytes, void *stream);
 int mosaic_distill_grad(const void *S, int64_t rows, int64_t vocab, int64_t lds, int dtype, const float *t_values,
                         const int32_t *t_indices, int64_t top, const float *t_lse, const float *row_weight,
                         float temperature, const float *lse, const float *grad_rows, float grad_scale, void *dS,
-                        int64_t ldd, void *stream);
+                        int64_t ldd, void *ws, size_t ws_bytes, void *stream);
 int mosaic_distill_loss_grad(const void *S, int64_t rows, int64_t vocab, int64_t lds, int dtype, const float *t_values,
                              const int32_t *t_indices, int64_t top, const float *t_lse, const float *row_weight,
                              float temperature, float *loss, float *lse, const float *grad_rows, float grad_scale,
-                             void *dS, int64_t ldd, void *stream);
+                             void *dS, int64_t ldd, void *ws, size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------
  * mosaic_bounded_wait_selftest - a diagnostic with no counterpart in the paper.

@@ -47,7 +47,7 @@ SYMBOLS = (
     "mosaic_linear_workspace_bytes", "mosaic_linear",
     "mosaic_linear_backward_workspace_bytes", "mosaic_linear_backward",
     "mosaic_top_logits",
-    "mosaic_distill_loss", "mosaic_distill_grad", "mosaic_distill_loss_grad",
+    "mosaic_distill_workspace_bytes", "mosaic_distill_loss", "mosaic_distill_grad", "mosaic_distill_loss_grad",
     "mosaic_bounded_wait_selftest",
 )
 
@@ -141,12 +141,14 @@ def lib() -> C.CDLL:
         L.mosaic_top_logits.restype = ci
         L.mosaic_top_logits.argtypes = [vp, i64, i64, i64, ci, i64, flt, vp, vp, vp, vp]
         teacher = [vp, i64, i64, i64, ci, vp, vp, i64, vp, vp, flt]
+        L.mosaic_distill_workspace_bytes.restype = sz
+        L.mosaic_distill_workspace_bytes.argtypes = [i64, i64]
         L.mosaic_distill_loss.restype = ci
-        L.mosaic_distill_loss.argtypes = teacher + [vp, vp, vp]
+        L.mosaic_distill_loss.argtypes = teacher + [vp, vp, vp, sz, vp]
         L.mosaic_distill_grad.restype = ci
-        L.mosaic_distill_grad.argtypes = teacher + [vp, vp, flt, vp, i64, vp]
+        L.mosaic_distill_grad.argtypes = teacher + [vp, vp, flt, vp, i64, vp, sz, vp]
         L.mosaic_distill_loss_grad.restype = ci
-        L.mosaic_distill_loss_grad.argtypes = teacher + [vp, vp, vp, flt, vp, i64, vp]
+        L.mosaic_distill_loss_grad.argtypes = teacher + [vp, vp, vp, flt, vp, i64, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -813,7 +815,7 @@ def _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature):
     tl = _vec_of(t_lse, "t_lse", rows, torch.float32)
     rw = _vec_of(row_weight, "row_weight", rows, torch.float32)
     _same_device(S, t_values, t_indices, t_lse, row_weight)
-    return (sp, rows, vocab, lds, code, t_values.data_ptr(), t_indices.data_ptr(), top, tl, rw, float(temperature)), rows, vocab
+    return (sp, rows, vocab, lds, code, t_values.data_ptr(), t_indices.data_ptr(), top, tl, rw, float(temperature)), rows, vocab, top
 
 
 def _distill_dS(S, dS, rows, vocab):
@@ -824,33 +826,40 @@ def _distill_dS(S, dS, rows, vocab):
     return p, ld
 
 
-def mosaic_distill_loss(S, t_values, t_indices, loss, lse=None, t_lse=None, row_weight=None, temperature: float = 1.0, stream=None) -> None:
+def mosaic_distill_loss(S, t_values, t_indices, loss, lse=None, t_lse=None, row_weight=None, temperature: float = 1.0,
+                        ws: Workspace | None = None, stream=None) -> None:
     """Distillation loss of every row of the student's logits S [rows, vocab] (fp32 or bf16) against a teacher's
     kept logits (t_values fp32, t_indices int32 [rows, top]); `loss` and `lse` (optional) are fp32 [rows]."""
-    args, rows, _ = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
+    args, rows, _, top = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
     lo, ls = _vec_of(loss, "loss", rows, torch.float32), _vec_of(lse, "lse", rows, torch.float32)
     _same_device(S, loss, lse)
-    _check(lib().mosaic_distill_loss(*args, lo, ls, _stream(stream)), "mosaic_distill_loss")
+    L = lib()
+    wp, wn = _ws(ws, S.device).get(L.mosaic_distill_workspace_bytes(rows, top))
+    _check(L.mosaic_distill_loss(*args, lo, ls, wp, wn, _stream(stream)), "mosaic_distill_loss")
 
 
 def mosaic_distill_grad(S, t_values, t_indices, lse, dS, t_lse=None, row_weight=None, grad_rows=None, grad_scale: float = 1.0,
-                        temperature: float = 1.0, stream=None) -> None:
+                        temperature: float = 1.0, ws: Workspace | None = None, stream=None) -> None:
     """Gradient of mosaic_distill_loss with respect to S, from the lse that call stored; `grad_rows` (fp32 [rows]) times
     `grad_scale` is the gradient of each row's loss.  dS may be S."""
-    args, rows, vocab = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
+    args, rows, vocab, top = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
     ls, gr = _vec_of(lse, "lse", rows, torch.float32), _vec_of(grad_rows, "grad_rows", rows, torch.float32)
     dp, ldd = _distill_dS(S, dS, rows, vocab)
     _same_device(S, lse, grad_rows)
-    _check(lib().mosaic_distill_grad(*args, ls, gr, float(grad_scale), dp, ldd, _stream(stream)), "mosaic_distill_grad")
+    L = lib()
+    wp, wn = _ws(ws, S.device).get(L.mosaic_distill_workspace_bytes(rows, top))
+    _check(L.mosaic_distill_grad(*args, ls, gr, float(grad_scale), dp, ldd, wp, wn, _stream(stream)), "mosaic_distill_grad")
 
 
 def mosaic_distill_loss_grad(S, t_values, t_indices, loss, lse, dS, t_lse=None, row_weight=None, grad_rows=None, grad_scale: float = 1.0,
-                             temperature: float = 1.0, stream=None) -> None:
+                             temperature: float = 1.0, ws: Workspace | None = None, stream=None) -> None:
     """mosaic_distill_loss and mosaic_distill_grad in one pass over S (the training step, where the gradient of each row's
     loss is known beforehand).  `lse` may be None; dS may be S."""
-    args, rows, vocab = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
+    args, rows, vocab, top = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
     lo, ls = _vec_of(loss, "loss", rows, torch.float32), _vec_of(lse, "lse", rows, torch.float32)
     gr = _vec_of(grad_rows, "grad_rows", rows, torch.float32)
     dp, ldd = _distill_dS(S, dS, rows, vocab)
     _same_device(S, loss, lse, grad_rows)
-    _check(lib().mosaic_distill_loss_grad(*args, lo, ls, gr, float(grad_scale), dp, ldd, _stream(stream)), "mosaic_distill_loss_grad")
+    L = lib()
+    wp, wn = _ws(ws, S.device).get(L.mosaic_distill_workspace_bytes(rows, top))
+    _check(L.mosaic_distill_loss_grad(*args, lo, ls, gr, float(grad_scale), dp, ldd, wp, wn, _stream(stream)), "mosaic_distill_loss_grad")

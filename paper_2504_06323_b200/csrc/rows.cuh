@@ -4,9 +4,7 @@
 // A row is its whole 16-byte vectors on 16-byte boundaries, one 16-byte load each, and at most a vector's
 // worth of single elements on either side of them (an odd vocabulary, a dense matrix whose rows start
 // anywhere), which the first threads of the row's first CTA take one each.  Nothing outside the row is read.
-// A thread streams over its vectors, kBatch loads in flight, and holds none: few registers, so that three
-// CTAs of 512 threads share an SM and one's loads run under another's exponentials and barriers (rows held
-// in registers, 64 KB per CTA and two CTAs an SM: 115 us instead of 75 for the top logits of 4096 x 32000).
+// A thread streams over its vectors, kBatch loads in flight, and holds none in registers.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -36,9 +34,6 @@ inline int row_cluster(int64_t rows, int64_t vectors) {
 // Vectors of a row (at most; one fewer if it starts off a boundary).
 inline int64_t row_vectors(int64_t cols, int dtype) { return cols * (int64_t)elem_size(dtype) / 16; }
 
-// How many rows further a CTA asks L2 for while it works on its own: those that the CTAs after the resident ones take.
-inline int rows_ahead(int cluster) { return sm_count() * kRowCtas / cluster; }
-
 #ifdef __CUDACC__
 // 2^x by the hardware's approximation (relative error about 2^-22, results below 2^-126 become 0).
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -50,6 +45,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // The two halves of a barrier over the cluster's CTAs.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// A kernel launched with the stream-serialization attribute may start while the one before it still runs: it waits
+// here before it touches what that one reads or writes.  The other side allows it to start.
+__device__ __forceinline__ void await_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Two fp32 values an instruction.
 struct Pair {
@@ -161,13 +161,6 @@ template <int DT> struct RowPart {
         return v >= v_lo && v < v_hi;
     }
     __device__ __forceinline__ float at(int col) const { return RV::widen(row[col]); }
-    // The same part of another row of the matrix (`rows` further down) on its way into L2, by one thread.
-    __device__ __forceinline__ void prefetch(int64_t rows_times_ld) const {
-        const Elem* next = row + rows_times_ld;
-        const uintptr_t lo = (reinterpret_cast<uintptr_t>(next + head + (int64_t)v_lo * RV::kElems) + 15u) & ~(uintptr_t)15u;
-        const uintptr_t hi = reinterpret_cast<uintptr_t>(next + head + (int64_t)v_hi * RV::kElems) & ~(uintptr_t)15u;
-        if (lo < hi) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(__cvta_generic_to_global((const void*)lo)), "r"((uint32_t)(hi - lo)) : "memory");
-    }
     __device__ __forceinline__ const Elem* vec(int v) const { return row + head + (int64_t)v * RV::kElems; }
     // kBatch vectors from v on, a block's stride apart, all loads issued before the first is used; -inf where there is none.
     __device__ __forceinline__ void load(int v, uint4 (&raw)[kBatch]) const {

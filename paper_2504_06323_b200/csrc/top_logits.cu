@@ -29,7 +29,6 @@ struct TopArgs {
     float* lse;
     double inv_t;
     float c;
-    int ahead;   // rows between a row and the one it prefetches
 };
 
 // Order-preserving pattern: larger value <=> larger key; -0 and +0 are equal, every NaN is above +inf.
@@ -130,7 +129,6 @@ __global__ void __launch_bounds__(kThreads, kRowCtas) top_logits_kernel(const __
     if (threadIdx.x == 0) {
         sh.count = 0u;
         sh.kept = 0u;
-        if (r + a.ahead < a.rows) part.prefetch((int64_t)a.ahead * a.ldl);
     }
     if (n_ctas > 1) cluster_arrive();   // waited for before the first write to another CTA
 
@@ -257,7 +255,6 @@ __global__ void __launch_bounds__(kThreads, kRowCtas) top_logits_kernel(const __
 
 template <int DT> int launch_top(TopArgs a, cudaStream_t st) {
     const int c = row_cluster(a.rows, row_vectors(a.vocab, DT));
-    a.ahead = rows_ahead(c);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.rows * c));
     cfg.blockDim = dim3(kThreads);

@@ -83,15 +83,20 @@ def test_top_logits_refusals_need_no_device(lib):
     assert top(lib, rows=0, L=None) == 0
 
 
+def test_distill_workspace(lib):
+    q = lib.mosaic_distill_workspace_bytes
+    assert q(4, 10) == 512 and q(1000, 64) == (1000 * (36 + 512) + 255) // 256 * 256 and q(0, 10) == 0
+
+
 def distill(lib, which, **k):
     g = k.get
     head = (g("S", A), g("rows", 4), g("vocab", 100), g("ld", 100), g("dtype", api.F32), g("tv", 2 * A), g("ti", 3 * A), g("top", 10), g("t_lse"),
             g("weight"), g("T", 1.0))
     if which == "loss":
-        return lib.mosaic_distill_loss(*head, g("loss", 4 * A), g("lse", 5 * A), None)
+        return lib.mosaic_distill_loss(*head, g("loss", 4 * A), g("lse", 5 * A), g("ws", 8 * A), g("ws_bytes", 1 << 16), None)
     if which == "grad":
-        return lib.mosaic_distill_grad(*head, g("lse", 5 * A), g("gr"), 1.0, g("dS", 6 * A), g("ldd", 100), None)
-    return lib.mosaic_distill_loss_grad(*head, g("loss", 4 * A), g("lse", 5 * A), g("gr"), 1.0, g("dS", 6 * A), g("ldd", 100), None)
+        return lib.mosaic_distill_grad(*head, g("lse", 5 * A), g("gr"), 1.0, g("dS", 6 * A), g("ldd", 100), g("ws", 8 * A), g("ws_bytes", 1 << 16), None)
+    return lib.mosaic_distill_loss_grad(*head, g("loss", 4 * A), g("lse", 5 * A), g("gr"), 1.0, g("dS", 6 * A), g("ldd", 100), g("ws", 8 * A), g("ws_bytes", 1 << 16), None)
 
 
 @pytest.mark.parametrize("which", ["loss", "grad", "both"])
@@ -102,6 +107,7 @@ def test_distill_refusals_need_no_device(lib, which):
     assert call(S=None) == NULL and call(tv=None) == NULL and call(ti=None) == NULL
     assert call(S=A + 2) == MISALIGNED and call(tv=A + 1) == MISALIGNED and call(weight=A + 2) == MISALIGNED
     assert call(rows=0, S=None) == 0
+    assert call(ws=None) == NULL and call(ws=8 * A + 64) == MISALIGNED and call(ws_bytes=128) == WS
     if which != "grad":
         assert call(loss=None) == NULL and call(loss=2 * A) == ALIAS and call(lse=4 * A) == ALIAS
     if which != "loss":
