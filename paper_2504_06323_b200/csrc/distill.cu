@@ -22,7 +22,7 @@ struct RowScale {
     float dense;   // with the loss: coef P, to be divided by the row's sum; from a saved log-sum-exp: complete
     float ref;     // from a saved log-sum-exp: T times it
     float coef;
-    int live;      // 0: the row counts for nothing
+    int live;      // 0: the row counts for nothing, 2: some vocabulary entry is kept twice
 };
 
 struct DistillArgs {
@@ -48,7 +48,6 @@ struct DistillArgs {
     float2* stat;       // [rows] maximum and sum of the row
     double* row_norm;   // [rows] log of what the kept exponentials are divided by
     float2* kept;       // [rows, top] the kept entries' probabilities and the student's logits there
-    int* doubled;       // [rows] some vocabulary entry is kept twice
 };
 
 constexpr int kWantLoss = 1, kWantGrad = 2;
@@ -65,96 +64,118 @@ __device__ __forceinline__ float dense_of(float x, float ref, float dense, float
 // The loss alone needs the second, and a third that is both others at once.  All of the kept entries' work inside
 // vocab_kernel made every row's barriers wait for the warps that did it: 137 us for the loss and gradient of 4096 x
 // 32000 bf16, 125 us with a warp of its own for it, and 10 us for the sum of p alone.
-constexpr int kKeptWarps = 8;
-inline int kept_warps(int top) { return top <= 64 ? 1 : top >= 64 * kKeptWarps ? kKeptWarps : (top + 63) / 64; }
-
-// One row's kept entries in the hands of a CTA of one to eight warps.  Shared memory: [top] each of place, teacher's
-// logit, student's logit; [slots] of the table (gradient).
-template <int DT> struct KeptRow {
-    using RV = RowVec<DT>;
-    int* j;            // -1: absent
-    float* t;
-    float* x;
-    uint32_t* table;
-    SoftStat st;       // renormalised: the kept logits' statistics
-    double norm;       // log of what the kept exponentials are divided by
-    float inv;         // 1 / st.s
-    float t_lse;
-    bool given;
-
-    __device__ __forceinline__ KeptRow(const DistillArgs& a, int64_t r, unsigned char* dyn, SoftStat* warp_stat) {
-        j = reinterpret_cast<int*>(dyn);
-        t = reinterpret_cast<float*>(j + a.top);
-        x = t + a.top;
-        table = reinterpret_cast<uint32_t*>(x + a.top);
-        given = a.t_lse != nullptr;
-        t_lse = given ? a.t_lse[r] : 0.0f;
-        const typename RV::Elem* row = reinterpret_cast<const typename RV::Elem*>(a.S) + r * a.lds;
-        const int n = (int)blockDim.x, warps = n >> 5;
-        st = {-INFINITY, 0.0f};
-        for (int i = threadIdx.x; i < a.top; i += n) {
-            int at = a.t_indices[r * a.top + i];
-            if (at < 0 || at >= (int)a.vocab) at = -1;
-            const float v = at >= 0 ? a.t_values[r * a.top + i] : -INFINITY;
-            j[i] = at;
-            t[i] = v;
-            x[i] = at >= 0 ? RV::widen(row[at]) : 0.0f;
-            if (!given) st = soft_merge(st, soft_one(v, a.c), a.c);
-        }
-        if (!given) {
-            st = soft_warp(st, a.c);
-            if (warps > 1) {
-                if ((threadIdx.x & 31) == 0) warp_stat[threadIdx.x >> 5] = st;
-                __syncthreads();
-                st = soft_all(warp_stat, warps, a.c);
-            }
-        }
-        inv = __fdividef(1.0f, st.s);
-        norm = given ? (double)t_lse : soft_lse(st, a.inv_t);
-    }
-    __device__ __forceinline__ float prob(int i, const DistillArgs& a) const {
-        const float v = t[i];
-        if (v == -INFINITY) return 0.0f;
-        return given ? teacher_p(v, t_lse, a.inv_t) : __fmul_rn(exp2_fast(__fmul_rn(__fsub_rn(v, soft_ref(st.m)), a.c)), inv);
-    }
+//
+// The kept entries' two launches are chains of dependent loads (place -> logit), so they are laid out for many rows in
+// flight: a row's entries, four a thread at most and all asked for at once, by a warp (up to 128 of them; four rows a
+// CTA) or by a CTA of eight.
+constexpr int kKeptEach = 4;
+constexpr int kKeptWarpRows = 4;
+template <bool WARP> struct KeptShape {
+    static constexpr int kThreads = WARP ? 32 * kKeptWarpRows : kMaxTop / kKeptEach;
+    static constexpr int kGroup = WARP ? 32 : kThreads;      // threads of a row
+    static constexpr int kRows = kThreads / kGroup;
 };
-// Sum over the CTA, in thread 0; `part` holds a warp's each.  With a barrier, if there is more than one warp.
-template <class T> __device__ __forceinline__ T kept_sum(T v, T* part) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    const int warps = (int)blockDim.x >> 5;
-    if (warps == 1) return v;
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    if (threadIdx.x == 0)
-        for (int w = 1; w < warps; ++w) v += part[w];
+template <bool WARP> struct KeptShared {
+    SoftStat stat[8];
+    double sum[8];
+    int flag;
+};
+template <bool WARP> __device__ __forceinline__ int kept_rank() { return WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x; }
+template <bool WARP> __device__ __forceinline__ int64_t kept_row() { return WARP ? (int64_t)blockIdx.x * kKeptWarpRows + (threadIdx.x >> 5) : (int64_t)blockIdx.x; }
+template <bool WARP> __device__ __forceinline__ void kept_sync() {
+    if (WARP) __syncwarp();
+    else __syncthreads();
+}
+// Sum over the row's threads, in each of them.
+template <bool WARP> __device__ __forceinline__ double kept_sum(double v, KeptShared<WARP>& sh) {
+    v = warp_sum(v);
+    if (!WARP) {
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) sh.sum[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = 0.0;
+        for (int w = 0; w < 8; ++w) v += sh.sum[w];
+    }
     return v;
 }
 
-template <int DT, int MODE> __global__ void __launch_bounds__(32 * kKeptWarps) kept_kernel(const __grid_constant__ DistillArgs a) {
-    extern __shared__ __align__(16) unsigned char dyn[];
-    __shared__ SoftStat warp_stat[kKeptWarps];
-    __shared__ float warp_mass[kKeptWarps];
+// One row's kept entries in the hands of its threads.
+template <int DT, bool WARP> struct KeptRow {
+    using RV = RowVec<DT>;
+    int j[kKeptEach];      // place, -1: absent
+    float t[kKeptEach];    // the teacher's logit
+    float x[kKeptEach];    // the student's there
+    SoftStat st;           // renormalised: the kept logits' statistics
+    float inv;             // 1 / st.s
+    float t_lse;
+    bool given;
+
+    __device__ __forceinline__ KeptRow(const DistillArgs& a, int64_t r, KeptShared<WARP>& sh) {
+        const int me = kept_rank<WARP>();
+        given = a.t_lse != nullptr;
+        t_lse = given ? a.t_lse[r] : 0.0f;
+        const typename RV::Elem* row = reinterpret_cast<const typename RV::Elem*>(a.S) + r * a.lds;
+#pragma unroll
+        for (int e = 0; e < kKeptEach; ++e) {
+            const int i = me + e * KeptShape<WARP>::kGroup;
+            j[e] = i < a.top ? a.t_indices[r * a.top + i] : -1;
+            t[e] = i < a.top ? a.t_values[r * a.top + i] : 0.0f;
+        }
+        st = {-INFINITY, 0.0f};
+#pragma unroll
+        for (int e = 0; e < kKeptEach; ++e) {
+            if (j[e] < 0 || j[e] >= (int)a.vocab) j[e] = -1;
+            x[e] = j[e] >= 0 ? RV::widen(row[j[e]]) : 0.0f;
+            if (j[e] < 0) t[e] = -INFINITY;
+            st.m = fmaxf(st.m, t[e]);
+        }
+        if (!given) {
+#pragma unroll
+            for (int e = 0; e < kKeptEach; ++e) st.s = __fadd_rn(st.s, exp2_fast(__fmul_rn(__fsub_rn(t[e], soft_ref(st.m)), a.c)));
+            st = soft_warp(st, a.c);
+            if (!WARP) {
+                if ((threadIdx.x & 31) == 0) sh.stat[threadIdx.x >> 5] = st;
+                __syncthreads();
+                st = soft_all(sh.stat, 8, a.c);
+            }
+        }
+        inv = __fdividef(1.0f, st.s);
+    }
+    __device__ __forceinline__ float prob(int e, const DistillArgs& a) const {
+        if (t[e] == -INFINITY) return 0.0f;
+        return given ? teacher_p(t[e], t_lse, a.inv_t) : __fmul_rn(exp2_fast(__fmul_rn(__fsub_rn(t[e], soft_ref(st.m)), a.c)), inv);
+    }
+    // log of what the kept exponentials are divided by
+    __device__ __forceinline__ double norm(const DistillArgs& a) const { return given ? (double)t_lse : soft_lse(st, a.inv_t); }
+};
+
+template <int DT, int MODE, bool WARP> __global__ void __launch_bounds__(KeptShape<WARP>::kThreads) kept_kernel(const __grid_constant__ DistillArgs a) {
+    extern __shared__ uint32_t tables[];   // [rows of the CTA][slots] places seen, to find doubled ones
+    __shared__ KeptShared<WARP> sh;
     allow_next_kernel();
-    const int64_t r = blockIdx.x;
-    const int n = (int)blockDim.x;
+    const int64_t r = kept_row<WARP>();
+    const int me = kept_rank<WARP>();
+    if (WARP && r >= a.rows) return;
+    uint32_t* table = tables + (WARP ? (threadIdx.x >> 5) * a.slots : 0);
     const float weight = a.row_weight != nullptr ? a.row_weight[r] : 1.0f;
     const float g = a.grad_rows != nullptr ? a.grad_rows[r] : 1.0f;
     const float saved_lse = MODE == kWantGrad ? a.lse[r] : 0.0f;
-    KeptRow<DT> k(a, r, dyn, warp_stat);
-    for (int i = threadIdx.x; i < a.slots; i += n) k.table[i] = 0xFFFFFFFFu;
-    __syncthreads();
+    for (int i = me; i < a.slots; i += KeptShape<WARP>::kGroup) table[i] = 0xFFFFFFFFu;
+    if (me == 0) sh.flag = 0;   // (a CTA a row; a warp's vote needs none)
+    KeptRow<DT, WARP> k(a, r, sh);
+    kept_sync<WARP>();
     float mass = 0.0f;
     bool doubled = false;   // some vocabulary entry is kept twice
-    for (int i = threadIdx.x; i < a.top; i += n) {
-        const float p = k.prob(i, a);
-        const int j = k.j[i];
+#pragma unroll
+    for (int e = 0; e < kKeptEach; ++e) {
+        const int i = me + e * KeptShape<WARP>::kGroup, j = k.j[e];
+        const float p = k.prob(e, a);
         mass = __fadd_rn(mass, p);
-        a.kept[r * a.top + i] = make_float2(p, k.x[i]);
+        if (i < a.top) a.kept[r * a.top + i] = make_float2(p, k.x[e]);
         if (j < 0) continue;
         uint32_t h = ((uint32_t)j * 2654435761u) & (uint32_t)(a.slots - 1);   // open addressing
         for (;;) {
-            const uint32_t old = atomicCAS(&k.table[h], 0xFFFFFFFFu, (uint32_t)j);
+            const uint32_t old = atomicCAS(&table[h], 0xFFFFFFFFu, (uint32_t)j);
             if (old == 0xFFFFFFFFu) break;
             if (old == (uint32_t)j) {
                 doubled = true;
@@ -163,23 +184,22 @@ template <int DT, int MODE> __global__ void __launch_bounds__(32 * kKeptWarps) k
             h = (h + 1u) & (uint32_t)(a.slots - 1);
         }
     }
-    doubled = __syncthreads_or(doubled) != 0;
-    mass = kept_sum(mass, warp_mass);
-    if (threadIdx.x == 0) {
-        if (!k.given) mass = k.st.s == 0.0f ? 0.0f : (k.st.s < INFINITY ? 1.0f : NAN);   // NaN and +inf among the kept logits: NaN
+    doubled = WARP ? __any_sync(0xFFFFFFFFu, doubled) : __syncthreads_or(doubled) != 0;
+    if (k.given) mass = (float)kept_sum<WARP>((double)mass, sh);
+    else mass = k.st.s == 0.0f ? 0.0f : (k.st.s < INFINITY ? 1.0f : NAN);   // NaN and +inf among the kept logits: NaN
+    if (me == 0) {
         RowScale s;
         s.coef = __fmul_rn(__fmul_rn(__fmul_rn(g, a.grad_scale), weight), a.t);
         s.dense = __fmul_rn(s.coef, mass);
         s.ref = 0.0f;
-        s.live = weight == 0.0f || mass == 0.0f ? 0 : 1;
+        s.live = weight == 0.0f || mass == 0.0f ? 0 : (doubled ? 2 : 1);
         if (MODE == kWantGrad) {   // T times the saved log-sum-exp, rounded, and what the rounding left out as a factor
             const double at = (double)saved_lse * (double)a.t;
             s.ref = (float)at;
             if (fabsf(s.ref) <= 3.402823466e38f) s.dense = __fmul_rn(s.dense, exp2_fast(__fmul_rn((float)((double)s.ref - at), a.c)));
         }
         a.scale[r] = s;
-        a.row_norm[r] = k.norm;
-        a.doubled[r] = doubled ? 1 : 0;
+        if (MODE & kWantLoss) a.row_norm[r] = k.norm(a);
     }
 }
 
@@ -288,68 +308,91 @@ __global__ void __launch_bounds__(kThreads, kRowCtas) vocab_kernel(const __grid_
     }
 }
 
-template <int DT, int MODE> __global__ void __launch_bounds__(32 * kKeptWarps) place_kernel(const __grid_constant__ DistillArgs a) {
+template <int DT, int MODE, bool WARP> __global__ void __launch_bounds__(KeptShape<WARP>::kThreads) place_kernel(const __grid_constant__ DistillArgs a) {
     using RV = RowVec<DT>;
     using Elem = typename RV::Elem;
     constexpr bool kLoss = (MODE & kWantLoss) != 0, kGrad = (MODE & kWantGrad) != 0;
-    extern __shared__ __align__(16) unsigned char dyn[];
-    __shared__ SoftStat warp_stat[kKeptWarps];
-    __shared__ double warp_loss[kKeptWarps];
-    const int64_t r = blockIdx.x;
-    const int n = (int)blockDim.x;
+    constexpr int kGroup = KeptShape<WARP>::kGroup;
+    __shared__ KeptShared<WARP> sh;
+    const int64_t r = kept_row<WARP>();
+    const int me = kept_rank<WARP>();
+    if (WARP && r >= a.rows) return;
     const float weight = a.row_weight != nullptr ? a.row_weight[r] : 1.0f;
-    if (kLoss) {   // in fp64: differences of logarithms that nearly cancel
-        double sum = 0.0, lse;
-        if constexpr (kGrad) {
-            await_previous_kernel();
-            const float2 stat = a.stat[r];
-            lse = soft_lse({stat.x, stat.y}, a.inv_t);
-            const double norm = a.row_norm[r];
-            for (int i = threadIdx.x; i < a.top; i += n) {
-                const float2 px = a.kept[r * a.top + i];
-                if (px.x != 0.0f) sum += (double)px.x * (((double)a.t_values[r * a.top + i] * a.inv_t - norm) - ((double)px.y * a.inv_t - lse));
-            }
-        } else {
-            KeptRow<DT> k(a, r, dyn, warp_stat);
-            await_previous_kernel();
-            const float2 stat = a.stat[r];
-            lse = soft_lse({stat.x, stat.y}, a.inv_t);
-            for (int i = threadIdx.x; i < a.top; i += n) {
-                const float p = k.prob(i, a);
-                if (p != 0.0f) sum += (double)p * (((double)k.t[i] * a.inv_t - k.norm) - ((double)k.x[i] * a.inv_t - lse));
-            }
+    double sum = 0.0, lse = 0.0;
+    if constexpr (!kGrad) {   // the kept entries, all of it
+        const KeptRow<DT, WARP> k(a, r, sh);
+        const double norm = k.norm(a);
+        await_previous_kernel();
+        const float2 stat = a.stat[r];
+        lse = soft_lse({stat.x, stat.y}, a.inv_t);
+#pragma unroll
+        for (int e = 0; e < kKeptEach; ++e) {   // in fp64: differences of logarithms that nearly cancel
+            const float p = k.prob(e, a);
+            if (p != 0.0f) sum += (double)p * (((double)k.t[e] * a.inv_t - norm) - ((double)k.x[e] * a.inv_t - lse));
         }
-        sum = kept_sum(sum, warp_loss);
-        if (threadIdx.x == 0) {
-            a.loss[r] = weight == 0.0f ? 0.0f : (float)((double)weight * (double)a.t * (double)a.t * sum);
-            if (a.lse != nullptr) a.lse[r] = (float)lse;
+    } else {
+        int j[kKeptEach];
+        float t[kKeptEach];
+        float2 px[kKeptEach];
+#pragma unroll
+        for (int e = 0; e < kKeptEach; ++e) {
+            const int i = me + e * kGroup;
+            j[e] = i < a.top ? a.t_indices[r * a.top + i] : -1;
+            t[e] = kLoss && i < a.top ? a.t_values[r * a.top + i] : 0.0f;
         }
-    }
-    if (kGrad) {
-        if (!kLoss) await_previous_kernel();
+        await_previous_kernel();
         const RowScale s = a.scale[r];
-        if (!s.live) return;   // zeros already
-        const bool doubled = a.doubled[r] != 0;
-        float ref = s.ref, dense = s.dense;
-        if (kLoss) {
-            const float2 stat = a.stat[r];
-            ref = soft_ref(stat.x);
-            dense = __fdiv_rn(dense, stat.y);
+        const float2 stat = kLoss ? a.stat[r] : make_float2(0.0f, 0.0f);
+        const double norm = kLoss ? a.row_norm[r] : 0.0;
+#pragma unroll
+        for (int e = 0; e < kKeptEach; ++e) {
+            const int i = me + e * kGroup;
+            px[e] = i < a.top ? a.kept[r * a.top + i] : make_float2(0.0f, 0.0f);
         }
-        Elem* out = reinterpret_cast<Elem*>(a.dS) + r * a.ldd;
-        for (int i = threadIdx.x; i < a.top; i += n) {   // their whole value, from the gathered logit
-            const int j = a.t_indices[r * a.top + i];
-            if (j < 0 || j >= (int)a.vocab) continue;
-            const float2 px = a.kept[r * a.top + i];
-            float p = px.x;
-            if (doubled) {   // every copy of the entry writes the same sum
-                p = 0.0f;
-                for (int o = 0; o < a.top; ++o)
-                    if (a.t_indices[r * a.top + o] == j) p = __fadd_rn(p, a.kept[r * a.top + o].x);
+        if (s.live) {   // the kept places' whole value, from the gathered logit
+            const float ref = kLoss ? soft_ref(stat.x) : s.ref, dense = kLoss ? __fdiv_rn(s.dense, stat.y) : s.dense;
+            Elem* out = reinterpret_cast<Elem*>(a.dS) + r * a.ldd;
+#pragma unroll
+            for (int e = 0; e < kKeptEach; ++e) {
+                if (j[e] < 0 || j[e] >= (int)a.vocab) continue;
+                float p = px[e].x;
+                if (s.live == 2) {   // some entry occurs twice: every copy writes the same sum
+                    p = 0.0f;
+                    for (int o = 0; o < a.top; ++o)
+                        if (a.t_indices[r * a.top + o] == j[e]) p = __fadd_rn(p, a.kept[r * a.top + o].x);
+                }
+                out[j[e]] = RV::narrow(__fsub_rn(dense_of(px[e].y, ref, dense, a.c), __fmul_rn(s.coef, p)));
             }
-            out[j] = RV::narrow(__fsub_rn(dense_of(px.y, ref, dense, a.c), __fmul_rn(s.coef, p)));
         }
+        if (!kLoss) return;
+        lse = soft_lse({stat.x, stat.y}, a.inv_t);
+#pragma unroll
+        for (int e = 0; e < kKeptEach; ++e)
+            if (px[e].x != 0.0f) sum += (double)px[e].x * (((double)t[e] * a.inv_t - norm) - ((double)px[e].y * a.inv_t - lse));
     }
+    sum = kept_sum<WARP>(sum, sh);
+    if (me == 0) {
+        a.loss[r] = weight == 0.0f ? 0.0f : (float)((double)weight * (double)a.t * (double)a.t * sum);
+        if (a.lse != nullptr) a.lse[r] = (float)lse;
+    }
+}
+
+// The launches before and after the vocabulary's.
+template <int DT, int MODE, bool WARP> int launch_kept(const DistillArgs& a, bool first, cudaLaunchAttribute* overlap, cudaStream_t st) {
+    using Shape = KeptShape<WARP>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((a.rows + Shape::kRows - 1) / Shape::kRows));
+    cfg.blockDim = dim3(Shape::kThreads);
+    cfg.stream = st;
+    if (first) {
+        cfg.dynamicSmemBytes = (size_t)Shape::kRows * (size_t)a.slots * 4u;   // at most 8 KB
+        MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, kept_kernel<DT, MODE, WARP>, a));
+    } else {
+        cfg.attrs = overlap;
+        cfg.numAttrs = 1;
+        MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, place_kernel<DT, MODE, WARP>, a));
+    }
+    return MOSAIC_OK;
 }
 
 template <int DT, int MODE> int launch_distill(DistillArgs a, cudaStream_t st) {
@@ -375,14 +418,10 @@ template <int DT, int MODE> int launch_distill(DistillArgs a, cudaStream_t st) {
     attr[1].val.clusterDim.x = (unsigned)c;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t kept = {};
-    kept.gridDim = dim3((unsigned)a.rows);
-    kept.blockDim = dim3(32 * kept_warps(a.top));
-    kept.stream = st;
-    kept.attrs = attr;
+    const bool warp_rows = a.top <= 32 * kKeptEach;
     if (MODE & kWantGrad) {
-        kept.dynamicSmemBytes = (size_t)a.top * 12u + (size_t)a.slots * 4u;   // at most 20 KB
-        MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&kept, kept_kernel<DT, MODE>, a));
+        const int rc = warp_rows ? launch_kept<DT, MODE, true>(a, true, attr, st) : launch_kept<DT, MODE, false>(a, true, attr, st);
+        if (rc != MOSAIC_OK) return rc;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.rows * c));
@@ -393,10 +432,7 @@ template <int DT, int MODE> int launch_distill(DistillArgs a, cudaStream_t st) {
     cfg.numAttrs = ((MODE & kWantGrad) ? 1 : 0) + (c > 1 ? 1 : 0);
     if (c > 1) MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, vocab_kernel<DT, MODE, true>, a));
     else MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, vocab_kernel<DT, MODE, false>, a));
-    kept.dynamicSmemBytes = (MODE & kWantGrad) ? 0 : (size_t)a.top * 12u;
-    kept.numAttrs = 1;
-    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&kept, place_kernel<DT, MODE>, a));
-    return MOSAIC_OK;
+    return warp_rows ? launch_kept<DT, MODE, true>(a, false, attr, st) : launch_kept<DT, MODE, false>(a, false, attr, st);
 }
 
 bool overlap(const void* a, size_t an, const void* b, size_t bn) {
@@ -444,7 +480,6 @@ template <int MODE> int distill(DistillArgs a, int64_t top, float temperature, i
     a.stat = reinterpret_cast<float2*>(a.scale + n);
     a.row_norm = reinterpret_cast<double*>(a.stat + n);
     a.kept = reinterpret_cast<float2*>(a.row_norm + n);
-    a.doubled = reinterpret_cast<int*>(a.kept + n * (size_t)top);
     a.t = temperature;
     a.slots = 64;
     while (a.slots < 2 * a.top) a.slots *= 2;
@@ -461,7 +496,7 @@ using namespace mosaic;
 
 extern "C" size_t mosaic_distill_workspace_bytes(int64_t rows, int64_t top) {
     if (rows <= 0 || top <= 0) return 0;
-    return align_up((size_t)rows * (sizeof(RowScale) + 8u + 8u + 4u + (size_t)top * 8u), 256);
+    return align_up((size_t)rows * (sizeof(RowScale) + 8u + 8u + (size_t)top * 8u), 256);
 }
 
 extern "C" int mosaic_distill_loss(const void* S, int64_t rows, int64_t vocab, int64_t lds, int dtype, const float* t_values,

@@ -85,7 +85,7 @@ def test_top_logits_refusals_need_no_device(lib):
 
 def test_distill_workspace(lib):
     q = lib.mosaic_distill_workspace_bytes
-    assert q(4, 10) == 512 and q(1000, 64) == (1000 * (36 + 512) + 255) // 256 * 256 and q(0, 10) == 0
+    assert q(4, 10) == 512 and q(1000, 64) == (1000 * (32 + 512) + 255) // 256 * 256 and q(0, 10) == 0
 
 
 def distill(lib, which, **k):
