@@ -685,6 +685,8 @@ def mosaic_compact_batch(jobs, stream=None) -> None:
 
 
 # ------------------------------------------------------------------ recovery of a pruned model
+# These calls are made many times per token or training step, so their marshalling is kept short: one helper per
+# kind of argument, the raw stream handle, the workspace query only where the answer is not zero by inspection.
 def _act_code(act) -> int:
     """An activation by its name or its code."""
     if isinstance(act, str):
@@ -694,33 +696,62 @@ def _act_code(act) -> int:
     return int(act)
 
 
-def _mat_of(t, name: str, rows: int, cols: int, dtype):
+def _matrix(t, name: str, dtype, device: int = -1):
+    """(pointer, rows, columns, leading dimension) of a row-major matrix; on `device`, if one is given."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor (no CPU path exists)")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have 2 dims")
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{name} must be row-major (unit stride along columns)")
+    if device >= 0 and t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}: the tensors of one call live on one device")
+    return t.data_ptr(), rows, cols, (ld if rows > 1 else max(ld, cols))
+
+
+def _like(t, name: str, dtype, device: int, rows: int, cols: int):
     """(pointer, leading dimension) of an optional [rows, cols] matrix."""
     if t is None:
-        return None, max(cols, 1)
-    _dev(t, name, dtype, 2)
-    if t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must be row-major (unit stride along columns)")
-    return t.data_ptr(), (t.stride(0) if rows > 1 else max(t.stride(0), cols))
+        return None, cols
+    p, r, c, ld = _matrix(t, name, dtype, device)
+    if r != rows or c != cols:
+        raise ValueError(f"{name} must be [{rows}, {cols}], got [{r}, {c}]")
+    return p, ld
 
 
-def _vec_of(t, name: str, n: int, dtype):
-    """Pointer of an optional contiguous vector of n entries."""
-    if t is None:
-        return None
-    _dev(t, name, dtype, 1)
-    if t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous with {n} entries")
+def _dense(t, name: str, dtype, device: int, *shape):
+    """Pointer of a contiguous tensor of this shape."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor (no CPU path exists)")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {list(shape)}, got {list(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}: the tensors of one call live on one device")
     return t.data_ptr()
 
 
-def _same_device(first: torch.Tensor, *others) -> None:
-    """All tensors of a call live on one device (that of the stream it runs on)."""
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"tensors of one call on different devices: {first.device} and {t.device}")
+def _dense_or_none(t, name: str, dtype, device: int, *shape):
+    return None if t is None else _dense(t, name, dtype, device, *shape)
+
+
+def _run_on(t: torch.Tensor, stream):
+    """(device index, raw stream) of a call: its tensors' device must be the current one, where it launches."""
+    device = t.get_device()
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"the call's tensors are on cuda:{device}, the current device is cuda:{torch._C._cuda_getDevice()}")
+    return device, (torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream) or None
+
+
+def _logits_code(t, name: str) -> int:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor (no CPU path exists)")
+    return _dtype_code(t)
 
 
 def mosaic_linear(X, W, Y, bias=None, residual=None, act=ACT_NONE, Z=None, status: torch.Tensor | None = None,
@@ -729,137 +760,116 @@ def mosaic_linear(X, W, Y, bias=None, residual=None, act=ACT_NONE, Z=None, statu
     and bias [out]; Z, if given, receives the value before the activation.  `act` is one of the ACT_*
     codes or "none" / "relu" / "gelu" / "silu"; `residual` may be Y (added in place).  `status` (int32, one
     word) as in mosaic_gram_accumulate."""
-    _dev(X, "X", torch.bfloat16, 2)
-    _dev(W, "W", torch.bfloat16, 2)
-    tokens, n_in = X.shape
-    n_out = W.shape[0]
-    xp, ldx = _mat_of(X, "X", tokens, n_in, torch.bfloat16)
-    wp, ldw = _mat_of(W, "W", n_out, n_in, torch.bfloat16)
+    bf16 = torch.bfloat16
+    xp, tokens, n_in, ldx = _matrix(X, "X", bf16)
+    dev, st = _run_on(X, stream)
+    wp, n_out, w_in, ldw = _matrix(W, "W", bf16, dev)
+    if w_in != n_in:
+        raise ValueError(f"W must be [out, {n_in}], got [{n_out}, {w_in}]")
     if Y is None:
         raise TypeError("Y must be a CUDA tensor")
-    yp, ldy = _mat_of(Y, "Y", tokens, n_out, torch.bfloat16)
-    rp, ldr = _mat_of(residual, "residual", tokens, n_out, torch.bfloat16)
-    zp, ldz = _mat_of(Z, "Z", tokens, n_out, torch.bfloat16)
-    bp = _vec_of(bias, "bias", n_out, torch.bfloat16)
-    sp = _vec_of(status, "status", 1, torch.int32)
-    _same_device(X, W, Y, bias, residual, Z, status)
-    L = lib()
-    need = L.mosaic_linear_workspace_bytes(xp, ldx, wp, ldw, tokens, n_out, n_in)
-    sc, sn = _ws(ws, X.device).get(need) if need else (None, 0)
-    _check(L.mosaic_linear(xp, ldx, wp, ldw, tokens, n_out, n_in, BF16, bp, rp, ldr, _act_code(act), yp, ldy, zp, ldz, sp, sc, sn,
-                           _stream(stream)), "mosaic_linear")
+    yp, ldy = _like(Y, "Y", bf16, dev, tokens, n_out)
+    rp, ldr = _like(residual, "residual", bf16, dev, tokens, n_out)
+    zp, ldz = _like(Z, "Z", bf16, dev, tokens, n_out)
+    bp = _dense_or_none(bias, "bias", bf16, dev, n_out)
+    sp = _dense_or_none(status, "status", torch.int32, dev, 1)
+    L, sc, sn = lib(), None, 0
+    if (xp | wp) & 15 or (ldx | ldw) & 7:      # an operand that is not 16-byte aligned is copied first
+        need = L.mosaic_linear_workspace_bytes(xp, ldx, wp, ldw, tokens, n_out, n_in)
+        if need:
+            sc, sn = _ws(ws, X.device).get(need)
+    _check(L.mosaic_linear(xp, ldx, wp, ldw, tokens, n_out, n_in, BF16, bp, rp, ldr, _act_code(act), yp, ldy, zp, ldz, sp, sc, sn, st),
+           "mosaic_linear")
 
 
 def mosaic_linear_backward(dY, X, W, Z=None, act=ACT_NONE, dX=None, dW=None, dbias=None, status: torch.Tensor | None = None,
                            ws: Workspace | None = None, stream=None) -> None:
     """Gradients of mosaic_linear: dX [tokens, in], dW [out, in], dbias [out] (each optional, all bf16) from dY
     [tokens, out], the inputs X and W, and - unless the activation is none - the stored Z."""
-    _dev(dY, "dY", torch.bfloat16, 2)
-    tokens, n_out = dY.shape
+    bf16 = torch.bfloat16
+    dyp, tokens, n_out, lddy = _matrix(dY, "dY", bf16)
+    dev, st = _run_on(dY, stream)
     if X is None and W is None:
         raise TypeError("X or W must be given")
-    n_in = (X if X is not None else W).shape[1]
     if (dW is not None and X is None) or (dX is not None and W is None):
         raise ValueError("dW needs X and dX needs W")
+    n_in = (X if X is not None else W).shape[1]
     act = _act_code(act)
     if act != ACT_NONE and Z is None:
         raise ValueError("the backward pass of an activation needs the stored Z")
-    dyp, lddy = _mat_of(dY, "dY", tokens, n_out, torch.bfloat16)
-    xp, ldx = _mat_of(X, "X", tokens, n_in, torch.bfloat16)
-    wp, ldw = _mat_of(W, "W", n_out, n_in, torch.bfloat16)
-    zp, ldz = _mat_of(Z, "Z", tokens, n_out, torch.bfloat16)
-    dxp, lddx = _mat_of(dX, "dX", tokens, n_in, torch.bfloat16)
-    dwp, lddw = _mat_of(dW, "dW", n_out, n_in, torch.bfloat16)
-    dbp = _vec_of(dbias, "dbias", n_out, torch.bfloat16)
-    sp = _vec_of(status, "status", 1, torch.int32)
-    _same_device(dY, X, W, Z, dX, dW, dbias, status)
+    xp, ldx = _like(X, "X", bf16, dev, tokens, n_in)
+    wp, ldw = _like(W, "W", bf16, dev, n_out, n_in)
+    zp, ldz = _like(Z, "Z", bf16, dev, tokens, n_out)
+    dxp, lddx = _like(dX, "dX", bf16, dev, tokens, n_in)
+    dwp, lddw = _like(dW, "dW", bf16, dev, n_out, n_in)
+    dbp = _dense_or_none(dbias, "dbias", bf16, dev, n_out)
+    sp = _dense_or_none(status, "status", torch.int32, dev, 1)
     L = lib()
     need = L.mosaic_linear_backward_workspace_bytes(dyp, lddy, xp, ldx, wp, ldw, tokens, n_out, n_in, act, dxp is not None, dwp is not None,
                                                     dbp is not None)
     sc, sn = _ws(ws, dY.device).get(need) if need else (None, 0)
-    _check(L.mosaic_linear_backward(dyp, lddy, xp, ldx, wp, ldw, zp, ldz, tokens, n_out, n_in, BF16, act, dxp, lddx, dwp, lddw, dbp, sp, sc, sn,
-                                    _stream(stream)), "mosaic_linear_backward")
-
-
-def _logits_of(t, name: str):
-    _dev(t, name, ndim=2)
-    p, ld = _mat_of(t, name, t.shape[0], t.shape[1], t.dtype)
-    return p, t.shape[0], t.shape[1], ld, _dtype_code(t)
+    _check(L.mosaic_linear_backward(dyp, lddy, xp, ldx, wp, ldw, zp, ldz, tokens, n_out, n_in, BF16, act, dxp, lddx, dwp, lddw, dbp, sp, sc, sn, st),
+           "mosaic_linear_backward")
 
 
 def mosaic_top_logits(L, values, indices, lse=None, temperature: float = 1.0, stream=None) -> None:
     """The values.shape[1] largest logits of every row of L [rows, vocab] (fp32 or bf16), in order (value
     descending, ties by index): `values` fp32 and `indices` int32 [rows, top]; `lse`, fp32 [rows], receives
     log sum exp(L / temperature) over the whole row."""
-    lp, rows, vocab, ldl, code = _logits_of(L, "L")
-    _dev(values, "values", torch.float32, 2)
-    _dev(indices, "indices", torch.int32, 2)
-    top = values.shape[1]
-    for t, nm in ((values, "values"), (indices, "indices")):
-        if tuple(t.shape) != (rows, top) or not t.is_contiguous():
-            raise ValueError(f"{nm} must be contiguous [{rows}, {top}]")
-    sp = _vec_of(lse, "lse", rows, torch.float32)
-    _same_device(L, values, indices, lse)
-    _check(lib().mosaic_top_logits(lp, rows, vocab, ldl, code, top, float(temperature), values.data_ptr(), indices.data_ptr(), sp,
-                                   _stream(stream)), "mosaic_top_logits")
+    code = _logits_code(L, "L")
+    lp, rows, vocab, ldl = _matrix(L, "L", L.dtype)
+    dev, st = _run_on(L, stream)
+    top = values.shape[-1] if isinstance(values, torch.Tensor) and values.dim() == 2 else 0
+    vp = _dense(values, "values", torch.float32, dev, rows, top)
+    ip = _dense(indices, "indices", torch.int32, dev, rows, top)
+    sp = _dense_or_none(lse, "lse", torch.float32, dev, rows)
+    _check(lib().mosaic_top_logits(lp, rows, vocab, ldl, code, top, temperature, vp, ip, sp, st), "mosaic_top_logits")
 
 
-def _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature):
-    sp, rows, vocab, lds, code = _logits_of(S, "S")
-    _dev(t_values, "t_values", torch.float32, 2)
-    _dev(t_indices, "t_indices", torch.int32, 2)
-    top = t_values.shape[1]
-    for t, nm in ((t_values, "t_values"), (t_indices, "t_indices")):
-        if tuple(t.shape) != (rows, top) or not t.is_contiguous():
-            raise ValueError(f"{nm} must be contiguous [{rows}, {top}]")
-    tl = _vec_of(t_lse, "t_lse", rows, torch.float32)
-    rw = _vec_of(row_weight, "row_weight", rows, torch.float32)
-    _same_device(S, t_values, t_indices, t_lse, row_weight)
-    return (sp, rows, vocab, lds, code, t_values.data_ptr(), t_indices.data_ptr(), top, tl, rw, float(temperature)), rows, vocab, top
-
-
-def _distill_dS(S, dS, rows, vocab):
-    if dS is None:
-        raise TypeError("dS must be a CUDA tensor")
-    p, ld = _mat_of(dS, "dS", rows, vocab, S.dtype)
-    _same_device(S, dS)
-    return p, ld
+def _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature, stream, ws):
+    """What the three distillation calls share: (leading arguments, (rows, vocab, device), workspace, its size, stream)."""
+    code = _logits_code(S, "S")
+    sp, rows, vocab, lds = _matrix(S, "S", S.dtype)
+    dev, st = _run_on(S, stream)
+    top = t_values.shape[-1] if isinstance(t_values, torch.Tensor) and t_values.dim() == 2 else 0
+    tv = _dense(t_values, "t_values", torch.float32, dev, rows, top)
+    ti = _dense(t_indices, "t_indices", torch.int32, dev, rows, top)
+    tl = _dense_or_none(t_lse, "t_lse", torch.float32, dev, rows)
+    rw = _dense_or_none(row_weight, "row_weight", torch.float32, dev, rows)
+    wp, wn = _ws(ws, S.device).get(lib().mosaic_distill_workspace_bytes(rows, top))
+    return (sp, rows, vocab, lds, code, tv, ti, top, tl, rw, temperature), (rows, vocab, dev), wp, wn, st
 
 
 def mosaic_distill_loss(S, t_values, t_indices, loss, lse=None, t_lse=None, row_weight=None, temperature: float = 1.0,
                         ws: Workspace | None = None, stream=None) -> None:
     """Distillation loss of every row of the student's logits S [rows, vocab] (fp32 or bf16) against a teacher's
     kept logits (t_values fp32, t_indices int32 [rows, top]); `loss` and `lse` (optional) are fp32 [rows]."""
-    args, rows, _, top = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
-    lo, ls = _vec_of(loss, "loss", rows, torch.float32), _vec_of(lse, "lse", rows, torch.float32)
-    _same_device(S, loss, lse)
-    L = lib()
-    wp, wn = _ws(ws, S.device).get(L.mosaic_distill_workspace_bytes(rows, top))
-    _check(L.mosaic_distill_loss(*args, lo, ls, wp, wn, _stream(stream)), "mosaic_distill_loss")
+    args, (rows, _, dev), wp, wn, st = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature, stream, ws)
+    lo, ls = _dense(loss, "loss", torch.float32, dev, rows), _dense_or_none(lse, "lse", torch.float32, dev, rows)
+    _check(lib().mosaic_distill_loss(*args, lo, ls, wp, wn, st), "mosaic_distill_loss")
 
 
 def mosaic_distill_grad(S, t_values, t_indices, lse, dS, t_lse=None, row_weight=None, grad_rows=None, grad_scale: float = 1.0,
                         temperature: float = 1.0, ws: Workspace | None = None, stream=None) -> None:
     """Gradient of mosaic_distill_loss with respect to S, from the lse that call stored; `grad_rows` (fp32 [rows]) times
     `grad_scale` is the gradient of each row's loss.  dS may be S."""
-    args, rows, vocab, top = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
-    ls, gr = _vec_of(lse, "lse", rows, torch.float32), _vec_of(grad_rows, "grad_rows", rows, torch.float32)
-    dp, ldd = _distill_dS(S, dS, rows, vocab)
-    _same_device(S, lse, grad_rows)
-    L = lib()
-    wp, wn = _ws(ws, S.device).get(L.mosaic_distill_workspace_bytes(rows, top))
-    _check(L.mosaic_distill_grad(*args, ls, gr, float(grad_scale), dp, ldd, wp, wn, _stream(stream)), "mosaic_distill_grad")
+    args, (rows, vocab, dev), wp, wn, st = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature, stream, ws)
+    ls = _dense(lse, "lse", torch.float32, dev, rows)
+    gr = _dense_or_none(grad_rows, "grad_rows", torch.float32, dev, rows)
+    if dS is None:
+        raise TypeError("dS must be a CUDA tensor")
+    dp, ldd = _like(dS, "dS", S.dtype, dev, rows, vocab)
+    _check(lib().mosaic_distill_grad(*args, ls, gr, grad_scale, dp, ldd, wp, wn, st), "mosaic_distill_grad")
 
 
 def mosaic_distill_loss_grad(S, t_values, t_indices, loss, lse, dS, t_lse=None, row_weight=None, grad_rows=None, grad_scale: float = 1.0,
                              temperature: float = 1.0, ws: Workspace | None = None, stream=None) -> None:
     """mosaic_distill_loss and mosaic_distill_grad in one pass over S (the training step, where the gradient of each row's
     loss is known beforehand).  `lse` may be None; dS may be S."""
-    args, rows, vocab, top = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature)
-    lo, ls = _vec_of(loss, "loss", rows, torch.float32), _vec_of(lse, "lse", rows, torch.float32)
-    gr = _vec_of(grad_rows, "grad_rows", rows, torch.float32)
-    dp, ldd = _distill_dS(S, dS, rows, vocab)
-    _same_device(S, loss, lse, grad_rows)
-    L = lib()
-    wp, wn = _ws(ws, S.device).get(L.mosaic_distill_workspace_bytes(rows, top))
-    _check(L.mosaic_distill_loss_grad(*args, lo, ls, gr, float(grad_scale), dp, ldd, wp, wn, _stream(stream)), "mosaic_distill_loss_grad")
+    args, (rows, vocab, dev), wp, wn, st = _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature, stream, ws)
+    lo, ls = _dense(loss, "loss", torch.float32, dev, rows), _dense_or_none(lse, "lse", torch.float32, dev, rows)
+    gr = _dense_or_none(grad_rows, "grad_rows", torch.float32, dev, rows)
+    if dS is None:
+        raise TypeError("dS must be a CUDA tensor")
+    dp, ldd = _like(dS, "dS", S.dtype, dev, rows, vocab)
+    _check(lib().mosaic_distill_loss_grad(*args, lo, ls, gr, grad_scale, dp, ldd, wp, wn, st), "mosaic_distill_loss_grad")
