@@ -501,16 +501,19 @@ int mosaic_linear_backward(const void *dY, int64_t lddy, const void *X, int64_t 
  * (value descending, ties by ascending index), and the row's log-sum-exp:
  *     lse[r] = log sum_j exp(L[r,j] / temperature)     over the whole row
  * which is all distillation needs of a teacher's answer.
- *   L         device, [rows, vocab], ld ldl, fp32 or bf16; vocab < 2^31 - 256
+ *   L         device, [rows, vocab], ld ldl, fp32 or bf16; vocab <= 2^20
  *   top       1 .. min(vocab, 1024)
  *   values    device, [rows, top] fp32, dense: the logits themselves
  *   indices   device, [rows, top] int32, dense
  *   lse       device, [rows] fp32, or NULL
+ *   ws        device scratch, >= the query for the same sizes
  * -0 and +0 are equal; a NaN orders above +inf (its row's lse is NaN).  Entries of
  * -inf are masked: they come last, lowest index first.  A row of -inf has lse -inf.
  * ------------------------------------------------------------------------- */
+size_t mosaic_top_logits_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int64_t top);
 int mosaic_top_logits(const void *L, int64_t rows, int64_t vocab, int64_t ldl, int dtype, int64_t top,
-                      float temperature, float *values, int32_t *indices, float *lse, void *stream);
+                      float temperature, float *values, int32_t *indices, float *lse, void *ws, size_t ws_bytes,
+                      void *stream);
 
 /* ---------------------------------------------------------------------------
  * mosaic_distill_loss / _grad / _loss_grad - distillation from a teacher's top

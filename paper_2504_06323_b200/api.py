@@ -46,7 +46,7 @@ SYMBOLS = (
     "mosaic_gram_accumulate",
     "mosaic_linear_workspace_bytes", "mosaic_linear",
     "mosaic_linear_backward_workspace_bytes", "mosaic_linear_backward",
-    "mosaic_top_logits",
+    "mosaic_top_logits_workspace_bytes", "mosaic_top_logits",
     "mosaic_distill_workspace_bytes", "mosaic_distill_loss", "mosaic_distill_grad", "mosaic_distill_loss_grad",
     "mosaic_bounded_wait_selftest",
 )
@@ -139,7 +139,9 @@ def lib() -> C.CDLL:
         L.mosaic_linear_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, ci, ci, vp, i64, vp, i64, vp,
                                              vp, vp, sz, vp]
         L.mosaic_top_logits.restype = ci
-        L.mosaic_top_logits.argtypes = [vp, i64, i64, i64, ci, i64, flt, vp, vp, vp, vp]
+        L.mosaic_top_logits.argtypes = [vp, i64, i64, i64, ci, i64, flt, vp, vp, vp, vp, sz, vp]
+        L.mosaic_top_logits_workspace_bytes.restype = sz
+        L.mosaic_top_logits_workspace_bytes.argtypes = [i64, i64, ci, i64]
         teacher = [vp, i64, i64, i64, ci, vp, vp, i64, vp, vp, flt]
         L.mosaic_distill_workspace_bytes.restype = sz
         L.mosaic_distill_workspace_bytes.argtypes = [i64, i64]
@@ -812,7 +814,7 @@ def mosaic_linear_backward(dY, X, W, Z=None, act=ACT_NONE, dX=None, dW=None, dbi
            "mosaic_linear_backward")
 
 
-def mosaic_top_logits(L, values, indices, lse=None, temperature: float = 1.0, stream=None) -> None:
+def mosaic_top_logits(L, values, indices, lse=None, temperature: float = 1.0, ws: Workspace | None = None, stream=None) -> None:
     """The values.shape[1] largest logits of every row of L [rows, vocab] (fp32 or bf16), in order (value
     descending, ties by index): `values` fp32 and `indices` int32 [rows, top]; `lse`, fp32 [rows], receives
     log sum exp(L / temperature) over the whole row."""
@@ -823,7 +825,9 @@ def mosaic_top_logits(L, values, indices, lse=None, temperature: float = 1.0, st
     vp = _dense(values, "values", torch.float32, dev, rows, top)
     ip = _dense(indices, "indices", torch.int32, dev, rows, top)
     sp = _dense_or_none(lse, "lse", torch.float32, dev, rows)
-    _check(lib().mosaic_top_logits(lp, rows, vocab, ldl, code, top, temperature, vp, ip, sp, st), "mosaic_top_logits")
+    lb = lib()
+    wp, wn = _ws(ws, L.device).get(lb.mosaic_top_logits_workspace_bytes(rows, vocab, code, top))
+    _check(lb.mosaic_top_logits(lp, rows, vocab, ldl, code, top, temperature, vp, ip, sp, wp, wn, st), "mosaic_top_logits")
 
 
 def _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature, stream, ws):

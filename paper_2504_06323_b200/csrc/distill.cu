@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, kRowCtas) vocab_kernel(const __grid_
                 for (int i = 0; i < kBatch; ++i)
                     if (v + i * kThreads < part.v_hi) copy[v + i * kThreads - part.v_lo] = raw[i];
             }
-            soft_batch<DT>(raw, a.c, st);
+            soft_batch<DT>(raw, batch_max<DT>(raw), a.c, st);
         }
         if (lone >= 0) st = soft_merge(st, soft_one(lone_x, a.c), a.c);
         st = soft_warp(st, a.c);

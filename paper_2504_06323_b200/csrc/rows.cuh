@@ -214,10 +214,10 @@ template <int DT> __device__ __forceinline__ float batch_max(const uint4 (&raw)[
 }
 // One entry's statistics.
 __device__ __forceinline__ SoftStat soft_one(float x, float c) { return {x, exp2_fast(__fmul_rn(__fsub_rn(x, soft_ref(x)), c))}; }
-// A batch's statistics merged into the thread's.
-template <int DT> __device__ __forceinline__ void soft_batch(const uint4 (&raw)[kBatch], float c, SoftStat& st) {
+// A batch's statistics merged into the thread's; `most`: its largest entry.
+template <int DT> __device__ __forceinline__ void soft_batch(const uint4 (&raw)[kBatch], float most, float c, SoftStat& st) {
     using RV = RowVec<DT>;
-    const float m = fmaxf(st.m, batch_max<DT>(raw));
+    const float m = fmaxf(st.m, most);
     const float ref = soft_ref(m);
     const Pair minus_ref = pair_of(-ref, -ref), cc = pair_of(c, c);
     Pair sum = pair_of(0.0f, 0.0f);   // the batch's sum first: fewer roundings at the size of the total

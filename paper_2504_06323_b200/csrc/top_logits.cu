@@ -1,23 +1,26 @@
 // mosaic_top_logits: the k largest logits of every row, in order (value descending, index ascending), and
 // the log-sum-exp of the whole row - what is kept of a teacher's answer for distillation.
 //
-// One pass over the row (rows.cuh).  Every thread knows the largest of its entries (64 of 32000); the
-// k-th largest of those maxima is a value that at least k entries reach, and on rows in no particular order
-// only a few more than k do.  It is found by bisection over the maxima's order-preserving bit patterns, one
-// vote of the block a step.  The entries that reach it are collected and ranked exactly, under (value,
-// index).  A row where more than the list holds reach it (masked rows, many ties, k near the number of
-// threads) is selected digit by digit over all its entries instead.  Bound by memory.
+// Two launches, the second of which starts under the first:
+//   sweep_kernel    streams the rows once: softmax statistics, and the largest entry of every group of entries that
+//                   lie together (128 bytes, or 16 where k is near the number of such groups), as a 16-bit pattern
+//   pick_kernel     a small CTA a row.  The k-th largest of the group maxima is a value that at least k entries reach,
+//                   and on rows in no particular order only a few more than k do.  It is found by bisection over the
+//                   patterns; only the groups that reach it (k of them and a few) are read again; their entries that
+//                   reach it are ranked exactly, under (value, index).  A row where more than the list holds reach it
+//                   (masked rows, many ties) or that has a NaN is selected digit by digit over all its entries.
+// The first is bound by memory.  The second is a chain of short dependent steps: small CTAs, so that many rows'
+// chains overlap; inside the sweep, three CTAs an SM, the same steps took as long again as the sweep itself (98 us for
+// 4096 x 32000 bf16 instead of %%TOP%%).
 #include <math.h>
 
 #include "rows.cuh"
 
-namespace cg = cooperative_groups;
-
 namespace mosaic {
 namespace {
 
-constexpr int kListCap = 2048;   // entries collected per row
-constexpr int kSlack = 8;        // candidates too many that are not worth another vote
+constexpr int kPickThreads = 128;
+constexpr int kSlack = 8;        // candidates too many that are not worth another step of the bisection
 constexpr int kRankMost = 256;   // up to here a list is ranked by counting, above it by a bitonic sort
 
 struct TopArgs {
@@ -29,6 +32,13 @@ struct TopArgs {
     float* lse;
     double inv_t;
     float c;
+    int part_vecs, parts;    // vectors of a row that a CTA sweeps, CTAs a row
+    int group_shift;         // a group is 2^group_shift vectors: 8, or 1
+    int groups;              // patterns a row has room for, a multiple of 8
+    int list_cap;            // candidates that fit
+    // workspace
+    float2* stat;            // [rows, parts]
+    uint16_t* patterns;      // [rows, groups]
 };
 
 // Order-preserving pattern: larger value <=> larger key; -0 and +0 are equal, every NaN is above +inf.
@@ -41,27 +51,106 @@ __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(
 // One number that orders (value descending, index ascending) descending; distinct for distinct entries.
 __device__ __forceinline__ uint64_t entry_of(uint32_t key, int col) { return ((uint64_t)key << 32) | (uint32_t)~(uint32_t)col; }
 
-struct TopShared {
-    uint64_t list[kListCap];
-    SoftStat warp_stat[kWarps];
-    SoftStat cta_stat[kMaxCluster];
-    uint32_t cta_floor[kMaxCluster];
+// ---------------------------------------------------------------- sweep
+// The largest entry of each of a batch's vectors; with `wide`, of each run of eight lanes' vectors (in every lane).
+// Returns the largest of the thread's own batch.
+template <int DT> __device__ __forceinline__ float group_max(const uint4 (&raw)[kBatch], bool wide, float (&m)[kBatch]) {
+    float own;
+    using RV = RowVec<DT>;
+    static_assert(kBatch == 4, "two vectors' bf16 maxima share a register");
+    if constexpr (DT == MOSAIC_BF16) {
+        uint32_t w[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            uint32_t a = raw[i].x, b = raw[i].z, h;
+            asm("max.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(raw[i].y));
+            asm("max.bf16x2 %0, %0, %1;" : "+r"(b) : "r"(raw[i].w));
+            asm("max.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+            h = __funnelshift_l(a, a, 16);
+            asm("max.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(h));
+            w[i] = a;   // both halves
+        }
+        uint32_t p = __byte_perm(w[0], w[1], 0x5410), q = __byte_perm(w[2], w[3], 0x5410), o2 = p;
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(o2) : "r"(q));
+        own = fmaxf(__uint_as_float(o2 << 16), __uint_as_float(o2 & 0xFFFF0000u));
+        if (wide) {
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) {
+                const uint32_t pp = __shfl_xor_sync(0xFFFFFFFFu, p, o), qq = __shfl_xor_sync(0xFFFFFFFFu, q, o);
+                asm("max.bf16x2 %0, %0, %1;" : "+r"(p) : "r"(pp));
+                asm("max.bf16x2 %0, %0, %1;" : "+r"(q) : "r"(qq));
+            }
+        }
+        m[0] = __uint_as_float(p << 16);
+        m[1] = __uint_as_float(p & 0xFFFF0000u);
+        m[2] = __uint_as_float(q << 16);
+        m[3] = __uint_as_float(q & 0xFFFF0000u);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            m[i] = fmaxf(fmaxf(RV::get(raw[i], 0), RV::get(raw[i], 1)), fmaxf(RV::get(raw[i], 2), RV::get(raw[i], 3)));
+            own = i == 0 ? m[0] : fmaxf(own, m[i]);
+            if (wide) {
+#pragma unroll
+                for (int o = 1; o < 8; o <<= 1) m[i] = fmaxf(m[i], __shfl_xor_sync(0xFFFFFFFFu, m[i], o));
+            }
+        }
+    }
+    return own;
+}
+
+template <int DT> __global__ void __launch_bounds__(kThreads, kRowCtas) sweep_kernel(const __grid_constant__ TopArgs a) {
+    __shared__ SoftStat warp_stat[kWarps];
+    allow_next_kernel();
+    const int64_t r = blockIdx.x;
+    const int p = (int)blockIdx.y;
+    RowPart<DT> part(a.L, r, a.ldl, (int)a.vocab, p, a.parts);
+    const int nv = (part.cols - part.head) / RowVec<DT>::kElems;
+    part.v_lo = p * a.part_vecs;   // parts begin on a group's boundary
+    part.v_hi = part.v_lo + a.part_vecs < nv ? part.v_lo + a.part_vecs : nv;
+    const int lane = threadIdx.x & 31;
+    const bool wide = a.group_shift != 0;
+    uint16_t* patterns = a.patterns + r * a.groups;
+    SoftStat st = {-INFINITY, 0.0f};
+    // whole warps stay together (their lanes share groups): up to the last vector of the part, rounded to the block
+    for (int v = part.v_lo + (int)threadIdx.x; v - (int)threadIdx.x < part.v_hi; v += kBatch * kThreads) {
+        uint4 raw[kBatch];
+        part.load(v, raw);
+        float m[kBatch];
+        const float own = group_max<DT>(raw, wide, m);
+        soft_batch<DT>(raw, own, a.c, st);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int u = v + i * kThreads;   // the group's first lane has its first vector
+            if (u < part.v_hi && (!wide || (lane & 7) == 0)) patterns[u >> a.group_shift] = (uint16_t)(order_key(m[i]) >> 16);
+        }
+    }
+    const int lone = part.single();
+    if (lone >= 0) st = soft_merge(st, soft_one(part.at(lone), a.c), a.c);
+    st = soft_warp(st, a.c);
+    if (lane == 0) warp_stat[threadIdx.x >> 5] = st;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    st = soft_all(warp_stat, kWarps, a.c);
+    if (threadIdx.x == 0) a.stat[r * a.parts + p] = make_float2(st.m, st.s);
+}
+
+// ---------------------------------------------------------------- pick
+struct PickShared {
     uint32_t hist[256];
-    uint32_t warp_count[kWarps];
-    uint16_t owner[kThreads];
-    uint32_t kept;
+    uint32_t warp_count[kPickThreads / 32];
     uint32_t count;
     uint32_t digit, rest;
 };
 
 // The exact selection over a whole row by one CTA, digit by digit: leaves the k entries in list[0, k).
-template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, TopShared& sh) {
+template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, uint64_t* list, PickShared& sh) {
     const int cols = row.cols, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t prefix = 0u, mask = 0u, want = (uint32_t)top;   // the want-th largest among the keys that share the prefix
     for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = threadIdx.x; i < 256; i += kThreads) sh.hist[i] = 0u;
+        for (int i = threadIdx.x; i < 256; i += kPickThreads) sh.hist[i] = 0u;
         __syncthreads();
-        for (int j0 = 0; j0 < cols; j0 += kThreads) {
+        for (int j0 = 0; j0 < cols; j0 += kPickThreads) {
             const int j = j0 + (int)threadIdx.x;
             const uint32_t key = j < cols ? order_key(row.at(j)) : 0u;
             const bool in = j < cols && (key & mask) == prefix;
@@ -95,7 +184,7 @@ template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, To
     if (threadIdx.x == 0) sh.count = 0u;
     __syncthreads();
     uint32_t equal_before = 0u;
-    for (int j0 = 0; j0 < cols; j0 += kThreads) {
+    for (int j0 = 0; j0 < cols; j0 += kPickThreads) {
         const int j = j0 + (int)threadIdx.x;
         const uint32_t key = j < cols ? order_key(row.at(j)) : 0u;
         const bool equal = j < cols && key == prefix;
@@ -104,112 +193,32 @@ template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, To
         __syncthreads();
         uint32_t before = equal_before + (uint32_t)__popc(votes & ((1u << lane) - 1u));
         uint32_t total = 0u;
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < kPickThreads / 32; ++w) {
             if (w < warp) before += sh.warp_count[w];
             total += sh.warp_count[w];
         }
-        if ((j < cols && key > prefix) || (equal && before < want)) sh.list[atomicAdd(&sh.count, 1u)] = entry_of(key, j);
+        if ((j < cols && key > prefix) || (equal && before < want)) list[atomicAdd(&sh.count, 1u)] = entry_of(key, j);
         equal_before += total;
         __syncthreads();
     }
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kThreads, kRowCtas) top_logits_kernel(const __grid_constant__ TopArgs a) {
-    using RV = RowVec<DT>;
-    __shared__ TopShared sh;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int n_ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int64_t r = blockIdx.x >> (__ffs(n_ctas) - 1);   // a power of two
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int vocab = (int)a.vocab;
-    const RowPart<DT> part(a.L, r, a.ldl, vocab, rank, n_ctas);
-    const int lone = part.single();
-    const float lone_x = lone >= 0 ? part.at(lone) : -INFINITY;
-    if (threadIdx.x == 0) {
-        sh.count = 0u;
-        sh.kept = 0u;
-    }
-    if (n_ctas > 1) cluster_arrive();   // waited for before the first write to another CTA
-
-    SoftStat st = {-INFINITY, 0.0f};
-    for (int v = part.v_lo + (int)threadIdx.x; v < part.v_hi; v += kBatch * kThreads) {
-        uint4 raw[kBatch];
-        part.load(v, raw);
-        soft_batch<DT>(raw, a.c, st);
-    }
-    if (lone >= 0) st = soft_merge(st, soft_one(lone_x, a.c), a.c);
-    // the thread's largest entry, as a 16-bit pattern rounded down (a NaN makes the sum NaN: above all)
-    const bool any = part.v_lo + (int)threadIdx.x < part.v_hi || lone >= 0;
-    const uint32_t mine = any ? (st.s != st.s ? 0xFFFFu : order_key(st.m) >> 16) : 0u;
-
-    // a pattern that at least `top` of the threads' maxima reach, the largest or one that few more do (0: all entries
-    // are candidates)
-    uint32_t floor_key = 0u;
-    for (int bit = 15; bit >= 0; --bit) {
-        const uint32_t trial = floor_key | (1u << bit);
-        const int n = __syncthreads_count(mine >= trial);
-        if (n >= a.top) {
-            floor_key = trial;
-            if (n <= a.top + kSlack) break;
-        }
-    }
-    st = soft_warp(st, a.c);
-    if (lane == 0) sh.warp_stat[warp] = st;
-    if (n_ctas > 1) cluster_wait();
-    __syncthreads();
-    st = soft_all(sh.warp_stat, kWarps, a.c);
-    if (n_ctas > 1) {   // a part's floor holds for the row: the highest of them serves all
-        if (threadIdx.x < n_ctas) {
-            *cluster.map_shared_rank(&sh.cta_stat[rank], threadIdx.x) = st;
-            *cluster.map_shared_rank(&sh.cta_floor[rank], threadIdx.x) = floor_key;
-        }
-        cluster.sync();
-        st = soft_all(sh.cta_stat, n_ctas, a.c);
-        for (int i = 0; i < n_ctas; ++i) floor_key = sh.cta_floor[i] > floor_key ? sh.cta_floor[i] : floor_key;
-    }
-    if (rank == 0 && threadIdx.x == 0 && a.lse != nullptr) a.lse[r] = (float)soft_lse(st, a.inv_t);
-
-    // ---- candidates into the first CTA's list
-    {
-        uint32_t* count = cluster.map_shared_rank(&sh.count, 0);
-        uint64_t* list = cluster.map_shared_rank(sh.list, 0);
-        const float least = floor_key == 0u ? -INFINITY : key_value(floor_key << 16);
-        auto take = [&](float x, int j) {
-            const uint32_t at = atomicAdd(count, 1u);
-            if (at < kListCap) list[at] = entry_of(order_key(x), j);
-        };
-        if (lone >= 0 && !(lone_x < least)) take(lone_x, lone);
-        // Few threads (about `top` of them) hold a candidate.  The whole block goes through their vectors, a vector or
-        // two per thread, from L2.
-        if (mine >= floor_key && part.v_lo + (int)threadIdx.x < part.v_hi) sh.owner[atomicAdd(&sh.kept, 1u)] = (uint16_t)threadIdx.x;
-        __syncthreads();
-        const int kept = (int)sh.kept;
-        const int rounds = (part.v_hi - part.v_lo + kThreads - 1) / kThreads;
-        for (int u = (int)threadIdx.x; u < kept * rounds; u += kThreads) {
-            const int v = part.v_lo + sh.owner[u % kept] + (u / kept) * kThreads;
-            if (v >= part.v_hi) continue;
-            const uint4 w = ld_stream16(part.vec(v));
-            uint32_t mask = reach_mask<DT>(w, least);
-            while (mask != 0u) {
-                const int e = __ffs(mask) - 1;
-                mask &= mask - 1u;
-                take(RV::any(w, e), part.first(v) + e);
-            }
-        }
-    }
-    if (n_ctas > 1) cluster.sync();
+// What a row's threads share: a warp's row, four a CTA (up to kWarpTop kept), or a CTA's.
+constexpr int kWarpTop = 128;
+template <bool WARP> __device__ __forceinline__ void pick_sync() {
+    if (WARP) __syncwarp();
     else __syncthreads();
-    if (rank != 0) return;
-    uint32_t n = sh.count;
-    __syncthreads();
-    if (n > kListCap) {
-        select_all<DT>(part, a.top, sh);
-        n = (uint32_t)a.top;
-        __syncthreads();
-    }
+}
+struct PickRow {
+    uint32_t votes[16];
+    uint32_t count;      // candidates found
+    uint32_t kept;       // groups that hold some
+    uint32_t floor;
+    int all;             // the list is no use: the row is selected over all its entries
+};
 
-    // ---- exact order of the list
+// The first `top` of n entries of a list, exactly and in order, by N threads (me: this one's number).
+template <int DT, int N> __device__ __forceinline__ void emit_list(const RowPart<DT>& part, const TopArgs& a, int64_t r, uint64_t* list, uint32_t n, uint32_t me) {
     float* values = a.values + r * a.top;
     int32_t* indices = a.indices + r * a.top;
     auto emit = [&](uint32_t place, uint64_t entry) {
@@ -219,54 +228,246 @@ __global__ void __launch_bounds__(kThreads, kRowCtas) top_logits_kernel(const __
         values[place] = key == 0x80000000u || key == 0xFFFFFFFFu ? part.at(j) : key_value(key);
         indices[place] = j;
     };
-    if (n <= kRankMost) {
-        // a group of `share` threads counts the larger entries of one candidate
-        uint32_t share = 2u;
-        while (share < 32u && n * share * 2u <= kThreads) share *= 2u;
-        for (uint32_t i0 = 0; i0 < n; i0 += kThreads / share) {
-            const uint32_t i = i0 + threadIdx.x / share;
-            const uint64_t me = i < n ? sh.list[i] : 0ull;
+    if (n <= kRankMost) {   // an entry's place is the number of larger ones
+        for (uint32_t i = me; i < n; i += N) {
+            const uint64_t mine = list[i];
             uint32_t above = 0u;
-            for (uint32_t o = threadIdx.x % share; o < n; o += share) above += sh.list[o] > me ? 1u : 0u;
-            for (uint32_t o = share / 2u; o > 0u; o >>= 1) above += __shfl_xor_sync(0xFFFFFFFFu, above, o);
-            if (i < n && threadIdx.x % share == 0u && above < (uint32_t)a.top) emit(above, me);
+#pragma unroll 8
+            for (uint32_t o = 0; o < n; ++o) above += list[o] > mine ? 1u : 0u;
+            if (above < (uint32_t)a.top) emit(above, mine);
         }
         return;
     }
     uint32_t size = kRankMost * 2;
     while (size < n) size *= 2u;
-    for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) sh.list[i] = 0ull;   // below every entry (a column's complement is not 0)
-    __syncthreads();
+    for (uint32_t i = n + me; i < size; i += N) list[i] = 0ull;   // below every entry (a column's complement is not 0)
+    pick_sync<N == 32>();
     for (uint32_t k = 2u; k <= size; k <<= 1) {
         for (uint32_t d = k >> 1; d > 0u; d >>= 1) {
-            for (uint32_t p = threadIdx.x; p < size / 2u; p += kThreads) {
-                const uint32_t lo = 2u * d * (p / d) + (p % d), hi = lo + d;
-                const uint64_t x = sh.list[lo], y = sh.list[hi];
+            for (uint32_t p = me; p < size / 2u; p += N) {
+                const uint32_t lo = 2u * p - (p & (d - 1u)), hi = lo + d;
+                const uint64_t x = list[lo], y = list[hi];
                 if ((x < y) == ((lo & k) == 0u)) {
-                    sh.list[lo] = y;
-                    sh.list[hi] = x;
+                    list[lo] = y;
+                    list[hi] = x;
                 }
             }
-            __syncthreads();
+            pick_sync<N == 32>();
         }
     }
-    for (uint32_t i = threadIdx.x; i < (uint32_t)a.top; i += kThreads) emit(i, sh.list[i]);
+    for (uint32_t i = me; i < (uint32_t)a.top; i += N) emit(i, list[i]);
 }
 
-template <int DT> int launch_top(TopArgs a, cudaStream_t st) {
-    const int c = row_cluster(a.rows, row_vectors(a.vocab, DT));
+template <int DT, bool WARP> __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constant__ TopArgs a) {
+    using RV = RowVec<DT>;
+    constexpr int N = WARP ? 32 : kPickThreads, kRows = kPickThreads / N;   // threads of a row, rows of a CTA
+    __shared__ PickRow rows[kRows];
+    __shared__ PickShared sh;
+    extern __shared__ __align__(16) unsigned char dyn[];
+    const int slot = WARP ? (int)threadIdx.x >> 5 : 0, me = (int)threadIdx.x & (N - 1), lane = (int)threadIdx.x & 31;
+    const size_t row_bytes = (size_t)a.list_cap * 10u + (size_t)a.groups * 2u;
+    uint64_t* list = reinterpret_cast<uint64_t*>(dyn + slot * row_bytes);              // [list_cap] candidates
+    uint32_t* pairs = reinterpret_cast<uint32_t*>(list + a.list_cap);                  // [groups / 2] patterns, two a word
+    uint16_t* owner = reinterpret_cast<uint16_t*>(pairs + a.groups / 2);               // [list_cap] groups that hold candidates
+    PickRow& row = rows[slot];
+    const int64_t r = (int64_t)blockIdx.x * kRows + slot;
+    const bool there = r < a.rows;
+    if (me < 16) row.votes[me] = 0u;
+    if (me == 0) {
+        row.count = row.kept = 0u;
+        row.all = 0;
+    }
+    await_previous_kernel();
+    if (there) {
+        const RowPart<DT> part(a.L, r, a.ldl, (int)a.vocab, 0, 1);
+        const int nv = part.v_hi, n_groups = (nv + (1 << a.group_shift) - 1) >> a.group_shift, words = (n_groups + 1) / 2;
+        // the singles' threads ask for their element now
+        const int t = me, n_lone = part.head + part.tail;
+        const int lone = t < n_lone ? (t < part.head ? t : part.cols - part.tail + (t - part.head)) : -1;
+        const float lone_x = lone >= 0 ? part.at(lone) : -INFINITY;
+        const uint32_t* in = reinterpret_cast<const uint32_t*>(a.patterns + r * a.groups);
+        uint32_t top_pattern = 0u;
+        for (int i = me; i < words; i += N) {
+            uint32_t w = in[i];
+            if (2 * i + 1 >= n_groups) w &= 0xFFFFu;   // nothing behind the last group
+            pairs[i] = w;
+            top_pattern = max(top_pattern, max(w & 0xFFFFu, w >> 16));
+        }
+        SoftStat st = {-INFINITY, 0.0f};
+        if (me >= N - 32) {   // the last warp, which has the least to do elsewhere
+            for (int p = lane; p < a.parts; p += 32) {
+                const float2 s = a.stat[r * a.parts + p];
+                st = soft_merge(st, {s.x, s.y}, a.c);
+            }
+            st = soft_warp(st, a.c);
+            if (lane == 0 && st.s != st.s) row.all = 1;   // a NaN
+        }
+        // ---- a pattern that at least `top` of the groups' maxima reach, the largest or one that few more do (0: all
+        // entries are candidates): steps of growing size down from the largest, then bisection of the last
+        top_pattern = __reduce_max_sync(0xFFFFFFFFu, top_pattern);
+        if (!WARP) {
+            if (lane == 0) sh.warp_count[threadIdx.x >> 5] = top_pattern;
+            __syncthreads();
+            for (int w = 0; w < kPickThreads / 32; ++w) top_pattern = max(top_pattern, sh.warp_count[w]);
+        } else {
+            __syncwarp();
+        }
+        uint32_t floor_key = 0u;
+        if (n_groups >= a.top) {
+            int vote = 0;
+            auto reach = [&](uint32_t trial) -> int {   // groups that do
+                uint32_t n = 0u;
+#pragma unroll 4
+                for (int i = me; i < words; i += N) {
+                    const uint32_t w = pairs[i];
+                    n += ((w & 0xFFFFu) >= trial ? 1u : 0u) + ((w >> 16) >= trial ? 1u : 0u);
+                }
+                n = __reduce_add_sync(0xFFFFFFFFu, n);
+                if (!WARP) {
+                    uint32_t* v = &row.votes[vote];
+                    if (lane == 0) atomicAdd(v, n);
+                    __syncthreads();
+                    n = *v;
+                    if (threadIdx.x == 0) row.votes[(vote + 15) & 15] = 0u;   // the one before, read by all by now
+                    vote = (vote + 1) & 15;
+                }
+                return (int)n;
+            };
+            uint32_t high = top_pattern + 1u, step = 32u, low;   // fewer than `top` reach `high`
+            int n;
+            for (;;) {
+                low = high > step ? high - step : 0u;
+                n = reach(low);
+                if (n >= a.top || low == 0u) break;
+                high = low;
+                step *= 2u;
+            }
+            while (n > a.top + kSlack && high - low > 1u) {
+                const uint32_t mid = low + (high - low) / 2u;
+                const int m = reach(mid);
+                if (m >= a.top) {
+                    low = mid;
+                    n = m;
+                } else {
+                    high = mid;
+                }
+            }
+            floor_key = low;
+        }
+        const float least = floor_key == 0u ? -INFINITY : key_value(floor_key << 16);
+
+        // ---- the groups that reach it, and their entries that do
+        for (int i = me; i < words; i += N) {
+            const uint32_t w = pairs[i];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t k = h != 0 ? w >> 16 : w & 0xFFFFu;
+                if (2 * i + h < n_groups && k >= floor_key) {
+                    const uint32_t at = atomicAdd(&row.kept, 1u);
+                    if (at < (uint32_t)a.list_cap) owner[at] = (uint16_t)(2 * i + h);
+                }
+            }
+        }
+        auto take = [&](float x, int j) {
+            const uint32_t at = atomicAdd(&row.count, 1u);
+            if (at < (uint32_t)a.list_cap) list[at] = entry_of(order_key(x), j);
+        };
+        if (lone >= 0 && !(lone_x < least)) take(lone_x, lone);
+        pick_sync<WARP>();
+        const uint32_t kept = row.kept;
+        bool all = row.all != 0 || kept > (uint32_t)a.list_cap;
+        if (!all) {
+            const int per = 1 << a.group_shift, work = (int)kept * per;
+            for (int u0 = me; u0 < work; u0 += kBatch * N) {   // kBatch loads in flight
+                uint4 w[kBatch];
+                int v[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    const int u = u0 + i * N;
+                    v[i] = u < work ? owner[u >> a.group_shift] * per + (u & (per - 1)) : nv;
+                    if (v[i] < nv) w[i] = ld_stream16(part.vec(v[i]));
+                }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    uint32_t mask = v[i] < nv ? reach_mask<DT>(w[i], least) : 0u;
+                    while (mask != 0u) {
+                        const int e = __ffs(mask) - 1;
+                        mask &= mask - 1u;
+                        take(RV::any(w[i], e), part.first(v[i]) + e);
+                    }
+                }
+            }
+            pick_sync<WARP>();
+            all = row.count > (uint32_t)a.list_cap;
+        }
+        if (!all) emit_list<DT, N>(part, a, r, list, row.count, (uint32_t)me);
+        if (me == N - 32 && a.lse != nullptr) a.lse[r] = (float)soft_lse(st, a.inv_t);   // last: a long fp64 logarithm
+        if (me == 0) row.all = all ? 1 : 0;
+    }
+    // ---- rows whose list is no use, by the whole CTA
+    __syncthreads();
+    for (int s = 0; s < kRows; ++s) {
+        if (!rows[s].all) continue;
+        const int64_t rr = (int64_t)blockIdx.x * kRows + s;
+        const RowPart<DT> part(a.L, rr, a.ldl, (int)a.vocab, 0, 1);
+        uint64_t* l = reinterpret_cast<uint64_t*>(dyn + s * row_bytes);
+        select_all<DT>(part, a.top, l, sh);
+        __syncthreads();
+        emit_list<DT, kPickThreads>(part, a, rr, l, (uint32_t)a.top, threadIdx.x);
+        __syncthreads();
+    }
+}
+
+// Everything a call's sizes decide.  Groups are eight vectors (128 bytes: what is read again lies together), or one
+// where `top` comes near their number: the k-th largest of barely more than k maxima is far down, and most of the row
+// a candidate.
+void plan_top(TopArgs& a, int dtype) {
+    const int64_t nv = row_vectors(a.vocab, dtype);
+    a.group_shift = a.top * 4 <= (nv / 8) * 3 ? 3 : 0;
+    a.groups = (int)(((nv + 7) / 8 * 8 >> a.group_shift) + 7) / 8 * 8;
+    if (a.groups < 8) a.groups = 8;
+    a.list_cap = 512;
+    while (a.list_cap < 3 * a.top && a.list_cap < 4096) a.list_cap *= 2;
+    int64_t per = 4096;   // 64 KB; less where the rows alone would leave SMs idle
+    while (per > kThreads && a.rows * ((nv + per - 1) / per) < sm_count() * kRowCtas) per /= 2;
+    a.part_vecs = (int)per;
+    a.parts = nv > 0 ? (int)((nv + per - 1) / per) : 1;
+}
+constexpr int64_t kMostVocab = 1 << 20;   // entries of a row: its patterns lie in the shared memory of one CTA
+constexpr int kMostGroups = 32768;        // 2^20 fp32 entries
+
+// A warp's row has a quarter of a CTA's shared memory; a row with more patterns than that takes a CTA.
+constexpr int kWarpRowMost = 64 * 1024;
+
+template <int DT> int launch_top(const TopArgs& a, cudaStream_t st) {
+    static DeviceCache opted;   // the shared-memory opt-in belongs to one device's copy of the kernel
+    const int ok = opted.get([&]() -> int {
+        if (cudaFuncSetAttribute(pick_kernel<DT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4096 * 10 + kMostGroups * 2) != cudaSuccess ||
+            cudaFuncSetAttribute(pick_kernel<DT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWarpRowMost) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return -1;
+        }
+        return 1;
+    });
+    if (ok < 0) return MOSAIC_ERR_CUDA;
+    sweep_kernel<DT><<<dim3((unsigned)a.rows, (unsigned)a.parts), kThreads, 0, st>>>(a);
+    MOSAIC_LAUNCH_CHECK();
+    // a row a warp where there are rows enough for that (4096 x 32000 bf16, k 64: 29 us, a CTA a row: 53); with few, its
+    // steps follow one another faster with four warps on them
+    const bool warp_rows = a.top <= kWarpTop && a.rows >= 8 * sm_count() && 4u * ((size_t)a.list_cap * 10u + (size_t)a.groups * 2u) <= (size_t)kWarpRowMost;
+    const int per_cta = warp_rows ? kPickThreads / 32 : 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.rows * c));
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3((unsigned)((a.rows + per_cta - 1) / per_cta));
+    cfg.blockDim = dim3(kPickThreads);
+    cfg.dynamicSmemBytes = (size_t)per_cta * ((size_t)a.list_cap * 10u + (size_t)a.groups * 2u);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)c;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, top_logits_kernel<DT>, a));
+    if (warp_rows) MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, pick_kernel<DT, true>, a));
+    else MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, pick_kernel<DT, false>, a));
     return MOSAIC_OK;
 }
 
@@ -275,10 +476,18 @@ template <int DT> int launch_top(TopArgs a, cudaStream_t st) {
 
 using namespace mosaic;
 
+extern "C" size_t mosaic_top_logits_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int64_t top) {
+    if (rows <= 0 || vocab <= 0 || vocab > kMostVocab || top < 1 || top > kMaxTop || (dtype != MOSAIC_F32 && dtype != MOSAIC_BF16)) return 0;
+    TopArgs a = {};
+    a.rows = rows; a.vocab = vocab; a.top = (int)top;
+    plan_top(a, dtype);
+    return align_up((size_t)rows * ((size_t)a.parts * sizeof(float2) + (size_t)a.groups * 2u), 256);
+}
+
 extern "C" int mosaic_top_logits(const void* L, int64_t rows, int64_t vocab, int64_t ldl, int dtype, int64_t top, float temperature,
-                                 float* values, int32_t* indices, float* lse, void* stream) {
+                                 float* values, int32_t* indices, float* lse, void* ws, size_t ws_bytes, void* stream) {
     if (dtype != MOSAIC_F32 && dtype != MOSAIC_BF16) return MOSAIC_ERR_BAD_DTYPE;
-    if (rows < 0 || rows > 0x7FFFFFFF / kMaxCluster || vocab <= 0 || vocab > kMaxRow || ldl < vocab || top < 1 || top > kMaxTop || top > vocab)
+    if (rows < 0 || rows > 0x7FFFFFFF || vocab <= 0 || vocab > kMostVocab || ldl < vocab || top < 1 || top > kMaxTop || top > vocab)
         return MOSAIC_ERR_INVALID_ARG;
     if (!(temperature >= 1.17549435e-38f) || !(temperature <= 3.402823466e38f)) return MOSAIC_ERR_INVALID_ARG;
     if (rows == 0) return MOSAIC_OK;
@@ -296,11 +505,17 @@ extern "C" int mosaic_top_logits(const void* L, int64_t rows, int64_t vocab, int
             for (int o = i + 1; o < 4; ++o)
                 if (len[i] > 0 && len[o] > 0 && p[i] < p[o] + len[o] && p[o] < p[i] + len[i]) return MOSAIC_ERR_ALIASING;
     }
+    if (ws == nullptr) return MOSAIC_ERR_NULL_PTR;
+    if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return MOSAIC_ERR_MISALIGNED;
+    if (ws_bytes < mosaic_top_logits_workspace_bytes(rows, vocab, dtype, top)) return MOSAIC_ERR_WORKSPACE_TOO_SMALL;
     TopArgs a = {};
     a.L = L; a.rows = rows; a.vocab = vocab; a.ldl = ldl; a.top = (int)top;
     a.values = values; a.indices = indices; a.lse = lse;
     a.inv_t = 1.0 / (double)temperature;
     a.c = (float)(1.4426950408889634 / (double)temperature);
+    plan_top(a, dtype);
+    a.patterns = static_cast<uint16_t*>(ws);   // rows of 16 bytes
+    a.stat = reinterpret_cast<float2*>(a.patterns + (size_t)rows * (size_t)a.groups);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return dtype == MOSAIC_BF16 ? launch_top<MOSAIC_BF16>(a, st) : launch_top<MOSAIC_F32>(a, st);
 }

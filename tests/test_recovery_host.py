@@ -69,7 +69,7 @@ def test_backward_refusals_need_no_device(lib):
 def top(lib, **k):
     g = k.get
     return lib.mosaic_top_logits(g("L", A), g("rows", 4), g("vocab", 100), g("ld", 100), g("dtype", api.F32), g("top", 10), g("T", 1.0),
-                                 g("values", 2 * A), g("indices", 3 * A), g("lse"), None)
+                                 g("values", 2 * A), g("indices", 3 * A), g("lse"), g("ws", 8 * A), g("ws_bytes", 1 << 16), None)
 
 
 def test_top_logits_refusals_need_no_device(lib):
@@ -80,7 +80,11 @@ def test_top_logits_refusals_need_no_device(lib):
     assert top(lib, L=None) == NULL and top(lib, values=None) == NULL and top(lib, indices=None) == NULL
     assert top(lib, L=A + 2) == MISALIGNED and top(lib, values=A + 2) == MISALIGNED and top(lib, lse=A + 1) == MISALIGNED
     assert top(lib, values=A) == ALIAS and top(lib, indices=2 * A) == ALIAS and top(lib, lse=3 * A) == ALIAS
-    assert top(lib, rows=0, L=None) == 0
+    assert top(lib, rows=0, L=None) == 0 and top(lib, vocab=(1 << 20) + 1, ld=1 << 21) == INVALID
+    assert top(lib, ws=None) == NULL and top(lib, ws=8 * A + 16) == MISALIGNED and top(lib, rows=100, ws_bytes=64) == WS
+    q = lib.mosaic_top_logits_workspace_bytes
+    assert q(0, 100, 0, 10) == 0 and q(4, (1 << 20) + 1, 0, 10) == 0 and q(4, 100, 0, 10) == 512
+    assert q(4096, 32000, 1, 64) >= 4096 * (500 * 2 + 8)
 
 
 def test_distill_workspace(lib):
