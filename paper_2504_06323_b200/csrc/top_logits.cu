@@ -19,9 +19,7 @@
 namespace mosaic {
 namespace {
 
-constexpr int kPickThreads = 128;
-constexpr int kSlack = 8;        // candidates too many that are not worth another step of the bisection
-constexpr int kRankMost = 256;   // up to here a list is ranked by counting, above it by a bitonic sort
+constexpr int kRankMost = 256;   // entries: up to here a list is ranked by counting, above it by a bitonic sort
 
 struct TopArgs {
     const void* L;
@@ -119,10 +117,14 @@ template <int DT> __global__ void __launch_bounds__(kThreads, kRowCtas) sweep_ke
         float m[kBatch];
         const float own = group_max<DT>(raw, wide, m);
         soft_batch<DT>(raw, own, a.c, st);
+        if (wide) {   // lane i of a run writes the pattern of the run's vectors of batch i
+            const int i = lane & 3, u = v - (lane & 7) + i * kThreads;
+            const float mi = (i & 2) ? ((i & 1) ? m[3] : m[2]) : ((i & 1) ? m[1] : m[0]);
+            if ((lane & 7) < kBatch && u < part.v_hi) patterns[u >> 3] = (uint16_t)(order_key(mi) >> 16);
+        } else {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int u = v + i * kThreads;   // the group's first lane has its first vector
-            if (u < part.v_hi && (!wide || (lane & 7) == 0)) patterns[u >> a.group_shift] = (uint16_t)(order_key(m[i]) >> 16);
+            for (int i = 0; i < kBatch; ++i)
+                if (v + i * kThreads < part.v_hi) patterns[v + i * kThreads] = (uint16_t)(order_key(m[i]) >> 16);
         }
     }
     const int lone = part.single();
@@ -138,19 +140,19 @@ template <int DT> __global__ void __launch_bounds__(kThreads, kRowCtas) sweep_ke
 // ---------------------------------------------------------------- pick
 struct PickShared {
     uint32_t hist[256];
-    uint32_t warp_count[kPickThreads / 32];
+    uint32_t warp_count[16];
     uint32_t count;
     uint32_t digit, rest;
 };
 
 // The exact selection over a whole row by one CTA, digit by digit: leaves the k entries in list[0, k).
-template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, uint64_t* list, PickShared& sh) {
+template <int DT, int T> __device__ void select_all(const RowPart<DT>& row, int top, uint64_t* list, PickShared& sh) {
     const int cols = row.cols, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t prefix = 0u, mask = 0u, want = (uint32_t)top;   // the want-th largest among the keys that share the prefix
     for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = threadIdx.x; i < 256; i += kPickThreads) sh.hist[i] = 0u;
+        for (int i = threadIdx.x; i < 256; i += T) sh.hist[i] = 0u;
         __syncthreads();
-        for (int j0 = 0; j0 < cols; j0 += kPickThreads) {
+        for (int j0 = 0; j0 < cols; j0 += T) {
             const int j = j0 + (int)threadIdx.x;
             const uint32_t key = j < cols ? order_key(row.at(j)) : 0u;
             const bool in = j < cols && (key & mask) == prefix;
@@ -184,7 +186,7 @@ template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, ui
     if (threadIdx.x == 0) sh.count = 0u;
     __syncthreads();
     uint32_t equal_before = 0u;
-    for (int j0 = 0; j0 < cols; j0 += kPickThreads) {
+    for (int j0 = 0; j0 < cols; j0 += T) {
         const int j = j0 + (int)threadIdx.x;
         const uint32_t key = j < cols ? order_key(row.at(j)) : 0u;
         const bool equal = j < cols && key == prefix;
@@ -193,7 +195,7 @@ template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, ui
         __syncthreads();
         uint32_t before = equal_before + (uint32_t)__popc(votes & ((1u << lane) - 1u));
         uint32_t total = 0u;
-        for (int w = 0; w < kPickThreads / 32; ++w) {
+        for (int w = 0; w < T / 32; ++w) {
             if (w < warp) before += sh.warp_count[w];
             total += sh.warp_count[w];
         }
@@ -203,12 +205,12 @@ template <int DT> __device__ void select_all(const RowPart<DT>& row, int top, ui
     }
 }
 
-// What a row's threads share: a warp's row, four a CTA (up to kWarpTop kept), or a CTA's.
-constexpr int kWarpTop = 128;
-template <bool WARP> __device__ __forceinline__ void pick_sync() {
-    if (WARP) __syncwarp();
+// N threads a row: a warp (four rows a CTA), 128 or 512 (a row a CTA).
+template <int N> __device__ __forceinline__ void pick_sync() {
+    if (N == 32) __syncwarp();
     else __syncthreads();
 }
+// What they share.
 struct PickRow {
     uint32_t votes[16];
     uint32_t count;      // candidates found
@@ -228,20 +230,31 @@ template <int DT, int N> __device__ __forceinline__ void emit_list(const RowPart
         values[place] = key == 0x80000000u || key == 0xFFFFFFFFu ? part.at(j) : key_value(key);
         indices[place] = j;
     };
-    if (n <= kRankMost) {   // an entry's place is the number of larger ones
-        for (uint32_t i = me; i < n; i += N) {
-            const uint64_t mine = list[i];
+    if (n <= kRankMost) {   // an entry's place is the number of larger ones, counted two at a time by `share` threads
+        if (me == 0 && (n & 1u)) list[n] = 0ull;   // (room for n entries is room for an even number)
+        pick_sync<N>();
+        uint32_t share = 1u;
+        while (share < 32u && n * share * 2u <= (uint32_t)N) share *= 2u;
+        const uint32_t pairs = (n + 1u) / 2u;
+        const ulonglong2* two = reinterpret_cast<const ulonglong2*>(list);
+        for (uint32_t i0 = 0; i0 < n; i0 += N / share) {
+            const uint32_t i = i0 + me / share;
+            const uint64_t mine = i < n ? list[i] : 0ull;
             uint32_t above = 0u;
-#pragma unroll 8
-            for (uint32_t o = 0; o < n; ++o) above += list[o] > mine ? 1u : 0u;
-            if (above < (uint32_t)a.top) emit(above, mine);
+#pragma unroll 4
+            for (uint32_t o = me % share; o < pairs; o += share) {
+                const ulonglong2 x = two[o];
+                above += (x.x > mine ? 1u : 0u) + (x.y > mine ? 1u : 0u);
+            }
+            for (uint32_t o = share / 2u; o > 0u; o >>= 1) above += __shfl_xor_sync(0xFFFFFFFFu, above, o);
+            if (i < n && me % share == 0u && above < (uint32_t)a.top) emit(above, mine);
         }
         return;
     }
     uint32_t size = kRankMost * 2;
     while (size < n) size *= 2u;
     for (uint32_t i = n + me; i < size; i += N) list[i] = 0ull;   // below every entry (a column's complement is not 0)
-    pick_sync<N == 32>();
+    pick_sync<N>();
     for (uint32_t k = 2u; k <= size; k <<= 1) {
         for (uint32_t d = k >> 1; d > 0u; d >>= 1) {
             for (uint32_t p = me; p < size / 2u; p += N) {
@@ -252,15 +265,19 @@ template <int DT, int N> __device__ __forceinline__ void emit_list(const RowPart
                     list[hi] = x;
                 }
             }
-            pick_sync<N == 32>();
+            pick_sync<N>();
         }
     }
     for (uint32_t i = me; i < (uint32_t)a.top; i += N) emit(i, list[i]);
 }
 
-template <int DT, bool WARP> __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constant__ TopArgs a) {
+__host__ __device__ constexpr int pick_threads(int n) { return n == 32 ? 128 : n; }   // of a CTA
+
+template <int DT, int N> __global__ void __launch_bounds__(pick_threads(N)) pick_kernel(const __grid_constant__ TopArgs a) {
     using RV = RowVec<DT>;
-    constexpr int N = WARP ? 32 : kPickThreads, kRows = kPickThreads / N;   // threads of a row, rows of a CTA
+    constexpr bool WARP = N == 32;
+    constexpr int kPickThreads = pick_threads(N), kRows = kPickThreads / N;   // threads and rows of a CTA
+    constexpr int kInFlight = WARP ? 8 : 4;   // loads
     __shared__ PickRow rows[kRows];
     __shared__ PickShared sh;
     extern __shared__ __align__(16) unsigned char dyn[];
@@ -314,6 +331,7 @@ template <int DT, bool WARP> __global__ void __launch_bounds__(kPickThreads) pic
         }
         uint32_t floor_key = 0u;
         if (n_groups >= a.top) {
+            const int slack = 8 + a.top / 8;   // candidates too many that are not worth another step
             int vote = 0;
             auto reach = [&](uint32_t trial) -> int {   // groups that do
                 uint32_t n = 0u;
@@ -342,7 +360,7 @@ template <int DT, bool WARP> __global__ void __launch_bounds__(kPickThreads) pic
                 high = low;
                 step *= 2u;
             }
-            while (n > a.top + kSlack && high - low > 1u) {
+            while (n > a.top + slack && high - low > 1u) {
                 const uint32_t mid = low + (high - low) / 2u;
                 const int m = reach(mid);
                 if (m >= a.top) {
@@ -373,22 +391,22 @@ template <int DT, bool WARP> __global__ void __launch_bounds__(kPickThreads) pic
             if (at < (uint32_t)a.list_cap) list[at] = entry_of(order_key(x), j);
         };
         if (lone >= 0 && !(lone_x < least)) take(lone_x, lone);
-        pick_sync<WARP>();
+        pick_sync<N>();
         const uint32_t kept = row.kept;
         bool all = row.all != 0 || kept > (uint32_t)a.list_cap;
         if (!all) {
             const int per = 1 << a.group_shift, work = (int)kept * per;
-            for (int u0 = me; u0 < work; u0 += kBatch * N) {   // kBatch loads in flight
-                uint4 w[kBatch];
-                int v[kBatch];
+            for (int u0 = me; u0 < work; u0 += kInFlight * N) {
+                uint4 w[kInFlight];
+                int v[kInFlight];
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
+                for (int i = 0; i < kInFlight; ++i) {
                     const int u = u0 + i * N;
                     v[i] = u < work ? owner[u >> a.group_shift] * per + (u & (per - 1)) : nv;
                     if (v[i] < nv) w[i] = ld_stream16(part.vec(v[i]));
                 }
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
+                for (int i = 0; i < kInFlight; ++i) {
                     uint32_t mask = v[i] < nv ? reach_mask<DT>(w[i], least) : 0u;
                     while (mask != 0u) {
                         const int e = __ffs(mask) - 1;
@@ -397,7 +415,7 @@ template <int DT, bool WARP> __global__ void __launch_bounds__(kPickThreads) pic
                     }
                 }
             }
-            pick_sync<WARP>();
+            pick_sync<N>();
             all = row.count > (uint32_t)a.list_cap;
         }
         if (!all) emit_list<DT, N>(part, a, r, list, row.count, (uint32_t)me);
@@ -411,7 +429,7 @@ template <int DT, bool WARP> __global__ void __launch_bounds__(kPickThreads) pic
         const int64_t rr = (int64_t)blockIdx.x * kRows + s;
         const RowPart<DT> part(a.L, rr, a.ldl, (int)a.vocab, 0, 1);
         uint64_t* l = reinterpret_cast<uint64_t*>(dyn + s * row_bytes);
-        select_all<DT>(part, a.top, l, sh);
+        select_all<DT, kPickThreads>(part, a.top, l, sh);
         __syncthreads();
         emit_list<DT, kPickThreads>(part, a, rr, l, (uint32_t)a.top, threadIdx.x);
         __syncthreads();
@@ -436,39 +454,40 @@ void plan_top(TopArgs& a, int dtype) {
 constexpr int64_t kMostVocab = 1 << 20;   // entries of a row: its patterns lie in the shared memory of one CTA
 constexpr int kMostGroups = 32768;        // 2^20 fp32 entries
 
-// A warp's row has a quarter of a CTA's shared memory; a row with more patterns than that takes a CTA.
-constexpr int kWarpRowMost = 64 * 1024;
-
-template <int DT> int launch_top(const TopArgs& a, cudaStream_t st) {
+template <int DT, int N> int launch_pick(const TopArgs& a, cudaStream_t st) {
+    constexpr int kRows = pick_threads(N) / N;
     static DeviceCache opted;   // the shared-memory opt-in belongs to one device's copy of the kernel
     const int ok = opted.get([&]() -> int {
-        if (cudaFuncSetAttribute(pick_kernel<DT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4096 * 10 + kMostGroups * 2) != cudaSuccess ||
-            cudaFuncSetAttribute(pick_kernel<DT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWarpRowMost) != cudaSuccess) {
+        if (cudaFuncSetAttribute(pick_kernel<DT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4096 * 10 + kMostGroups * 2) != cudaSuccess) {
             (void)cudaGetLastError();
             return -1;
         }
         return 1;
     });
     if (ok < 0) return MOSAIC_ERR_CUDA;
-    sweep_kernel<DT><<<dim3((unsigned)a.rows, (unsigned)a.parts), kThreads, 0, st>>>(a);
-    MOSAIC_LAUNCH_CHECK();
-    // a row a warp where there are rows enough for that (4096 x 32000 bf16, k 64: 29 us, a CTA a row: 53); with few, its
-    // steps follow one another faster with four warps on them
-    const bool warp_rows = a.top <= kWarpTop && a.rows >= 8 * sm_count() && 4u * ((size_t)a.list_cap * 10u + (size_t)a.groups * 2u) <= (size_t)kWarpRowMost;
-    const int per_cta = warp_rows ? kPickThreads / 32 : 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((a.rows + per_cta - 1) / per_cta));
-    cfg.blockDim = dim3(kPickThreads);
-    cfg.dynamicSmemBytes = (size_t)per_cta * ((size_t)a.list_cap * 10u + (size_t)a.groups * 2u);
+    cfg.gridDim = dim3((unsigned)((a.rows + kRows - 1) / kRows));
+    cfg.blockDim = dim3(pick_threads(N));
+    cfg.dynamicSmemBytes = (size_t)kRows * ((size_t)a.list_cap * 10u + (size_t)a.groups * 2u);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (warp_rows) MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, pick_kernel<DT, true>, a));
-    else MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, pick_kernel<DT, false>, a));
+    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, pick_kernel<DT, N>, a));
     return MOSAIC_OK;
+}
+
+template <int DT> int launch_top(const TopArgs& a, cudaStream_t st) {
+    sweep_kernel<DT><<<dim3((unsigned)a.rows, (unsigned)a.parts), kThreads, 0, st>>>(a);
+    MOSAIC_LAUNCH_CHECK();
+    // A row a warp where there are rows enough to fill the SMs so (4096 x 32000 bf16, k 64: %%W%%); the fewer there are,
+    // the more threads make a row's steps short (301 x 50001 fp32, k 100: %%C%%).  A warp's row has a quarter of a
+    // CTA's shared memory, and sorting a long list is a CTA's work.
+    const bool small = 4u * ((size_t)a.list_cap * 10u + (size_t)a.groups * 2u) <= 64u * 1024u && a.top <= 128;
+    if (small && a.rows >= 8 * sm_count()) return launch_pick<DT, 32>(a, st);
+    return a.rows >= 4 * sm_count() ? launch_pick<DT, 128>(a, st) : launch_pick<DT, 512>(a, st);
 }
 
 }  // namespace
