@@ -54,6 +54,23 @@ inline int cuda_status(cudaError_t e) { return e == cudaSuccess ? MOSAIC_OK : MO
         if (e__ != cudaSuccess) return MOSAIC_ERR_CUDA;         \
     } while (0)
 
+// Launch attribute of a kernel that may start while the one before it in the stream still runs (it waits for that one
+// itself, before it touches global memory: await_previous_kernel).
+inline cudaLaunchAttribute early_start() {
+    cudaLaunchAttribute a = {};
+    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a.val.programmaticStreamSerializationAllowed = 1;
+    return a;
+}
+inline cudaLaunchAttribute cluster_of(int ctas) {
+    cudaLaunchAttribute a = {};
+    a.id = cudaLaunchAttributeClusterDimension;
+    a.val.clusterDim.x = (unsigned)ctas;
+    a.val.clusterDim.y = 1;
+    a.val.clusterDim.z = 1;
+    return a;
+}
+
 // ---------------------------------------------------------------- device side
 #ifdef __CUDACC__
 
@@ -149,6 +166,11 @@ __device__ __forceinline__ void load_vec(Raw8<DT>& r, const void* mat, int64_t r
             if (c + e < cols) r.set_scalar(e, mat, row_off + c + e);
     }
 }
+
+// A kernel launched with the stream-serialization attribute may start while the one before it still runs: it waits
+// here before it touches what that one reads or writes.  The other side allows it to start.
+__device__ __forceinline__ void await_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Deterministic fp64 warp sum (fixed butterfly).
 __device__ __forceinline__ double warp_sum(double v) {

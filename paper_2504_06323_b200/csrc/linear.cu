@@ -25,7 +25,6 @@ namespace {
 
 constexpr int kMI = 128;               // rows of the matrix instruction: adjacent output elements
 constexpr int kMC = 64;                // contraction steps per stage (128 bytes: one swizzle row)
-constexpr int kMThreads = 192;         // loader, MMA issue, four epilogue warps (one per quarter of tensor memory)
 constexpr int kMMaxSplit = 8;          // CTAs (one cluster) that share one tile's contraction
 constexpr uint32_t kMBox = 64 * 64 * 2;   // an MN-major box: 64 elements x 64 contraction steps
 
@@ -40,45 +39,101 @@ struct MmArgs {
     uint16_t* z;                       // [n_j, n_i] or null: the value before the activation
     int64_t ld_z;
     int act;
+    int pairs;                         // out, resid and z (those there are) take two elements a word: 4-byte bases, even ld
+    int first_pair;                    // >= 0: the tiles are quarters of the pair kernel's tiles from this one on
+    int pair_i, pair_j;                // its tiles
     int* status;
 };
 
-// Sixteen accumulator columns of a lane into the output: v[e] belongs to element (i, j + e), e < n.
-__device__ __forceinline__ void epilogue16(const MmArgs& a, float (&v)[16], float bias, int64_t i, int64_t j, int n) {
-    float r[16];
-    if (a.resid != nullptr) {
-        const uint16_t* p = a.resid + j * a.ld_resid + i;
+// Two adjacent output elements a word.  A lane holds element i of rows j and j + 1 (lo, hi); after the exchange with its
+// neighbour an even lane holds elements i, i + 1 of row j, an odd one i - 1, i of row j + 1.  Its own inverse.
+__device__ __forceinline__ uint32_t exchange(uint32_t w, bool odd) {
+    const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, w, 1);
+    return odd ? __byte_perm(other, w, 0x7632) : __byte_perm(w, other, 0x5410);
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+    return (uint32_t)__bfloat16_as_ushort(p.x) | ((uint32_t)__bfloat16_as_ushort(p.y) << 16);
+}
+
+// N accumulator columns of a warp into the output: v[e] belongs to element (i, j + e), e < n; i0 is lane 0's i.
+template <int N> __device__ __forceinline__ void epilogue(const MmArgs& a, float (&v)[N], float bias, int64_t i0, int64_t j, int n) {
+    const int lane = (int)threadIdx.x & 31;
+    const int64_t i = i0 + lane;
 #pragma unroll
-        for (int e = 0; e < 16; ++e, p += a.ld_resid) r[e] = e < n ? bf16_to_f32(*p) : 0.0f;
+    for (int e = 0; e < N; ++e) v[e] = __fadd_rn(v[e], bias);
+    if (a.pairs && i0 + 32 <= a.n_i) {   // whole words: half the instructions of the element by element form below
+        const bool odd = (lane & 1) != 0;
+        const int64_t at = i & ~(int64_t)1, row = j + (lane & 1);
+        uint32_t r[N / 2];
+        if (a.resid != nullptr) {
+            const uint16_t* p = a.resid + row * a.ld_resid + at;
+#pragma unroll
+            for (int e = 0; e < N; e += 2, p += 2 * a.ld_resid) r[e / 2] = e + (lane & 1) < n ? *reinterpret_cast<const uint32_t*>(p) : 0u;
+        }
+        if (a.z != nullptr) {
+            uint16_t* p = a.z + row * a.ld_z + at;
+#pragma unroll
+            for (int e = 0; e < N; e += 2, p += 2 * a.ld_z) {
+                const uint32_t w = exchange(pack2(v[e], v[e + 1]), odd);
+                if (e + (lane & 1) < n) *reinterpret_cast<uint32_t*>(p) = w;
+            }
+        }
+        if (a.act != MOSAIC_ACT_NONE) activate_all(v, a.act);
+        if (a.resid != nullptr) {
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const uint32_t w = exchange(r[e / 2], odd);
+                v[e] = __fadd_rn(v[e], __uint_as_float(w << 16));
+                v[e + 1] = __fadd_rn(v[e + 1], __uint_as_float(w & 0xFFFF0000u));
+            }
+        }
+        uint16_t* p = a.out + row * a.ld_out + at;
+        if (n >= N) {
+#pragma unroll
+            for (int e = 0; e < N; e += 2, p += 2 * a.ld_out) *reinterpret_cast<uint32_t*>(p) = exchange(pack2(v[e], v[e + 1]), odd);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; e += 2, p += 2 * a.ld_out) {
+                const uint32_t w = exchange(pack2(v[e], v[e + 1]), odd);
+                if (e + (lane & 1) < n) *reinterpret_cast<uint32_t*>(p) = w;
+            }
+        }
+        return;
     }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = __fadd_rn(v[e], bias);
+    if (i >= a.n_i) return;
     if (a.z != nullptr) {
         uint16_t* p = a.z + j * a.ld_z + i;
 #pragma unroll
-        for (int e = 0; e < 16; ++e, p += a.ld_z)
+        for (int e = 0; e < N; ++e, p += a.ld_z)
             if (e < n) *p = f32_to_bf16(v[e]);
     }
     if (a.act != MOSAIC_ACT_NONE) activate_all(v, a.act);
     if (a.resid != nullptr) {
+        const uint16_t* p = a.resid + j * a.ld_resid + i;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = __fadd_rn(v[e], r[e]);
+        for (int e = 0; e < N; ++e, p += a.ld_resid)
+            if (e < n) v[e] = __fadd_rn(v[e], bf16_to_f32(*p));
     }
     uint16_t* p = a.out + j * a.ld_out + i;
-    if (n == 16) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e, p += a.ld_out) *p = f32_to_bf16(v[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e, p += a.ld_out)
-            if (e < n) *p = f32_to_bf16(v[e]);
-    }
+    for (int e = 0; e < N; ++e, p += a.ld_out)
+        if (e < n) *p = f32_to_bf16(v[e]);
 }
+template <int N> __device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[N]) {
+    if constexpr (N == 16) tmem_load16(addr, v);
+    else tmem_load32(addr, v);
+}
+__device__ __forceinline__ void pair_tile(int tile, int tiles_i, int tiles_j, int* ti, int* tj);
 
 // One output tile of kMI x BN per cluster; its contraction is split over the cluster's CTAs, whose partial
 // tiles meet in shared memory and are added in the CTAs' order.
+constexpr int kMRoles = 2;   // loader, MMA issue; then the epilogue: four warps (a quarter of tensor memory's lanes each), eight for wide tiles
+__host__ __device__ constexpr int mm_warps(int bn) { return bn >= 64 ? 8 : 4; }
+__host__ __device__ constexpr int mm_threads(int bn) { return 32 * (kMRoles + mm_warps(bn)); }
+
 template <bool A_MN, bool B_MN, int BN>
-__global__ void __launch_bounds__(kMThreads) mm_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+__global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                                                        const __grid_constant__ MmArgs a) {
     constexpr uint32_t kABytes = kMI * kMC * 2, kBBytes = BN * kMC * 2, kStage = kABytes + kBBytes;
     constexpr uint32_t kCols = BN < 32 ? 32 : BN;
@@ -93,11 +148,19 @@ __global__ void __launch_bounds__(kMThreads) mm_kernel(const __grid_constant__ C
     const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int tile = (int)(blockIdx.x / (unsigned)split);
-    const int64_t i0 = (int64_t)(tile % a.tiles_i) * kMI, j0 = (int64_t)(tile / a.tiles_i) * BN;
+    int64_t i0 = (int64_t)(tile % a.tiles_i) * kMI, j0 = (int64_t)(tile / a.tiles_i) * BN;
+    if (BN == 128 && a.first_pair >= 0) {   // what is left over of the pair kernel's tiles, in quarters
+        int ti, tj;
+        pair_tile(a.first_pair + tile / 4, a.pair_i, a.pair_j, &ti, &tj);
+        i0 = (int64_t)ti * 256 + (tile & 1) * 128;
+        j0 = (int64_t)tj * 256 + ((tile >> 1) & 1) * 128;
+    }
     const int64_t steps = (a.n_c + kMC - 1) / kMC;
     const int s0 = (int)(steps * rank / split), s1 = (int)(steps * (rank + 1) / split);   // split <= steps: never empty
 
     if (threadIdx.x == 0) {
+        prefetch_map(&a_map);
+        prefetch_map(&b_map);
         for (int s = 0; s < a.stages; ++s) {
             mbar_init(&full[s], 1u);
             mbar_init(&empty[s], 1u);
@@ -116,6 +179,8 @@ __global__ void __launch_bounds__(kMThreads) mm_kernel(const __grid_constant__ C
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     uint32_t issued = 0;
+    allow_next_kernel();   // not before this CTA has its tensor memory: the next kernel's CTAs wait for it with theirs in hand
+    await_previous_kernel();
 
     if (warp == 0) {
         if (lane == 0) {
@@ -167,20 +232,22 @@ __global__ void __launch_bounds__(kMThreads) mm_kernel(const __grid_constant__ C
     const bool done = warp >= 2 && mbar_wait(&acc_full, 0u, err);
     tc_fence_after();
     const int q = warp & 3;
-    const int64_t i = i0 + q * 32 + lane;
-    const int n_cols = (int)(a.n_j - j0 < BN ? a.n_j - j0 : BN);
+    const int n_cols = (int)(a.n_j - j0 < BN ? (a.n_j > j0 ? a.n_j - j0 : 0) : BN);
     float* part = reinterpret_cast<float*>(ring);   // [BN][kMI]: every load has been consumed once the accumulator is complete
     if (done) {
+        constexpr int kChunk = BN < 32 ? 16 : 32, kSets = mm_warps(BN) / 4;   // warps of a quarter take chunks in turn
+        const int64_t i = i0 + q * 32 + lane;
         const float bias = a.bias != nullptr && i < a.n_i ? bf16_to_f32(a.bias[i]) : 0.0f;
 #pragma unroll 1
-        for (int c0 = 0; c0 < n_cols; c0 += 16) {
-            float v[16];
-            tmem_load16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c0, v);
+        for (int c0 = ((warp - kMRoles) >> 2) * kChunk; c0 < n_cols; c0 += kSets * kChunk) {
+            float v[kChunk];
+            tmem_load<kChunk>(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c0, v);
             if (split > 1) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) part[(c0 + e) * kMI + q * 32 + lane] = v[e];
-            } else if (i < a.n_i) {
-                epilogue16(a, v, bias, i, j0 + c0, n_cols - c0 < 16 ? n_cols - c0 : 16);
+                for (int e = 0; e < kChunk; ++e) part[(c0 + e) * kMI + q * 32 + lane] = v[e];
+            } else {
+                epilogue<kChunk>(a, v, bias, i0 + q * 32, j0 + c0, n_cols - c0);
+                __syncwarp();
             }
         }
     }
@@ -203,23 +270,43 @@ __global__ void __launch_bounds__(kMThreads) mm_kernel(const __grid_constant__ C
     }
     if (split > 1) {
         cluster.sync();
-        const int all = n_cols * kMI, per = (all + split - 1) / split;
-        const int e1 = (rank + 1) * per < all ? (rank + 1) * per : all;
-        for (int e = rank * per + (int)threadIdx.x; e < e1; e += kMThreads) {
-            float v[kMMaxSplit];
+        // four adjacent elements a thread and step
+        const int quads = n_cols * (kMI / 4), per = (quads + split - 1) / split;
+        const int e1 = (rank + 1) * per < quads ? (rank + 1) * per : quads;
+        for (int e = rank * per + (int)threadIdx.x; e < e1; e += mm_threads(BN)) {
+            float4 v[kMMaxSplit];
 #pragma unroll
-            for (int p = 0; p < kMMaxSplit; ++p) v[p] = p < split ? *cluster.map_shared_rank(part + e, p) : 0.0f;
-            float sum = v[0];
+            for (int p = 0; p < kMMaxSplit; ++p)
+                if (p < split) v[p] = *cluster.map_shared_rank(reinterpret_cast<float4*>(part) + e, p);
+            float sum[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
 #pragma unroll
-            for (int p = 1; p < kMMaxSplit; ++p)
-                if (p < split) sum = __fadd_rn(sum, v[p]);
-            const int64_t oi = i0 + e % kMI, oj = j0 + e / kMI;
-            if (oi < a.n_i) {
-                const float bias = a.bias != nullptr ? bf16_to_f32(a.bias[oi]) : 0.0f;
-                const float r = a.resid != nullptr ? bf16_to_f32(a.resid[oj * a.ld_resid + oi]) : 0.0f;
-                sum = __fadd_rn(sum, bias);
-                if (a.z != nullptr) a.z[oj * a.ld_z + oi] = f32_to_bf16(sum);
-                a.out[oj * a.ld_out + oi] = f32_to_bf16(__fadd_rn(activate(sum, a.act), r));
+            for (int p = 1; p < kMMaxSplit; ++p) {
+                if (p < split) {
+                    sum[0] = __fadd_rn(sum[0], v[p].x);
+                    sum[1] = __fadd_rn(sum[1], v[p].y);
+                    sum[2] = __fadd_rn(sum[2], v[p].z);
+                    sum[3] = __fadd_rn(sum[3], v[p].w);
+                }
+            }
+            const int64_t oi = i0 + 4 * (e % (kMI / 4)), oj = j0 + e / (kMI / 4);
+            float y[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                y[h] = 0.0f;
+                if (oi + h >= a.n_i) continue;
+                float x = __fadd_rn(sum[h], a.bias != nullptr ? bf16_to_f32(a.bias[oi + h]) : 0.0f);
+                if (a.z != nullptr) a.z[oj * a.ld_z + oi + h] = f32_to_bf16(x);
+                x = activate(x, a.act);
+                y[h] = a.resid != nullptr ? __fadd_rn(x, bf16_to_f32(a.resid[oj * a.ld_resid + oi + h])) : x;
+            }
+            uint16_t* o = a.out + oj * a.ld_out + oi;
+            if (a.pairs && oi + 4 <= a.n_i) {
+                reinterpret_cast<uint32_t*>(o)[0] = pack2(y[0], y[1]);
+                reinterpret_cast<uint32_t*>(o)[1] = pack2(y[2], y[3]);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    if (oi + h < a.n_i) o[h] = f32_to_bf16(y[h]);
             }
         }
         cluster.sync();   // nobody leaves while its partial tile is being read
@@ -235,7 +322,7 @@ __global__ void __launch_bounds__(kMThreads) mm_kernel(const __grid_constant__ C
 constexpr int kPTile = 256, kPHalf = 128;
 constexpr int kPStages = 6;
 constexpr uint32_t kPOperand = kPHalf * kMC * 2, kPStage = 2 * kPOperand;
-constexpr int kPEpiWarps = 8;
+constexpr int kPEpiWarps = 16;   // four per quarter of the lanes
 constexpr int kPThreads = 64 + 32 * kPEpiWarps;
 constexpr int kPBand = 8;
 constexpr size_t kPSmem = (size_t)kPStages * kPStage + 1024;
@@ -264,6 +351,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
     const int steps = (int)((a.n_c + kMC - 1) / kMC);
 
     if (threadIdx.x == 0) {
+        prefetch_map(&a_map);
+        prefetch_map(&b_map);
         for (int s = 0; s < kPStages; ++s) {
             mbar_init(&full[s], 1u);    // first CTA's: both CTAs' loads of a stage have landed
             mbar_init(&empty[s], 1u);   // the products reading a stage have completed
@@ -285,6 +374,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     uint32_t issued = 0;
+    allow_next_kernel();   // not before this CTA has its tensor memory: the next kernel's CTAs wait for it with theirs in hand
+    await_previous_kernel();
 
     if (warp == 0) {
         if (lane == 0) {
@@ -348,22 +439,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
             }
         }
     } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;   // quarter of the lanes, half of the columns
+        const int q = warp & 3, set = (warp - 2) >> 2;   // quarter of the lanes, quarter of the columns
         uint32_t n = 0;
         for (int tile = pair; tile < tiles; tile += pairs, ++n) {
             int ti, tj;
             pair_tile(tile, a.tiles_i, a.tiles_j, &ti, &tj);
             const uint32_t buf = n & 1u;
-            const int64_t i = (int64_t)ti * kPTile + rank * kPHalf + q * 32 + lane, j0 = (int64_t)tj * kPTile;
+            const int64_t i0 = (int64_t)ti * kPTile + rank * kPHalf + q * 32, j0 = (int64_t)tj * kPTile;
             const int n_cols = (int)(a.n_j - j0 < kPTile ? a.n_j - j0 : kPTile);
-            const float bias = a.bias != nullptr && i < a.n_i ? bf16_to_f32(a.bias[i]) : 0.0f;
+            const float bias = a.bias != nullptr && i0 + lane < a.n_i ? bf16_to_f32(a.bias[i0 + lane]) : 0.0f;
             if (!mbar_wait(&acc_full[buf], (n >> 1) & 1u, err)) break;
             tc_fence_after();
 #pragma unroll 1
-            for (int c0 = half * 128; c0 < half * 128 + 128 && c0 < n_cols; c0 += 16) {
-                float v[16];
-                tmem_load16(tmem + ((uint32_t)(q * 32) << 16) + buf * 256u + (uint32_t)c0, v);
-                if (i < a.n_i) epilogue16(a, v, bias, i, j0 + c0, n_cols - c0 < 16 ? n_cols - c0 : 16);
+            for (int c0 = set * 64; c0 < set * 64 + 64 && c0 < n_cols; c0 += 32) {
+                float v[32];
+                tmem_load32(tmem + ((uint32_t)(q * 32) << 16) + buf * 256u + (uint32_t)c0, v);
+                epilogue<32>(a, v, bias, i0, j0 + c0, n_cols - c0);
+                __syncwarp();
             }
             tc_fence_before();
             __syncwarp();
@@ -394,34 +486,85 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
 
 // ---------------------------------------------------------------- elementwise passes
 // dst[r, c] = src[r, c] * act'(z[r, c]) (z null: a plain copy), dst with rows on 16-byte boundaries; column sums of
-// the unrounded values over the rows of this CTA's band into partial[band, c] if wanted.  A thread owns a column.
-constexpr int kBandCols = 128;
-__global__ void __launch_bounds__(kBandCols) slope_kernel(const uint16_t* __restrict__ src, int64_t ld_src, const uint16_t* __restrict__ z,
-                                                          int64_t ld_z, int act, uint16_t* __restrict__ dst, int64_t ld_dst, int64_t rows,
-                                                          int64_t cols, int64_t band, float* __restrict__ partial) {
-    const int64_t c = (int64_t)blockIdx.x * kBandCols + threadIdx.x;
-    if (c >= cols) return;
-    const int64_t r0 = (int64_t)blockIdx.y * band, r1 = r0 + band < rows ? r0 + band : rows;
-    float sum = 0.0f;
-    for (int64_t r = r0; r < r1; ++r) {
-        const uint16_t raw = src[r * ld_src + c];
-        float v = bf16_to_f32(raw);
-        if (z != nullptr) v = __fmul_rn(v, activate_slope(bf16_to_f32(z[r * ld_z + c]), act));
-        // dZ is rounded to bf16 here because the tensor cores take bf16; the column sums are not
-        if (dst != nullptr) dst[r * ld_dst + c] = z != nullptr ? f32_to_bf16(v) : raw;
-        sum = __fadd_rn(sum, v);
+// the unrounded values over the rows of this CTA's band into partial[band, c] if wanted.  A warp takes 256 columns, a
+// lane eight of them (16 bytes where src and z have 16-byte rows), the CTA's eight warps every eighth row; the warps'
+// sums meet in shared memory in their order.
+constexpr int kSlopeWarps = 8, kSlopeCols = 256;
+template <bool VEC> __device__ __forceinline__ void load8(const uint16_t* row, int64_t c, int64_t cols, uint32_t (&w)[4]) {
+    if (VEC) {   // rows on 16-byte boundaries; nothing past the last column is read
+        if (c + 8 <= cols) {
+            const uint4 v = ld_stream16_ro(row + c);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+            return;
+        }
     }
-    if (partial != nullptr) partial[(int64_t)blockIdx.y * cols + c] = sum;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t lo = c + 2 * e < cols ? row[c + 2 * e] : 0u, hi = c + 2 * e + 1 < cols ? row[c + 2 * e + 1] : 0u;
+        w[e] = lo | (hi << 16);
+    }
 }
-__global__ void __launch_bounds__(kBandCols) column_sum_kernel(const float* __restrict__ partial, int64_t bands, int64_t cols, uint16_t* __restrict__ out) {
-    const int64_t c = (int64_t)blockIdx.x * kBandCols + threadIdx.x;
+template <bool VEC>
+__global__ void __launch_bounds__(32 * kSlopeWarps) slope_kernel(const uint16_t* __restrict__ src, int64_t ld_src, const uint16_t* __restrict__ z,
+                                                                 int64_t ld_z, int act, uint16_t* __restrict__ dst, int64_t ld_dst, int64_t rows,
+                                                                 int64_t cols, int64_t band, float* __restrict__ partial) {
+    __shared__ float sums[kSlopeWarps][kSlopeCols];
+    allow_next_kernel();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t c = (int64_t)blockIdx.x * kSlopeCols + lane * 8;
+    const int64_t r0 = (int64_t)blockIdx.y * band, r1 = r0 + band < rows ? r0 + band : rows;
+    await_previous_kernel();
+    float sum[8] = {};
+    if (c < cols) {
+        for (int64_t r = r0 + warp; r < r1; r += kSlopeWarps) {
+            uint32_t w[4], y[4];
+            load8<VEC>(src + r * ld_src, c, cols, w);
+            if (z != nullptr) load8<VEC>(z + r * ld_z, c, cols, y);
+            float v[8], s[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __uint_as_float((e & 1) ? (w[e >> 1] & 0xFFFF0000u) : (w[e >> 1] << 16));
+            if (z != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[e] = __uint_as_float((e & 1) ? (y[e >> 1] & 0xFFFF0000u) : (y[e >> 1] << 16));
+                slope_all(s, act);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], s[e]);
+                // dZ is rounded to bf16 here because the tensor cores take bf16; the column sums are not
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
+            }
+            if (dst != nullptr) *reinterpret_cast<uint4*>(dst + r * ld_dst + c) = make_uint4(w[0], w[1], w[2], w[3]);   // rows are padded to whole vectors
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = __fadd_rn(sum[e], v[e]);
+        }
+    }
+    if (partial == nullptr) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[warp][lane * 8 + e] = sum[e];
+    __syncthreads();
+    const int64_t col = (int64_t)blockIdx.x * kSlopeCols + threadIdx.x;
+    if (col >= cols) return;
+    float total = 0.0f;
+    for (int w = 0; w < kSlopeWarps; ++w) total = __fadd_rn(total, sums[w][threadIdx.x]);
+    partial[(int64_t)blockIdx.y * cols + col] = total;
+}
+constexpr int kSumCols = 128;
+__global__ void __launch_bounds__(kSumCols) column_sum_kernel(const float* __restrict__ partial, int64_t bands, int64_t cols, uint16_t* __restrict__ out) {
+    allow_next_kernel();
+    await_previous_kernel();
+    const int64_t c = (int64_t)blockIdx.x * kSumCols + threadIdx.x;
     if (c >= cols) return;
     float sum = 0.0f;
+#pragma unroll 8
     for (int64_t b = 0; b < bands; ++b) sum = __fadd_rn(sum, partial[b * cols + c]);
     out[c] = f32_to_bf16(sum);
 }
 
 // ---------------------------------------------------------------- host side
+// Cycles: of a pair's 64 contraction steps of a 256 x 256 tile, of its tile beside them, of a launch; of a stage of a
+// 128 x 128 tile with two CTAs an SM (their operands come from L2: 32 KB for a quarter of a pair's work), of its launch.
+constexpr int64_t kPairStep = 520, kPairTile = 1500, kPairFixed = 7000, kSmallStep = 1230, kSmallFixed = 6000;
+
 struct Matrix {
     const void* p;
     int64_t rows, cols, ld;
@@ -431,20 +574,39 @@ struct Matrix {
     size_t padded_bytes() const { return align_up((size_t)rows * (size_t)padded_ld() * 2u, 256); }
 };
 
-int64_t band_rows(int64_t rows) { return rows <= 64 ? rows : (rows + 63) / 64 < 32 ? 32 : (rows + 63) / 64; }
-int64_t bands_of(int64_t rows) { return rows > 0 ? (rows + band_rows(rows) - 1) / band_rows(rows) : 0; }
+// Bands of rows: a CTA's eight warps take four rows each of the shortest; at most 64 bands.
+int64_t band_rows(int64_t rows) { return rows <= 32 * 64 ? 32 : (rows + 63) / 64; }
+int64_t bands_of(int64_t rows) { return (rows + band_rows(rows) - 1) / band_rows(rows); }
+
+// A launch that may start under the one before it; `cluster` CTAs a cluster.
+struct Launch {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    Launch(dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster = 1) {
+        attr[0] = early_start();
+        attr[1] = cluster_of(cluster);
+        cfg.gridDim = grid;
+        cfg.blockDim = dim3((unsigned)threads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cfg.attrs = attr;
+        cfg.numAttrs = cluster > 1 ? 2 : 1;
+    }
+};
 
 int run_slope(const Matrix& src, const void* z, int64_t ld_z, int act, void* dst, int64_t ld_dst, float* partial, void* db, cudaStream_t st) {
     const int64_t bands = bands_of(src.rows);
     if (bands > 0) {
-        const dim3 grid((unsigned)((src.cols + kBandCols - 1) / kBandCols), (unsigned)bands);
-        slope_kernel<<<grid, kBandCols, 0, st>>>(static_cast<const uint16_t*>(src.p), src.ld, static_cast<const uint16_t*>(z), ld_z, act,
-                                                 static_cast<uint16_t*>(dst), ld_dst, src.rows, src.cols, band_rows(src.rows), partial);
-        MOSAIC_LAUNCH_CHECK();
+        Launch l(dim3((unsigned)((src.cols + kSlopeCols - 1) / kSlopeCols), (unsigned)bands), 32 * kSlopeWarps, 0, st);
+        const Matrix zm{z, src.rows, src.cols, ld_z};
+        const bool vec = src.tma_ok() && (z == nullptr || zm.tma_ok());
+        MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, vec ? slope_kernel<true> : slope_kernel<false>, static_cast<const uint16_t*>(src.p), src.ld,
+                                           static_cast<const uint16_t*>(z), ld_z, act, static_cast<uint16_t*>(dst), ld_dst, src.rows, src.cols,
+                                           band_rows(src.rows), partial));
     }
     if (db != nullptr) {
-        column_sum_kernel<<<(unsigned)((src.cols + kBandCols - 1) / kBandCols), kBandCols, 0, st>>>(partial, bands, src.cols, static_cast<uint16_t*>(db));
-        MOSAIC_LAUNCH_CHECK();
+        Launch l(dim3((unsigned)((src.cols + kSumCols - 1) / kSumCols)), kSumCols, 0, st);
+        MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, column_sum_kernel, static_cast<const float*>(partial), bands, src.cols, static_cast<uint16_t*>(db)));
     }
     return MOSAIC_OK;
 }
@@ -460,24 +622,34 @@ int readable(Matrix& m, char** ws, cudaStream_t st) {
     return MOSAIC_OK;
 }
 
+template <bool A_MN, bool B_MN> int encode_operands(CUtensorMap* a_map, CUtensorMap* b_map, const Matrix& A, const Matrix& B, int rows_a, int rows_b) {
+    const bool a_ok = A_MN ? encode_bf16(a_map, A.p, A.rows, A.cols, A.ld, kMC, 64) : encode_bf16(a_map, A.p, A.rows, A.cols, A.ld, rows_a, kMC);
+    const bool b_ok = B_MN ? encode_bf16(b_map, B.p, B.rows, B.cols, B.ld, kMC, 64) : encode_bf16(b_map, B.p, B.rows, B.cols, B.ld, rows_b, kMC);
+    return a_ok && b_ok ? MOSAIC_OK : MOSAIC_ERR_CUDA;
+}
+
+// CTAs that share a tile's contraction: while SMs would stay idle and each keeps four stages.
+int split_of(int64_t tiles, int64_t steps) {
+    int split = 1;
+    while (split < kMMaxSplit && tiles * split * 2 <= 2 * sm_count() && steps >= 8 * split) split *= 2;
+    return split;
+}
+
 template <bool A_MN, bool B_MN, int BN>
-int launch_mm(const Matrix& A, const Matrix& B, MmArgs a, cudaStream_t st) {
+int launch_mm(const Matrix& A, const Matrix& B, MmArgs a, int64_t quarters, cudaStream_t st) {
     constexpr size_t kStage = (size_t)(kMI + BN) * kMC * 2;
     CUtensorMap a_map, b_map;
-    if (!(A_MN ? encode_bf16(&a_map, A.p, A.rows, A.cols, A.ld, kMC, 64) : encode_bf16(&a_map, A.p, A.rows, A.cols, A.ld, kMI, kMC))) return MOSAIC_ERR_CUDA;
-    if (!(B_MN ? encode_bf16(&b_map, B.p, B.rows, B.cols, B.ld, kMC, 64) : encode_bf16(&b_map, B.p, B.rows, B.cols, B.ld, BN, kMC))) return MOSAIC_ERR_CUDA;
+    if (encode_operands<A_MN, B_MN>(&a_map, &b_map, A, B, kMI, BN) != MOSAIC_OK) return MOSAIC_ERR_CUDA;
     a.tiles_i = (int)((a.n_i + kMI - 1) / kMI);
     a.tiles_j = (int)((a.n_j + BN - 1) / BN);
-    const int64_t tiles = (int64_t)a.tiles_i * a.tiles_j, steps = (a.n_c + kMC - 1) / kMC;
-    int split = 1;   // share a tile's contraction while SMs would stay idle and each share keeps four stages
-    while (split < kMMaxSplit && tiles * split * 2 <= 2 * sm_count() && steps >= 8 * split) split *= 2;
+    const int64_t tiles = quarters > 0 ? quarters : (int64_t)a.tiles_i * a.tiles_j, steps = (a.n_c + kMC - 1) / kMC;
+    const int split = split_of(tiles, steps);
     if (tiles * split > 0x7FFFFFFF) return MOSAIC_ERR_INVALID_ARG;
     // two CTAs an SM (100 KB of stages each): one's epilogue under the other's products
     a.stages = (int)(100 * 1024 / kStage);
     if (a.stages > 8) a.stages = 8;
     size_t smem = a.stages * kStage;
     if (split > 1 && smem < (size_t)BN * kMI * 4u) smem = (size_t)BN * kMI * 4u;
-    smem += 1024;
     static DeviceCache opted;
     const int ok = opted.get([&]() -> int {
         if (cudaFuncSetAttribute(mm_kernel<A_MN, B_MN, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, 110 * 1024) != cudaSuccess) {
@@ -487,30 +659,16 @@ int launch_mm(const Matrix& A, const Matrix& B, MmArgs a, cudaStream_t st) {
         return 1;
     });
     if (ok < 0) return MOSAIC_ERR_CUDA;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * split));
-    cfg.blockDim = dim3(kMThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)split;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&cfg, mm_kernel<A_MN, B_MN, BN>, a_map, b_map, a));
+    Launch l(dim3((unsigned)(tiles * split)), mm_threads(BN), smem + 1024, st, split);
+    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, mm_kernel<A_MN, B_MN, BN>, a_map, b_map, a));
     return MOSAIC_OK;
 }
 
-template <bool A_MN, bool B_MN> int launch_pair(const Matrix& A, const Matrix& B, MmArgs a, cudaStream_t st) {
+template <bool A_MN, bool B_MN> int launch_pair(const Matrix& A, const Matrix& B, MmArgs a, int64_t tiles, cudaStream_t st) {
     CUtensorMap a_map, b_map;
-    if (!(A_MN ? encode_bf16(&a_map, A.p, A.rows, A.cols, A.ld, kMC, 64) : encode_bf16(&a_map, A.p, A.rows, A.cols, A.ld, kPHalf, kMC))) return MOSAIC_ERR_CUDA;
-    if (!(B_MN ? encode_bf16(&b_map, B.p, B.rows, B.cols, B.ld, kMC, 64) : encode_bf16(&b_map, B.p, B.rows, B.cols, B.ld, kPHalf, kMC))) return MOSAIC_ERR_CUDA;
-    a.tiles_i = (int)((a.n_i + kPTile - 1) / kPTile);
-    a.tiles_j = (int)((a.n_j + kPTile - 1) / kPTile);
-    const int64_t tiles = (int64_t)a.tiles_i * a.tiles_j;
-    if (tiles > 0x3FFFFFFF) return MOSAIC_ERR_INVALID_ARG;
+    if (encode_operands<A_MN, B_MN>(&a_map, &b_map, A, B, kPHalf, kPHalf) != MOSAIC_OK) return MOSAIC_ERR_CUDA;
+    a.tiles_i = a.pair_i;
+    a.tiles_j = a.pair_j;
     static DeviceCache opted;
     const int ok = opted.get([&]() -> int {
         if (cudaFuncSetAttribute(mm_pair_kernel<A_MN, B_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPSmem) != cudaSuccess) {
@@ -521,21 +679,53 @@ template <bool A_MN, bool B_MN> int launch_pair(const Matrix& A, const Matrix& B
     });
     if (ok < 0) return MOSAIC_ERR_CUDA;
     const int64_t pairs = sm_count() / 2;
-    mm_pair_kernel<A_MN, B_MN><<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), kPThreads, kPSmem, st>>>(a_map, b_map, a, (int)tiles);
-    MOSAIC_LAUNCH_CHECK();
+    Launch l(dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), kPThreads, kPSmem, st);   // the cluster is the kernel's own
+    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, mm_pair_kernel<A_MN, B_MN>, a_map, b_map, a, (int)tiles));
     return MOSAIC_OK;
 }
 
 // out[j, i] = sum_c A B; A: [n_i, n_c] (or [n_c, n_i] if A_MN), B likewise.
-template <bool A_MN, bool B_MN> int run_mm(const Matrix& A, const Matrix& B, const MmArgs& a, cudaStream_t st) {
-    if constexpr (!B_MN) {   // narrow instructions for few output rows
-        if (a.n_j <= 16) return launch_mm<A_MN, B_MN, 16>(A, B, a, st);
-        if (a.n_j <= 32) return launch_mm<A_MN, B_MN, 32>(A, B, a, st);
+template <bool A_MN, bool B_MN> int run_mm(const Matrix& A, const Matrix& B, MmArgs a, cudaStream_t st) {
+    const int64_t steps = (a.n_c + kMC - 1) / kMC, sms = sm_count();
+    const auto even = [](const void* p, int64_t ld) { return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & 3u) == 0 && ld % 2 == 0); };
+    a.pairs = even(a.out, a.ld_out) && even(a.resid, a.ld_resid) && even(a.z, a.ld_z) ? 1 : 0;
+    a.first_pair = -1;
+    const int64_t pi = (a.n_i + kPTile - 1) / kPTile, pj = (a.n_j + kPTile - 1) / kPTile, large = pi * pj, pairs = sms / 2;
+    if (large > 0x3FFFFFFF) return MOSAIC_ERR_INVALID_ARG;
+    a.pair_i = (int)pi;
+    a.pair_j = (int)pj;
+    // Which kernel: in cycles of the tensor cores, what each would take (measured, see the figures at the top).
+    const int64_t ti = (a.n_i + kMI - 1) / kMI;
+    const int64_t small_tiles = ti * ((a.n_j + 127) / 128), small_split = split_of(small_tiles, steps);
+    const int64_t small_cost = (small_tiles * small_split + 2 * sms - 1) / (2 * sms) * ((steps + small_split - 1) / small_split) * kSmallStep + kSmallFixed;
+    const int64_t waves = large / pairs, rest = large % pairs;
+    const int64_t wave_cost = steps * kPairStep + kPairTile;
+    const int64_t pair_cost = (waves + (rest > 0 ? 1 : 0)) * wave_cost + kPairFixed;
+    if (a.n_j > 64 && pair_cost < small_cost) {
+        // a last wave of few tiles is cheaper cut up, its contraction shared
+        const int64_t rest_split = split_of(rest * 4, steps);
+        const int64_t rest_cost = (rest * 4 * rest_split + 2 * sms - 1) / (2 * sms) * ((steps + rest_split - 1) / rest_split) * kSmallStep + kSmallFixed;
+        const bool cut = waves > 0 && rest > 0 && rest_cost < wave_cost;
+        int rc = launch_pair<A_MN, B_MN>(A, B, a, cut ? waves * pairs : large, st);
+        if (rc != MOSAIC_OK || !cut) return rc;
+        a.first_pair = (int)(waves * pairs);
+        return launch_mm<A_MN, B_MN, 128>(A, B, a, rest * 4, st);
     }
-    if (a.n_j <= 64) return launch_mm<A_MN, B_MN, 64>(A, B, a, st);
-    const int64_t tiles = ((a.n_i + kPTile - 1) / kPTile) * ((a.n_j + kPTile - 1) / kPTile);
-    if (tiles >= sm_count() / 2) return launch_pair<A_MN, B_MN>(A, B, a, st);
-    return launch_mm<A_MN, B_MN, 128>(A, B, a, st);
+    // the widest tile that leaves few SMs idle
+    int64_t bn = 128;
+    const int64_t least = B_MN ? 64 : 16;
+    while (bn > least && bn / 2 >= a.n_j) bn /= 2;
+    while (bn > least) {
+        const int64_t tiles = ti * ((a.n_j + bn - 1) / bn);
+        if (tiles * split_of(tiles, steps) * 2 > sms) break;
+        bn /= 2;
+    }
+    if constexpr (!B_MN) {
+        if (bn == 16) return launch_mm<A_MN, B_MN, 16>(A, B, a, 0, st);
+        if (bn == 32) return launch_mm<A_MN, B_MN, 32>(A, B, a, 0, st);
+    }
+    if (bn == 64) return launch_mm<A_MN, B_MN, 64>(A, B, a, 0, st);
+    return launch_mm<A_MN, B_MN, 128>(A, B, a, 0, st);
 }
 
 bool overlap(const Matrix& a, const Matrix& b) {

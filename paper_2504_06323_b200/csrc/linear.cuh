@@ -48,5 +48,17 @@ __device__ __forceinline__ float activate_slope(float z, int act) {
         default: return 1.0f;
     }
 }
+template <int N> __device__ __forceinline__ void slope_all(float (&z)[N], int act) {
+    if (act == MOSAIC_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = activate_slope(z[e], MOSAIC_ACT_RELU);
+    } else if (act == MOSAIC_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = activate_slope(z[e], MOSAIC_ACT_SILU);
+    } else if (act == MOSAIC_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = activate_slope(z[e], MOSAIC_ACT_GELU);
+    }
+}
 #endif
 }  // namespace mosaic

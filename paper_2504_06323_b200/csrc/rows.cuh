@@ -46,11 +46,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// A kernel launched with the stream-serialization attribute may start while the one before it still runs: it waits
-// here before it touches what that one reads or writes.  The other side allows it to start.
-__device__ __forceinline__ void await_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // Two fp32 values an instruction.
 struct Pair {
     uint64_t v;

@@ -69,7 +69,7 @@ SHAPES = [  # tokens, out, in: one token to many, around tile edges (16 / 32 / 6
     (1, 1, 1), (1, 128, 64), (1, 1000, 4096), (3, 130, 65), (15, 257, 129), (16, 128, 2048), (17, 127, 63), (32, 640, 320), (33, 300, 1031),
     (64, 513, 777), (65, 96, 64), (100, 1, 500), (127, 200, 8), (128, 688, 256), (129, 129, 129), (257, 385, 1000), (500, 260, 4100),
     (1000, 1025, 96), (2049, 300, 200),
-    (2049, 2500, 136), (260, 5000, 4100), (4100, 4200, 264), (2304, 2305, 64),   # enough tiles for pairs of CTAs
+    (2049, 2500, 136), (260, 5000, 4100), (4100, 4200, 264), (2304, 2305, 64), (2560, 2050, 1500), (1000, 4096, 2048),   # pairs of CTAs, a last wave cut up
 ]
 
 
