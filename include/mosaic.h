@@ -460,8 +460,8 @@ typedef enum mosaic_act {
  *   status_dev  as in mosaic_gram_accumulate, or NULL
  *   ws        device scratch, >= mosaic_linear_workspace_bytes() for the same
  *             arguments: 0 when X and W have 16-byte aligned bases and leading
- *             dimensions (ws may then be NULL), else room for an aligned copy of each
- *             that has not
+ *             dimensions, and for up to four tokens (ws may then be NULL), else room
+ *             for an aligned copy of each that has not
  * Sums in fp32 on the tensor cores; bias, activation and residual in fp32 on the
  * sum; one rounding to bf16 for Y and one for Z.  tokens = 0 is legal.  Outputs
  * must not overlap the inputs (Y and residual excepted) or each other.

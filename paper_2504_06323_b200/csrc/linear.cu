@@ -484,14 +484,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
     cluster.sync();   // the error words have been read, the loads have landed
 }
 
-// ---------------------------------------------------------------- elementwise passes
-// dst[r, c] = src[r, c] * act'(z[r, c]) (z null: a plain copy), dst with rows on 16-byte boundaries; column sums of
-// the unrounded values over the rows of this CTA's band into partial[band, c] if wanted.  A warp takes 256 columns, a
-// lane eight of them (16 bytes where src and z have 16-byte rows), the CTA's eight warps every eighth row; the warps'
-// sums meet in shared memory in their order.
-constexpr int kSlopeWarps = 8, kSlopeCols = 256;
+// Eight elements of a row from c on; zeros past the last column, which nothing is read of.
 template <bool VEC> __device__ __forceinline__ void load8(const uint16_t* row, int64_t c, int64_t cols, uint32_t (&w)[4]) {
-    if (VEC) {   // rows on 16-byte boundaries; nothing past the last column is read
+    if (VEC) {   // rows on 16-byte boundaries
         if (c + 8 <= cols) {
             const uint4 v = ld_stream16_ro(row + c);
             w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
@@ -504,6 +499,90 @@ template <bool VEC> __device__ __forceinline__ void load8(const uint16_t* row, i
         w[e] = lo | (hi << 16);
     }
 }
+
+// ---------------------------------------------------------------- few tokens
+// Up to kFewTokens tokens (a decoding step): the weights are read once for next to no arithmetic, so what counts is
+// that they stream.  A CTA takes kFewRows weight rows and a quarter to an eighth of the contraction per warp; a lane
+// multiplies 16 bytes of each row (VEC: rows on 16-byte boundaries; else element by element, any alignment) with the
+// tokens' values from L1.  fp32 sums: per lane in order, over the lanes by a butterfly, over the warps in their order.
+// Bound by memory; no shared-memory ring, tensor memory or cluster to set up: %%FEW%%
+constexpr int kFewTokens = 4, kFewRows = 4, kFewWarps = 8;
+template <int M, bool VEC>
+__global__ void __launch_bounds__(32 * kFewWarps) few_kernel(const uint16_t* __restrict__ X, int64_t ldx, const uint16_t* __restrict__ W, int64_t ldw,
+                                                             const __grid_constant__ MmArgs a) {
+    __shared__ float part[kFewWarps][kFewRows][M];
+    allow_next_kernel();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t o0 = (int64_t)blockIdx.x * kFewRows;
+    float acc[kFewRows][M] = {};
+    await_previous_kernel();
+    const uint16_t* w[kFewRows];
+#pragma unroll
+    for (int r = 0; r < kFewRows; ++r) w[r] = W + (o0 + r < a.n_i ? o0 + r : o0) * ldw;   // past the end: the first row again, not stored
+    if (VEC) {
+        // chunks of 256 contraction steps, dealt to the warps in turn
+#pragma unroll 2
+        for (int64_t c = warp * 256 + lane * 8; c < a.n_c; c += kFewWarps * 256) {
+            uint32_t x[M][4], y[kFewRows][4];
+#pragma unroll
+            for (int r = 0; r < kFewRows; ++r) load8<true>(w[r], c, a.n_c, y[r]);
+#pragma unroll
+            for (int m = 0; m < M; ++m) load8<true>(X + m * ldx, c, a.n_c, x[m]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int r = 0; r < kFewRows; ++r) {
+                    const float lo = __uint_as_float(y[r][e] << 16), hi = __uint_as_float(y[r][e] & 0xFFFF0000u);
+#pragma unroll
+                    for (int m = 0; m < M; ++m) {
+                        acc[r][m] = __fmaf_rn(lo, __uint_as_float(x[m][e] << 16), acc[r][m]);
+                        acc[r][m] = __fmaf_rn(hi, __uint_as_float(x[m][e] & 0xFFFF0000u), acc[r][m]);
+                    }
+                }
+        }
+    } else {
+#pragma unroll 8
+        for (int64_t c = warp * 32 + lane; c < a.n_c; c += kFewWarps * 32) {
+            float x[M];
+#pragma unroll
+            for (int m = 0; m < M; ++m) x[m] = bf16_to_f32(X[m * ldx + c]);
+#pragma unroll
+            for (int r = 0; r < kFewRows; ++r) {
+                const float y = bf16_to_f32(w[r][c]);
+#pragma unroll
+                for (int m = 0; m < M; ++m) acc[r][m] = __fmaf_rn(y, x[m], acc[r][m]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kFewRows; ++r)
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            float v = acc[r][m];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v = __fadd_rn(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+            if (lane == 0) part[warp][r][m] = v;
+        }
+    __syncthreads();
+    if (threadIdx.x >= kFewRows * M) return;
+    const int r = threadIdx.x % kFewRows, m = threadIdx.x / kFewRows;
+    const int64_t i = o0 + r;
+    if (i >= a.n_i) return;
+    float v = 0.0f;
+    for (int k = 0; k < kFewWarps; ++k) v = __fadd_rn(v, part[k][r][m]);
+    v = __fadd_rn(v, a.bias != nullptr ? bf16_to_f32(a.bias[i]) : 0.0f);
+    if (a.z != nullptr) a.z[m * a.ld_z + i] = f32_to_bf16(v);
+    v = activate(v, a.act);
+    if (a.resid != nullptr) v = __fadd_rn(v, bf16_to_f32(a.resid[m * a.ld_resid + i]));
+    a.out[m * a.ld_out + i] = f32_to_bf16(v);
+}
+
+// ---------------------------------------------------------------- elementwise passes
+// dst[r, c] = src[r, c] * act'(z[r, c]) (z null: a plain copy), dst with rows on 16-byte boundaries; column sums of
+// the unrounded values over the rows of this CTA's band into partial[band, c] if wanted.  A warp takes 256 columns, a
+// lane eight of them (16 bytes where src and z have 16-byte rows), the CTA's eight warps every eighth row; the warps'
+// sums meet in shared memory in their order.
+constexpr int kSlopeWarps = 8, kSlopeCols = 256;
 template <bool VEC>
 __global__ void __launch_bounds__(32 * kSlopeWarps) slope_kernel(const uint16_t* __restrict__ src, int64_t ld_src, const uint16_t* __restrict__ z,
                                                                  int64_t ld_z, int act, uint16_t* __restrict__ dst, int64_t ld_dst, int64_t rows,
@@ -622,9 +701,12 @@ int readable(Matrix& m, char** ws, cudaStream_t st) {
     return MOSAIC_OK;
 }
 
+// A box's rows are 128 bytes of rows far apart, and the next 128 bytes are asked for a stage later: L2 fetches 128
+// bytes (256: 1024 x 4096 x 8832 took 82 us instead of 61).
 template <bool A_MN, bool B_MN> int encode_operands(CUtensorMap* a_map, CUtensorMap* b_map, const Matrix& A, const Matrix& B, int rows_a, int rows_b) {
-    const bool a_ok = A_MN ? encode_bf16(a_map, A.p, A.rows, A.cols, A.ld, kMC, 64) : encode_bf16(a_map, A.p, A.rows, A.cols, A.ld, rows_a, kMC);
-    const bool b_ok = B_MN ? encode_bf16(b_map, B.p, B.rows, B.cols, B.ld, kMC, 64) : encode_bf16(b_map, B.p, B.rows, B.cols, B.ld, rows_b, kMC);
+    constexpr CUtensorMapL2promotion kFetch = CU_TENSOR_MAP_L2_PROMOTION_L2_128B;
+    const bool a_ok = A_MN ? encode_bf16(a_map, A.p, A.rows, A.cols, A.ld, kMC, 64, kFetch) : encode_bf16(a_map, A.p, A.rows, A.cols, A.ld, rows_a, kMC, kFetch);
+    const bool b_ok = B_MN ? encode_bf16(b_map, B.p, B.rows, B.cols, B.ld, kMC, 64, kFetch) : encode_bf16(b_map, B.p, B.rows, B.cols, B.ld, rows_b, kMC, kFetch);
     return a_ok && b_ok ? MOSAIC_OK : MOSAIC_ERR_CUDA;
 }
 
@@ -728,6 +810,17 @@ template <bool A_MN, bool B_MN> int run_mm(const Matrix& A, const Matrix& B, MmA
     return launch_mm<A_MN, B_MN, 128>(A, B, a, 0, st);
 }
 
+int launch_few(const Matrix& x, const Matrix& w, const MmArgs& a, cudaStream_t st) {
+    using Kernel = void (*)(const uint16_t*, int64_t, const uint16_t*, int64_t, MmArgs);
+    static const Kernel kernels[2][kFewTokens] = {{few_kernel<1, false>, few_kernel<2, false>, few_kernel<3, false>, few_kernel<4, false>},
+                                                  {few_kernel<1, true>, few_kernel<2, true>, few_kernel<3, true>, few_kernel<4, true>}};
+    const int64_t ctas = (a.n_i + kFewRows - 1) / kFewRows;
+    Launch l(dim3((unsigned)ctas), 32 * kFewWarps, 0, st);
+    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, kernels[x.tma_ok() && w.tma_ok() ? 1 : 0][a.n_j - 1], static_cast<const uint16_t*>(x.p), x.ld,
+                                       static_cast<const uint16_t*>(w.p), w.ld, a));
+    return MOSAIC_OK;
+}
+
 bool overlap(const Matrix& a, const Matrix& b) {
     const char *x = static_cast<const char*>(a.p), *y = static_cast<const char*>(b.p);
     return x != nullptr && y != nullptr && a.bytes() > 0 && b.bytes() > 0 && x < y + b.bytes() && y < x + a.bytes();
@@ -770,6 +863,7 @@ using namespace mosaic;
 extern "C" size_t mosaic_linear_workspace_bytes(const void* X, int64_t ldx, const void* W, int64_t ldw, int64_t tokens, int64_t out_features,
                                                 int64_t in_features) {
     if (!extents_ok(tokens, out_features, in_features)) return 0;
+    if (tokens <= kFewTokens) return 0;   // read as they are
     const Matrix x{X, tokens, in_features, ldx}, w{W, out_features, in_features, ldw};
     return (x.tma_ok() ? 0 : x.padded_bytes()) + (w.tma_ok() ? 0 : w.padded_bytes());
 }
@@ -796,8 +890,6 @@ extern "C" int mosaic_linear(const void* X, int64_t ldx, const void* W, int64_t 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (status_dev != nullptr) MOSAIC_CUDA_TRY(cudaMemsetAsync(status_dev, 0, sizeof(int), st));
     if (tokens == 0) return MOSAIC_OK;
-    char* scratch = static_cast<char*>(ws);
-    if ((rc = readable(x, &scratch, st)) != MOSAIC_OK || (rc = readable(w, &scratch, st)) != MOSAIC_OK) return rc;
     MmArgs a = {};
     a.n_i = out_features; a.n_j = tokens; a.n_c = in_features;
     a.out = static_cast<uint16_t*>(Y); a.ld_out = ldy;
@@ -805,6 +897,9 @@ extern "C" int mosaic_linear(const void* X, int64_t ldx, const void* W, int64_t 
     a.resid = static_cast<const uint16_t*>(residual); a.ld_resid = ldr;
     a.z = static_cast<uint16_t*>(Z); a.ld_z = ldz;
     a.act = act; a.status = status_dev;
+    if (tokens <= kFewTokens) return launch_few(x, w, a, st);
+    char* scratch = static_cast<char*>(ws);
+    if ((rc = readable(x, &scratch, st)) != MOSAIC_OK || (rc = readable(w, &scratch, st)) != MOSAIC_OK) return rc;
     return run_mm<false, false>(w, x, a, st);
 }
 
