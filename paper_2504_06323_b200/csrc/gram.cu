@@ -276,7 +276,7 @@ extern "C" int mosaic_gram_accumulate(const void* X, int64_t tokens, int64_t col
         return MOSAIC_OK;
     }
     CUtensorMap map;
-    if (!encode_bf16(&map, X, tokens, cols, ldx, kGTok, kGBoxCols, CU_TENSOR_MAP_L2_PROMOTION_L2_256B)) return MOSAIC_ERR_CUDA;
+    if (!encode_bf16(&map, X, tokens, cols, ldx, kGTok, kGBoxCols)) return MOSAIC_ERR_CUDA;
     static DeviceCache opted;   // the shared-memory opt-in belongs to one device's copy of the kernel
     const int ok = opted.get([&]() -> int {
         if (cudaFuncSetAttribute(gram_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGSmemBytes) != cudaSuccess) {

@@ -315,13 +315,14 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
 
 // ---------------------------------------------------------------- large products
 // Two CTAs (a cluster, two SMs) share each matrix instruction: 256 x 256 output elements, each CTA holding its half
-// of both operands in shared memory (32 KB a stage for 256 x 256 x 64 products: half of what a CTA alone would have
+// of both operands in shared memory (64 KB a stage for 256 x 256 x 128 products: half of what a CTA alone would have
 // to load for the same work) and 128 x 256 of the accumulator in its tensor memory, twice: the epilogue of a tile
 // runs under the products of the next.  Persistent: a pair takes tile after tile.  The tiles go band by band
 // (kPBand tiles of output rows), so that the tiles in flight share operands in L2.
 constexpr int kPTile = 256, kPHalf = 128;
-constexpr int kPStages = 6;
-constexpr uint32_t kPOperand = kPHalf * kMC * 2, kPStage = 2 * kPOperand;
+constexpr int kPSub = 2;   // 64 contraction steps each: eight instructions a barrier (with four, 1377 instead of 1505 Tflop/s at 4096 x 13824 x 5120)
+constexpr int kPStages = 3;
+constexpr uint32_t kPOperand = kPHalf * kMC * 2, kPStage = kPSub * 2 * kPOperand;
 constexpr int kPEpiWarps = 16;   // four per quarter of the lanes
 constexpr int kPThreads = 64 + 32 * kPEpiWarps;
 constexpr int kPBand = 8;
@@ -348,7 +349,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
     const int rank = (int)cluster.block_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
-    const int steps = (int)((a.n_c + kMC - 1) / kMC);
+    const int steps = (int)((a.n_c + kPSub * kMC - 1) / (kPSub * kMC));
 
     if (threadIdx.x == 0) {
         prefetch_map(&a_map);
@@ -391,21 +392,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
                         ok = false;
                         break;
                     }
-                    unsigned char* sa = ring + (size_t)slot * kPStage;
-                    unsigned char* sb = sa + kPOperand;
                     if (rank == 0) mbar_expect_tx(&full[slot], 2u * kPStage);
                     const uint32_t bar = cluster_addr(&full[slot], 0u);
-                    if (A_MN) {
-                        tma_load_box_pair(sa, &a_map, bar, i0, s * kMC);
-                        tma_load_box_pair(sa + kMBox, &a_map, bar, i0 + 64, s * kMC);
-                    } else {
-                        tma_load_box_pair(sa, &a_map, bar, s * kMC, i0);
-                    }
-                    if (B_MN) {
-                        tma_load_box_pair(sb, &b_map, bar, j0, s * kMC);
-                        tma_load_box_pair(sb + kMBox, &b_map, bar, j0 + 64, s * kMC);
-                    } else {
-                        tma_load_box_pair(sb, &b_map, bar, s * kMC, j0);
+#pragma unroll
+                    for (int h = 0; h < kPSub; ++h) {
+                        unsigned char* sa = ring + (size_t)slot * kPStage + (size_t)h * 2u * kPOperand;
+                        unsigned char* sb = sa + kPOperand;
+                        const int c = (s * kPSub + h) * kMC;
+                        if (A_MN) {
+                            tma_load_box_pair(sa, &a_map, bar, i0, c);
+                            tma_load_box_pair(sa + kMBox, &a_map, bar, i0 + 64, c);
+                        } else {
+                            tma_load_box_pair(sa, &a_map, bar, c, i0);
+                        }
+                        if (B_MN) {
+                            tma_load_box_pair(sb, &b_map, bar, j0, c);
+                            tma_load_box_pair(sb + kMBox, &b_map, bar, j0 + 64, c);
+                        } else {
+                            tma_load_box_pair(sb, &b_map, bar, c, j0);
+                        }
                     }
                 }
             }
@@ -426,12 +431,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t sa = smem_u32(ring + (size_t)slot * kPStage), sb = sa + kPOperand;
+                    const uint32_t stage = smem_u32(ring + (size_t)slot * kPStage);
 #pragma unroll
-                    for (int kk = 0; kk < kMC / 16; ++kk) {
-                        const uint64_t da = operand_desc(sa + (uint32_t)kk * (A_MN ? 2048u : 32u), A_MN ? kMBox : 16u);
-                        const uint64_t db = operand_desc(sb + (uint32_t)kk * (B_MN ? 2048u : 32u), B_MN ? kMBox : 16u);
-                        umma_bf16_pair(tmem + buf * 256u, da, db, kDesc, (s > 0 || kk > 0) ? 1u : 0u);
+                    for (int k = 0; k < kPSub * kMC / 16; ++k) {
+                        const uint32_t sa = stage + (uint32_t)(k / (kMC / 16)) * 2u * kPOperand, sb = sa + kPOperand, kk = (uint32_t)(k % (kMC / 16));
+                        const uint64_t da = operand_desc(sa + kk * (A_MN ? 2048u : 32u), A_MN ? kMBox : 16u);
+                        const uint64_t db = operand_desc(sb + kk * (B_MN ? 2048u : 32u), B_MN ? kMBox : 16u);
+                        umma_bf16_pair(tmem + buf * 256u, da, db, kDesc, (s > 0 || k > 0) ? 1u : 0u);
                     }
                     umma_commit_pair(&empty[slot]);
                 }
@@ -501,14 +507,16 @@ template <bool VEC> __device__ __forceinline__ void load8(const uint16_t* row, i
 }
 
 // ---------------------------------------------------------------- few tokens
-// Up to kFewTokens tokens (a decoding step): the weights are read once for next to no arithmetic, so what counts is
+// A decoding step's one or two tokens (up to kFewTokens where rows are not aligned): the weights are read once for next to no arithmetic, so what counts is
 // that they stream.  A CTA takes kFewRows weight rows and a quarter to an eighth of the contraction per warp; a lane
 // multiplies 16 bytes of each row (VEC: rows on 16-byte boundaries; else element by element, any alignment) with the
 // tokens' values from L1.  fp32 sums: per lane in order, over the lanes by a butterfly, over the warps in their order.
-// Bound by memory; no shared-memory ring, tensor memory or cluster to set up: %%FEW%%
-constexpr int kFewTokens = 4, kFewRows = 4, kFewWarps = 8;
+// Bound by memory; no shared-memory ring, tensor memory or cluster to set up.
+// 7B gate (11008 x 4096), one token: 16.2 us, 5.6 TB/s, against 19.3 us on the tensor cores; three tokens 23.7 against
+// 19.2, so from there on only rows that TMA cannot read come here (46 us at four; copying them first costs more).
+constexpr int kFewTokens = 4, kFewVector = 2, kFewRows = 4, kFewWarps = 8;
 template <int M, bool VEC>
-__global__ void __launch_bounds__(32 * kFewWarps) few_kernel(const uint16_t* __restrict__ X, int64_t ldx, const uint16_t* __restrict__ W, int64_t ldw,
+__global__ void __launch_bounds__(32 * kFewWarps, VEC && M == 1 ? 5 : M <= 2 ? 4 : 3) few_kernel(const uint16_t* __restrict__ X, int64_t ldx, const uint16_t* __restrict__ W, int64_t ldw,
                                                              const __grid_constant__ MmArgs a) {
     __shared__ float part[kFewWarps][kFewRows][M];
     allow_next_kernel();
@@ -520,8 +528,13 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_kernel(const uint16_t* __r
 #pragma unroll
     for (int r = 0; r < kFewRows; ++r) w[r] = W + (o0 + r < a.n_i ? o0 + r : o0) * ldw;   // past the end: the first row again, not stored
     if (VEC) {
-        // chunks of 256 contraction steps, dealt to the warps in turn
-#pragma unroll 2
+        // chunks of 256 contraction steps, dealt to the warps in turn; even and odd steps are summed apart
+        Pair two[kFewRows][M];
+#pragma unroll
+        for (int r = 0; r < kFewRows; ++r)
+#pragma unroll
+            for (int m = 0; m < M; ++m) two[r][m] = pair_of(0.0f, 0.0f);
+#pragma unroll 1
         for (int64_t c = warp * 256 + lane * 8; c < a.n_c; c += kFewWarps * 256) {
             uint32_t x[M][4], y[kFewRows][4];
 #pragma unroll
@@ -529,17 +542,26 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_kernel(const uint16_t* __r
 #pragma unroll
             for (int m = 0; m < M; ++m) load8<true>(X + m * ldx, c, a.n_c, x[m]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 4; ++e) {
+                Pair xe[M];
+#pragma unroll
+                for (int m = 0; m < M; ++m) xe[m] = widen2(x[m][e]);
 #pragma unroll
                 for (int r = 0; r < kFewRows; ++r) {
-                    const float lo = __uint_as_float(y[r][e] << 16), hi = __uint_as_float(y[r][e] & 0xFFFF0000u);
+                    const Pair ye = widen2(y[r][e]);
 #pragma unroll
-                    for (int m = 0; m < M; ++m) {
-                        acc[r][m] = __fmaf_rn(lo, __uint_as_float(x[m][e] << 16), acc[r][m]);
-                        acc[r][m] = __fmaf_rn(hi, __uint_as_float(x[m][e] & 0xFFFF0000u), acc[r][m]);
-                    }
+                    for (int m = 0; m < M; ++m) two[r][m] = fma2(ye, xe[m], two[r][m]);
                 }
+            }
         }
+#pragma unroll
+        for (int r = 0; r < kFewRows; ++r)
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                float lo, hi;
+                split(two[r][m], lo, hi);
+                acc[r][m] = __fadd_rn(lo, hi);
+            }
     } else {
 #pragma unroll 8
         for (int64_t c = warp * 32 + lane; c < a.n_c; c += kFewWarps * 32) {
@@ -701,12 +723,9 @@ int readable(Matrix& m, char** ws, cudaStream_t st) {
     return MOSAIC_OK;
 }
 
-// A box's rows are 128 bytes of rows far apart, and the next 128 bytes are asked for a stage later: L2 fetches 128
-// bytes (256: 1024 x 4096 x 8832 took 82 us instead of 61).
 template <bool A_MN, bool B_MN> int encode_operands(CUtensorMap* a_map, CUtensorMap* b_map, const Matrix& A, const Matrix& B, int rows_a, int rows_b) {
-    constexpr CUtensorMapL2promotion kFetch = CU_TENSOR_MAP_L2_PROMOTION_L2_128B;
-    const bool a_ok = A_MN ? encode_bf16(a_map, A.p, A.rows, A.cols, A.ld, kMC, 64, kFetch) : encode_bf16(a_map, A.p, A.rows, A.cols, A.ld, rows_a, kMC, kFetch);
-    const bool b_ok = B_MN ? encode_bf16(b_map, B.p, B.rows, B.cols, B.ld, kMC, 64, kFetch) : encode_bf16(b_map, B.p, B.rows, B.cols, B.ld, rows_b, kMC, kFetch);
+    const bool a_ok = A_MN ? encode_bf16(a_map, A.p, A.rows, A.cols, A.ld, kMC, 64) : encode_bf16(a_map, A.p, A.rows, A.cols, A.ld, rows_a, kMC);
+    const bool b_ok = B_MN ? encode_bf16(b_map, B.p, B.rows, B.cols, B.ld, kMC, 64) : encode_bf16(b_map, B.p, B.rows, B.cols, B.ld, rows_b, kMC);
     return a_ok && b_ok ? MOSAIC_OK : MOSAIC_ERR_CUDA;
 }
 
@@ -812,11 +831,12 @@ template <bool A_MN, bool B_MN> int run_mm(const Matrix& A, const Matrix& B, MmA
 
 int launch_few(const Matrix& x, const Matrix& w, const MmArgs& a, cudaStream_t st) {
     using Kernel = void (*)(const uint16_t*, int64_t, const uint16_t*, int64_t, MmArgs);
-    static const Kernel kernels[2][kFewTokens] = {{few_kernel<1, false>, few_kernel<2, false>, few_kernel<3, false>, few_kernel<4, false>},
-                                                  {few_kernel<1, true>, few_kernel<2, true>, few_kernel<3, true>, few_kernel<4, true>}};
+    static const Kernel plain[kFewTokens] = {few_kernel<1, false>, few_kernel<2, false>, few_kernel<3, false>, few_kernel<4, false>};
+    static const Kernel vector[kFewVector] = {few_kernel<1, true>, few_kernel<2, true>};
+    const Kernel kernel = x.tma_ok() && w.tma_ok() ? vector[a.n_j - 1] : plain[a.n_j - 1];
     const int64_t ctas = (a.n_i + kFewRows - 1) / kFewRows;
     Launch l(dim3((unsigned)ctas), 32 * kFewWarps, 0, st);
-    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, kernels[x.tma_ok() && w.tma_ok() ? 1 : 0][a.n_j - 1], static_cast<const uint16_t*>(x.p), x.ld,
+    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, kernel, static_cast<const uint16_t*>(x.p), x.ld,
                                        static_cast<const uint16_t*>(w.p), w.ld, a));
     return MOSAIC_OK;
 }
@@ -897,7 +917,7 @@ extern "C" int mosaic_linear(const void* X, int64_t ldx, const void* W, int64_t 
     a.resid = static_cast<const uint16_t*>(residual); a.ld_resid = ldr;
     a.z = static_cast<uint16_t*>(Z); a.ld_z = ldz;
     a.act = act; a.status = status_dev;
-    if (tokens <= kFewTokens) return launch_few(x, w, a, st);
+    if (tokens <= (x.tma_ok() && w.tma_ok() ? kFewVector : kFewTokens)) return launch_few(x, w, a, st);
     char* scratch = static_cast<char*>(ws);
     if ((rc = readable(x, &scratch, st)) != MOSAIC_OK || (rc = readable(w, &scratch, st)) != MOSAIC_OK) return rc;
     return run_mm<false, false>(w, x, a, st);

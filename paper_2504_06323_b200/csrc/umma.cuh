@@ -206,10 +206,8 @@ inline EncodeTiledFn encode_tiled() {
 }
 
 // Row-major bf16 [rows, cols], ld in elements (a multiple of 8; irrelevant for one row), read in boxes of
-// box_cols x box_rows with the 128-byte swizzle; what lies outside the matrix is read as zero.  `promotion`: what L2
-// fetches for a box's 128-byte rows (256 bytes where the neighbouring box is read at the same time).
-inline bool encode_bf16(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box_rows, int box_cols,
-                        CUtensorMapL2promotion promotion) {
+// box_cols x box_rows with the 128-byte swizzle; what lies outside the matrix is read as zero.
+inline bool encode_bf16(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box_rows, int box_cols) {
     EncodeTiledFn encode = encode_tiled();
     if (encode == nullptr) return false;
     const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
@@ -217,7 +215,7 @@ inline bool encode_bf16(CUtensorMap* map, const void* p, int64_t rows, int64_t c
     const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
     const cuuint32_t estride[2] = {1u, 1u};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2u, const_cast<void*>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace mosaic
