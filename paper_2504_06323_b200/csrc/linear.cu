@@ -30,7 +30,9 @@ constexpr uint32_t kMBox = 64 * 64 * 2;   // an MN-major box: 64 elements x 64 c
 
 struct MmArgs {
     int64_t n_i, n_j, n_c;             // extents
-    int tiles_i, tiles_j, stages;
+    int tiles_i, tiles_j, stages, split;
+    int first_pair;                    // >= 0: the tiles are quarters of the pair kernel's tiles from this one on
+    int pair_i, pair_j;                // its tiles
     uint16_t* out;
     int64_t ld_out;
     const uint16_t* bias;              // [n_i] or null
@@ -40,8 +42,6 @@ struct MmArgs {
     int64_t ld_z;
     int act;
     int pairs;                         // out, resid and z (those there are) take two elements a word: 4-byte bases, even ld
-    int first_pair;                    // >= 0: the tiles are quarters of the pair kernel's tiles from this one on
-    int pair_i, pair_j;                // its tiles
     int* status;
 };
 
@@ -112,8 +112,17 @@ template <int N> __device__ __forceinline__ void epilogue(const MmArgs& a, float
     if (a.resid != nullptr) {
         const uint16_t* p = a.resid + j * a.ld_resid + i;
 #pragma unroll
-        for (int e = 0; e < N; ++e, p += a.ld_resid)
-            if (e < n) v[e] = __fadd_rn(v[e], bf16_to_f32(*p));
+        for (int h = 0; h < N; h += N / 2) {   // half of them on their way before the first is used
+            uint16_t r[N / 2];
+#pragma unroll
+            for (int e = 0; e < N / 2; ++e) {
+                r[e] = 0;
+                if (h + e < n) asm volatile("ld.global.u16 %0, [%1];" : "=h"(r[e]) : "l"(p));   // volatile: not one by one with the additions
+                p += a.ld_resid;
+            }
+#pragma unroll
+            for (int e = 0; e < N / 2; ++e) v[h + e] = __fadd_rn(v[h + e], bf16_to_f32(r[e]));
+        }
     }
     uint16_t* p = a.out + j * a.ld_out + i;
 #pragma unroll
@@ -125,17 +134,29 @@ template <int N> __device__ __forceinline__ void tmem_load(uint32_t addr, float 
     else tmem_load32(addr, v);
 }
 __device__ __forceinline__ void pair_tile(int tile, int tiles_i, int tiles_j, int* ti, int* tj);
+// Four adjacent elements, or the first n of them.
+__device__ __forceinline__ void store4(uint16_t* p, const float (&y)[4], bool words, int64_t n) {
+    if (words) {
+        reinterpret_cast<uint32_t*>(p)[0] = pack2(y[0], y[1]);
+        reinterpret_cast<uint32_t*>(p)[1] = pack2(y[2], y[3]);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+            if (h < n) p[h] = f32_to_bf16(y[h]);
+    }
+}
 
 // One output tile of kMI x BN per cluster; its contraction is split over the cluster's CTAs, whose partial
 // tiles meet in shared memory and are added in the CTAs' order.
+constexpr int kMSub = 2;     // 64 contraction steps each a stage: eight instructions a barrier
 constexpr int kMRoles = 2;   // loader, MMA issue; then the epilogue: four warps (a quarter of tensor memory's lanes each), eight for wide tiles
-__host__ __device__ constexpr int mm_warps(int bn) { return bn >= 64 ? 8 : 4; }
+__host__ __device__ constexpr int mm_warps(int bn) { return bn >= 256 ? 16 : bn >= 64 ? 8 : 4; }
 __host__ __device__ constexpr int mm_threads(int bn) { return 32 * (kMRoles + mm_warps(bn)); }
 
 template <bool A_MN, bool B_MN, int BN>
 __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                                                        const __grid_constant__ MmArgs a) {
-    constexpr uint32_t kABytes = kMI * kMC * 2, kBBytes = BN * kMC * 2, kStage = kABytes + kBBytes;
+    constexpr uint32_t kABytes = kMI * kMC * 2, kBBytes = BN * kMC * 2, kHalf = kABytes + kBBytes, kStage = kMSub * kHalf;
     constexpr uint32_t kCols = BN < 32 ? 32 : BN;
     constexpr uint32_t kDesc = instr_desc(A_MN, B_MN, kMI, BN);
     extern __shared__ unsigned char mm_smem_raw[];
@@ -144,18 +165,17 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
     __shared__ int err_word;
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(mm_smem_raw) + 1023u) & ~(uintptr_t)1023u);
     volatile int* err = &err_word;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int split = a.split, rank = (int)(blockIdx.x % (unsigned)split);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int tile = (int)(blockIdx.x / (unsigned)split);
     int64_t i0 = (int64_t)(tile % a.tiles_i) * kMI, j0 = (int64_t)(tile / a.tiles_i) * BN;
-    if (BN == 128 && a.first_pair >= 0) {   // what is left over of the pair kernel's tiles, in quarters
+    if (BN == 128 && a.first_pair >= 0) {   // what is left over of the pair kernel's tiles
         int ti, tj;
         pair_tile(a.first_pair + tile / 4, a.pair_i, a.pair_j, &ti, &tj);
         i0 = (int64_t)ti * 256 + (tile & 1) * 128;
         j0 = (int64_t)tj * 256 + ((tile >> 1) & 1) * 128;
     }
-    const int64_t steps = (a.n_c + kMC - 1) / kMC;
+    const int64_t steps = (a.n_c + kMSub * kMC - 1) / (kMSub * kMC);
     const int s0 = (int)(steps * rank / split), s1 = (int)(steps * (rank + 1) / split);   // split <= steps: never empty
 
     if (threadIdx.x == 0) {
@@ -187,20 +207,24 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
             for (int s = s0; s < s1; ++s) {
                 const uint32_t it = (uint32_t)(s - s0), slot = it % (uint32_t)a.stages, ph = (it / (uint32_t)a.stages) & 1u;
                 if (!mbar_wait(&empty[slot], ph ^ 1u, err)) break;
-                unsigned char* sa = ring + (size_t)slot * kStage;
-                unsigned char* sb = sa + kABytes;
                 mbar_expect_tx(&full[slot], kStage);
-                if (A_MN) {
 #pragma unroll
-                    for (int b = 0; b < kMI / 64; ++b) tma_load_box(sa + (size_t)b * kMBox, &a_map, &full[slot], (int)i0 + b * 64, s * kMC);
-                } else {
-                    tma_load_box(sa, &a_map, &full[slot], s * kMC, (int)i0);
-                }
-                if (B_MN) {
+                for (int h = 0; h < kMSub; ++h) {
+                    unsigned char* sa = ring + (size_t)slot * kStage + (size_t)h * kHalf;
+                    unsigned char* sb = sa + kABytes;
+                    const int c = (s * kMSub + h) * kMC;
+                    if (A_MN) {
 #pragma unroll
-                    for (int b = 0; b < BN / 64; ++b) tma_load_box(sb + (size_t)b * kMBox, &b_map, &full[slot], (int)j0 + b * 64, s * kMC);
-                } else {
-                    tma_load_box(sb, &b_map, &full[slot], s * kMC, (int)j0);
+                        for (int b = 0; b < kMI / 64; ++b) tma_load_box(sa + (size_t)b * kMBox, &a_map, &full[slot], (int)i0 + b * 64, c);
+                    } else {
+                        tma_load_box(sa, &a_map, &full[slot], c, (int)i0);
+                    }
+                    if (B_MN) {
+#pragma unroll
+                        for (int b = 0; b < BN / 64; ++b) tma_load_box(sb + (size_t)b * kMBox, &b_map, &full[slot], (int)j0 + b * 64, c);
+                    } else {
+                        tma_load_box(sb, &b_map, &full[slot], c, (int)j0);
+                    }
                 }
                 issued = it + 1u;
             }
@@ -215,13 +239,14 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
                     break;
                 }
                 tc_fence_after();
-                const uint32_t sa = smem_u32(ring + (size_t)slot * kStage), sb = sa + kABytes;
+                const uint32_t stage = smem_u32(ring + (size_t)slot * kStage);
 #pragma unroll
-                for (int kk = 0; kk < kMC / 16; ++kk) {
+                for (int k = 0; k < kMSub * kMC / 16; ++k) {
                     // 16 contraction steps further: 16 swizzle rows (MN-major) or 32 bytes along one (K-major)
-                    const uint64_t da = operand_desc(sa + (uint32_t)kk * (A_MN ? 2048u : 32u), A_MN ? kMBox : 16u);
-                    const uint64_t db = operand_desc(sb + (uint32_t)kk * (B_MN ? 2048u : 32u), B_MN ? kMBox : 16u);
-                    umma_bf16(tmem, da, db, kDesc, (it > 0 || kk > 0) ? 1u : 0u);
+                    const uint32_t sa = stage + (uint32_t)(k / (kMC / 16)) * kHalf, sb = sa + kABytes, kk = (uint32_t)(k % (kMC / 16));
+                    const uint64_t da = operand_desc(sa + kk * (A_MN ? 2048u : 32u), A_MN ? kMBox : 16u);
+                    const uint64_t db = operand_desc(sb + kk * (B_MN ? 2048u : 32u), B_MN ? kMBox : 16u);
+                    umma_bf16(tmem, da, db, kDesc, (it > 0 || k > 0) ? 1u : 0u);
                 }
                 umma_commit(&empty[slot]);
             }
@@ -233,7 +258,14 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
     tc_fence_after();
     const int q = warp & 3;
     const int n_cols = (int)(a.n_j - j0 < BN ? (a.n_j > j0 ? a.n_j - j0 : 0) : BN);
-    float* part = reinterpret_cast<float*>(ring);   // [BN][kMI]: every load has been consumed once the accumulator is complete
+    const int per = (n_cols + split - 1) / split;   // columns of the tile that a CTA of the cluster adds up and writes
+    float* part = reinterpret_cast<float*>(ring);   // [split][per][kMI]: the cluster's partial sums of this CTA's columns
+    if (split > 1) {
+        // Every CTA's accumulator is complete, so its loads have been consumed, before its stages take partial sums.
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+    }
     if (done) {
         constexpr int kChunk = BN < 32 ? 16 : 32, kSets = mm_warps(BN) / 4;   // warps of a quarter take chunks in turn
         const int64_t i = i0 + q * 32 + lane;
@@ -243,8 +275,18 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
             float v[kChunk];
             tmem_load<kChunk>(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c0, v);
             if (split > 1) {
+                int owner = c0 / per, at = c0 - owner * per;
+                uint32_t to = cluster_addr(part + ((size_t)rank * per + at) * kMI + q * 32 + lane, owner);
 #pragma unroll
-                for (int e = 0; e < kChunk; ++e) part[(c0 + e) * kMI + q * 32 + lane] = v[e];
+                for (int e = 0; e < kChunk; ++e) {
+                    if (c0 + e < n_cols) store_remote(to, v[e]);
+                    to += kMI * 4;
+                    if (++at == per) {
+                        at = 0;
+                        ++owner;
+                        to = cluster_addr(part + (size_t)rank * per * kMI + q * 32 + lane, owner < split ? owner : 0);
+                    }
+                }
             } else {
                 epilogue<kChunk>(a, v, bias, i0 + q * 32, j0 + c0, n_cols - c0);
                 __syncwarp();
@@ -254,7 +296,7 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 1) {   // tensor memory goes back before the cluster's CTAs wait for one another
+    if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
     }
@@ -269,47 +311,64 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
         if (a.status != nullptr) atomicExch(a.status, 1);
     }
     if (split > 1) {
-        cluster.sync();
-        // four adjacent elements a thread and step
-        const int quads = n_cols * (kMI / 4), per = (quads + split - 1) / split;
-        const int e1 = (rank + 1) * per < quads ? (rank + 1) * per : quads;
-        for (int e = rank * per + (int)threadIdx.x; e < e1; e += mm_threads(BN)) {
-            float4 v[kMMaxSplit];
+        __syncwarp();
+        cluster_arrive();
+        // Four adjacent elements a thread and turn; the residual's are on their way while the partial sums come in.
+        constexpr int kTurns = 4;
+        const int mine = n_cols - rank * per < per ? n_cols - rank * per : per, quads = mine > 0 ? mine * (kMI / 4) : 0;
+        uint32_t r[kTurns][2];
+        const auto fetch = [&](int e0) {
 #pragma unroll
-            for (int p = 0; p < kMMaxSplit; ++p)
-                if (p < split) v[p] = *cluster.map_shared_rank(reinterpret_cast<float4*>(part) + e, p);
-            float sum[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
-#pragma unroll
-            for (int p = 1; p < kMMaxSplit; ++p) {
-                if (p < split) {
-                    sum[0] = __fadd_rn(sum[0], v[p].x);
-                    sum[1] = __fadd_rn(sum[1], v[p].y);
-                    sum[2] = __fadd_rn(sum[2], v[p].z);
-                    sum[3] = __fadd_rn(sum[3], v[p].w);
+            for (int u = 0; u < kTurns; ++u) {
+                const int e = e0 + u * mm_threads(BN);
+                const int64_t oi = i0 + 4 * (e % (kMI / 4)), oj = j0 + rank * per + e / (kMI / 4);
+                r[u][0] = r[u][1] = 0;
+                if (a.resid == nullptr || e >= quads || oi >= a.n_i) continue;
+                const uint16_t* p = a.resid + oj * a.ld_resid + oi;
+                if (a.pairs && oi + 4 <= a.n_i) {
+                    r[u][0] = reinterpret_cast<const uint32_t*>(p)[0];
+                    r[u][1] = reinterpret_cast<const uint32_t*>(p)[1];
+                } else {
+                    r[u][0] = p[0] | (oi + 1 < a.n_i ? (uint32_t)p[1] << 16 : 0u);
+                    r[u][1] = (oi + 2 < a.n_i ? (uint32_t)p[2] : 0u) | (oi + 3 < a.n_i ? (uint32_t)p[3] << 16 : 0u);
                 }
             }
-            const int64_t oi = i0 + 4 * (e % (kMI / 4)), oj = j0 + e / (kMI / 4);
-            float y[4];
+        };
+        fetch((int)threadIdx.x);
+        cluster_wait();
+        for (int e0 = (int)threadIdx.x; e0 < quads; e0 += kTurns * mm_threads(BN)) {
+            if (e0 != (int)threadIdx.x) fetch(e0);
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                y[h] = 0.0f;
-                if (oi + h >= a.n_i) continue;
-                float x = __fadd_rn(sum[h], a.bias != nullptr ? bf16_to_f32(a.bias[oi + h]) : 0.0f);
-                if (a.z != nullptr) a.z[oj * a.ld_z + oi + h] = f32_to_bf16(x);
-                x = activate(x, a.act);
-                y[h] = a.resid != nullptr ? __fadd_rn(x, bf16_to_f32(a.resid[oj * a.ld_resid + oi + h])) : x;
-            }
-            uint16_t* o = a.out + oj * a.ld_out + oi;
-            if (a.pairs && oi + 4 <= a.n_i) {
-                reinterpret_cast<uint32_t*>(o)[0] = pack2(y[0], y[1]);
-                reinterpret_cast<uint32_t*>(o)[1] = pack2(y[2], y[3]);
-            } else {
+            for (int u = 0; u < kTurns; ++u) {
+                const int e = e0 + u * mm_threads(BN);
+                if (e >= quads) break;
+                const float4* from = reinterpret_cast<const float4*>(part) + e;
+                const float4 first = *from;
+                float y[4] = {first.x, first.y, first.z, first.w};
+                for (int p = 1; p < split; ++p) {   // in the CTAs' order
+                    const float4 more = from[p * per * (kMI / 4)];
+                    y[0] = __fadd_rn(y[0], more.x);
+                    y[1] = __fadd_rn(y[1], more.y);
+                    y[2] = __fadd_rn(y[2], more.z);
+                    y[3] = __fadd_rn(y[3], more.w);
+                }
+                const int64_t oi = i0 + 4 * (e % (kMI / 4)), oj = j0 + rank * per + e / (kMI / 4);
+                const bool words = a.pairs && oi + 4 <= a.n_i;
+                if (a.bias != nullptr) {
 #pragma unroll
-                for (int h = 0; h < 4; ++h)
-                    if (oi + h < a.n_i) o[h] = f32_to_bf16(y[h]);
+                    for (int h = 0; h < 4; ++h)
+                        if (oi + h < a.n_i) y[h] = __fadd_rn(y[h], bf16_to_f32(a.bias[oi + h]));
+                }
+                if (a.z != nullptr) store4(a.z + oj * a.ld_z + oi, y, words, a.n_i - oi);
+                activate_all(y, a.act);
+                if (a.resid != nullptr) {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+                        y[h] = __fadd_rn(y[h], __uint_as_float((h & 1) ? r[u][h / 2] & 0xFFFF0000u : r[u][h / 2] << 16));
+                }
+                store4(a.out + oj * a.ld_out + oi, y, words, a.n_i - oi);
             }
         }
-        cluster.sync();   // nobody leaves while its partial tile is being read
     }
 }
 
@@ -662,9 +721,10 @@ __global__ void __launch_bounds__(kSumCols) column_sum_kernel(const float* __res
 }
 
 // ---------------------------------------------------------------- host side
-// Cycles: of a pair's 64 contraction steps of a 256 x 256 tile, of its tile beside them, of a launch; of a stage of a
-// 128 x 128 tile with two CTAs an SM (their operands come from L2: 32 KB for a quarter of a pair's work), of its launch.
-constexpr int64_t kPairStep = 520, kPairTile = 1500, kPairFixed = 7000, kSmallStep = 1230, kSmallFixed = 6000;
+// Nanoseconds, measured with the contractions' lengths from 16 to 138 steps: 64 contraction steps of a pair's 256 x 256,
+// of a CTA's 128 x 256, 128 x 128 and narrower tiles; an epilogue's column; a launch or a further wave; a shared contraction.
+constexpr int64_t kPairStep = 350, kPairFixed = 6900, kWideStep = 454, kMidStep = 294, kNarrowStep = 260, kTileColumn = 5, kFixed = 3600,
+                  kSplitFixed = 2000, kSplitColumn = 10, kSecondLaunch = 2000;
 
 struct Matrix {
     const void* p;
@@ -729,38 +789,59 @@ template <bool A_MN, bool B_MN> int encode_operands(CUtensorMap* a_map, CUtensor
     return a_ok && b_ok ? MOSAIC_OK : MOSAIC_ERR_CUDA;
 }
 
-// CTAs that share a tile's contraction: while SMs would stay idle and each keeps four stages.
-int split_of(int64_t tiles, int64_t steps) {
-    int split = 1;
-    while (split < kMMaxSplit && tiles * split * 2 <= 2 * sm_count() && steps >= 8 * split) split *= 2;
-    return split;
+template <int BN> constexpr size_t kMRing = 196 * 1024 / ((size_t)(kMI + BN) * kMC * 2 * kMSub) * ((size_t)(kMI + BN) * kMC * 2 * kMSub);   // one CTA an SM
+template <bool A_MN, bool B_MN, int BN> bool opt_in() {
+    static DeviceCache opted;
+    return opted.get([]() -> int {
+        if (cudaFuncSetAttribute(mm_kernel<A_MN, B_MN, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMRing<BN> + 1024) == cudaSuccess) return 1;
+        (void)cudaGetLastError();
+        return -1;
+    }) > 0;
+}
+
+// Clusters of `split` one-an-SM CTAs that run at a time: fewer than the SMs divided by split, as a cluster's SMs are of
+// one processing cluster (148 SMs hold 33 clusters of four and 15 of eight).
+int64_t resident_clusters(int split) {
+    if (split == 1) return sm_count();
+    static DeviceCache held[kMMaxSplit + 1];
+    return held[split].get([&]() -> int {
+        if (opt_in<false, false, 64>()) {
+            Launch l(dim3((unsigned)split), mm_threads(64), kMRing<64> + 1024, nullptr, split);
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, mm_kernel<false, false, 64>, &l.cfg) == cudaSuccess && n > 0) return n;
+            (void)cudaGetLastError();
+        }
+        const int n = sm_count() / split;
+        return n > 0 ? n : 1;
+    });
+}
+
+// What mm_kernel's tiles would take, and the CTAs that share one's contraction (each keeps two stages or more).
+struct MmPlan {
+    int64_t nanoseconds;
+    int split;
+};
+MmPlan plan_mm(int64_t tiles, int64_t steps, int64_t bn) {
+    MmPlan best = {0, 1};
+    const int64_t step = bn == 256 ? kWideStep : bn == 128 ? kMidStep : kNarrowStep;
+    for (int split = 1; split <= kMMaxSplit && (split == 1 || steps >= 4 * split); ++split) {
+        const int64_t held = resident_clusters(split), waves = (tiles + held - 1) / held;
+        const int64_t c = waves * ((steps + split - 1) / split * step + bn * kTileColumn + kFixed + (split > 1 ? kSplitFixed + bn * kSplitColumn : 0));
+        if (split == 1 || c < best.nanoseconds) best = {c, split};
+    }
+    return best;
 }
 
 template <bool A_MN, bool B_MN, int BN>
-int launch_mm(const Matrix& A, const Matrix& B, MmArgs a, int64_t quarters, cudaStream_t st) {
-    constexpr size_t kStage = (size_t)(kMI + BN) * kMC * 2;
+int launch_mm(const Matrix& A, const Matrix& B, MmArgs a, int64_t tiles, int split, cudaStream_t st) {
+    static_assert(kMRing<BN> >= (size_t)(BN + kMMaxSplit) * kMI * 4, "the partial sums lie where the stages were");
     CUtensorMap a_map, b_map;
-    if (encode_operands<A_MN, B_MN>(&a_map, &b_map, A, B, kMI, BN) != MOSAIC_OK) return MOSAIC_ERR_CUDA;
+    if (encode_operands<A_MN, B_MN>(&a_map, &b_map, A, B, kMI, BN) != MOSAIC_OK || !opt_in<A_MN, B_MN, BN>()) return MOSAIC_ERR_CUDA;
     a.tiles_i = (int)((a.n_i + kMI - 1) / kMI);
-    a.tiles_j = (int)((a.n_j + BN - 1) / BN);
-    const int64_t tiles = quarters > 0 ? quarters : (int64_t)a.tiles_i * a.tiles_j, steps = (a.n_c + kMC - 1) / kMC;
-    const int split = split_of(tiles, steps);
+    a.split = split;
+    a.stages = (int)(kMRing<BN> / ((size_t)(kMI + BN) * kMC * 2 * kMSub));
     if (tiles * split > 0x7FFFFFFF) return MOSAIC_ERR_INVALID_ARG;
-    // two CTAs an SM (100 KB of stages each): one's epilogue under the other's products
-    a.stages = (int)(100 * 1024 / kStage);
-    if (a.stages > 8) a.stages = 8;
-    size_t smem = a.stages * kStage;
-    if (split > 1 && smem < (size_t)BN * kMI * 4u) smem = (size_t)BN * kMI * 4u;
-    static DeviceCache opted;
-    const int ok = opted.get([&]() -> int {
-        if (cudaFuncSetAttribute(mm_kernel<A_MN, B_MN, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, 110 * 1024) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return -1;
-        }
-        return 1;
-    });
-    if (ok < 0) return MOSAIC_ERR_CUDA;
-    Launch l(dim3((unsigned)(tiles * split)), mm_threads(BN), smem + 1024, st, split);
+    Launch l(dim3((unsigned)(tiles * split)), mm_threads(BN), kMRing<BN> + 1024, st, split);
     MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, mm_kernel<A_MN, B_MN, BN>, a_map, b_map, a));
     return MOSAIC_OK;
 }
@@ -790,43 +871,41 @@ template <bool A_MN, bool B_MN> int run_mm(const Matrix& A, const Matrix& B, MmA
     const int64_t steps = (a.n_c + kMC - 1) / kMC, sms = sm_count();
     const auto even = [](const void* p, int64_t ld) { return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & 3u) == 0 && ld % 2 == 0); };
     a.pairs = even(a.out, a.ld_out) && even(a.resid, a.ld_resid) && even(a.z, a.ld_z) ? 1 : 0;
-    a.first_pair = -1;
     const int64_t pi = (a.n_i + kPTile - 1) / kPTile, pj = (a.n_j + kPTile - 1) / kPTile, large = pi * pj, pairs = sms / 2;
-    if (large > 0x3FFFFFFF) return MOSAIC_ERR_INVALID_ARG;
+    if (large > 0x0FFFFFFF) return MOSAIC_ERR_INVALID_ARG;
     a.pair_i = (int)pi;
     a.pair_j = (int)pj;
-    // Which kernel: in cycles of the tensor cores, what each would take (measured, see the figures at the top).
+    a.first_pair = -1;
+    // Which kernel and tile: what each would take.
     const int64_t ti = (a.n_i + kMI - 1) / kMI;
-    const int64_t small_tiles = ti * ((a.n_j + 127) / 128), small_split = split_of(small_tiles, steps);
-    const int64_t small_cost = (small_tiles * small_split + 2 * sms - 1) / (2 * sms) * ((steps + small_split - 1) / small_split) * kSmallStep + kSmallFixed;
-    const int64_t waves = large / pairs, rest = large % pairs;
-    const int64_t wave_cost = steps * kPairStep + kPairTile;
-    const int64_t pair_cost = (waves + (rest > 0 ? 1 : 0)) * wave_cost + kPairFixed;
-    if (a.n_j > 64 && pair_cost < small_cost) {
-        // a last wave of few tiles is cheaper cut up, its contraction shared
-        const int64_t rest_split = split_of(rest * 4, steps);
-        const int64_t rest_cost = (rest * 4 * rest_split + 2 * sms - 1) / (2 * sms) * ((steps + rest_split - 1) / rest_split) * kSmallStep + kSmallFixed;
-        const bool cut = waves > 0 && rest > 0 && rest_cost < wave_cost;
-        int rc = launch_pair<A_MN, B_MN>(A, B, a, cut ? waves * pairs : large, st);
+    MmPlan plan = {0, 1};
+    int64_t bn = 0;
+    for (int64_t w = B_MN ? 64 : 16; w <= 256; w *= 2) {
+        const MmPlan p = plan_mm(ti * ((a.n_j + w - 1) / w), steps, w);
+        if (bn == 0 || p.nanoseconds < plan.nanoseconds) {
+            plan = p;
+            bn = w;
+        }
+        if (w >= a.n_j) break;
+    }
+    // The pair kernel, and its last wave, if of few tiles, in quarters whose contraction is shared (14336 x 2048 outputs
+    // from 4096, 448 tiles for 74 pairs: 178 instead of 184 us).
+    const int64_t waves = large / pairs, rest = large % pairs, wave = steps * kPairStep;
+    const MmPlan quarters = plan_mm(rest * 4, steps, 128);
+    const bool cut = waves > 0 && rest > 0 && quarters.nanoseconds + kSecondLaunch < wave;
+    if (waves * wave + (cut ? quarters.nanoseconds + kSecondLaunch : rest > 0 ? wave : 0) + kPairFixed < plan.nanoseconds) {
+        const int rc = launch_pair<A_MN, B_MN>(A, B, a, cut ? waves * pairs : large, st);
         if (rc != MOSAIC_OK || !cut) return rc;
         a.first_pair = (int)(waves * pairs);
-        return launch_mm<A_MN, B_MN, 128>(A, B, a, rest * 4, st);
+        return launch_mm<A_MN, B_MN, 128>(A, B, a, rest * 4, quarters.split, st);
     }
-    // the widest tile that leaves few SMs idle
-    int64_t bn = 128;
-    const int64_t least = B_MN ? 64 : 16;
-    while (bn > least && bn / 2 >= a.n_j) bn /= 2;
-    while (bn > least) {
-        const int64_t tiles = ti * ((a.n_j + bn - 1) / bn);
-        if (tiles * split_of(tiles, steps) * 2 > sms) break;
-        bn /= 2;
-    }
+    const int64_t tiles = ti * ((a.n_j + bn - 1) / bn);
     if constexpr (!B_MN) {
-        if (bn == 16) return launch_mm<A_MN, B_MN, 16>(A, B, a, 0, st);
-        if (bn == 32) return launch_mm<A_MN, B_MN, 32>(A, B, a, 0, st);
+        if (bn == 16) return launch_mm<A_MN, B_MN, 16>(A, B, a, tiles, plan.split, st);
+        if (bn == 32) return launch_mm<A_MN, B_MN, 32>(A, B, a, tiles, plan.split, st);
     }
-    if (bn == 64) return launch_mm<A_MN, B_MN, 64>(A, B, a, 0, st);
-    return launch_mm<A_MN, B_MN, 128>(A, B, a, 0, st);
+    if (bn == 64) return launch_mm<A_MN, B_MN, 64>(A, B, a, tiles, plan.split, st);
+    return bn == 128 ? launch_mm<A_MN, B_MN, 128>(A, B, a, tiles, plan.split, st) : launch_mm<A_MN, B_MN, 256>(A, B, a, tiles, plan.split, st);
 }
 
 int launch_few(const Matrix& x, const Matrix& w, const MmArgs& a, cudaStream_t st) {
