@@ -24,7 +24,7 @@ GLOBAL_NORM, PER_CATEGORY_NORM = 0, 1
 WEIGHTED_MEAN = 2        # flag, or-ed into the mode
 REDISTRIBUTE = 4         # flag, or-ed into the mode: clamp and redistribute
 ROWS_GIVEN, COLS_GIVEN, RANK_ONLY, SCORES_ONLY, SCORES_ACCUM = 1, 2, 4, 8, 16
-OK, ERR_INFEASIBLE = 0, -9
+OK, ERR_INFEASIBLE, ERR_TIMEOUT = 0, -9, -10
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 _ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "silu": ACT_SILU}
 

@@ -22,7 +22,6 @@ from paper_2504_06323_b200 import api
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
 INF = float("inf")
-HELD = {torch.bfloat16: 32768, torch.float32: 16384}   # entries of a row one CTA keeps in registers
 
 
 def logits(rows, cols, dtype, seed, pitch=0, offset=0, kind="normal"):
