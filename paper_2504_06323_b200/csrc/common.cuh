@@ -171,6 +171,9 @@ __device__ __forceinline__ void load_vec(Raw8<DT>& r, const void* mat, int64_t r
 // here before it touches what that one reads or writes.  The other side allows it to start.
 __device__ __forceinline__ void await_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// The two halves of a barrier over the cluster's CTAs: what a thread wrote before it arrived, its peers see after they waited.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // Two fp32 values an instruction.
 struct Pair {

@@ -335,6 +335,7 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
             }
         };
         fetch((int)threadIdx.x);
+        __syncwarp();
         cluster_wait();
         for (int e0 = (int)threadIdx.x; e0 < quads; e0 += kTurns * mm_threads(BN)) {
             if (e0 != (int)threadIdx.x) fetch(e0);

@@ -42,10 +42,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
-// The two halves of a barrier over the cluster's CTAs.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 // 2^((x - ref) c) of both.  (x - ref) first, then the factor: near the maximum the difference is exact, so the
 // factor's rounding costs next to nothing there; folded into one multiply-add, ref * c would shift every term
 // alike, and overflow for logits near the type's ends.
@@ -129,11 +125,6 @@ template <int DT> struct RowPart {
     __device__ __forceinline__ int single() const {
         const int t = (int)threadIdx.x;
         return first_cta && t < head + tail ? (t < head ? t : cols - tail + (t - head)) : -1;
-    }
-    __device__ __forceinline__ bool owns(int col) const {
-        if (col < head || col >= cols - tail) return first_cta;
-        const int v = (col - head) / RV::kElems;
-        return v >= v_lo && v < v_hi;
     }
     __device__ __forceinline__ float at(int col) const { return RV::widen(row[col]); }
     __device__ __forceinline__ const Elem* vec(int v) const { return row + head + (int64_t)v * RV::kElems; }

@@ -11,7 +11,7 @@
 //                   (masked rows, many ties) or that has a NaN is selected digit by digit over all its entries.
 // The first is bound by memory.  The second is a chain of short dependent steps: small CTAs, so that many rows'
 // chains overlap; inside the sweep, three CTAs an SM, the same steps took as long again as the sweep itself (98 us for
-// 4096 x 32000 bf16 instead of %%TOP%%).
+// 4096 x 32000 bf16 instead of 83, of which the sweep is 57).
 #include <math.h>
 
 #include "rows.cuh"
@@ -19,7 +19,10 @@
 namespace mosaic {
 namespace {
 
-constexpr int kRankMost = 256;   // entries: up to here a list is ranked by counting, above it by a bitonic sort
+// Entries a list is ranked by counting up to, then by sorted runs of 32, above by a bitonic sort of the whole.  Counting
+// costs the list's square (342 entries, 512 threads: 12000 cycles, and 13000 sorted whole), a run's sort fifteen exchanges.
+__host__ __device__ constexpr uint32_t count_most(int n) { return n == 32 ? 256u : 128u; }
+constexpr uint32_t kRunsMost = 1024u;
 
 struct TopArgs {
     const void* L;
@@ -212,7 +215,7 @@ template <int N> __device__ __forceinline__ void pick_sync() {
 }
 // What they share.
 struct PickRow {
-    uint32_t votes[16];
+    uint32_t votes[2][16];   // of each warp
     uint32_t count;      // candidates found
     uint32_t kept;       // groups that hold some
     uint32_t floor;
@@ -230,7 +233,7 @@ template <int DT, int N> __device__ __forceinline__ void emit_list(const RowPart
         values[place] = key == 0x80000000u || key == 0xFFFFFFFFu ? part.at(j) : key_value(key);
         indices[place] = j;
     };
-    if (n <= kRankMost) {   // an entry's place is the number of larger ones, counted two at a time by `share` threads
+    if (n <= count_most(N)) {   // an entry's place is the number of larger ones, counted two at a time by `share` threads
         if (me == 0 && (n & 1u)) list[n] = 0ull;   // (room for n entries is room for an even number)
         pick_sync<N>();
         uint32_t share = 1u;
@@ -251,7 +254,39 @@ template <int DT, int N> __device__ __forceinline__ void emit_list(const RowPart
         }
         return;
     }
-    uint32_t size = kRankMost * 2;
+    if (N > 32 && n <= kRunsMost) {   // an entry's place is its place in its run and the larger ones of each other run
+        const uint32_t lane = threadIdx.x & 31u, runs = (n + 31u) / 32u;
+        for (uint32_t run = me >> 5; run < runs; run += N / 32) {
+            const uint32_t i = run * 32u + lane;
+            uint64_t x = i < n ? list[i] : 0ull;
+            for (uint32_t k = 2u; k <= 32u; k <<= 1) {
+                for (uint32_t d = k >> 1; d > 0u; d >>= 1) {
+                    const uint64_t y = __shfl_xor_sync(0xFFFFFFFFu, x, d);
+                    const bool larger = ((lane & d) == 0u) == ((lane & k) == 0u);   // the lane that keeps the larger of the two
+                    if (larger == (y > x)) x = y;
+                }
+            }
+            list[i] = x;
+        }
+        pick_sync<N>();
+        for (uint32_t i = me; i < n; i += N) {
+            const uint64_t mine = list[i];
+            uint32_t place = i & 31u;
+#pragma unroll 4
+            for (uint32_t run = 0; run < runs; ++run) {
+                const uint64_t* in = list + run * 32u;
+                uint32_t above = 0u;
+#pragma unroll
+                for (uint32_t s = 16u; s > 0u; s >>= 1) above += in[above + s - 1u] > mine ? s : 0u;
+                above += in[above] > mine ? 1u : 0u;
+                place += run == i >> 5 ? 0u : above;
+            }
+            if (place < (uint32_t)a.top) emit(place, mine);
+        }
+        return;
+    }
+    uint32_t size = 2048u;
+    if (N == 32) size = 512u;
     while (size < n) size *= 2u;
     for (uint32_t i = n + me; i < size; i += N) list[i] = 0ull;   // below every entry (a column's complement is not 0)
     pick_sync<N>();
@@ -277,7 +312,9 @@ template <int DT, int N> __global__ void __launch_bounds__(pick_threads(N)) pick
     using RV = RowVec<DT>;
     constexpr bool WARP = N == 32;
     constexpr int kPickThreads = pick_threads(N), kRows = kPickThreads / N;   // threads and rows of a CTA
-    constexpr int kInFlight = WARP ? 8 : 4;   // loads
+    // Loads in flight and steps unrolled, where a thread has that many: a CTA of 512 has one or two, and comes to its code for
+    // the first time, when every further line of it is a wait.
+    constexpr int kInFlight = WARP ? 8 : N == 128 ? 4 : 1, kAhead = N == 512 ? 1 : 4;
     __shared__ PickRow rows[kRows];
     __shared__ PickShared sh;
     extern __shared__ __align__(16) unsigned char dyn[];
@@ -289,7 +326,6 @@ template <int DT, int N> __global__ void __launch_bounds__(pick_threads(N)) pick
     PickRow& row = rows[slot];
     const int64_t r = (int64_t)blockIdx.x * kRows + slot;
     const bool there = r < a.rows;
-    if (me < 16) row.votes[me] = 0u;
     if (me == 0) {
         row.count = row.kept = 0u;
         row.all = 0;
@@ -335,19 +371,17 @@ template <int DT, int N> __global__ void __launch_bounds__(pick_threads(N)) pick
             int vote = 0;
             auto reach = [&](uint32_t trial) -> int {   // groups that do
                 uint32_t n = 0u;
-#pragma unroll 4
+#pragma unroll kAhead
                 for (int i = me; i < words; i += N) {
                     const uint32_t w = pairs[i];
                     n += ((w & 0xFFFFu) >= trial ? 1u : 0u) + ((w >> 16) >= trial ? 1u : 0u);
                 }
                 n = __reduce_add_sync(0xFFFFFFFFu, n);
                 if (!WARP) {
-                    uint32_t* v = &row.votes[vote];
-                    if (lane == 0) atomicAdd(v, n);
+                    vote ^= 1;   // two sets in turn: the one before last has been read by all
+                    if (lane == 0) row.votes[vote][threadIdx.x >> 5] = n;
                     __syncthreads();
-                    n = *v;
-                    if (threadIdx.x == 0) row.votes[(vote + 15) & 15] = 0u;   // the one before, read by all by now
-                    vote = (vote + 1) & 15;
+                    n = __reduce_add_sync(0xFFFFFFFFu, lane < N / 32 ? row.votes[vote][lane] : 0u);
                 }
                 return (int)n;
             };
@@ -453,12 +487,13 @@ void plan_top(TopArgs& a, int dtype) {
 }
 constexpr int64_t kMostVocab = 1 << 20;   // entries of a row: its patterns lie in the shared memory of one CTA
 constexpr int kMostGroups = 32768;        // 2^20 fp32 entries
+constexpr size_t kPickSmem = 4096 * 10 + kMostGroups * 2;
 
 template <int DT, int N> int launch_pick(const TopArgs& a, cudaStream_t st) {
     constexpr int kRows = pick_threads(N) / N;
     static DeviceCache opted;   // the shared-memory opt-in belongs to one device's copy of the kernel
     const int ok = opted.get([&]() -> int {
-        if (cudaFuncSetAttribute(pick_kernel<DT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4096 * 10 + kMostGroups * 2) != cudaSuccess) {
+        if (cudaFuncSetAttribute(pick_kernel<DT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPickSmem) != cudaSuccess) {
             (void)cudaGetLastError();
             return -1;
         }
@@ -469,6 +504,14 @@ template <int DT, int N> int launch_pick(const TopArgs& a, cudaStream_t st) {
     cfg.gridDim = dim3((unsigned)((a.rows + kRows - 1) / kRows));
     cfg.blockDim = dim3(pick_threads(N));
     cfg.dynamicSmemBytes = (size_t)kRows * ((size_t)a.list_cap * 10u + (size_t)a.groups * 2u);
+    // Where a CTA's row is all that an SM gets, it asks for the shared memory that spreads the rows evenly: four CTAs that
+    // start early on one SM while another has none took 28.0 instead of 25.5 us (301 x 50001 fp32).
+    const int64_t per_sm = (a.rows + sm_count() - 1) / sm_count();
+    if (N == 512 && per_sm <= 4) {
+        size_t even = 220 * 1024 / (size_t)per_sm - 3 * 1024;
+        if (even > kPickSmem) even = kPickSmem;
+        if (cfg.dynamicSmemBytes < even) cfg.dynamicSmemBytes = even;
+    }
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -482,12 +525,13 @@ template <int DT, int N> int launch_pick(const TopArgs& a, cudaStream_t st) {
 template <int DT> int launch_top(const TopArgs& a, cudaStream_t st) {
     sweep_kernel<DT><<<dim3((unsigned)a.rows, (unsigned)a.parts), kThreads, 0, st>>>(a);
     MOSAIC_LAUNCH_CHECK();
-    // A row a warp where there are rows enough to fill the SMs so (4096 x 32000 bf16, k 64: %%W%%); the fewer there are,
-    // the more threads make a row's steps short (301 x 50001 fp32, k 100: %%C%%).  A warp's row has a quarter of a
-    // CTA's shared memory, and sorting a long list is a CTA's work.
+    // A row a warp where there are rows enough to fill the SMs so (4096 x 32000 bf16, k 64: 83 us, by 128 threads 87, by
+    // 512 116); the fewer there are, the more threads make a row's steps short (1200 rows: 35 us by 128 threads, 48 by a
+    // warp, 40 by 512; 301 x 50001 fp32, k 100: 25.5 us by 512 threads, 36 by 128, 49 by a warp).  A warp's row has a
+    // quarter of a CTA's shared memory, and sorting a long list is a CTA's work (k 256: 159 us by 128 threads, 188).
     const bool small = 4u * ((size_t)a.list_cap * 10u + (size_t)a.groups * 2u) <= 64u * 1024u && a.top <= 128;
-    if (small && a.rows >= 8 * sm_count()) return launch_pick<DT, 32>(a, st);
-    return a.rows >= 4 * sm_count() ? launch_pick<DT, 128>(a, st) : launch_pick<DT, 512>(a, st);
+    if (small && a.rows >= 20 * sm_count()) return launch_pick<DT, 32>(a, st);
+    return a.rows > 5 * sm_count() ? launch_pick<DT, 128>(a, st) : launch_pick<DT, 512>(a, st);
 }
 
 }  // namespace
