@@ -128,12 +128,12 @@ template <int DT> struct RowPart {
     }
     __device__ __forceinline__ float at(int col) const { return RV::widen(row[col]); }
     __device__ __forceinline__ const Elem* vec(int v) const { return row + head + (int64_t)v * RV::kElems; }
-    // kBatch vectors from v on, a block's stride apart, all loads issued before the first is used; -inf where there is none.
-    __device__ __forceinline__ void load(int v, uint4 (&raw)[kBatch]) const {
+    // kBatch vectors from v on, a block's stride (T threads) apart, all loads issued before the first is used; -inf where there is none.
+    template <int T = kThreads> __device__ __forceinline__ void load(int v, uint4 (&raw)[kBatch]) const {
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             raw[i] = make_uint4(RV::kFill, RV::kFill, RV::kFill, RV::kFill);
-            if (v + i * kThreads < v_hi) raw[i] = ld_stream16(vec(v + i * kThreads));
+            if (v + i * T < v_hi) raw[i] = ld_stream16(vec(v + i * T));
         }
     }
 };

@@ -100,8 +100,11 @@ template <int DT> __device__ __forceinline__ float group_max(const uint4 (&raw)[
     return own;
 }
 
-template <int DT> __global__ void __launch_bounds__(kThreads, kRowCtas) sweep_kernel(const __grid_constant__ TopArgs a) {
-    __shared__ SoftStat warp_stat[kWarps];
+// Small CTAs, many an SM: while one waits for its loads the others compute (4096 x 32000 bf16 with the pick: 256 threads
+// and six CTAs 77 us, 512 and three 82, 512 and two 90, 256 and eight - 32 registers - 84).
+constexpr int kSweepThreads = 256, kSweepCtas = 6;
+template <int DT> __global__ void __launch_bounds__(kSweepThreads, kSweepCtas) sweep_kernel(const __grid_constant__ TopArgs a) {
+    __shared__ SoftStat warp_stat[kSweepThreads / 32];
     allow_next_kernel();
     const int64_t r = blockIdx.x;
     const int p = (int)blockIdx.y;
@@ -114,20 +117,20 @@ template <int DT> __global__ void __launch_bounds__(kThreads, kRowCtas) sweep_ke
     uint16_t* patterns = a.patterns + r * a.groups;
     SoftStat st = {-INFINITY, 0.0f};
     // whole warps stay together (their lanes share groups): up to the last vector of the part, rounded to the block
-    for (int v = part.v_lo + (int)threadIdx.x; v - (int)threadIdx.x < part.v_hi; v += kBatch * kThreads) {
+    for (int v = part.v_lo + (int)threadIdx.x; v - (int)threadIdx.x < part.v_hi; v += kBatch * kSweepThreads) {
         uint4 raw[kBatch];
-        part.load(v, raw);
+        part.template load<kSweepThreads>(v, raw);
         float m[kBatch];
         const float own = group_max<DT>(raw, wide, m);
         soft_batch<DT>(raw, own, a.c, st);
         if (wide) {   // lane i of a run writes the pattern of the run's vectors of batch i
-            const int i = lane & 3, u = v - (lane & 7) + i * kThreads;
+            const int i = lane & 3, u = v - (lane & 7) + i * kSweepThreads;
             const float mi = (i & 2) ? ((i & 1) ? m[3] : m[2]) : ((i & 1) ? m[1] : m[0]);
             if ((lane & 7) < kBatch && u < part.v_hi) patterns[u >> 3] = (uint16_t)(order_key(mi) >> 16);
         } else {
 #pragma unroll
             for (int i = 0; i < kBatch; ++i)
-                if (v + i * kThreads < part.v_hi) patterns[v + i * kThreads] = (uint16_t)(order_key(m[i]) >> 16);
+                if (v + i * kSweepThreads < part.v_hi) patterns[v + i * kSweepThreads] = (uint16_t)(order_key(m[i]) >> 16);
         }
     }
     const int lone = part.single();
@@ -136,7 +139,7 @@ template <int DT> __global__ void __launch_bounds__(kThreads, kRowCtas) sweep_ke
     if (lane == 0) warp_stat[threadIdx.x >> 5] = st;
     __syncthreads();
     if (threadIdx.x >= 32) return;
-    st = soft_all(warp_stat, kWarps, a.c);
+    st = soft_all(warp_stat, kSweepThreads / 32, a.c);
     if (threadIdx.x == 0) a.stat[r * a.parts + p] = make_float2(st.m, st.s);
 }
 
@@ -481,7 +484,7 @@ void plan_top(TopArgs& a, int dtype) {
     a.list_cap = 512;
     while (a.list_cap < 3 * a.top && a.list_cap < 4096) a.list_cap *= 2;
     int64_t per = 4096;   // 64 KB; less where the rows alone would leave SMs idle
-    while (per > kThreads && a.rows * ((nv + per - 1) / per) < sm_count() * kRowCtas) per /= 2;
+    while (per > kSweepThreads && a.rows * ((nv + per - 1) / per) < sm_count() * kSweepCtas) per /= 2;
     a.part_vecs = (int)per;
     a.parts = nv > 0 ? (int)((nv + per - 1) / per) : 1;
 }
@@ -523,7 +526,7 @@ template <int DT, int N> int launch_pick(const TopArgs& a, cudaStream_t st) {
 }
 
 template <int DT> int launch_top(const TopArgs& a, cudaStream_t st) {
-    sweep_kernel<DT><<<dim3((unsigned)a.rows, (unsigned)a.parts), kThreads, 0, st>>>(a);
+    sweep_kernel<DT><<<dim3((unsigned)a.rows, (unsigned)a.parts), kSweepThreads, 0, st>>>(a);
     MOSAIC_LAUNCH_CHECK();
     // A row a warp where there are rows enough to fill the SMs so (4096 x 32000 bf16, k 64: 83 us, by 128 threads 87, by
     // 512 116); the fewer there are, the more threads make a row's steps short (1200 rows: 35 us by 128 threads, 48 by a
