@@ -10,6 +10,7 @@ of a function here fails loudly.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -207,11 +208,11 @@ class Workspace:
         self.buf = None
 
     def get(self, nbytes: int) -> tuple[int, int]:
-        nbytes = max(int(nbytes), 256)
-        if self.buf is None or self.buf.numel() < nbytes:
-            self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        assert self.buf.data_ptr() % 256 == 0
-        return self.buf.data_ptr(), self.buf.numel()
+        buf = self.buf
+        if buf is None or buf.numel() < nbytes:
+            buf = self.buf = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
+            assert buf.data_ptr() % 256 == 0
+        return buf.data_ptr(), buf.numel()
 
 
 _default_ws: dict[int, Workspace] = {}
@@ -220,7 +221,7 @@ _default_ws: dict[int, Workspace] = {}
 def _ws(ws: Workspace | None, device) -> Workspace:
     if ws is not None:
         return ws
-    idx = torch.device(device).index
+    idx = device if isinstance(device, int) else torch.device(device).index
     idx = torch.cuda.current_device() if idx is None else idx
     if idx not in _default_ws:
         _default_ws[idx] = Workspace(torch.device("cuda", idx))
@@ -750,6 +751,12 @@ def _run_on(t: torch.Tensor, stream):
     return device, (torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream) or None
 
 
+@functools.lru_cache(maxsize=1024)
+def _scratch(query: str, device: int, *sizes) -> int:
+    """A workspace query whose answer depends on sizes (and the device) alone."""
+    return getattr(lib(), query)(*sizes)
+
+
 def _logits_code(t, name: str) -> int:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor (no CPU path exists)")
@@ -779,7 +786,7 @@ def mosaic_linear(X, W, Y, bias=None, residual=None, act=ACT_NONE, Z=None, statu
     if (xp | wp) & 15 or (ldx | ldw) & 7:      # an operand that is not 16-byte aligned is copied first
         need = L.mosaic_linear_workspace_bytes(xp, ldx, wp, ldw, tokens, n_out, n_in)
         if need:
-            sc, sn = _ws(ws, X.device).get(need)
+            sc, sn = _ws(ws, dev).get(need)
     _check(L.mosaic_linear(xp, ldx, wp, ldw, tokens, n_out, n_in, BF16, bp, rp, ldr, _act_code(act), yp, ldy, zp, ldz, sp, sc, sn, st),
            "mosaic_linear")
 
@@ -809,7 +816,7 @@ def mosaic_linear_backward(dY, X, W, Z=None, act=ACT_NONE, dX=None, dW=None, dbi
     L = lib()
     need = L.mosaic_linear_backward_workspace_bytes(dyp, lddy, xp, ldx, wp, ldw, tokens, n_out, n_in, act, dxp is not None, dwp is not None,
                                                     dbp is not None)
-    sc, sn = _ws(ws, dY.device).get(need) if need else (None, 0)
+    sc, sn = _ws(ws, dev).get(need) if need else (None, 0)
     _check(L.mosaic_linear_backward(dyp, lddy, xp, ldx, wp, ldw, zp, ldz, tokens, n_out, n_in, BF16, act, dxp, lddx, dwp, lddw, dbp, sp, sc, sn, st),
            "mosaic_linear_backward")
 
@@ -825,9 +832,8 @@ def mosaic_top_logits(L, values, indices, lse=None, temperature: float = 1.0, ws
     vp = _dense(values, "values", torch.float32, dev, rows, top)
     ip = _dense(indices, "indices", torch.int32, dev, rows, top)
     sp = _dense_or_none(lse, "lse", torch.float32, dev, rows)
-    lb = lib()
-    wp, wn = _ws(ws, L.device).get(lb.mosaic_top_logits_workspace_bytes(rows, vocab, code, top))
-    _check(lb.mosaic_top_logits(lp, rows, vocab, ldl, code, top, temperature, vp, ip, sp, wp, wn, st), "mosaic_top_logits")
+    wp, wn = _ws(ws, dev).get(_scratch("mosaic_top_logits_workspace_bytes", dev, rows, vocab, code, top))
+    _check(lib().mosaic_top_logits(lp, rows, vocab, ldl, code, top, temperature, vp, ip, sp, wp, wn, st), "mosaic_top_logits")
 
 
 def _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature, stream, ws):
@@ -840,7 +846,7 @@ def _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature, stream
     ti = _dense(t_indices, "t_indices", torch.int32, dev, rows, top)
     tl = _dense_or_none(t_lse, "t_lse", torch.float32, dev, rows)
     rw = _dense_or_none(row_weight, "row_weight", torch.float32, dev, rows)
-    wp, wn = _ws(ws, S.device).get(lib().mosaic_distill_workspace_bytes(rows, top))
+    wp, wn = _ws(ws, dev).get(_scratch("mosaic_distill_workspace_bytes", dev, rows, top))
     return (sp, rows, vocab, lds, code, tv, ti, top, tl, rw, temperature), (rows, vocab, dev), wp, wn, st
 
 
