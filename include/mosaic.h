@@ -506,6 +506,7 @@ int mosaic_linear_backward(const void *dY, int64_t lddy, const void *X, int64_t 
  *   values    device, [rows, top] fp32, dense: the logits themselves
  *   indices   device, [rows, top] int32, dense
  *   lse       device, [rows] fp32, or NULL
+ *   temperature  a normal positive float (here and below), else MOSAIC_ERR_INVALID_ARG
  *   ws        device scratch, >= the query for the same sizes
  * -0 and +0 are equal; a NaN orders above +inf (its row's lse is NaN).  Entries of
  * -inf are masked: they come last, lowest index first.  A row of -inf has lse -inf.
