@@ -333,6 +333,7 @@ template <int DT, int N> __global__ void __launch_bounds__(pick_threads(N)) pick
         row.count = row.kept = 0u;
         row.all = 0;
     }
+    pick_sync<N>();   // before another warp finds a NaN
     await_previous_kernel();
     if (there) {
         const RowPart<DT> part(a.L, r, a.ldl, (int)a.vocab, 0, 1);
