@@ -146,8 +146,12 @@ __device__ __forceinline__ void store4(uint16_t* p, const float (&y)[4], bool wo
     }
 }
 
-// One output tile of kMI x BN per cluster; its contraction is split over the cluster's CTAs, whose partial
-// tiles meet in shared memory and are added in the CTAs' order.
+// One output tile of kMI x BN per cluster; its contraction is split over the cluster's CTAs.  Each of them adds up and writes
+// an equal share of the tile's columns: the others push their partial sums of it into its shared memory (the stages, free
+// by then), and it adds them in the CTAs' order.  Bound by the loads of a tile's operands into one SM (about 110 GB/s an
+// SM for wide tiles) or, with few tokens, by the weights' stream: 37 tokens, 4096 outputs from 8807, 18.0 us against
+// 11.2 of the weights alone; 512 tokens, 4096 from 4096, 23 us.  One CTA an SM (its stages fill shared memory), so a CTA
+// never waits for tensor memory that another one of this kernel holds.
 constexpr int kMSub = 2;     // 64 contraction steps each a stage: eight instructions a barrier
 constexpr int kMRoles = 2;   // loader, MMA issue; then the epilogue: four warps (a quarter of tensor memory's lanes each), eight for wide tiles
 __host__ __device__ constexpr int mm_warps(int bn) { return bn >= 256 ? 16 : bn >= 64 ? 8 : 4; }
@@ -378,7 +382,8 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
 // of both operands in shared memory (64 KB a stage for 256 x 256 x 128 products: half of what a CTA alone would have
 // to load for the same work) and 128 x 256 of the accumulator in its tensor memory, twice: the epilogue of a tile
 // runs under the products of the next.  Persistent: a pair takes tile after tile.  The tiles go band by band
-// (kPBand tiles of output rows), so that the tiles in flight share operands in L2.
+// (kPBand tiles of output rows), so that the tiles in flight share operands in L2.  Bound by the tensor pipe, 76 % busy at
+// 14336 outputs from 4096 and 2048 tokens with bias, silu and Z (179 us, of which 147 are the flop at the measured peak).
 constexpr int kPTile = 256, kPHalf = 128;
 constexpr int kPSub = 2;   // 64 contraction steps each: eight instructions a barrier (with four, 1377 instead of 1505 Tflop/s at 4096 x 13824 x 5120)
 constexpr int kPStages = 3;
@@ -567,12 +572,12 @@ template <bool VEC> __device__ __forceinline__ void load8(const uint16_t* row, i
 }
 
 // ---------------------------------------------------------------- few tokens
-// A decoding step's one or two tokens (up to kFewTokens where rows are not aligned): the weights are read once for next to no arithmetic, so what counts is
-// that they stream.  A CTA takes kFewRows weight rows and a quarter to an eighth of the contraction per warp; a lane
+// A decoding step's one or two tokens (up to kFewTokens where rows are not aligned): the weights are read once for next
+// to no arithmetic, so what counts is that they stream.  A CTA takes kFewRows weight rows and a quarter to an eighth of the contraction per warp; a lane
 // multiplies 16 bytes of each row (VEC: rows on 16-byte boundaries; else element by element, any alignment) with the
 // tokens' values from L1.  fp32 sums: per lane in order, over the lanes by a butterfly, over the warps in their order.
 // Bound by memory; no shared-memory ring, tensor memory or cluster to set up.
-// 7B gate (11008 x 4096), one token: 16.2 us, 5.6 TB/s, against 19.3 us on the tensor cores; three tokens 23.7 against
+// 11008 outputs from 4096, one token: 16.3 us, 5.5 TB/s, against 19.3 us on the tensor cores; three tokens 23.7 against
 // 19.2, so from there on only rows that TMA cannot read come here (46 us at four; copying them first costs more).
 constexpr int kFewTokens = 4, kFewVector = 2, kFewRows = 4, kFewWarps = 8;
 template <int M, bool VEC>
