@@ -11,7 +11,7 @@
 //                   (masked rows, many ties) or that has a NaN is selected digit by digit over all its entries.
 // The first is bound by memory.  The second is a chain of short dependent steps: small CTAs, so that many rows'
 // chains overlap; inside the sweep, three CTAs an SM, the same steps took as long again as the sweep itself (98 us for
-// 4096 x 32000 bf16 instead of 83, of which the sweep is 57).
+// 4096 x 32000 bf16 instead of 77, of which the sweep is 50 at DRAM 64 % busy and an instruction in 73 % of the cycles).
 #include <math.h>
 
 #include "rows.cuh"
@@ -529,10 +529,10 @@ template <int DT, int N> int launch_pick(const TopArgs& a, cudaStream_t st) {
 template <int DT> int launch_top(const TopArgs& a, cudaStream_t st) {
     sweep_kernel<DT><<<dim3((unsigned)a.rows, (unsigned)a.parts), kSweepThreads, 0, st>>>(a);
     MOSAIC_LAUNCH_CHECK();
-    // A row a warp where there are rows enough to fill the SMs so (4096 x 32000 bf16, k 64: 83 us, by 128 threads 87, by
-    // 512 116); the fewer there are, the more threads make a row's steps short (1200 rows: 35 us by 128 threads, 48 by a
-    // warp, 40 by 512; 301 x 50001 fp32, k 100: 25.5 us by 512 threads, 36 by 128, 49 by a warp).  A warp's row has a
-    // quarter of a CTA's shared memory, and sorting a long list is a CTA's work (k 256: 159 us by 128 threads, 188).
+    // A row a warp where there are rows enough to fill the SMs so (4096 x 32000 bf16, k 64: 78 us, by 128 threads 82, by
+    // 512 110); the fewer there are, the more threads make a row's steps short (1200 rows: 35 us by 128 threads, 47 by a
+    // warp, 39 by 512; 301 x 50001 fp32, k 100: 25.5 us by 512 threads, 36 by 128, 51 by a warp).  A warp's row has a
+    // quarter of a CTA's shared memory, and sorting a long list is a CTA's work (k 256: 153 us by 128 threads, 182).
     const bool small = 4u * ((size_t)a.list_cap * 10u + (size_t)a.groups * 2u) <= 64u * 1024u && a.top <= 128;
     if (small && a.rows >= 20 * sm_count()) return launch_pick<DT, 32>(a, st);
     return a.rows > 5 * sm_count() ? launch_pick<DT, 128>(a, st) : launch_pick<DT, 512>(a, st);
