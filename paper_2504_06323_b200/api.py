@@ -688,6 +688,9 @@ def mosaic_compact_batch(jobs, stream=None) -> None:
 
 
 # ------------------------------------------------------------------ recovery of a pruned model
+_Tensor, _device, _raw_stream = torch.Tensor, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
 # These calls are made many times per token or training step, so their marshalling is kept short: one helper per
 # kind of argument, the raw stream handle, the workspace query only where the answer is not zero by inspection.
 def _act_code(act) -> int:
@@ -699,20 +702,26 @@ def _act_code(act) -> int:
     return int(act)
 
 
-def _matrix(t, name: str, dtype, device: int = -1):
-    """(pointer, rows, columns, leading dimension) of a row-major matrix; on `device`, if one is given."""
+def _refuse(t, name: str, dtype, device: int, ndim: int | None):
+    """The error of an argument that is no tensor of this type, number of dimensions (None: any) and device (-1: any)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor (no CPU path exists)")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2:
-        raise ValueError(f"{name} must have 2 dims")
+    if ndim is not None and t.dim() != ndim:
+        raise ValueError(f"{name} must have {ndim} dims")
+    if device >= 0 and t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}: the tensors of one call live on one device")
+
+
+def _matrix(t, name: str, dtype, device: int = -1):
+    """(pointer, rows, columns, leading dimension) of a row-major matrix; on `device`, if one is given."""
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.dim() != 2 or (t.get_device() != device if device >= 0 else not t.is_cuda):
+        _refuse(t, name, dtype, device, 2)
     rows, cols = t.shape
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"{name} must be row-major (unit stride along columns)")
-    if device >= 0 and t.get_device() != device:
-        raise ValueError(f"{name} is on {t.device}: the tensors of one call live on one device")
     return t.data_ptr(), rows, cols, (ld if rows > 1 else max(ld, cols))
 
 
@@ -728,14 +737,10 @@ def _like(t, name: str, dtype, device: int, rows: int, cols: int):
 
 def _dense(t, name: str, dtype, device: int, *shape):
     """Pointer of a contiguous tensor of this shape."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor (no CPU path exists)")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.get_device() != device:
+        _refuse(t, name, dtype, device, None)
     if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous {list(shape)}, got {list(t.shape)}")
-    if t.get_device() != device:
-        raise ValueError(f"{name} is on {t.device}: the tensors of one call live on one device")
     return t.data_ptr()
 
 
@@ -746,9 +751,9 @@ def _dense_or_none(t, name: str, dtype, device: int, *shape):
 def _run_on(t: torch.Tensor, stream):
     """(device index, raw stream) of a call: its tensors' device must be the current one, where it launches."""
     device = t.get_device()
-    if device != torch._C._cuda_getDevice():
-        raise ValueError(f"the call's tensors are on cuda:{device}, the current device is cuda:{torch._C._cuda_getDevice()}")
-    return device, (torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream) or None
+    if device != _device():
+        raise ValueError(f"the call's tensors are on cuda:{device}, the current device is cuda:{_device()}")
+    return device, (_raw_stream(device) if stream is None else stream.cuda_stream) or None
 
 
 @functools.lru_cache(maxsize=1024)
