@@ -19,6 +19,8 @@
  *   - The library allocates no memory and owns none: outputs and workspaces
  *     are the caller's.  A workspace must be 256-byte aligned and at least
  *     the matching *_workspace_bytes() query; its contents are scratch.
+ *     Calls that may run at the same time (two streams, or two host threads
+ *     issuing to one) need a workspace each.
  *   - Device calls only enqueue work on `stream` (a cudaStream_t passed as
  *     void*, NULL = default stream) and never synchronise.  Results are
  *     deterministic: the same inputs give the same bytes, run to run.

@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+from threading import get_ident as _thread
 
 import numpy as np
 import torch
@@ -201,18 +202,33 @@ def _stream(stream) -> int | None:
 
 
 class Workspace:
-    """A caller-owned, growable scratch buffer (the library itself allocates nothing)."""
+    """Growable scratch (the library itself allocates nothing): a buffer of its own for every stream that calls are issued
+    to and every host thread that issues them.  What two streams run at once, or two threads interleave on one, must not
+    meet in one buffer; within a thread a stream's calls run one after another, and their scratch may be the same.
+    A buffer belongs to its stream in the allocator's books as well: one that was replaced by a larger one is handed on
+    only behind the work that still uses it."""
 
     def __init__(self, device="cuda"):
         self.device = torch.device(device)
-        self.buf = None
+        self._bufs: dict[tuple, torch.Tensor] = {}     # (raw stream, thread) -> buffer
 
-    def get(self, nbytes: int) -> tuple[int, int]:
-        buf = self.buf
+    def get(self, nbytes: int, stream: int | None = None) -> tuple[int, int]:
+        """(pointer, size) of at least `nbytes` for calls on `stream`: a raw handle (0: the default stream), None the current one."""
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device).cuda_stream
+        key = (stream, _thread())
+        buf = self._bufs.get(key)
         if buf is None or buf.numel() < nbytes:
-            buf = self.buf = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
-            assert buf.data_ptr() % 256 == 0
+            buf = self._bufs[key] = self._new(max(int(nbytes), 256), stream)
+            assert buf.data_ptr() % 256 == 0 or not buf.is_cuda
         return buf.data_ptr(), buf.numel()
+
+    def _new(self, nbytes: int, stream: int) -> torch.Tensor:
+        if self.device.type != "cuda":
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        on = torch.cuda.ExternalStream(stream, self.device) if stream else torch.cuda.default_stream(self.device)
+        with torch.cuda.stream(on):
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
 
 _default_ws: dict[int, Workspace] = {}
@@ -223,9 +239,8 @@ def _ws(ws: Workspace | None, device) -> Workspace:
         return ws
     idx = device if isinstance(device, int) else torch.device(device).index
     idx = torch.cuda.current_device() if idx is None else idx
-    if idx not in _default_ws:
-        _default_ws[idx] = Workspace(torch.device("cuda", idx))
-    return _default_ws[idx]
+    found = _default_ws.get(idx)
+    return found if found is not None else _default_ws.setdefault(idx, Workspace(torch.device("cuda", idx)))
 
 
 # --------------------------------------------------------------------------- calls
@@ -243,9 +258,10 @@ def mosaic_act_norms(X: torch.Tensor, sumsq_accum: torch.Tensor, norms_out: torc
     if norms_out is not None:
         _dev(norms_out, "norms_out", torch.float32)
     L = lib()
-    wp, wn = _ws(ws, X.device).get(L.mosaic_act_norms_workspace_bytes(tokens, cols))
+    st = _stream(stream)
+    wp, wn = _ws(ws, X.device).get(L.mosaic_act_norms_workspace_bytes(tokens, cols), st or 0)
     _check(L.mosaic_act_norms(xp, tokens, cols, ldx, _dtype_code(X), sumsq_accum.data_ptr(), _ptr(norms_out),
-                              int(flags), wp, wn, _stream(stream)), "mosaic_act_norms")
+                              int(flags), wp, wn, st), "mosaic_act_norms")
 
 
 def mosaic_gram_accumulate(X: torch.Tensor, G: torch.Tensor, flags: int = 0, status: torch.Tensor | None = None,
@@ -294,9 +310,10 @@ def mosaic_outlier_ratio(W: torch.Tensor, norms: torch.Tensor, alpha: float, out
     if norms.numel() != cols:
         raise ValueError("norms must be [cols]")
     L = lib()
-    wp, wn = _ws(ws, W.device).get(L.mosaic_outlier_ratio_workspace_bytes(rows, cols))
+    st = _stream(stream)
+    wp, wn = _ws(ws, W.device).get(L.mosaic_outlier_ratio_workspace_bytes(rows, cols), st or 0)
     _check(L.mosaic_outlier_ratio(p, rows, cols, ldw, _dtype_code(W), norms.data_ptr(), float(alpha),
-                                  outlier_count_out.data_ptr(), _ptr(score_sum_out), wp, wn, _stream(stream)),
+                                  outlier_count_out.data_ptr(), _ptr(score_sum_out), wp, wn, st),
            "mosaic_outlier_ratio")
 
 
@@ -354,16 +371,17 @@ class OutlierBatch:
     def run(self, alpha: float, ws: Workspace | None = None, stream=None, group_of=None) -> None:
         """group_of: None (every matrix against its own mean, Eq. 6) or one group id per job - adjacent jobs
         with equal ids are counted against the mean over the whole group (Eq. 3-4, layer outlier distribution)."""
-        wp, wn = _ws(ws, self.device).get(self.ws_bytes)
+        st = _stream(stream)
+        wp, wn = _ws(ws, self.device).get(self.ws_bytes, st or 0)
         if group_of is None:
             _check(lib().mosaic_outlier_ratio_batch(C.addressof(self.arr), len(self.jobs), self.code, float(alpha), wp, wn,
-                                                    _stream(stream)), "mosaic_outlier_ratio_batch")
+                                                    st), "mosaic_outlier_ratio_batch")
             return
         if len(group_of) != len(self.jobs):
             raise ValueError("one group id per job")
         g = (C.c_int32 * len(self.jobs))(*[int(v) for v in group_of])
         _check(lib().mosaic_outlier_ratio_grouped(C.addressof(self.arr), C.addressof(g), len(self.jobs), self.code, float(alpha),
-                                                  wp, wn, _stream(stream)), "mosaic_outlier_ratio_grouped")
+                                                  wp, wn, st), "mosaic_outlier_ratio_grouped")
 
 
 def mosaic_outlier_ratio_batch(jobs, alpha: float, ws: Workspace | None = None, stream=None) -> None:
@@ -471,8 +489,9 @@ class PruneBatch:
             # (the k fields of all jobs in one strided write: a job is 8 words, k the seventh)
             np.frombuffer(self.arr, dtype=np.int64).reshape(len(self.jobs), 8)[:, 6] = np.asarray(k, dtype=np.int64)
             self.ws_bytes = lib().mosaic_prune_unstructured_batch_workspace_bytes(C.addressof(self.arr), len(self.jobs), self.code)
-        wp, wn = _ws(ws, self.device).get(self.ws_bytes)
-        _check(lib().mosaic_prune_unstructured_batch(C.addressof(self.arr), len(self.jobs), self.code, wp, wn, _stream(stream)),
+        st = _stream(stream)
+        wp, wn = _ws(ws, self.device).get(self.ws_bytes, st or 0)
+        _check(lib().mosaic_prune_unstructured_batch(C.addressof(self.arr), len(self.jobs), self.code, wp, wn, st),
                "mosaic_prune_unstructured_batch")
 
 
@@ -505,11 +524,12 @@ def mosaic_prune_structured_compact(W_in: torch.Tensor, norms: torch.Tensor | No
         if unit_scores_out.numel() < rows // row_group + cols // col_group:
             raise ValueError("unit_scores_out too short")
     L = lib()
-    wp, wn = _ws(ws, W_in.device).get(L.mosaic_prune_structured_compact_workspace_bytes(rows, cols))
+    st = _stream(stream)
+    wp, wn = _ws(ws, W_in.device).get(L.mosaic_prune_structured_compact_workspace_bytes(rows, cols), st or 0)
     _check(L.mosaic_prune_structured_compact(p, rows, cols, ldw, _dtype_code(W_in), _ptr(norms), int(row_group),
                                              int(col_group), int(row_units_keep), int(col_units_keep),
                                              _ptr(row_keep_units), _ptr(col_keep_units), int(flags), _ptr(W_out),
-                                             _ptr(unit_scores_out), wp, wn, _stream(stream)),
+                                             _ptr(unit_scores_out), wp, wn, st),
            "mosaic_prune_structured_compact")
 
 
@@ -587,8 +607,9 @@ class UnitScoreBatch:
         self.ws_bytes = lib().mosaic_unit_scores_batch_workspace_bytes(C.addressof(self.arr), len(self.jobs))
 
     def run(self, ws: Workspace | None = None, stream=None) -> None:
-        wp, wn = _ws(ws, self.device).get(self.ws_bytes)
-        _check(lib().mosaic_unit_scores_batch(C.addressof(self.arr), len(self.jobs), self.code, wp, wn, _stream(stream)),
+        st = _stream(stream)
+        wp, wn = _ws(ws, self.device).get(self.ws_bytes, st or 0)
+        _check(lib().mosaic_unit_scores_batch(C.addressof(self.arr), len(self.jobs), self.code, wp, wn, st),
                "mosaic_unit_scores_batch")
 
 
@@ -791,7 +812,7 @@ def mosaic_linear(X, W, Y, bias=None, residual=None, act=ACT_NONE, Z=None, statu
     if (xp | wp) & 15 or (ldx | ldw) & 7:      # an operand that is not 16-byte aligned is copied first
         need = L.mosaic_linear_workspace_bytes(xp, ldx, wp, ldw, tokens, n_out, n_in)
         if need:
-            sc, sn = _ws(ws, dev).get(need)
+            sc, sn = _ws(ws, dev).get(need, st or 0)
     _check(L.mosaic_linear(xp, ldx, wp, ldw, tokens, n_out, n_in, BF16, bp, rp, ldr, _act_code(act), yp, ldy, zp, ldz, sp, sc, sn, st),
            "mosaic_linear")
 
@@ -821,7 +842,7 @@ def mosaic_linear_backward(dY, X, W, Z=None, act=ACT_NONE, dX=None, dW=None, dbi
     L = lib()
     need = L.mosaic_linear_backward_workspace_bytes(dyp, lddy, xp, ldx, wp, ldw, tokens, n_out, n_in, act, dxp is not None, dwp is not None,
                                                     dbp is not None)
-    sc, sn = _ws(ws, dev).get(need) if need else (None, 0)
+    sc, sn = _ws(ws, dev).get(need, st or 0) if need else (None, 0)
     _check(L.mosaic_linear_backward(dyp, lddy, xp, ldx, wp, ldw, zp, ldz, tokens, n_out, n_in, BF16, act, dxp, lddx, dwp, lddw, dbp, sp, sc, sn, st),
            "mosaic_linear_backward")
 
@@ -837,7 +858,7 @@ def mosaic_top_logits(L, values, indices, lse=None, temperature: float = 1.0, ws
     vp = _dense(values, "values", torch.float32, dev, rows, top)
     ip = _dense(indices, "indices", torch.int32, dev, rows, top)
     sp = _dense_or_none(lse, "lse", torch.float32, dev, rows)
-    wp, wn = _ws(ws, dev).get(_scratch("mosaic_top_logits_workspace_bytes", dev, rows, vocab, code, top))
+    wp, wn = _ws(ws, dev).get(_scratch("mosaic_top_logits_workspace_bytes", dev, rows, vocab, code, top), st or 0)
     _check(lib().mosaic_top_logits(lp, rows, vocab, ldl, code, top, temperature, vp, ip, sp, wp, wn, st), "mosaic_top_logits")
 
 
@@ -851,7 +872,7 @@ def _distill_args(S, t_values, t_indices, t_lse, row_weight, temperature, stream
     ti = _dense(t_indices, "t_indices", torch.int32, dev, rows, top)
     tl = _dense_or_none(t_lse, "t_lse", torch.float32, dev, rows)
     rw = _dense_or_none(row_weight, "row_weight", torch.float32, dev, rows)
-    wp, wn = _ws(ws, dev).get(_scratch("mosaic_distill_workspace_bytes", dev, rows, top))
+    wp, wn = _ws(ws, dev).get(_scratch("mosaic_distill_workspace_bytes", dev, rows, top), st or 0)
     return (sp, rows, vocab, lds, code, tv, ti, top, tl, rw, temperature), (rows, vocab, dev), wp, wn, st
 
 

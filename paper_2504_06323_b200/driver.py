@@ -132,14 +132,10 @@ def accumulate_norms(st: ModelState, layer: int, X: dict, first: bool = True, la
                                  api.RESET_ACCUM if first else 0, st.ws)
         return len(X)
     _side_streams(st, 2)
-    need = max(api.lib().mosaic_act_norms_workspace_bytes(x.shape[0], x.shape[1]) for x in X.values())
     cur = torch.cuda.current_stream(st.device)
     fork = torch.cuda.Event()
     fork.record(cur)
-    for s, ws in st.side[:2]:
-        if ws.buf is None or ws.buf.numel() < need:   # grown before anything is in flight on the side stream
-            s.synchronize()
-            ws.get(need)
+    for s, _ in st.side[:2]:
         s.wait_event(fork)
     for i, (xk, x) in enumerate(X.items()):
         s, ws = st.side[i % 2]
