@@ -555,11 +555,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
     cluster.sync();   // the error words have been read, the loads have landed
 }
 
-// Eight elements of a row from c on; zeros past the last column, which nothing is read of.
+// Eight elements of a row from c on; zeros past the last column, which nothing is read of.  Ordinary loads here and in the
+// kernels below, no read-only ones (nor __restrict__, which lets the compiler make them so): they may start while the
+// kernel that writes what they read still runs, and nothing orders read-only loads behind the wait for it.
 template <bool VEC> __device__ __forceinline__ void load8(const uint16_t* row, int64_t c, int64_t cols, uint32_t (&w)[4]) {
     if (VEC) {   // rows on 16-byte boundaries
         if (c + 8 <= cols) {
-            const uint4 v = ld_stream16_ro(row + c);
+            const uint4 v = ld_stream16(row + c);
             w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
             return;
         }
@@ -581,7 +583,7 @@ template <bool VEC> __device__ __forceinline__ void load8(const uint16_t* row, i
 // 19.2, so from there on only rows that TMA cannot read come here (46 us at four; copying them first costs more).
 constexpr int kFewTokens = 4, kFewVector = 2, kFewRows = 4, kFewWarps = 8;
 template <int M, bool VEC>
-__global__ void __launch_bounds__(32 * kFewWarps, VEC && M == 1 ? 5 : M <= 2 ? 4 : 3) few_kernel(const uint16_t* __restrict__ X, int64_t ldx, const uint16_t* __restrict__ W, int64_t ldw,
+__global__ void __launch_bounds__(32 * kFewWarps, VEC && M == 1 ? 5 : M <= 2 ? 4 : 3) few_kernel(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t ldw,
                                                              const __grid_constant__ MmArgs a) {
     __shared__ float part[kFewWarps][kFewRows][M];
     allow_next_kernel();
@@ -673,9 +675,8 @@ __global__ void __launch_bounds__(32 * kFewWarps, VEC && M == 1 ? 5 : M <= 2 ? 4
 // registers) 17.
 constexpr int kSlopeWarps = 8, kSlopeCols = 256;
 template <bool VEC>
-__global__ void __launch_bounds__(32 * kSlopeWarps) slope_kernel(const uint16_t* __restrict__ src, int64_t ld_src, const uint16_t* __restrict__ z,
-                                                                 int64_t ld_z, int act, uint16_t* __restrict__ dst, int64_t ld_dst, int64_t rows,
-                                                                 int64_t cols, int64_t band, float* __restrict__ partial, uint16_t* __restrict__ db) {
+__global__ void __launch_bounds__(32 * kSlopeWarps) slope_kernel(const uint16_t* src, int64_t ld_src, const uint16_t* z, int64_t ld_z, int act, uint16_t* dst,
+                                                                 int64_t ld_dst, int64_t rows, int64_t cols, int64_t band, float* partial, uint16_t* db) {
     __shared__ float sums[kSlopeWarps][kSlopeCols];
     allow_next_kernel();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -718,7 +719,7 @@ __global__ void __launch_bounds__(32 * kSlopeWarps) slope_kernel(const uint16_t*
     else partial[(int64_t)blockIdx.y * cols + col] = total;
 }
 constexpr int kSumCols = 128;
-__global__ void __launch_bounds__(kSumCols) column_sum_kernel(const float* __restrict__ partial, int64_t bands, int64_t cols, uint16_t* __restrict__ out) {
+__global__ void __launch_bounds__(kSumCols) column_sum_kernel(const float* partial, int64_t bands, int64_t cols, uint16_t* out) {
     allow_next_kernel();
     await_previous_kernel();
     const int64_t c = (int64_t)blockIdx.x * kSumCols + threadIdx.x;
