@@ -828,7 +828,7 @@ def mosaic_linear_backward(dY, X, W, Z=None, act=ACT_NONE, dX=None, dW=None, dbi
         raise TypeError("X or W must be given")
     if (dW is not None and X is None) or (dX is not None and W is None):
         raise ValueError("dW needs X and dX needs W")
-    n_in = (X if X is not None else W).shape[1]
+    n_in = _matrix(X, "X", bf16, dev)[2] if X is not None else _matrix(W, "W", bf16, dev)[2]
     act = _act_code(act)
     if act != ACT_NONE and Z is None:
         raise ValueError("the backward pass of an activation needs the stored Z")
