@@ -78,7 +78,6 @@ template <bool WARP> struct KeptShape {
 template <bool WARP> struct KeptShared {
     SoftStat stat[8];
     double sum[8];
-    int flag;
 };
 template <bool WARP> __device__ __forceinline__ int kept_rank() { return WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x; }
 template <bool WARP> __device__ __forceinline__ int64_t kept_row() { return WARP ? (int64_t)blockIdx.x * kKeptWarpRows + (threadIdx.x >> 5) : (int64_t)blockIdx.x; }
@@ -161,7 +160,6 @@ template <int DT, int MODE, bool WARP> __global__ void __launch_bounds__(KeptSha
     const float g = a.grad_rows != nullptr ? a.grad_rows[r] : 1.0f;
     const float saved_lse = MODE == kWantGrad ? a.lse[r] : 0.0f;
     for (int i = me; i < a.slots; i += KeptShape<WARP>::kGroup) table[i] = 0xFFFFFFFFu;
-    if (me == 0) sh.flag = 0;   // (a CTA a row; a warp's vote needs none)
     KeptRow<DT, WARP> k(a, r, sh);
     kept_sync<WARP>();
     float mass = 0.0f;

@@ -221,7 +221,6 @@ struct PickRow {
     uint32_t votes[2][16];   // of each warp
     uint32_t count;      // candidates found
     uint32_t kept;       // groups that hold some
-    uint32_t floor;
     int all;             // the list is no use: the row is selected over all its entries
 };
 
