@@ -92,7 +92,8 @@ class Block:
 class Recovery:
     """Trains `student` to answer as `teacher` does: gradient descent on the mean distillation loss over the tokens.
     With `renormalise` the kept logits are the teacher's whole answer (the loss is then never negative); without, they
-    keep the probabilities that they have among all."""
+    keep the probabilities that they have among all.  Entries of gate, up and down that are 0 when training begins, the ones
+    that unstructured pruning removed, stay 0."""
 
     def __init__(self, student: Block, teacher: Block, top: int = 64, temperature: float = 2.0, rate: float = 0.1, renormalise: bool = True):
         if student.head.shape[0] != teacher.head.shape[0]:
@@ -100,6 +101,8 @@ class Recovery:
         self.student, self.teacher, self.top, self.temperature, self.rate = student, teacher, top, temperature, rate
         self.renormalise = renormalise
         self.master = {w: getattr(student, w).float() for w in Block.WEIGHTS if getattr(student, w) is not None}
+        zeros = {w: self.master[w] == 0 for w in ("gate", "up", "down") if w in self.master}
+        self.removed = {w: z for w, z in zeros.items() if bool(z.any())}
 
     def targets(self, X: torch.Tensor) -> tuple:
         """(values [tokens, top], indices, log of the whole sum or None) of the teacher's logits."""
@@ -131,6 +134,8 @@ class Recovery:
         loss, grads = self.gradients(X, targets if targets is not None else self.targets(X))
         for w, g in grads.items():
             self.master[w].add_(g, alpha=-self.rate)
+            if w in self.removed:
+                self.master[w].masked_fill_(self.removed[w], 0.0)
             getattr(self.student, w).copy_(self.master[w])
         return loss
 
