@@ -205,12 +205,15 @@ class Workspace:
     """Growable scratch (the library itself allocates nothing): a buffer of its own for every stream that calls are issued
     to and every host thread that issues them.  What two streams run at once, or two threads interleave on one, must not
     meet in one buffer; within a thread a stream's calls run one after another, and their scratch may be the same.
-    A buffer belongs to its stream in the allocator's books as well: one that was replaced by a larger one is handed on
-    only behind the work that still uses it."""
+    A buffer belongs to its stream in the allocator's books as well: when the Workspace goes, it is handed on only behind
+    the work that still uses it.  One that was outgrown is kept as long as the Workspace, for a captured graph may go on
+    using it; each is at least twice the one before, so all that were outgrown are together smaller than the last.
+    Graphs captured on one stream share its buffer: to replay two of them at once, give each a Workspace."""
 
     def __init__(self, device="cuda"):
         self.device = torch.device(device)
         self._bufs: dict[tuple, torch.Tensor] = {}     # (raw stream, thread) -> buffer
+        self._outgrown: list[torch.Tensor] = []
 
     def get(self, nbytes: int, stream: int | None = None) -> tuple[int, int]:
         """(pointer, size) of at least `nbytes` for calls on `stream`: a raw handle (0: the default stream), None the current one."""
@@ -219,7 +222,11 @@ class Workspace:
         key = (stream, _thread())
         buf = self._bufs.get(key)
         if buf is None or buf.numel() < nbytes:
-            buf = self._bufs[key] = self._new(max(int(nbytes), 256), stream)
+            least = 256
+            if buf is not None:
+                self._outgrown.append(buf)
+                least = 2 * buf.numel()
+            buf = self._bufs[key] = self._new(max(int(nbytes), least), stream)
             assert buf.data_ptr() % 256 == 0 or not buf.is_cuda
         return buf.data_ptr(), buf.numel()
 

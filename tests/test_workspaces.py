@@ -30,6 +30,19 @@ def test_growth_replaces_one_stream_s_buffer_only():
     assert n >= 1 << 20 and ws.get(300, 1) == (grown, n) and ws.get(300, 2)[0] == b
 
 
+def test_an_outgrown_buffer_is_kept():
+    """(a captured graph may go on using it), and there are few of them however slowly the need grows"""
+    ws, seen = api.Workspace("cpu"), []
+    for n in range(256, 200_000, 256):
+        p, size = ws.get(n, 0)
+        assert size >= n
+        if p not in (q for q, _ in seen):
+            seen.append((p, size))
+    kept = {t.data_ptr() for t in ws._outgrown} | {ws.get(1, 0)[0]}
+    assert {p for p, _ in seen} == kept and len(seen) <= 11
+    assert sum(n for _, n in seen[:-1]) < seen[-1][1] <= 400_000
+
+
 def test_a_thread_has_its_own_buffer():
     ws, got, hold = api.Workspace("cpu"), {}, threading.Barrier(4)
 
