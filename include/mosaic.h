@@ -432,12 +432,15 @@ int mosaic_gram_accumulate(const void *X, int64_t tokens, int64_t cols, int64_t 
 
 /* ---------------------------------------------------------------------------
  * Recovery of a pruned model (Section 3.3, Post-Pruning Optimizer: the pruned
- * model is trained to restore its quality).  The calls below run its compacted
+ * model is trained to restore its quality; the paper does so by LoRA fine-tuning,
+ * distillation is this library's choice).  The calls below run its compacted
  * dense projections forward and backward, keep the top logits of the foundation
  * model's answer, and give the distillation loss against them with its gradient.
  * Unlike the matrices of the pruning path, theirs may have any leading dimension
  * and any base aligned to their element (a compacted matrix of odd width, logits
- * over an odd vocabulary); rows on 16-byte boundaries are faster.
+ * over an odd vocabulary); rows on 16-byte boundaries are faster.  Where arguments
+ * must not overlap, a matrix reaches from its first element to its last, the gaps
+ * between its rows included: halves of one buffer side by side do overlap.
  * ------------------------------------------------------------------------- */
 typedef enum mosaic_act {
     MOSAIC_ACT_NONE = 0,

@@ -671,8 +671,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, VEC && M == 1 ? 5 : M <= 2 ? 4
 // the unrounded values over the rows of this CTA's band into partial[band, c], or, of the only band, into db[c] if wanted.  A warp
 // takes 256 columns, a lane eight of them (16 bytes where src and z have 16-byte rows), the CTA's eight warps every eighth
 // row; the warps' sums meet in shared memory in their order.  Bound by the latency of a row's loads at the occupancy
-// that the slopes' registers leave: 1001 x 8807 with silu 14.6 us, 8 of them the bytes; four rows' loads at once (128
-// registers) 17.
+// that the slopes' registers leave: 1001 x 8807 with silu 18 us from cold caches (gelu 21), an instruction issued in 64 %
+// of the cycles, 8 us of them the bytes.  In a row of launches, with the column sums, 16 (gelu 19, no activation 13); four
+// rows' loads at once (128 registers) cost 2.4 more.
 constexpr int kSlopeWarps = 8, kSlopeCols = 256;
 template <bool VEC>
 __global__ void __launch_bounds__(32 * kSlopeWarps) slope_kernel(const uint16_t* src, int64_t ld_src, const uint16_t* z, int64_t ld_z, int act, uint16_t* dst,
