@@ -116,3 +116,48 @@ def test_two_streams_at_once_give_the_bits_of_one_after_another():
             train(got)
         torch.cuda.synchronize()
         assert all(torch.equal(got[k], want[k]) for k in want)
+
+
+@pytest.mark.gpu
+def test_two_threads_on_one_stream_give_the_bits_of_one_after_another():
+    """The launches of two threads' calls interleave on the stream; each call's own order is kept."""
+    g = torch.Generator(device=DEV).manual_seed(8)
+    logits = [torch.randn(400, 5003 + 10 * i, generator=g, device=DEV).to(torch.bfloat16) for i in range(3)]
+    kept = []
+    for x in logits:
+        v, i = torch.topk(x.float() + 0.5, 30, dim=1)
+        kept.append((v.contiguous(), i.to(torch.int32)))
+
+    def buffers(x):
+        f = lambda *s, dtype=torch.float32: torch.full(s, -7, device=DEV, dtype=dtype)  # noqa: E731
+        return [f(400, 30), f(400, 30, dtype=torch.int32), f(400), f(400), torch.zeros_like(x), torch.zeros_like(x)]
+
+    def calls(x, k, o):
+        api.mosaic_top_logits(x, o[0], o[1], o[2])
+        api.mosaic_distill_loss_grad(x, *k, o[3], None, o[4])
+        api.mosaic_distill_grad(x, *k, o[2], o[5])
+
+    want = [buffers(x) for x in logits]
+    for x, k, o in zip(logits, kept, want):
+        calls(x, k, o)
+        torch.cuda.synchronize()
+    got = [buffers(x) for x in logits]
+    torch.cuda.synchronize()
+    start, failed = threading.Barrier(3), []
+
+    def work(n):
+        try:
+            start.wait(timeout=30)
+            for _ in range(40):
+                calls(logits[n], kept[n], got[n])
+        except Exception as e:   # noqa: BLE001   (a thread's error is the test's)
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(n,)) for n in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed
+    assert all(torch.equal(p, q) for a, b in zip(got, want) for p, q in zip(a, b))
