@@ -502,6 +502,96 @@ int mosaic_linear_backward(const void *dY, int64_t lddy, const void *X, int64_t 
                            int *status_dev, void *ws, size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------
+ * mosaic_checkpoint - a matrix of activations kept in 8 bits.  16 adjacent columns
+ * of a row (the last group may be shorter) share an exponent:
+ *     E     = biased exponent of the largest finite magnitude of the group, >= 1
+ *     code  = x 2^(133 - E), rounded to the nearest whole number (ties to even) and
+ *             kept within +-127; -128 for a NaN or an infinity
+ *     value = code 2^(E - 133), a bf16 number again; -128 is read as NaN, -0 as +0
+ * A value differs from what was stored by at most 2^-7 of the group's largest.
+ *   codes       device, int8 [rows, cols], row pitch ldc: a multiple of 16, at least
+ *               cols rounded up to it; 16-byte aligned.  Codes from cols on up to the
+ *               next multiple of 16 are written as 0 and never used
+ *   exponents   device, uint8 [rows, ceil(cols / 16)], row pitch lde
+ * The struct is host memory, read during the call.
+ *
+ * mosaic_checkpoint_store keeps X (bf16, [rows, cols], ld ldx); mosaic_checkpoint_load
+ * writes the values.  mosaic_gated_linear writes checkpoints and its backward call reads
+ * them without a stop in bf16.  rows = 0 is legal.
+ * ------------------------------------------------------------------------- */
+typedef struct mosaic_checkpoint {
+    void *codes;
+    int64_t ldc;
+    void *exponents;
+    int64_t lde;
+} mosaic_checkpoint;
+int mosaic_checkpoint_store(const void *X, int64_t rows, int64_t cols, int64_t ldx, int dtype,
+                            const mosaic_checkpoint *out, void *stream);
+int mosaic_checkpoint_load(const mosaic_checkpoint *in, int64_t rows, int64_t cols, void *X, int64_t ldx, int dtype,
+                           void *stream);
+
+/* ---------------------------------------------------------------------------
+ * mosaic_gated_linear - the gated pair of projections of a LLaMA-shaped MLP:
+ *     Z = X W_gate^T + bias_gate,   U = X W_up^T + bias_up,   H = act(Z) * U
+ *   X               device, [tokens, in_features], ld ldx
+ *   W_gate, W_up    device, [channels, in_features], ld ld_gate, ld_up
+ *   dtype           MOSAIC_BF16 for every matrix and both biases
+ *   bias_gate, bias_up   device, [channels], each or NULL
+ *   H               device, [tokens, channels], ld ldh
+ *   Z, U            device, [tokens, channels], ld ldz, ldu, each or NULL: kept for the
+ *                   backward call
+ *   z_saved, u_saved   both or neither: Z and U kept in 8 bits instead (the arguments Z
+ *                   and U are then NULL): what mosaic_checkpoint_store makes of them
+ *   status_dev      as in mosaic_gram_accumulate, or NULL
+ *   ws              device scratch, >= the query for the same arguments (saved: whether
+ *                   checkpoints are given); 0 when X and both W have 16-byte aligned
+ *                   bases and leading dimensions and nothing is saved in 8 bits
+ * Sums in fp32 on the tensor cores; biases, activation and product in fp32 on the sums; one
+ * rounding to bf16 for each of H, Z and U.  tokens = 0 is legal.  Outputs must not
+ * overlap the inputs or each other.
+ * ------------------------------------------------------------------------- */
+size_t mosaic_gated_linear_workspace_bytes(const void *X, int64_t ldx, const void *W_gate, int64_t ld_gate,
+                                           const void *W_up, int64_t ld_up, int64_t tokens, int64_t channels,
+                                           int64_t in_features, int saved);
+int mosaic_gated_linear(const void *X, int64_t ldx, const void *W_gate, int64_t ld_gate, const void *W_up,
+                        int64_t ld_up, int64_t tokens, int64_t channels, int64_t in_features, int dtype,
+                        const void *bias_gate, const void *bias_up, int act, void *H, int64_t ldh, void *Z, int64_t ldz,
+                        void *U, int64_t ldu, const mosaic_checkpoint *z_saved, const mosaic_checkpoint *u_saved,
+                        int *status_dev, void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * mosaic_gated_linear_backward - the gradients of mosaic_gated_linear:
+ *     dZ = dH * U * act'(Z),   dU = dH * act(Z),   dX = dZ W_gate + dU W_up,
+ *     dW_gate = dZ^T X,   dW_up = dU^T X,   dbias = sums over the tokens of dZ and dU
+ *   dH        device, [tokens, channels], ld lddh
+ *   X         device, [tokens, in_features], ld ldx; or NULL and x_saved its checkpoint
+ *   Z, U      device, [tokens, channels], as the forward call kept them; or NULL both and
+ *             z_saved, u_saved their checkpoints
+ *   dX, dW_gate, dW_up, dbias_gate, dbias_up   device outputs of the shapes of X, W_gate,
+ *             W_up and the biases; each may be NULL (not wanted; both W are needed for dX
+ *             only, X for the dW only)
+ *   H         device, [tokens, channels], ld ldh, or NULL: act(Z) * U once more, from what
+ *             was kept - the input of the projection behind
+ *   ws        device scratch, >= the query for the same arguments (x_saved: whether a
+ *             checkpoint of X is given)
+ * dZ and dU are rounded once to bf16 before the products (the tensor cores' input type);
+ * dX sums both products in fp32 and is rounded once; the biases' gradients sum the
+ * unrounded values in fp32 in a fixed order.  With tokens = 0 the dW and dbias are zero.
+ * ------------------------------------------------------------------------- */
+size_t mosaic_gated_linear_backward_workspace_bytes(const void *X, int64_t ldx, int x_saved, const void *W_gate,
+                                                    int64_t ld_gate, const void *W_up, int64_t ld_up, int64_t tokens,
+                                                    int64_t channels, int64_t in_features, int want_dx, int want_dw,
+                                                    int want_dbias);
+int mosaic_gated_linear_backward(const void *dH, int64_t lddh, const void *X, int64_t ldx,
+                                 const mosaic_checkpoint *x_saved, const void *W_gate, int64_t ld_gate,
+                                 const void *W_up, int64_t ld_up, const void *Z, int64_t ldz, const void *U, int64_t ldu,
+                                 const mosaic_checkpoint *z_saved, const mosaic_checkpoint *u_saved, int64_t tokens,
+                                 int64_t channels, int64_t in_features, int dtype, int act, void *dX, int64_t lddx,
+                                 void *dW_gate, int64_t lddwg, void *dW_up, int64_t lddwu, void *dbias_gate,
+                                 void *dbias_up, void *H, int64_t ldh, int *status_dev, void *ws, size_t ws_bytes,
+                                 void *stream);
+
+/* ---------------------------------------------------------------------------
  * mosaic_top_logits - the `top` largest entries of every row of logits, in order
  * (value descending, ties by ascending index), and the row's log-sum-exp:
  *     lse[r] = log sum_j exp(L[r,j] / temperature)     over the whole row

@@ -48,6 +48,9 @@ SYMBOLS = (
     "mosaic_gram_accumulate",
     "mosaic_linear_workspace_bytes", "mosaic_linear",
     "mosaic_linear_backward_workspace_bytes", "mosaic_linear_backward",
+    "mosaic_checkpoint_store", "mosaic_checkpoint_load",
+    "mosaic_gated_linear_workspace_bytes", "mosaic_gated_linear",
+    "mosaic_gated_linear_backward_workspace_bytes", "mosaic_gated_linear_backward",
     "mosaic_top_logits_workspace_bytes", "mosaic_top_logits",
     "mosaic_distill_workspace_bytes", "mosaic_distill_loss", "mosaic_distill_grad", "mosaic_distill_loss_grad",
     "mosaic_bounded_wait_selftest",
@@ -142,6 +145,19 @@ def lib() -> C.CDLL:
                                              vp, vp, sz, vp]
         L.mosaic_top_logits.restype = ci
         L.mosaic_top_logits.argtypes = [vp, i64, i64, i64, ci, i64, flt, vp, vp, vp, vp, sz, vp]
+        L.mosaic_checkpoint_store.restype = ci
+        L.mosaic_checkpoint_store.argtypes = [vp, i64, i64, i64, ci, vp, vp]
+        L.mosaic_checkpoint_load.restype = ci
+        L.mosaic_checkpoint_load.argtypes = [vp, i64, i64, vp, i64, ci, vp]
+        L.mosaic_gated_linear_workspace_bytes.restype = sz
+        L.mosaic_gated_linear_workspace_bytes.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, ci]
+        L.mosaic_gated_linear.restype = ci
+        L.mosaic_gated_linear.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, ci, vp, vp, ci, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, sz, vp]
+        L.mosaic_gated_linear_backward_workspace_bytes.restype = sz
+        L.mosaic_gated_linear_backward_workspace_bytes.argtypes = [vp, i64, ci, vp, i64, vp, i64, i64, i64, i64, ci, ci, ci]
+        L.mosaic_gated_linear_backward.restype = ci
+        L.mosaic_gated_linear_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, ci, ci, vp, i64,
+                                                   vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, sz, vp]
         L.mosaic_top_logits_workspace_bytes.restype = sz
         L.mosaic_top_logits_workspace_bytes.argtypes = [i64, i64, ci, i64]
         teacher = [vp, i64, i64, i64, ci, vp, vp, i64, vp, vp, flt]
@@ -852,6 +868,136 @@ def mosaic_linear_backward(dY, X, W, Z=None, act=ACT_NONE, dX=None, dW=None, dbi
     sc, sn = _ws(ws, dev).get(need, st or 0) if need else (None, 0)
     _check(L.mosaic_linear_backward(dyp, lddy, xp, ldx, wp, ldw, zp, ldz, tokens, n_out, n_in, BF16, act, dxp, lddx, dwp, lddw, dbp, sp, sc, sn, st),
            "mosaic_linear_backward")
+
+
+class _CheckpointStruct(C.Structure):
+    """mosaic_checkpoint of include/mosaic.h."""
+    _fields_ = [("codes", C.c_void_p), ("ldc", C.c_int64), ("exponents", C.c_void_p), ("lde", C.c_int64)]
+
+
+class Checkpoint:
+    """A matrix of activations in 8 bits: `codes` int8 [rows, cols rounded up to 16 or more] and `exponents` uint8
+    [rows, ceil(cols / 16)], both with unit column stride.  The tensors are checked here and kept alive by the object."""
+
+    def __init__(self, codes: torch.Tensor, exponents: torch.Tensor, cols: int):
+        cols = int(cols)
+        groups = -(-cols // 16)
+        for t, name, dtype, least in ((codes, "codes", torch.int8, 16 * groups), (exponents, "exponents", torch.uint8, groups)):
+            _, rows, width, _ = _matrix(t, name, dtype)
+            if cols <= 0 or width < least or rows != codes.shape[0]:
+                raise ValueError(f"{name} must be [{codes.shape[0]}, {least}] or wider for {cols} columns, got {list(t.shape)}")
+        if codes.device != exponents.device:
+            raise ValueError("codes and exponents must be on one device")
+        self.codes, self.exponents, self.rows, self.cols, self.device = codes, exponents, codes.shape[0], cols, codes.get_device()
+        ldc = _matrix(codes, "codes", torch.int8)[3]
+        self._struct = _CheckpointStruct(codes.data_ptr(), -(-ldc // 16) * 16 if self.rows <= 1 else ldc, exponents.data_ptr(),
+                                         _matrix(exponents, "exponents", torch.uint8)[3])
+        self.ptr = C.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda") -> "Checkpoint":
+        groups = -(-int(cols) // 16)
+        return cls(torch.empty(rows, 16 * groups, dtype=torch.int8, device=device), torch.empty(rows, groups, dtype=torch.uint8, device=device), cols)
+
+
+def _saved(c, name: str, device: int, rows: int, cols: int):
+    """Pointer of a checkpoint of a [rows, cols] matrix."""
+    if c.rows != rows or c.cols != cols:
+        raise ValueError(f"{name} must keep [{rows}, {cols}], keeps [{c.rows}, {c.cols}]")
+    if c.device != device:
+        raise ValueError(f"{name} is on cuda:{c.device}: the tensors of one call live on one device")
+    return c.ptr
+
+
+def _either(t, name: str, device: int, rows: int, cols: int):
+    """(pointer, leading dimension, checkpoint pointer) of a bf16 matrix or its Checkpoint (None: neither)."""
+    if isinstance(t, Checkpoint):
+        return None, cols, _saved(t, name, device, rows, cols)
+    return *_like(t, name, torch.bfloat16, device, rows, cols), None
+
+
+def mosaic_checkpoint_store(X, out: Checkpoint, stream=None) -> None:
+    """Keeps X (bf16 [rows, cols]) in 8 bits."""
+    xp, rows, cols, ldx = _matrix(X, "X", torch.bfloat16)
+    dev, st = _run_on(X, stream)
+    _check(lib().mosaic_checkpoint_store(xp, rows, cols, ldx, BF16, _saved(out, "out", dev, rows, cols), st), "mosaic_checkpoint_store")
+
+
+def mosaic_checkpoint_load(saved: Checkpoint, X, stream=None) -> None:
+    """Writes the values that a checkpoint keeps to X (bf16 [rows, cols])."""
+    xp, rows, cols, ldx = _matrix(X, "X", torch.bfloat16)
+    dev, st = _run_on(X, stream)
+    _check(lib().mosaic_checkpoint_load(_saved(saved, "saved", dev, rows, cols), rows, cols, xp, ldx, BF16, st), "mosaic_checkpoint_load")
+
+
+def mosaic_gated_linear(X, W_gate, W_up, H, bias_gate=None, bias_up=None, act="silu", Z=None, U=None, status: torch.Tensor | None = None,
+                        ws: Workspace | None = None, stream=None) -> None:
+    """H = act(X W_gate^T + bias_gate) * (X W_up^T + bias_up) for bf16 X [tokens, in], W [channels, in], H [tokens,
+    channels] and biases [channels].  Z and U, if given, receive the two before the activation and the product: bf16
+    [tokens, channels], or both a Checkpoint."""
+    bf16 = torch.bfloat16
+    xp, tokens, n_in, ldx = _matrix(X, "X", bf16)
+    dev, st = _run_on(X, stream)
+    gp, n, g_in, ldg = _matrix(W_gate, "W_gate", bf16, dev)
+    if g_in != n_in:
+        raise ValueError(f"W_gate must be [channels, {n_in}], got [{n}, {g_in}]")
+    if W_up is None or H is None:
+        raise TypeError("W_up and H must be CUDA tensors")
+    up, ldu = _like(W_up, "W_up", bf16, dev, n, n_in)
+    hp, ldh = _like(H, "H", bf16, dev, tokens, n)
+    zp, ldz, z8 = _either(Z, "Z", dev, tokens, n)
+    vp, ldv, u8 = _either(U, "U", dev, tokens, n)
+    if (z8 is None) != (u8 is None):
+        raise ValueError("Z and U must both be checkpoints, or neither")
+    bg = _dense_or_none(bias_gate, "bias_gate", bf16, dev, n)
+    bu = _dense_or_none(bias_up, "bias_up", bf16, dev, n)
+    sp = _dense_or_none(status, "status", torch.int32, dev, 1)
+    L, sc, sn = lib(), None, 0
+    if (xp | gp | up) & 15 or (ldx | ldg | ldu) & 7 or z8:
+        need = L.mosaic_gated_linear_workspace_bytes(xp, ldx, gp, ldg, up, ldu, tokens, n, n_in, z8 is not None)
+        if need:
+            sc, sn = _ws(ws, dev).get(need, st or 0)
+    _check(L.mosaic_gated_linear(xp, ldx, gp, ldg, up, ldu, tokens, n, n_in, BF16, bg, bu, _act_code(act), hp, ldh, zp, ldz, vp, ldv, z8, u8, sp,
+                                 sc, sn, st), "mosaic_gated_linear")
+
+
+def mosaic_gated_linear_backward(dH, X, W_gate, W_up, Z, U, act="silu", dX=None, dW_gate=None, dW_up=None, dbias_gate=None, dbias_up=None,
+                                 H=None, status: torch.Tensor | None = None, ws: Workspace | None = None, stream=None) -> None:
+    """Gradients of mosaic_gated_linear from dH [tokens, channels], its inputs and the Z and U that it kept: dX [tokens, in],
+    dW_gate and dW_up [channels, in], dbias_gate and dbias_up [channels] (each optional, all bf16); H, if given, receives
+    act(Z) * U once more.  X, and Z with U, may be a Checkpoint."""
+    bf16 = torch.bfloat16
+    dhp, tokens, n, lddh = _matrix(dH, "dH", bf16)
+    dev, st = _run_on(dH, stream)
+    want_dw = dW_gate is not None or dW_up is not None
+    if Z is None or U is None:
+        raise ValueError("the backward pass needs the Z and U that the forward pass kept")
+    if (want_dw and X is None) or (dX is not None and (W_gate is None or W_up is None)):
+        raise ValueError("dW_gate and dW_up need X, dX needs W_gate and W_up")
+    sized = next((t for t in (X, W_gate, W_up) if t is not None), None)
+    if sized is None:
+        raise TypeError("X or a weight matrix must be given")
+    n_in = sized.cols if isinstance(sized, Checkpoint) else _matrix(sized, "X" if sized is X else "W", bf16, dev)[2]
+    xp, ldx, x8 = _either(X, "X", dev, tokens, n_in)
+    gp, ldg = _like(W_gate, "W_gate", bf16, dev, n, n_in)
+    up, ldu = _like(W_up, "W_up", bf16, dev, n, n_in)
+    zp, ldz, z8 = _either(Z, "Z", dev, tokens, n)
+    vp, ldv, u8 = _either(U, "U", dev, tokens, n)
+    if (z8 is None) != (u8 is None):
+        raise ValueError("Z and U must both be checkpoints, or neither")
+    dxp, lddx = _like(dX, "dX", bf16, dev, tokens, n_in)
+    dgp, lddg = _like(dW_gate, "dW_gate", bf16, dev, n, n_in)
+    dup, lddu = _like(dW_up, "dW_up", bf16, dev, n, n_in)
+    hp, ldh = _like(H, "H", bf16, dev, tokens, n)
+    dbg = _dense_or_none(dbias_gate, "dbias_gate", bf16, dev, n)
+    dbu = _dense_or_none(dbias_up, "dbias_up", bf16, dev, n)
+    sp = _dense_or_none(status, "status", torch.int32, dev, 1)
+    L = lib()
+    need = L.mosaic_gated_linear_backward_workspace_bytes(xp, ldx, x8 is not None, gp, ldg, up, ldu, tokens, n, n_in, dX is not None, want_dw,
+                                                          dbg is not None or dbu is not None)
+    sc, sn = _ws(ws, dev).get(need, st or 0) if need else (None, 0)
+    _check(L.mosaic_gated_linear_backward(dhp, lddh, xp, ldx, x8, gp, ldg, up, ldu, zp, ldz, vp, ldv, z8, u8, tokens, n, n_in, BF16, _act_code(act),
+                                          dxp, lddx, dgp, lddg, dup, lddu, dbg, dbu, hp, ldh, sp, sc, sn, st), "mosaic_gated_linear_backward")
 
 
 def mosaic_top_logits(L, values, indices, lse=None, temperature: float = 1.0, ws: Workspace | None = None, stream=None) -> None:
