@@ -592,6 +592,61 @@ int mosaic_gated_linear_backward(const void *dH, int64_t lddh, const void *X, in
                                  void *stream);
 
 /* ---------------------------------------------------------------------------
+ * mosaic_weight4 - a weight matrix in 4 bits.  `group` adjacent columns of a row (the
+ * last group may be shorter) share a scale:
+ *     s     = (largest magnitude of the group / 7), rounded to five significant bits
+ *             (nearest, ties to even); 0 if that is below 2^-126, at most 2^123
+ *     code  = w / s, rounded to the nearest whole number (ties to even) and kept within
+ *             +-7; 0 where s is 0
+ *     value = code s, exactly a bf16 number: zeros stay zero, so what pruning removed
+ *             stays removed
+ * A group that holds a NaN or an infinity has the scale NaN, and all its values are NaN.
+ *   codes    device, [rows, ceil(cols / 2)] bytes, two codes each with 8 added to them
+ *            (the even column in the low half), row pitch ldc bytes: a multiple of 16,
+ *            at least 16 for every 32 columns; 16-byte aligned.  Codes from cols on are
+ *            never used
+ *   scales   device, bf16 [rows, ceil(cols / group)], row pitch lds.  The products rely
+ *            on five significant bits
+ *   group    32, 64 or 128
+ * The struct is host memory, read during the call.  mosaic_quantize4 packs W (bf16,
+ * [rows, cols], ld ldw), mosaic_dequantize4 writes the values.  rows = 0 is legal.
+ * ------------------------------------------------------------------------- */
+typedef struct mosaic_weight4 {
+    void *codes;
+    int64_t ldc;
+    void *scales;
+    int64_t lds;
+    int64_t group;
+} mosaic_weight4;
+int mosaic_quantize4(const void *W, int64_t rows, int64_t cols, int64_t ldw, int dtype, const mosaic_weight4 *out,
+                     void *stream);
+int mosaic_dequantize4(const mosaic_weight4 *in, int64_t rows, int64_t cols, void *W, int64_t ldw, int dtype,
+                       void *stream);
+
+/* ---------------------------------------------------------------------------
+ * mosaic_linear4 / mosaic_gated_linear4 - mosaic_linear and mosaic_gated_linear with
+ * weights in 4 bits (the groups of W_gate and W_up may differ):
+ *     Y = act(X W^T + bias) + residual,   H = act(X W_gate^T + bias_gate) * (X W_up^T + bias_up)
+ * Arguments as there; the residual may be Y itself.  dtype is that of X, the biases, the
+ * residual and the output: MOSAIC_BF16.
+ *   ws        device scratch, >= the query for the same arguments: 0 for up to 32 tokens
+ *             when X has a 16-byte aligned base and leading dimension; for more tokens
+ *             it holds the weights in bf16
+ * Products are exact, sums in fp32, one rounding to bf16 for the output.
+ * ------------------------------------------------------------------------- */
+size_t mosaic_linear4_workspace_bytes(const void *X, int64_t ldx, int64_t tokens, int64_t out_features,
+                                      int64_t in_features);
+int mosaic_linear4(const void *X, int64_t ldx, const mosaic_weight4 *W, int64_t tokens, int64_t out_features,
+                   int64_t in_features, int dtype, const void *bias, const void *residual, int64_t ldr, int act, void *Y,
+                   int64_t ldy, int *status_dev, void *ws, size_t ws_bytes, void *stream);
+size_t mosaic_gated_linear4_workspace_bytes(const void *X, int64_t ldx, int64_t tokens, int64_t channels,
+                                            int64_t in_features);
+int mosaic_gated_linear4(const void *X, int64_t ldx, const mosaic_weight4 *W_gate, const mosaic_weight4 *W_up,
+                         int64_t tokens, int64_t channels, int64_t in_features, int dtype, const void *bias_gate,
+                         const void *bias_up, int act, void *H, int64_t ldh, int *status_dev, void *ws, size_t ws_bytes,
+                         void *stream);
+
+/* ---------------------------------------------------------------------------
  * mosaic_top_logits - the `top` largest entries of every row of logits, in order
  * (value descending, ties by ascending index), and the row's log-sum-exp:
  *     lse[r] = log sum_j exp(L[r,j] / temperature)     over the whole row

@@ -51,6 +51,8 @@ SYMBOLS = (
     "mosaic_checkpoint_store", "mosaic_checkpoint_load",
     "mosaic_gated_linear_workspace_bytes", "mosaic_gated_linear",
     "mosaic_gated_linear_backward_workspace_bytes", "mosaic_gated_linear_backward",
+    "mosaic_quantize4", "mosaic_dequantize4",
+    "mosaic_linear4_workspace_bytes", "mosaic_linear4", "mosaic_gated_linear4_workspace_bytes", "mosaic_gated_linear4",
     "mosaic_top_logits_workspace_bytes", "mosaic_top_logits",
     "mosaic_distill_workspace_bytes", "mosaic_distill_loss", "mosaic_distill_grad", "mosaic_distill_loss_grad",
     "mosaic_bounded_wait_selftest",
@@ -158,6 +160,18 @@ def lib() -> C.CDLL:
         L.mosaic_gated_linear_backward.restype = ci
         L.mosaic_gated_linear_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, ci, ci, vp, i64,
                                                    vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, sz, vp]
+        L.mosaic_quantize4.restype = ci
+        L.mosaic_quantize4.argtypes = [vp, i64, i64, i64, ci, vp, vp]
+        L.mosaic_dequantize4.restype = ci
+        L.mosaic_dequantize4.argtypes = [vp, i64, i64, vp, i64, ci, vp]
+        L.mosaic_linear4_workspace_bytes.restype = sz
+        L.mosaic_linear4_workspace_bytes.argtypes = [vp, i64, i64, i64, i64]
+        L.mosaic_linear4.restype = ci
+        L.mosaic_linear4.argtypes = [vp, i64, vp, i64, i64, i64, ci, vp, vp, i64, ci, vp, i64, vp, vp, sz, vp]
+        L.mosaic_gated_linear4_workspace_bytes.restype = sz
+        L.mosaic_gated_linear4_workspace_bytes.argtypes = [vp, i64, i64, i64, i64]
+        L.mosaic_gated_linear4.restype = ci
+        L.mosaic_gated_linear4.argtypes = [vp, i64, vp, vp, i64, i64, i64, ci, vp, vp, ci, vp, i64, vp, vp, sz, vp]
         L.mosaic_top_logits_workspace_bytes.restype = sz
         L.mosaic_top_logits_workspace_bytes.argtypes = [i64, i64, ci, i64]
         teacher = [vp, i64, i64, i64, ci, vp, vp, i64, vp, vp, flt]
@@ -998,6 +1012,118 @@ def mosaic_gated_linear_backward(dH, X, W_gate, W_up, Z, U, act="silu", dX=None,
     sc, sn = _ws(ws, dev).get(need, st or 0) if need else (None, 0)
     _check(L.mosaic_gated_linear_backward(dhp, lddh, xp, ldx, x8, gp, ldg, up, ldu, zp, ldz, vp, ldv, z8, u8, tokens, n, n_in, BF16, _act_code(act),
                                           dxp, lddx, dgp, lddg, dup, lddu, dbg, dbu, hp, ldh, sp, sc, sn, st), "mosaic_gated_linear_backward")
+
+
+class _Weight4Struct(C.Structure):
+    """mosaic_weight4 of include/mosaic.h."""
+    _fields_ = [("codes", C.c_void_p), ("ldc", C.c_int64), ("scales", C.c_void_p), ("lds", C.c_int64), ("group", C.c_int64)]
+
+
+class Weight4:
+    """A weight matrix in 4 bits: `codes` uint8 [rows, 16 for every 32 columns, or more] and `scales` bf16 [rows, ceil(cols /
+    group)], both with unit column stride; `group` is 32, 64 or 128.  The tensors are checked here and kept alive by the
+    object."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, group: int):
+        cols, group = int(cols), int(group)
+        if group not in (32, 64, 128):
+            raise ValueError(f"group must be 32, 64 or 128, got {group}")
+        for t, name, dtype, least in ((codes, "codes", torch.uint8, -(-cols // 32) * 16), (scales, "scales", torch.bfloat16, -(-cols // group))):
+            _, rows, width, _ = _matrix(t, name, dtype)
+            if cols <= 0 or width < least or rows != codes.shape[0]:
+                raise ValueError(f"{name} must be [{codes.shape[0]}, {least}] or wider for {cols} columns, got {list(t.shape)}")
+        if codes.device != scales.device:
+            raise ValueError("codes and scales must be on one device")
+        self.codes, self.scales, self.rows, self.cols, self.group, self.device = codes, scales, codes.shape[0], cols, group, codes.get_device()
+        ldc = _matrix(codes, "codes", torch.uint8)[3]
+        self._struct = _Weight4Struct(codes.data_ptr(), -(-ldc // 16) * 16 if self.rows <= 1 else ldc, scales.data_ptr(),
+                                      _matrix(scales, "scales", torch.bfloat16)[3], group)
+        self.ptr = C.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, group: int = 128, device="cuda") -> "Weight4":
+        return cls(torch.empty(rows, -(-int(cols) // 32) * 16, dtype=torch.uint8, device=device),
+                   torch.empty(rows, -(-int(cols) // max(int(group), 1)), dtype=torch.bfloat16, device=device), cols, group)
+
+    @classmethod
+    def of(cls, W: torch.Tensor, group: int = 128) -> "Weight4":
+        """W (bf16 [rows, cols]) in 4 bits."""
+        out = cls.empty(*W.shape, group, W.device)
+        mosaic_quantize4(W, out)
+        return out
+
+
+def _weight4(w, name: str, device: int, rows: int | None, cols: int):
+    """Pointer of a 4-bit [rows, cols] matrix (rows None: any number)."""
+    if not isinstance(w, Weight4):
+        raise TypeError(f"{name} must be a Weight4")
+    if (rows is not None and w.rows != rows) or w.cols != cols:
+        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {cols}], is [{w.rows}, {w.cols}]")
+    if w.device != device:
+        raise ValueError(f"{name} is on cuda:{w.device}: the tensors of one call live on one device")
+    return w.ptr
+
+
+def mosaic_quantize4(W, out: Weight4, stream=None) -> None:
+    """Packs W (bf16 [rows, cols]) into 4 bits."""
+    wp, rows, cols, ldw = _matrix(W, "W", torch.bfloat16)
+    dev, st = _run_on(W, stream)
+    _check(lib().mosaic_quantize4(wp, rows, cols, ldw, BF16, _weight4(out, "out", dev, rows, cols), st), "mosaic_quantize4")
+
+
+def mosaic_dequantize4(W4: Weight4, W, stream=None) -> None:
+    """Writes the values of a 4-bit matrix to W (bf16 [rows, cols]); they are bf16 numbers, exactly."""
+    wp, rows, cols, ldw = _matrix(W, "W", torch.bfloat16)
+    dev, st = _run_on(W, stream)
+    _check(lib().mosaic_dequantize4(_weight4(W4, "W4", dev, rows, cols), rows, cols, wp, ldw, BF16, st), "mosaic_dequantize4")
+
+
+FEW4_TOKENS = 32   # up to here the products read 4-bit weights as they are; beyond, a bf16 copy in the workspace
+
+
+def mosaic_linear4(X, W: Weight4, Y, bias=None, residual=None, act=ACT_NONE, status: torch.Tensor | None = None, ws: Workspace | None = None,
+                   stream=None) -> None:
+    """mosaic_linear with 4-bit weights: Y = act(X W^T + bias) + residual.  `residual` may be Y (added in place)."""
+    bf16 = torch.bfloat16
+    xp, tokens, n_in, ldx = _matrix(X, "X", bf16)
+    dev, st = _run_on(X, stream)
+    wp = _weight4(W, "W", dev, None, n_in)
+    n_out = W.rows
+    if Y is None:
+        raise TypeError("Y must be a CUDA tensor")
+    yp, ldy = _like(Y, "Y", bf16, dev, tokens, n_out)
+    rp, ldr = _like(residual, "residual", bf16, dev, tokens, n_out)
+    bp = _dense_or_none(bias, "bias", bf16, dev, n_out)
+    sp = _dense_or_none(status, "status", torch.int32, dev, 1)
+    L, sc, sn = lib(), None, 0
+    if xp & 15 or ldx & 7 or tokens > FEW4_TOKENS:
+        need = L.mosaic_linear4_workspace_bytes(xp, ldx, tokens, n_out, n_in)
+        if need:
+            sc, sn = _ws(ws, dev).get(need, st or 0)
+    _check(L.mosaic_linear4(xp, ldx, wp, tokens, n_out, n_in, BF16, bp, rp, ldr, _act_code(act), yp, ldy, sp, sc, sn, st), "mosaic_linear4")
+
+
+def mosaic_gated_linear4(X, W_gate: Weight4, W_up: Weight4, H, bias_gate=None, bias_up=None, act="silu", status: torch.Tensor | None = None,
+                         ws: Workspace | None = None, stream=None) -> None:
+    """mosaic_gated_linear with 4-bit weights: H = act(X W_gate^T + bias_gate) * (X W_up^T + bias_up)."""
+    bf16 = torch.bfloat16
+    xp, tokens, n_in, ldx = _matrix(X, "X", bf16)
+    dev, st = _run_on(X, stream)
+    gp = _weight4(W_gate, "W_gate", dev, None, n_in)
+    n = W_gate.rows
+    up = _weight4(W_up, "W_up", dev, n, n_in)
+    if H is None:
+        raise TypeError("H must be a CUDA tensor")
+    hp, ldh = _like(H, "H", bf16, dev, tokens, n)
+    bg = _dense_or_none(bias_gate, "bias_gate", bf16, dev, n)
+    bu = _dense_or_none(bias_up, "bias_up", bf16, dev, n)
+    sp = _dense_or_none(status, "status", torch.int32, dev, 1)
+    L, sc, sn = lib(), None, 0
+    if xp & 15 or ldx & 7 or tokens > FEW4_TOKENS:
+        need = L.mosaic_gated_linear4_workspace_bytes(xp, ldx, tokens, n, n_in)
+        if need:
+            sc, sn = _ws(ws, dev).get(need, st or 0)
+    _check(L.mosaic_gated_linear4(xp, ldx, gp, up, tokens, n, n_in, BF16, bg, bu, _act_code(act), hp, ldh, sp, sc, sn, st), "mosaic_gated_linear4")
 
 
 def mosaic_top_logits(L, values, indices, lse=None, temperature: float = 1.0, ws: Workspace | None = None, stream=None) -> None:

@@ -25,10 +25,6 @@ inline size_t saved_code_bytes(const Saved& s, int64_t rows, int64_t cols) {
 inline size_t saved_exponent_bytes(const Saved& s, int64_t rows, int64_t cols) {
     return rows > 0 ? (size_t)(rows - 1) * (size_t)s.lde + (size_t)saved_groups(cols) : 0u;
 }
-inline bool spans_meet(const void* p, size_t n, const void* q, size_t m) {
-    const char *x = static_cast<const char*>(p), *y = static_cast<const char*>(q);
-    return x != nullptr && y != nullptr && n > 0 && m > 0 && x < y + m && y < x + n;
-}
 int check_saved(const mosaic_checkpoint* c, int64_t rows, int64_t cols);
 inline Saved as_saved(const mosaic_checkpoint* c) {
     return {static_cast<int8_t*>(c->codes), c->ldc, static_cast<uint8_t*>(c->exponents), c->lde};

@@ -42,6 +42,12 @@ inline size_t elem_size(int dtype) { return dtype == MOSAIC_F32 ? 4 : 2; }
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int cuda_status(cudaError_t e) { return e == cudaSuccess ? MOSAIC_OK : MOSAIC_ERR_CUDA; }
 
+// Whether two spans of bytes (none where a pointer is null) have one in common.
+inline bool spans_meet(const void* p, size_t n, const void* q, size_t m) {
+    const char *x = static_cast<const char*>(p), *y = static_cast<const char*>(q);
+    return x != nullptr && y != nullptr && n > 0 && m > 0 && x < y + m && y < x + n;
+}
+
 #define MOSAIC_CUDA_TRY(expr)                                   \
     do {                                                        \
         cudaError_t e__ = (expr);                               \

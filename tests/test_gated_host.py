@@ -115,3 +115,61 @@ def test_binding_refuses_cpu_tensors(lib):
         api.mosaic_gated_linear_backward(x, x, x, x, x, x)
     with pytest.raises(TypeError):
         api.Checkpoint.empty(4, 16, "cpu")
+
+
+class W4(api._Weight4Struct):
+    alive = []
+
+    @property
+    def at(self):
+        W4.alive.append(self)
+        return C.addressof(self)
+
+
+def w4(codes=2 * A, ldc=32, scales=3 * A, lds=2, group=32):
+    return W4(codes, ldc, scales, lds, group).at
+
+
+def linear4(lib, **k):
+    g = k.get
+    return lib.mosaic_linear4(g("X", A), g("ldx", 64), g("W", w4()), g("m", 8), g("n", 32), g("k", 64), g("dtype", api.BF16), g("bias"), g("R"), g("ldr", 32),
+                              g("act", 0), g("Y", 4 * A), g("ldy", 32), g("status"), g("ws"), g("ws_bytes", 0), None)
+
+
+def gated4(lib, **k):
+    g = k.get
+    return lib.mosaic_gated_linear4(g("X", A), g("ldx", 64), g("W", w4()), g("W2", w4(5 * A, scales=6 * A)), g("m", 8), g("n", 32), g("k", 64), g("dtype", api.BF16),
+                                    g("bias"), g("bu"), g("act", 3), g("Y", 4 * A), g("ldy", 32), g("status"), g("ws"), g("ws_bytes", 0), None)
+
+
+@pytest.mark.parametrize("call", [linear4, gated4])
+def test_products4_refusals_need_no_device(lib, call):
+    assert call(lib, dtype=api.F32) == DTYPE and call(lib, n=0) == INVALID and call(lib, act=5) == INVALID and call(lib, ldx=63) == INVALID and call(lib, ldy=31) == INVALID
+    assert call(lib, X=None) == NULL and call(lib, Y=None) == NULL and call(lib, W=None) == NULL
+    assert call(lib, W=w4(codes=None)) == NULL and call(lib, W=w4(scales=None)) == NULL
+    assert call(lib, W=w4(group=16)) == INVALID and call(lib, W=w4(group=96)) == INVALID and call(lib, W=w4(ldc=16)) == INVALID and call(lib, W=w4(lds=1)) == INVALID
+    assert call(lib, W=w4(codes=2 * A + 8)) == MISALIGNED and call(lib, W=w4(ldc=40)) == MISALIGNED and call(lib, W=w4(scales=3 * A + 1)) == MISALIGNED
+    assert call(lib, status=A + 2) == MISALIGNED and call(lib, Y=A) == ALIAS and call(lib, Y=2 * A) == ALIAS and call(lib, Y=3 * A) == ALIAS and call(lib, bias=4 * A) == ALIAS
+    assert call(lib, X=A + 2) == NULL and call(lib, X=A + 2, ws=8 * A, ws_bytes=100) == WS and call(lib, X=A + 2, ws=8 * A + 8, ws_bytes=1 << 20) == MISALIGNED
+    assert call(lib, m=33) == NULL and call(lib, m=33, ws=8 * A, ws_bytes=32 * 64 * 2 - 1) == WS   # many tokens: the weights in bf16
+    if call is linear4:
+        assert call(lib, R=4 * A, ldr=40) == ALIAS and call(lib, R=4 * A + 32) == ALIAS
+    else:
+        assert call(lib, W2=None) == NULL and call(lib, Y=5 * A) == ALIAS and call(lib, bu=4 * A) == ALIAS and call(lib, W2=w4(group=3)) == INVALID
+
+
+def test_products4_workspaces(lib):
+    q, g = lib.mosaic_linear4_workspace_bytes, lib.mosaic_gated_linear4_workspace_bytes
+    assert q(A, 64, 32, 32, 64) == 0 and g(A, 64, 32, 32, 64) == 0
+    assert q(A, 64, api.FEW4_TOKENS, 32, 64) == 0 and q(A, 64, api.FEW4_TOKENS + 1, 32, 64) == 32 * 64 * 2 and g(A, 64, api.FEW4_TOKENS + 1, 32, 64) == 2 * 32 * 64 * 2
+    assert q(A + 2, 64, 8, 32, 64) == 8 * 64 * 2 and q(A, 63, 8, 32, 63) == 8 * 64 * 2 and q(A, 63, 1, 32, 63) == 0
+
+
+def test_packing_refusals_need_no_device(lib):
+    for call in (lambda **k: lib.mosaic_quantize4(k.get("W", A), k.get("rows", 4), k.get("cols", 40), k.get("ld", 40), k.get("dtype", 1), k.get("c", w4()), None),
+                 lambda **k: lib.mosaic_dequantize4(k.get("c", w4()), k.get("rows", 4), k.get("cols", 40), k.get("W", A), k.get("ld", 40), k.get("dtype", 1), None)):
+        assert call(dtype=0) == DTYPE and call(rows=-1) == INVALID and call(cols=0) == INVALID and call(ld=39) == INVALID
+        assert call(W=None) == NULL and call(c=None) == NULL and call(c=w4(scales=None)) == NULL
+        assert call(W=A + 1) == MISALIGNED and call(c=w4(codes=2 * A + 4)) == MISALIGNED and call(c=w4(ldc=16)) == INVALID and call(c=w4(group=0)) == INVALID
+        assert call(W=2 * A) == ALIAS and call(W=3 * A) == ALIAS and call(c=w4(scales=2 * A + 16)) == ALIAS
+        assert call(rows=0, W=None, c=w4(None, 32, None)) == 0
