@@ -27,17 +27,11 @@ __global__ void __launch_bounds__(32 * kSavedWarps) store_kernel(const uint16_t*
     }
 #pragma unroll
     for (int r = 0; r < kSavedRows; ++r) {
-        uint32_t largest = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) largest = max(largest, max(finite_bits(w[r][e] & 0xFFFFu), finite_bits(w[r][e] >> 16)));
+        uint32_t largest = largest_finite8(w[r]);
         largest = max(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, 1));
         if (r0 + r >= rows || c >= (cols + kSavedGroup - 1) / kSavedGroup * kSavedGroup) continue;
         const uint32_t E = saved_exponent(largest);
-        const SavedScale scale(E);
-        uint32_t q[2] = {};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) q[e >> 2] |= ((uint32_t)saved_code(half_of(w[r], e), scale) & 0xFFu) << (8 * (e & 3));
-        *reinterpret_cast<uint2*>(out.codes + (r0 + r) * out.ldc + c) = make_uint2(q[0], q[1]);
+        *reinterpret_cast<uint2*>(out.codes + (r0 + r) * out.ldc + c) = saved_codes8(w[r], E);
         if ((lane & 1) == 0) out.exponents[(r0 + r) * out.lde + c / kSavedGroup] = (uint8_t)E;
     }
 }
@@ -72,7 +66,7 @@ __global__ void __launch_bounds__(32 * kSavedWarps) load_kernel(const __grid_con
         saved_values8(q[r], E[r], v);
         uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);   // exact
+        for (int e = 0; e < 4; ++e) w[e] = pack_exact(v[2 * e], v[2 * e + 1]);
         lane_store8<VEC>(X + (r0 + r) * ldx, c0, cols, turn, w);
     }
 }

@@ -34,31 +34,69 @@ int store_saved(const void* X, int64_t ldx, int64_t rows, int64_t cols, const Sa
 int load_saved(const Saved& in, int64_t rows, int64_t cols, void* X, int64_t ldx, cudaStream_t st);
 
 #ifdef __CUDACC__
-// The exponent of a group from its largest finite magnitude (bf16 bits without the sign).
-__device__ __forceinline__ uint32_t saved_exponent(uint32_t largest) { return largest >> 7 > 1u ? largest >> 7 : 1u; }
-// Magnitude bits that count for the exponent.
+// The largest magnitude's bits among eight values: of all, unless one is not finite, then of the finite ones.
 __device__ __forceinline__ uint32_t finite_bits(uint32_t half) { return (half & 0x7F80u) == 0x7F80u ? 0u : half & 0x7FFFu; }
-// 2^(133 - E) as a product of two factors that are normal numbers.
-struct SavedScale {
-    float first, second;
-    __device__ __forceinline__ explicit SavedScale(uint32_t E) {
-        first = __uint_as_float((E >= 6u ? 260u - E : 254u) << 23);
-        second = E >= 6u ? 1.0f : __uint_as_float((133u - E) << 23);
-    }
-};
-__device__ __forceinline__ int saved_code(float x, const SavedScale& s) {
-    const float y = __fmul_rn(__fmul_rn(x, s.first), s.second);
-    const int q = min(127, max(-127, __float2int_rn(y)));
-    return fabsf(x) <= 3.4e38f ? q : -128;
-}
-__device__ __forceinline__ float saved_value(int code, uint32_t E) {
-    const float v = __fmul_rn(__fmul_rn((float)code, 0.015625f), __uint_as_float(E << 23));
-    return code == -128 ? __uint_as_float(0x7FC00000u) : v;
-}
-// Eight values of a lane from their codes.
-__device__ __forceinline__ void saved_values8(uint2 codes, uint32_t E, float (&v)[8]) {
+__device__ __forceinline__ uint32_t largest_finite8(const uint32_t (&w)[4]) {
+    const uint32_t m = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
+    uint32_t largest = max(m & 0xFFFFu, m >> 16);
+    if (largest >= 0x7F80u) {
+        largest = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = saved_value((int)(int8_t)((e < 4 ? codes.x : codes.y) >> (8 * (e & 3))), E);
+        for (int e = 0; e < 4; ++e) largest = max(largest, max(finite_bits(w[e] & 0xFFFFu), finite_bits(w[e] >> 16)));
+    }
+    return largest;
 }
+__device__ __forceinline__ uint32_t saved_exponent(uint32_t largest) { return largest >> 7 > 1u ? largest >> 7 : 1u; }
+
+// Eight values' codes.  Adding 3 2^22 rounds a small number to a whole one (ties to even) in the float's low bits; the eight
+// sums are packed by multiplying them into place and taking off what the exponents' bits add up to.  128 more in each keeps
+// borrows out, and comes off as the bytes' top bits.
+__device__ __forceinline__ uint2 saved_codes8(const uint32_t (&w)[4], uint32_t E) {
+    const float up = __uint_as_float((E >= 6u ? 260u - E : 254u) << 23);   // 2^(133 - E), or as much of it as a float holds
+    constexpr float kRound = 12582912.0f + 128.0f;
+    constexpr uint32_t kBits = 0x4B400000u, kAll = kBits * 0x01010101u;
+    uint32_t q[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t sum = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float y = __fmul_rn(half_of(w, h * 4 + e), up);
+            if (E < 6u) y = __fmul_rn(y, __uint_as_float((133u - E) << 23));
+            y = __fadd_rn(fminf(fmaxf(y, -127.0f), 127.0f), kRound);   // +-127.5 is the one that would leave the range
+            sum += __float_as_uint(y) << (8 * e);
+        }
+        q[h] = (sum - kAll) ^ 0x80808080u;
+    }
+    const uint32_t m = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
+    if (max(m & 0xFFFFu, m >> 16) >= 0x7F80u) {   // rare
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t half = (e & 1) ? w[e >> 1] >> 16 : w[e >> 1];
+            if ((half & 0x7F80u) == 0x7F80u) q[e >> 2] = (q[e >> 2] & ~(0xFFu << (8 * (e & 3)))) | (0x80u << (8 * (e & 3)));
+        }
+    }
+    return make_uint2(q[0], q[1]);
+}
+
+// Eight values from their codes, exactly: a byte under the exponent of 2^23 is 2^23 + code + 128.
+__device__ __forceinline__ void saved_values8(uint2 codes, uint32_t E, float (&v)[8]) {
+    // 2^(E - 133): a normal number from E = 7 on, below a subnormal one
+    const float step = __uint_as_float(E >= 7u ? (E - 6u) << 23 : (E == 0u ? 0u : 1u << (E + 16u)));
+    const uint32_t u[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float f = __uint_as_float(__byte_perm(u[e >> 2], 0x4B000000u, 0x7440 | (e & 3)));
+        v[e] = __fmul_rn(__fsub_rn(f, 8388736.0f), step);
+    }
+    const auto no_zero = [](uint32_t x) { return ((x - 0x01010101u) & ~x & 0x80808080u) == 0u; };
+    if (!no_zero(u[0]) || !no_zero(u[1])) {   // a zero byte is the code of what was not finite: rare
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (((u[e >> 2] >> (8 * (e & 3))) & 0xFFu) == 0u) v[e] = __uint_as_float(0x7FC00000u);
+    }
+}
+// Two values that are bf16 numbers.
+__device__ __forceinline__ uint32_t pack_exact(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
 #endif
 }  // namespace mosaic

@@ -40,15 +40,52 @@ struct GatedSlope {
     int64_t ld_h;
     int64_t rows, cols, band;
     int act;
-    float *z_sums, *u_sums;            // [bands, cols] column sums of the unrounded dz and du, or null
+    float *z_sums, *u_sums;            // [bands, cols] column sums of the unrounded dz and du, with SUMS
 };
 
-// A warp takes 256 columns, a lane eight of them, the CTA's eight warps every eighth row of its band; the warps' column sums
-// meet in shared memory in their order.
-template <bool VEC, bool SAVED>
+// What a lane reads of a row.
+template <bool VEC, bool SAVED> struct SlopeRow {
+    uint32_t dh[4], z[SAVED ? 2 : 4], u[SAVED ? 2 : 4], ze, ue;
+    __device__ __forceinline__ void load(const GatedSlope& a, int64_t r, int64_t c0, uint4* turn) {
+        const int64_t c = c0 + ((int)threadIdx.x & 31) * kLaneCols;
+        lane_load8<VEC>(a.dh + r * a.ld_dh, c0, a.cols, turn, dh);
+        if constexpr (SAVED) {
+            z[0] = z[1] = u[0] = u[1] = 0u;
+            ze = ue = 1u;
+            if (c < a.cols) {
+                const uint2 zq = *reinterpret_cast<const uint2*>(a.z8.codes + r * a.z8.ldc + c), uq = *reinterpret_cast<const uint2*>(a.u8.codes + r * a.u8.ldc + c);
+                z[0] = zq.x; z[1] = zq.y;
+                u[0] = uq.x; u[1] = uq.y;
+                ze = a.z8.exponents[r * a.z8.lde + c / kSavedGroup];
+                ue = a.u8.exponents[r * a.u8.lde + c / kSavedGroup];
+            }
+        } else {
+            lane_load8<VEC>(a.z + r * a.ld_z, c0, a.cols, turn, z);
+            lane_load8<VEC>(a.u + r * a.ld_u, c0, a.cols, turn, u);
+        }
+    }
+    __device__ __forceinline__ void values(float (&d)[8], float (&zv)[8], float (&uv)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = half_of(dh, e);
+        if constexpr (SAVED) {
+            saved_values8(make_uint2(z[0], z[1]), ze, zv);
+            saved_values8(make_uint2(u[0], u[1]), ue, uv);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                zv[e] = half_of(z, e);
+                uv[e] = half_of(u, e);
+            }
+        }
+    }
+};
+
+// A warp takes 256 columns, a lane eight of them, the CTA's eight warps every eighth row of its band, the next row on its way
+// while one is computed; with SUMS the warps' column sums meet in shared memory in their order.
+template <bool VEC, bool SAVED, bool SUMS>
 __global__ void __launch_bounds__(32 * 8) gated_slope_kernel(const __grid_constant__ GatedSlope a) {
     constexpr int kWarps = 8;
-    __shared__ float sums[kWarps][kWarpCols];
+    __shared__ float sums[SUMS ? kWarps : 1][kWarpCols];
     __shared__ uint4 turns[VEC ? 1 : kWarps][32];
     allow_next_kernel();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -57,33 +94,13 @@ __global__ void __launch_bounds__(32 * 8) gated_slope_kernel(const __grid_consta
     const int64_t r0 = (int64_t)blockIdx.y * a.band, r1 = r0 + a.band < a.rows ? r0 + a.band : a.rows;
     await_previous_kernel();
     float zs[8] = {}, us[8] = {};
+    SlopeRow<VEC, SAVED> next;
+    if (r0 + warp < r1) next.load(a, r0 + warp, c0, turn);
+#pragma unroll 1
     for (int64_t r = r0 + warp; r < r1; r += kWarps) {
-        uint32_t w[4];
         float dh[8], z[8], u[8];
-        lane_load8<VEC>(a.dh + r * a.ld_dh, c0, a.cols, turn, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dh[e] = half_of(w, e);
-        if (SAVED) {
-            uint2 zq = make_uint2(0u, 0u), uq = zq;
-            uint32_t ze = 1, ue = 1;
-            if (c < a.cols) {
-                zq = *reinterpret_cast<const uint2*>(a.z8.codes + r * a.z8.ldc + c);
-                uq = *reinterpret_cast<const uint2*>(a.u8.codes + r * a.u8.ldc + c);
-                ze = a.z8.exponents[r * a.z8.lde + c / kSavedGroup];
-                ue = a.u8.exponents[r * a.u8.lde + c / kSavedGroup];
-            }
-            saved_values8(zq, ze, z);
-            saved_values8(uq, ue, u);
-        } else {
-            uint32_t v[4];
-            lane_load8<VEC>(a.z + r * a.ld_z, c0, a.cols, turn, w);
-            lane_load8<VEC>(a.u + r * a.ld_u, c0, a.cols, turn, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                z[e] = half_of(w, e);
-                u[e] = half_of(v, e);
-            }
-        }
+        next.values(dh, z, u);
+        if (r + kWarps < r1) next.load(a, r + kWarps, c0, turn);
         // dz and du are rounded to bf16 here because the tensor cores take bf16; the column sums are not
         uint32_t pz[4], pu[4], ph[4];
         const auto pass = [&](int act) {
@@ -95,14 +112,16 @@ __global__ void __launch_bounds__(32 * 8) gated_slope_kernel(const __grid_consta
                 z[e] = __fmul_rn(__fmul_rn(dh[e], u[e]), slope);
                 dh[e] = __fmul_rn(dh[e], h[e]);
                 h[e] = __fmul_rn(h[e], u[e]);
-                zs[e] = __fadd_rn(zs[e], z[e]);
-                us[e] = __fadd_rn(us[e], dh[e]);
+                if (SUMS) {
+                    zs[e] = __fadd_rn(zs[e], z[e]);
+                    us[e] = __fadd_rn(us[e], dh[e]);
+                }
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                pz[e] = pack_bf16(z[2 * e], z[2 * e + 1]);
-                pu[e] = pack_bf16(dh[2 * e], dh[2 * e + 1]);
-                ph[e] = pack_bf16(h[2 * e], h[2 * e + 1]);
+                pz[e] = pack2(z[2 * e], z[2 * e + 1]);
+                pu[e] = pack2(dh[2 * e], dh[2 * e + 1]);
+                ph[e] = pack2(h[2 * e], h[2 * e + 1]);
             }
         };
         switch (a.act) {   // one branch a row, then straight code
@@ -117,34 +136,53 @@ __global__ void __launch_bounds__(32 * 8) gated_slope_kernel(const __grid_consta
         }
         if (a.h != nullptr) lane_store8<VEC>(a.h + r * a.ld_h, c0, a.cols, turn, ph);
     }
+    if constexpr (SUMS) {
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        float* to = which == 0 ? a.z_sums : a.u_sums;
-        if (to == nullptr) continue;
-        __syncthreads();
+        for (int which = 0; which < 2; ++which) {
+            __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums[warp][lane * 8 + e] = which == 0 ? zs[e] : us[e];
-        __syncthreads();
-        const int64_t col = c0 + threadIdx.x;
-        if (col >= a.cols) continue;
-        float total = 0.0f;
-        for (int w = 0; w < kWarps; ++w) total = __fadd_rn(total, sums[w][threadIdx.x]);
-        to[(int64_t)blockIdx.y * a.cols + col] = total;
+            for (int e = 0; e < 8; ++e) sums[warp][lane * 8 + e] = which == 0 ? zs[e] : us[e];
+            __syncthreads();
+            const int64_t col = c0 + threadIdx.x;
+            if (col >= a.cols) continue;
+            float total = 0.0f;
+            for (int w = 0; w < kWarps; ++w) total = __fadd_rn(total, sums[w][threadIdx.x]);
+            (which == 0 ? a.z_sums : a.u_sums)[(int64_t)blockIdx.y * a.cols + col] = total;
+        }
     }
 }
 
-int run_gated_slope(const GatedSlope& a, bool vec, bool saved, cudaStream_t st) {
-    if (a.rows == 0) return MOSAIC_OK;
-    using Kernel = void (*)(GatedSlope);
-    const Kernel kernel = vec ? (saved ? gated_slope_kernel<true, true> : gated_slope_kernel<true, false>)
-                              : (saved ? gated_slope_kernel<false, true> : gated_slope_kernel<false, false>);
-    Launch l(dim3((unsigned)((a.cols + kWarpCols - 1) / kWarpCols), (unsigned)bands_of(a.rows)), 32 * 8, 0, st);
-    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, kernel, a));
-    return MOSAIC_OK;
+// Sums over the bands: of dz and, in the grid's second half, of du.
+__global__ void __launch_bounds__(kSumCols) gated_sums_kernel(const float* z_sums, const float* u_sums, int64_t bands, int64_t cols, uint16_t* z_out, uint16_t* u_out) {
+    allow_next_kernel();
+    await_previous_kernel();
+    const int64_t c = (int64_t)blockIdx.x * kSumCols + threadIdx.x;
+    const float* from = blockIdx.y == 0 ? z_sums : u_sums;
+    uint16_t* out = blockIdx.y == 0 ? z_out : u_out;
+    if (c >= cols || out == nullptr) return;
+    float sum = 0.0f;
+#pragma unroll 8
+    for (int64_t b = 0; b < bands; ++b) sum = __fadd_rn(sum, from[b * cols + c]);
+    out[c] = f32_to_bf16(sum);
 }
-int run_column_sums(const float* partial, int64_t bands, int64_t cols, void* out, cudaStream_t st) {
-    Launch l(dim3((unsigned)((cols + kSumCols - 1) / kSumCols)), kSumCols, 0, st);
-    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, column_sum_kernel, partial, bands, cols, static_cast<uint16_t*>(out)));
+
+int run_gated_slope(const GatedSlope& a, bool vec, bool saved, void* dbias_gate, void* dbias_up, cudaStream_t st) {
+    const bool sums = dbias_gate != nullptr || dbias_up != nullptr;
+    const int64_t bands = bands_of(a.rows);
+    if (bands > 0) {
+        using Kernel = void (*)(GatedSlope);
+        static const Kernel kernels[2][2][2] = {{{gated_slope_kernel<false, false, false>, gated_slope_kernel<false, false, true>},
+                                                 {gated_slope_kernel<false, true, false>, gated_slope_kernel<false, true, true>}},
+                                                {{gated_slope_kernel<true, false, false>, gated_slope_kernel<true, false, true>},
+                                                 {gated_slope_kernel<true, true, false>, gated_slope_kernel<true, true, true>}}};
+        Launch l(dim3((unsigned)((a.cols + kWarpCols - 1) / kWarpCols), (unsigned)bands), 32 * 8, 0, st);
+        MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, kernels[vec ? 1 : 0][saved ? 1 : 0][sums ? 1 : 0], a));
+    }
+    if (sums) {
+        Launch l(dim3((unsigned)((a.cols + kSumCols - 1) / kSumCols), 2), kSumCols, 0, st);
+        MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, gated_sums_kernel, static_cast<const float*>(a.z_sums), static_cast<const float*>(a.u_sums), bands, a.cols,
+                                           static_cast<uint16_t*>(dbias_gate), static_cast<uint16_t*>(dbias_up)));
+    }
     return MOSAIC_OK;
 }
 
@@ -331,8 +369,8 @@ extern "C" int mosaic_gated_linear_backward(const void* dH, int64_t lddh, const 
     const int64_t bands = bands_of(tokens);
     if (want_db) {
         const size_t sums = align_up((size_t)bands * (size_t)channels * 4u, 256);
-        if (dbias_gate != nullptr) s.z_sums = reinterpret_cast<float*>(scratch);
-        if (dbias_up != nullptr) s.u_sums = reinterpret_cast<float*>(scratch + sums);
+        s.z_sums = reinterpret_cast<float*>(scratch);
+        s.u_sums = reinterpret_cast<float*>(scratch + sums);
         scratch += 2 * sums;
     }
     Matrix dz = plain(dh), du = plain(dh);
@@ -344,9 +382,7 @@ extern "C" int mosaic_gated_linear_backward(const void* dH, int64_t lddh, const 
     }
     const bool vec = dh.tma_ok() && (saved || (z.tma_ok() && u.tma_ok())) && (H == nullptr || h.tma_ok());
     if (dX != nullptr || want_dw || want_db || H != nullptr)
-        if ((rc = run_gated_slope(s, vec, saved, st)) != MOSAIC_OK) return rc;
-    if (dbias_gate != nullptr && (rc = run_column_sums(s.z_sums, bands, channels, dbias_gate, st)) != MOSAIC_OK) return rc;
-    if (dbias_up != nullptr && (rc = run_column_sums(s.u_sums, bands, channels, dbias_up, st)) != MOSAIC_OK) return rc;
+        if ((rc = run_gated_slope(s, vec, saved, dbias_gate, dbias_up, st)) != MOSAIC_OK) return rc;
     if (tokens == 0) {   // empty sums
         const size_t wide = (size_t)in_features * 2u;
         if (dW_gate != nullptr) MOSAIC_CUDA_TRY(cudaMemset2DAsync(dW_gate, (size_t)lddwg * 2u, 0, wide, (size_t)channels, st));

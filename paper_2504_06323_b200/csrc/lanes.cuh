@@ -67,6 +67,5 @@ template <bool VEC> __device__ __forceinline__ void lane_store8(uint16_t* row, i
 __device__ __forceinline__ float half_of(const uint32_t (&w)[4], int e) {
     return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) { return (uint32_t)f32_to_bf16(lo) | ((uint32_t)f32_to_bf16(hi) << 16); }
 #endif
 }  // namespace mosaic

@@ -32,6 +32,26 @@ __device__ __forceinline__ float scale_of(float largest) {
     return __uint_as_float(u & 0xFFF80000u);
 }
 
+// Eight codes, 8 added to each.  w / s is made correctly rounded from the correctly rounded reciprocal by one correction (Markstein's
+// division; every step but the last exact or harmless while nothing underflows, so tiny scales divide).  Adding 3 2^22 rounds
+// it to a whole number in the float's low bits; the eight are packed by multiplying them into place and taking off what
+// the exponents' bits add up to.
+__device__ __forceinline__ uint32_t codes_of8(const uint32_t (&w)[4], float s) {
+    const float r = __frcp_rn(s);
+    constexpr float kRound = 12582912.0f + 8.0f;
+    constexpr uint32_t kBits = 0x4B400000u, kAll = kBits * 0x11111111u;
+    uint32_t sum = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = half_of(w, e);
+        float y = __fmul_rn(x, r);
+        y = __fmaf_rn(__fmaf_rn(-y, s, x), r, y);
+        if (s < 7.8886091e-31f) y = __fdiv_rn(x, s);   // 2^-100
+        sum += __float_as_uint(__fadd_rn(fminf(fmaxf(y, -7.0f), 7.0f), kRound)) << (4 * e);
+    }
+    return sum - kAll;
+}
+
 template <bool VEC>
 __global__ void __launch_bounds__(32 * kPackWarps) quantize4_kernel(const uint16_t* W, int64_t ldw, int64_t rows, int64_t cols, const __grid_constant__ Weight4 out,
                                                                     unsigned chunks) {
@@ -48,26 +68,33 @@ __global__ void __launch_bounds__(32 * kPackWarps) quantize4_kernel(const uint16
     for (int r = 0; r < kPackRows; ++r) lane_load8<VEC>(W + (r0 + r < rows ? r0 + r : rows - 1) * ldw, c0, cols, turn, w[r]);
 #pragma unroll
     for (int r = 0; r < kPackRows; ++r) {
-        uint32_t bits = 0;   // of the largest magnitude: infinities and NaN are above all numbers
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bits = max(bits, max(w[r][e] & 0x7FFFu, (w[r][e] >> 16) & 0x7FFFu));
+        // the largest magnitude's bits: infinities and NaN are above all numbers
+        const uint32_t m = __vmaxu2(__vmaxu2(w[r][0] & 0x7FFF7FFFu, w[r][1] & 0x7FFF7FFFu), __vmaxu2(w[r][2] & 0x7FFF7FFFu, w[r][3] & 0x7FFF7FFFu));
+        uint32_t bits = max(m & 0xFFFFu, m >> 16);
         for (int o = 1; o < 1 << (out.shift - 3); o <<= 1) bits = max(bits, __shfl_xor_sync(0xFFFFFFFFu, bits, o));
         const float s = bits >= 0x7F80u ? __uint_as_float(0x7FC00000u) : scale_of(bf16_to_f32((uint16_t)bits));
         if (r0 + r >= rows || c >= (cols + 31) / 32 * 32) continue;
-        uint32_t packed = 0x88888888u;
-        if (s > 0.0f) {
-            packed = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int q = min(7, max(-7, __float2int_rn(__fdiv_rn(half_of(w[r], e), s))));
-                packed |= (uint32_t)(q + 8) << (4 * e);
-            }
-        }
-        *reinterpret_cast<uint32_t*>(out.codes + (r0 + r) * out.ldc + c / 2) = packed;
+        *reinterpret_cast<uint32_t*>(out.codes + (r0 + r) * out.ldc + c / 2) = s > 0.0f ? codes_of8(w[r], s) : 0x88888888u;
         if ((c & ((1 << out.shift) - 1)) == 0 && c < cols) out.scales[(r0 + r) * out.lds + (c >> out.shift)] = (uint16_t)(__float_as_uint(s) >> 16);
     }
 }
 
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+// -24 s, twice: exact
+__device__ __forceinline__ uint32_t minus24(uint32_t s2) { return fma_bf16x2(s2, 0xC1C0C1C0u, 0x80008000u); }
+// Codes i and i + 4 of a word (i = 0..3) as two bf16 weights, in three instructions: shifted to bits 3..6 of its half a code goes
+// under the exponent of 16, which makes it 16 + n with n = code + 8, and (16 + n) s - 24 s is one fma, exact because s has five
+// significant bits, 24 two and the result eight.  s2 and c2 hold s and -24 s twice.
+__device__ __forceinline__ uint32_t weights4(uint32_t word, int i, uint32_t s2, uint32_t c2) {
+    const uint32_t at = i == 0 ? word << 3 : word >> (4 * i - 3);
+    uint32_t sum;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(sum) : "r"(at), "r"(0x00780078u), "r"(0x41804180u));   // and, or: one instruction
+    return fma_bf16x2(sum, s2, c2);
+}
 template <bool VEC>
 __global__ void __launch_bounds__(32 * kPackWarps) dequantize4_kernel(const __grid_constant__ Weight4 in, int64_t rows, int64_t cols, uint16_t* W, int64_t ldw,
                                                                       unsigned chunks) {
@@ -80,43 +107,49 @@ __global__ void __launch_bounds__(32 * kPackWarps) dequantize4_kernel(const __gr
     if (c0 >= cols) return;
     await_previous_kernel();
     uint32_t q[kPackRows];
-    float s[kPackRows];
+    uint32_t s[kPackRows];
 #pragma unroll
     for (int r = 0; r < kPackRows; ++r) {
         const int64_t row = r0 + r < rows ? r0 + r : rows - 1;
         q[r] = 0x88888888u;
-        s[r] = 0.0f;
+        s[r] = 0u;
         if (c < cols) {
             q[r] = *reinterpret_cast<const uint32_t*>(in.codes + row * in.ldc + c / 2);
-            s[r] = bf16_to_f32(in.scales[row * in.lds + (c >> in.shift)]);
+            s[r] = in.scales[row * in.lds + (c >> in.shift)];
         }
     }
 #pragma unroll
     for (int r = 0; r < kPackRows; ++r) {
         if (r0 + r >= rows) break;
-        float v[8];
+        // a code under the exponent of 16 in each half of a word, then one exact fma; codes e and e + 4 come together
+        const uint32_t s2 = s[r] | (s[r] << 16), c2 = minus24(s2);
+        uint32_t f[4], w[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = __fmul_rn((float)((int)((q[r] >> (4 * e)) & 15u) - 8), s[r]);
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);   // exact
+        for (int i = 0; i < 4; ++i) f[i] = weights4(q[r], i, s2, c2);
+        w[0] = __byte_perm(f[0], f[1], 0x5410);
+        w[1] = __byte_perm(f[2], f[3], 0x5410);
+        w[2] = __byte_perm(f[0], f[1], 0x7632);
+        w[3] = __byte_perm(f[2], f[3], 0x7632);
         lane_store8<VEC>(W + (r0 + r) * ldw, c0, cols, turn, w);
     }
 }
 
 // ---------------------------------------------------------------- few tokens
-// The next tokens of up to k4Tokens sequences: the weights are read once, and what counts is that they stream.  A CTA takes 16
-// weight rows - with GATE eight of each matrix, so that one lane has both sums of a channel - and its warps deal out blocks of
-// 128 columns.  A lane loads 16 bytes, 32 codes, of two rows; each pair of codes becomes two bf16 weights in three
-// instructions: shifted to bits 3..6 of its half, put under the exponent of 16, which makes it 16 + (code + 8), and one fma,
-// (16 + n) s - 24 s, exact because s has five bits and 24 two.  The matrix instruction (16 rows, 8 tokens, 16 columns) does
-// not mind which columns it is given as long as both operands agree: a lane's own 32 columns, in the order that the
-// shifts yield, so neither operand moves between lanes.  Sums in fp32; over the warps in their order.
-constexpr int k4Warps = 8, k4Tokens = 32, k4Rows = 16, k4Block = 128;
+// The next tokens of up to eight sequences: the weights are read once, and what counts is that they stream.  A tile is 16 weight
+// rows - with GATE eight of each matrix, so that one lane has both sums of a channel.  The grid stays, one CTA an SM; `parts`
+// warps share a tile's columns in blocks of 128, the CTA's groups of warps take tile after tile.  A lane copies 16 bytes, 32 codes,
+// of two rows a block into its own place in shared memory, asynchronously, k4Ahead blocks a group of copies and two groups
+// in flight; it reads them back itself, so no thread waits for another.  The matrix instruction (16 rows, 8 tokens, 16
+// columns) does not mind which columns it is given as long as both operands agree: a lane's own 32 columns, in the order in
+// which codes become weights, so that nothing moves between lanes; X lies in shared memory in that order.  Sums in fp32;
+// over a tile's warps in their order.
+constexpr int k4Warps = 24, k4Tokens = 8, k4Rows = 16, k4Block = 128, k4Ahead = 2;
+constexpr size_t k4Ring = 2 * k4Ahead * 1024;   // a warp's codes in flight
 
 struct Few4Args {
     const uint16_t* x;                 // rows on 16-byte boundaries
-    int64_t ldx, tokens, outputs, cols;
+    int64_t ldx, outputs, cols;
+    int tokens, tiles, parts;
     Weight4 w, w2;                     // w2: GATE
     const uint16_t *bias, *bias2, *resid;
     int64_t ld_resid;
@@ -125,101 +158,152 @@ struct Few4Args {
     int64_t ldy;
 };
 
-__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t d;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-}
-// Codes i and i + 4 of a word (i = 0..3) as two bf16 weights; s2 and c2 hold s and -24 s twice.
-__device__ __forceinline__ uint32_t weights4(uint32_t word, int i, uint32_t s2, uint32_t c2) {
-    const uint32_t at = i == 0 ? word << 3 : word >> (4 * i - 3);
-    return fma_bf16x2((at & 0x00780078u) | 0x41804180u, s2, c2);
-}
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int NT, bool GATE>
+__device__ __forceinline__ void copy16_async(void* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <bool GATE>
 __global__ void __launch_bounds__(32 * k4Warps) few4_kernel(const __grid_constant__ Few4Args a) {
-    constexpr int kOutputs = GATE ? k4Rows / 2 : k4Rows, kCells = k4Rows * 8 * NT, kAhead = NT == 1 ? 4 : 2;
-    __shared__ float part[k4Warps][kCells];
+    constexpr int kOutputs = GATE ? k4Rows / 2 : k4Rows;
+    extern __shared__ uint4 smem4[];
+    __shared__ float partial[k4Warps][8 * k4Rows];
     allow_next_kernel();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int64_t o0 = (int64_t)blockIdx.x * kOutputs;
-    // the lane's two rows: past the end the first again, not stored
-    const int64_t lo = o0 + g < a.outputs ? o0 + g : o0, hi = GATE ? lo : (o0 + g + 8 < a.outputs ? o0 + g + 8 : o0);
-    const Weight4& second = GATE ? a.w2 : a.w;
-    const uint8_t *code0 = a.w.codes + lo * a.w.ldc, *code1 = second.codes + hi * second.ldc;
-    const uint16_t *scale0 = a.w.scales + lo * a.w.lds, *scale1 = second.scales + hi * second.lds;
-    float acc[NT][4] = {};
+    const int warps = (int)blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int parts = a.parts, groups = warps / parts, part = warp % parts;
+    const int blocks = (int)((a.cols + k4Block - 1) / k4Block), steps = (blocks + parts * k4Ahead - 1) / (parts * k4Ahead);
+    const int row4 = blocks * 16 + 4, hop = parts * k4Block;          // columns from one of a warp's blocks to its next
+    uint4* ring = smem4 + warp * (int)(k4Ring / 16) + lane;            // [group of copies][block][row][lane]
+    uint4* x4 = smem4 + warps * (int)(k4Ring / 16);                    // [token][block][word of eight columns][quarter of the block], 64 bytes between tokens
     await_previous_kernel();
-    const int blocks = (int)((a.cols + k4Block - 1) / k4Block);
-#pragma unroll 1
-    for (int b0 = warp; b0 < blocks; b0 += k4Warps * kAhead) {
-        uint4 q0[kAhead], q1[kAhead];
-        uint32_t s0[kAhead], s1[kAhead];
+
+    // where the lane reads next: its two rows' codes and scales at a step's first block
+    const Weight4& second = GATE ? a.w2 : a.w;
+    const int col0 = part * k4Block + t * 32, hop0 = hop >> a.w.shift, hop1 = hop >> second.shift;
+    const uint8_t *code0 = nullptr, *code1 = nullptr;
+    const uint16_t *scale0 = nullptr, *scale1 = nullptr;
+    int left = 0;                      // columns from the lane's first of the step on
+    const auto begin = [&](int tile) {
+        const int64_t o0 = (int64_t)tile * kOutputs;
+        // past the end the tile's first row, not stored
+        const int64_t lo = o0 + g < a.outputs ? o0 + g : o0, hi = GATE ? lo : (o0 + g + 8 < a.outputs ? o0 + g + 8 : o0);
+        code0 = a.w.codes + lo * a.w.ldc + (col0 >> 1);
+        code1 = second.codes + hi * second.ldc + (col0 >> 1);
+        scale0 = a.w.scales + lo * a.w.lds + (col0 >> a.w.shift);
+        scale1 = second.scales + hi * second.lds + (col0 >> second.shift);
+        left = (int)a.cols - col0;
+    };
+    uint32_t next[k4Ahead];            // both rows' scales of the step on its way; 0 where there are no columns
+    const auto fetch = [&](uint4* to) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int64_t k = (int64_t)(b0 + u * k4Warps) * k4Block + t * 32;
-            q0[u] = q1[u] = make_uint4(0u, 0u, 0u, 0u);
-            s0[u] = s1[u] = 0u;
-            if (k < a.cols) {
-                q0[u] = ld_stream16(code0 + (k >> 1));
-                q1[u] = ld_stream16(code1 + (k >> 1));
-                s0[u] = scale0[k >> a.w.shift];
-                s1[u] = scale1[k >> second.shift];
+        for (int u = 0; u < k4Ahead; ++u) {
+            next[u] = 0u;
+            if (left > u * hop) {
+                copy16_async(to + u * 64, code0 + u * (hop / 2));
+                copy16_async(to + u * 64 + 32, code1 + u * (hop / 2));
+                next[u] = scale0[u * hop0] | ((uint32_t)scale1[u * hop1] << 16);
             }
         }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (b0 + u * k4Warps >= blocks) break;
-            const int64_t k = (int64_t)(b0 + u * k4Warps) * k4Block + t * 32;
-            const uint32_t sa = s0[u] | (s0[u] << 16), sb = s1[u] | (s1[u] << 16);
-            const uint32_t ca = fma_bf16x2(sa, 0xC1C0C1C0u, 0x80008000u), cb = fma_bf16x2(sb, 0xC1C0C1C0u, 0x80008000u);   // -24 s
-#pragma unroll
-            for (int wd = 0; wd < 4; ++wd) {
-                const uint32_t wa = wd == 0 ? q0[u].x : wd == 1 ? q0[u].y : wd == 2 ? q0[u].z : q0[u].w;
-                const uint32_t wb = wd == 0 ? q1[u].x : wd == 1 ? q1[u].y : wd == 2 ? q1[u].z : q1[u].w;
-                uint32_t fa[4], fb[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    fa[i] = weights4(wa, i, sa, ca);
-                    fb[i] = weights4(wb, i, sb, cb);
-                }
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    uint32_t x[4] = {0u, 0u, 0u, 0u};
-                    const int64_t token = n * 8 + g, c = k + wd * 8;
-                    if (token < a.tokens) load8<true>(a.x + token * a.ldx, c, a.cols, x);
-                    // elements (0, 4), (1, 5), (2, 6), (3, 7), as the codes come
-                    mma_16816(acc[n], fa[0], fb[0], fa[1], fb[1], __byte_perm(x[0], x[2], 0x5410), __byte_perm(x[0], x[2], 0x7632));
-                    mma_16816(acc[n], fa[2], fb[2], fa[3], fb[3], __byte_perm(x[1], x[3], 0x5410), __byte_perm(x[1], x[3], 0x7632));
-                }
-            }
-        }
+        copies_commit();
+        code0 += k4Ahead * (hop / 2);
+        code1 += k4Ahead * (hop / 2);
+        scale0 += k4Ahead * hop0;
+        scale1 += k4Ahead * hop1;
+        left -= k4Ahead * hop;
+    };
+    const int stride = groups * (int)gridDim.x;
+    int tile = (warp / parts) * (int)gridDim.x + (int)blockIdx.x, half = 0;
+    if (tile < a.tiles) {
+        begin(tile);
+        fetch(ring);
     }
-    // a lane holds rows g and g + 8 of tokens 2 t and 2 t + 1
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) part[warp][(n * 8 + 2 * t + (e & 1)) * k4Rows + g + (e >> 1) * 8] = acc[n][e];
-    __syncthreads();
-    for (int at = threadIdx.x; at < kOutputs * 8 * NT; at += 32 * k4Warps) {
-        const int token = at / kOutputs, r = at % kOutputs;
-        const int64_t o = o0 + r;
-        if (token >= a.tokens || o >= a.outputs) continue;
-        float v = 0.0f, u = 0.0f;
-        for (int w = 0; w < k4Warps; ++w) v = __fadd_rn(v, part[w][token * k4Rows + r]);
-        v = __fadd_rn(v, a.bias != nullptr ? bf16_to_f32(a.bias[o]) : 0.0f);
-        v = activate(v, a.act);
-        if (GATE) {
-            for (int w = 0; w < k4Warps; ++w) u = __fadd_rn(u, part[w][token * k4Rows + r + 8]);
-            v = __fmul_rn(v, __fadd_rn(u, a.bias2 != nullptr ? bf16_to_f32(a.bias2[o]) : 0.0f));
+    for (int token = 0; token < a.tokens; ++token)
+        for (int at = (int)threadIdx.x; at < blocks * 16; at += (int)blockDim.x) {
+            uint32_t x[4];
+            load8<true>(a.x + token * a.ldx, (int64_t)(at >> 4) * k4Block + (at & 3) * 32 + ((at >> 2) & 3) * 8, a.cols, x);
+            // elements (0, 4), (1, 5), (2, 6), (3, 7), as the codes come
+            x4[token * row4 + at] = make_uint4(__byte_perm(x[0], x[2], 0x5410), __byte_perm(x[0], x[2], 0x7632), __byte_perm(x[1], x[3], 0x5410),
+                                               __byte_perm(x[1], x[3], 0x7632));
         }
+    __syncthreads();
+    const uint4* mine = x4 + min(g, a.tokens - 1) * row4 + part * 16 + t;   // columns of the product beyond the last token repeat it and are not stored
+    const auto store = [&](int token, int64_t o, float v, float u) {
+        if (token >= a.tokens || o >= a.outputs) return;
+        v = activate(__fadd_rn(v, a.bias != nullptr ? bf16_to_f32(a.bias[o]) : 0.0f), a.act);
+        if (GATE) v = __fmul_rn(v, __fadd_rn(u, a.bias2 != nullptr ? bf16_to_f32(a.bias2[o]) : 0.0f));
         if (a.resid != nullptr) v = __fadd_rn(v, bf16_to_f32(a.resid[token * a.ld_resid + o]));
         a.y[token * a.ldy + o] = f32_to_bf16(v);
+    };
+    for (int first = (int)blockIdx.x; first < a.tiles; first += stride, tile += stride) {   // the same turns for all of the CTA's warps
+        float acc[4] = {}, odd[4] = {};
+        if (tile < a.tiles) {
+#pragma unroll 1
+            for (int step = 0; step < steps; ++step, half ^= 1) {
+                uint32_t now[k4Ahead];
+#pragma unroll
+                for (int u = 0; u < k4Ahead; ++u) now[u] = next[u];
+                uint4* to = ring + (half ^ 1) * (k4Ahead * 64);
+                if (step + 1 < steps) {
+                    fetch(to);
+                    copies_wait<1>();
+                } else if (tile + stride < a.tiles) {
+                    begin(tile + stride);
+                    fetch(to);
+                    copies_wait<1>();
+                } else {
+                    copies_wait<0>();
+                }
+                const uint4 *from = ring + half * (k4Ahead * 64), *x = mine + step * (k4Ahead * parts * 16);
+#pragma unroll
+                for (int u = 0; u < k4Ahead; ++u) {
+                    if ((step * k4Ahead + u) * parts + part >= blocks) break;
+                    const uint4 qa = from[u * 64], qb = from[u * 64 + 32];   // of no copy where there are no columns: any codes, times a scale of zero
+                    const uint32_t sa = __byte_perm(now[u], 0u, 0x1010), sb = __byte_perm(now[u], 0u, 0x3232), ca = minus24(sa), cb = minus24(sb);
+#pragma unroll
+                    for (int wd = 0; wd < 4; ++wd) {
+                        const uint32_t wa = wd == 0 ? qa.x : wd == 1 ? qa.y : wd == 2 ? qa.z : qa.w, wb = wd == 0 ? qb.x : wd == 1 ? qb.y : wd == 2 ? qb.z : qb.w;
+                        const uint4 xv = x[u * parts * 16 + wd * 4];
+                        mma_16816(acc, weights4(wa, 0, sa, ca), weights4(wb, 0, sb, cb), weights4(wa, 1, sa, ca), weights4(wb, 1, sb, cb), xv.x, xv.y);
+                        mma_16816(odd, weights4(wa, 2, sa, ca), weights4(wb, 2, sb, cb), weights4(wa, 3, sa, ca), weights4(wb, 3, sb, cb), xv.z, xv.w);
+                    }
+                }
+            }
+        }
+        // a lane holds rows g and g + 8 of tokens 2 t and 2 t + 1
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = __fadd_rn(acc[e], odd[e]);
+        if (parts == 1) {
+            if (tile < a.tiles) {
+                const int64_t o = (int64_t)tile * kOutputs + g;
+                store(2 * t, o, acc[0], acc[2]);
+                store(2 * t + 1, o, acc[1], acc[3]);
+                if (!GATE) {
+                    store(2 * t, o + 8, acc[2], 0.0f);
+                    store(2 * t + 1, o + 8, acc[3], 0.0f);
+                }
+            }
+            continue;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) partial[warp][(2 * t + (e & 1)) * k4Rows + g + (e >> 1) * 8] = acc[e];
+        __syncthreads();
+        for (int at = part * 32 + lane; at < kOutputs * a.tokens; at += parts * 32) {
+            const int token = at / kOutputs, r = at % kOutputs;
+            float v = 0.0f, u = 0.0f;
+            for (int w = warp - part; w < warp - part + parts; ++w) {
+                v = __fadd_rn(v, partial[w][token * k4Rows + r]);
+                if (GATE) u = __fadd_rn(u, partial[w][token * k4Rows + r + 8]);
+            }
+            if (tile < a.tiles) store(token, (int64_t)tile * kOutputs + r, v, u);
+        }
+        __syncthreads();
     }
 }
 
@@ -270,18 +354,52 @@ int check_pack(const void* W, int64_t rows, int64_t cols, int64_t ldw, int dtype
     return s.meets(m) || spans_meet(s.codes, s.n_codes, s.scales, s.n_scales) ? MOSAIC_ERR_ALIASING : MOSAIC_OK;
 }
 
+// X in shared memory beside the codes in flight of so many warps (0: it does not fit).
+constexpr size_t k4Smem = 212 * 1024;
+size_t few4_x_bytes(int64_t tokens, int64_t cols) { return (size_t)tokens * ((size_t)((cols + k4Block - 1) / k4Block) * (k4Block * 2) + 64); }
+int few4_warps(int64_t tokens, int64_t cols) {
+    if (tokens > k4Tokens || cols > (1 << 20)) return 0;
+    const size_t x = few4_x_bytes(tokens, cols);
+    const int warps = x < k4Smem ? (int)((k4Smem - x) / k4Ring) : 0;
+    return warps >= k4Warps ? k4Warps : warps >= 8 ? warps : 0;
+}
+bool is_few4(int64_t tokens, int64_t cols) { return few4_warps(tokens, cols) > 0; }
+
 // Scratch: few tokens need an aligned copy of X if it is not; many need the weights in bf16 as well.
 size_t workspace4(const Matrix& x, int64_t outputs, int matrices) {
     size_t need = x.tma_ok() ? 0 : x.padded_bytes();
-    if (x.rows > k4Tokens) need += (size_t)matrices * Matrix{nullptr, outputs, x.cols, x.cols}.padded_bytes();
+    if (!is_few4(x.rows, x.cols)) need += (size_t)matrices * Matrix{nullptr, outputs, x.cols, x.cols}.padded_bytes();
     return need;
 }
 
-template <bool GATE> int launch_few4(const Few4Args& a, cudaStream_t st) {
+template <bool GATE> int launch_few4(Few4Args a, cudaStream_t st) {
     constexpr int kOutputs = GATE ? k4Rows / 2 : k4Rows;
-    Launch l(dim3((unsigned)((a.outputs + kOutputs - 1) / kOutputs)), 32 * k4Warps, 0, st);
-    const auto kernel = a.tokens <= 8 ? few4_kernel<1, GATE> : a.tokens <= 16 ? few4_kernel<2, GATE> : few4_kernel<4, GATE>;
-    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, kernel, a));
+    static DeviceCache opted;
+    if (opted.get([]() -> int {
+            if (cudaFuncSetAttribute(few4_kernel<GATE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k4Smem) == cudaSuccess) return 1;
+            (void)cudaGetLastError();
+            return -1;
+        }) < 0)
+        return MOSAIC_ERR_CUDA;
+    a.tiles = (int)((a.outputs + kOutputs - 1) / kOutputs);
+    const int most = few4_warps(a.tokens, a.cols), ctas = a.tiles < sm_count() ? a.tiles : sm_count(), blocks = (int)((a.cols + k4Block - 1) / k4Block);
+    // How many warps share a tile and how many tiles a CTA has in hand: the fewest blocks one after another, and a few
+    // more where sums meet.
+    const int each = (a.tiles + ctas - 1) / ctas;
+    int groups = 1;
+    int64_t best = 0;
+    for (int parts = 1; parts <= most && parts <= blocks; ++parts) {
+        const int g = most / parts < each ? most / parts : each, turns = (each + g - 1) / g;
+        const int64_t cost = (int64_t)turns * ((blocks + parts - 1) / parts + (parts > 1 ? 3 : 1));
+        if (parts == 1 || cost < best) {
+            best = cost;
+            a.parts = parts;
+            groups = (each + turns - 1) / turns;
+        }
+    }
+    const int warps = groups * a.parts;
+    Launch l(dim3((unsigned)ctas), 32 * warps, few4_x_bytes(a.tokens, a.cols) + warps * k4Ring, st);
+    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, few4_kernel<GATE>, a));
     return MOSAIC_OK;
 }
 
@@ -343,10 +461,10 @@ extern "C" int mosaic_linear4(const void* X, int64_t ldx, const mosaic_weight4* 
     if (tokens == 0) return MOSAIC_OK;
     char* scratch = static_cast<char*>(ws);
     if ((rc = readable(x, &scratch, st)) != MOSAIC_OK) return rc;
-    if (tokens <= k4Tokens) {
+    if (is_few4(tokens, in_features)) {
         Few4Args a = {};
         a.x = static_cast<const uint16_t*>(x.p); a.ldx = x.ld;
-        a.tokens = tokens; a.outputs = out_features; a.cols = in_features;
+        a.tokens = (int)tokens; a.outputs = out_features; a.cols = in_features;
         a.w = as_weight4(W);
         a.bias = static_cast<const uint16_t*>(bias);
         a.resid = static_cast<const uint16_t*>(residual); a.ld_resid = ldr;
@@ -385,10 +503,10 @@ extern "C" int mosaic_gated_linear4(const void* X, int64_t ldx, const mosaic_wei
     if (tokens == 0) return MOSAIC_OK;
     char* scratch = static_cast<char*>(ws);
     if ((rc = readable(x, &scratch, st)) != MOSAIC_OK) return rc;
-    if (tokens <= k4Tokens) {
+    if (is_few4(tokens, in_features)) {
         Few4Args a = {};
         a.x = static_cast<const uint16_t*>(x.p); a.ldx = x.ld;
-        a.tokens = tokens; a.outputs = channels; a.cols = in_features;
+        a.tokens = (int)tokens; a.outputs = channels; a.cols = in_features;
         a.w = as_weight4(W_gate);
         a.w2 = as_weight4(W_up);
         a.bias = static_cast<const uint16_t*>(bias_gate);

@@ -160,7 +160,7 @@ def test_products4_refusals_need_no_device(lib, call):
 
 def test_products4_workspaces(lib):
     q, g = lib.mosaic_linear4_workspace_bytes, lib.mosaic_gated_linear4_workspace_bytes
-    assert q(A, 64, 32, 32, 64) == 0 and g(A, 64, 32, 32, 64) == 0
+    assert q(A, 64, 1, 32, 64) == 0 and g(A, 64, 1, 32, 64) == 0
     assert q(A, 64, api.FEW4_TOKENS, 32, 64) == 0 and q(A, 64, api.FEW4_TOKENS + 1, 32, 64) == 32 * 64 * 2 and g(A, 64, api.FEW4_TOKENS + 1, 32, 64) == 2 * 32 * 64 * 2
     assert q(A + 2, 64, 8, 32, 64) == 8 * 64 * 2 and q(A, 63, 8, 32, 63) == 8 * 64 * 2 and q(A, 63, 1, 32, 63) == 0
 
