@@ -108,6 +108,28 @@ def test_gated_alignment_changes_no_bit(m):
         check_gated(X, Wg, Wu, bg, bu, "silu", H2, Z, U)
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 40, 72), (5, 100, 264), (300, 1000, 520), (2049, 1256, 136), (600, 4104, 2048)])
+def test_gated_weights_lie_anywhere(m, n, k):
+    """Gate before up in memory or behind it, of equal or unequal pitch, far apart, or one and the same: the same bits."""
+    g = torch.Generator(device=DEV).manual_seed(m + n)
+    X, Wg, Wu, bg = matrix(m, k, g, -k % 8), matrix(n, k, g, scale=0.1), matrix(n, k, g, scale=0.1), vector(n, g)
+    ld = k + -k % 8
+    H, Z, U = empty(m, n), empty(m, n), empty(m, n)
+    seen = []
+    for gate_at, up_at, gate_ld, up_ld in ((0, 1, ld, ld), (1, 0, ld, ld), (0, 1, ld + 8, ld), (1, 0, ld, ld + 16), (0, 5, ld, ld)):
+        room = n * (ld + 16) + 64
+        buf = torch.full((6 * room,), float("nan"), device=DEV, dtype=torch.bfloat16)
+        place = lambda at, pitch, W: buf[at * room:at * room + n * pitch].view(n, pitch)[:, :k].copy_(W)  # noqa: E731
+        run_gated(X, place(gate_at, gate_ld, Wg), place(up_at, up_ld, Wu), H, bias_gate=bg, act="silu", Z=Z, U=U)
+        seen.append((H.clone(), Z.clone(), U.clone()))
+    check_gated(X, Wg, Wu, bg, None, "silu", *seen[0])
+    for other in seen[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(seen[0], other))
+    W = matrix(n, k, g, -k % 8, scale=0.1)
+    run_gated(X, W, W, H, bias_gate=bg, act="silu", Z=Z, U=U)
+    check_gated(X, W, W, bg, None, "silu", H, Z, U)
+
+
 @pytest.mark.parametrize("m", [0, 1, 3, 50])
 def test_gated_extremes(m):
     """Infinite and NaN inputs stay in their token; rows of zeros give zero; no tokens is legal."""
