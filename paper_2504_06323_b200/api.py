@@ -1078,7 +1078,7 @@ def mosaic_dequantize4(W4: Weight4, W, stream=None) -> None:
     _check(lib().mosaic_dequantize4(_weight4(W4, "W4", dev, rows, cols), rows, cols, wp, ldw, BF16, st), "mosaic_dequantize4")
 
 
-FEW4_TOKENS = 8   # beyond, the products may need scratch for a bf16 copy of the weights
+FEW4_TOKENS = 256   # beyond, the products need scratch for a bf16 copy of the weights
 
 
 def mosaic_linear4(X, W: Weight4, Y, bias=None, residual=None, act=ACT_NONE, status: torch.Tensor | None = None, ws: Workspace | None = None,
@@ -1096,7 +1096,7 @@ def mosaic_linear4(X, W: Weight4, Y, bias=None, residual=None, act=ACT_NONE, sta
     bp = _dense_or_none(bias, "bias", bf16, dev, n_out)
     sp = _dense_or_none(status, "status", torch.int32, dev, 1)
     L, sc, sn = lib(), None, 0
-    if xp & 15 or ldx & 7 or tokens > FEW4_TOKENS or tokens * n_in > 64000:
+    if xp & 15 or ldx & 7 or tokens > FEW4_TOKENS:
         need = L.mosaic_linear4_workspace_bytes(xp, ldx, tokens, n_out, n_in)
         if need:
             sc, sn = _ws(ws, dev).get(need, st or 0)
@@ -1119,7 +1119,7 @@ def mosaic_gated_linear4(X, W_gate: Weight4, W_up: Weight4, H, bias_gate=None, b
     bu = _dense_or_none(bias_up, "bias_up", bf16, dev, n)
     sp = _dense_or_none(status, "status", torch.int32, dev, 1)
     L, sc, sn = lib(), None, 0
-    if xp & 15 or ldx & 7 or tokens > FEW4_TOKENS or tokens * n_in > 64000:
+    if xp & 15 or ldx & 7 or tokens > FEW4_TOKENS:
         need = L.mosaic_gated_linear4_workspace_bytes(xp, ldx, tokens, n, n_in)
         if need:
             sc, sn = _ws(ws, dev).get(need, st or 0)

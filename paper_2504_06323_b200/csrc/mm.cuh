@@ -270,12 +270,6 @@ __device__ __forceinline__ void store4(uint16_t* p, const float (&y)[4], bool wo
     }
 }
 
-// One output tile of kMI x BN per cluster; its contraction is split over the cluster's CTAs.  Each of them adds up and writes
-// an equal share of the tile's columns: the others push their partial sums of it into its shared memory (the stages, free
-// by then), and it adds them in the CTAs' order.  Bound by the loads of a tile's operands into one SM (about 110 GB/s an
-// SM for wide tiles) or, with few tokens, by the weights' stream: 37 tokens, 4096 outputs from 8807, 18.0 us against
-// 11.2 of the weights alone; 512 tokens, 4096 from 4096, 23 us.  One CTA an SM (its stages fill shared memory), so a CTA
-// never waits for tensor memory that another one of this kernel holds.
 constexpr int kGateRows = 16;   // rows of A, then of A2, in kGate's tiles
 constexpr uint32_t kGateBox = kGateRows * kMC * 2;
 template <int MODE> constexpr int kTileI = MODE == kGate ? kMI / 2 : kMI;   // output elements of a tile's 128 rows
@@ -284,6 +278,146 @@ constexpr int kMRoles = 2;   // loader, MMA issue; then the epilogue: four warps
 __host__ __device__ constexpr int mm_warps(int bn) { return bn >= 256 ? 16 : bn >= 64 ? 8 : 4; }
 __host__ __device__ constexpr int mm_threads(int bn) { return 32 * (kMRoles + mm_warps(bn)); }
 
+// A complete accumulator of kMI rows and BN columns, n_cols of them of the output: into the output, or, of a contraction that
+// `split` CTAs share, into the shared memory of the CTAs that add it up, each `per` columns.  By warps kMRoles on, SETS of them
+// a quarter of tensor memory's lanes, which take chunks in turn.
+template <int BN, int MODE, int SETS>
+__device__ __forceinline__ void tile_out(const MmArgs& a, const Second<MODE>& second, uint32_t tmem, float* part, int per, int rank, int split, int n_cols,
+                                         int64_t i0, int64_t j0) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3;
+    constexpr int kChunk = BN < 32 ? 16 : 32;   // warps of a quarter take chunks in turn
+    const float bias = lane_bias(a, second, i0 + q * (kTileI<MODE> / 4));
+#pragma unroll 1
+    for (int c0 = ((warp - kMRoles) >> 2) * kChunk; c0 < n_cols; c0 += SETS * kChunk) {
+        float v[kChunk];
+        tmem_load<kChunk>(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c0, v);
+        if (split > 1) {
+            int owner = c0 / per, at = c0 - owner * per;
+            uint32_t to = cluster_addr(part + ((size_t)rank * per + at) * kMI + q * 32 + lane, owner);
+#pragma unroll
+            for (int e = 0; e < kChunk; ++e) {
+                if (c0 + e < n_cols) store_remote(to, v[e]);
+                to += kMI * 4;
+                if (++at == per) {
+                    at = 0;
+                    ++owner;
+                    to = cluster_addr(part + (size_t)rank * per * kMI + q * 32 + lane, owner < split ? owner : 0);
+                }
+            }
+        } else {
+            if constexpr (MODE == kGate) gate_epilogue<kChunk>(a, second.g, v, bias, i0 + q * kGateRows, j0 + c0, n_cols - c0);
+            else epilogue<kChunk>(a, v, bias, i0 + q * 32, j0 + c0, n_cols - c0);
+            __syncwarp();
+        }
+    }
+}
+
+// The sum of the CTAs' parts of this CTA's columns, and its epilogue.  Between it and tile_out the CTAs arrive at their barrier.
+template <int MODE, int THREADS>
+__device__ __forceinline__ void tile_join(const MmArgs& a, const Second<MODE>& second, const float* part, int per, int rank, int split, int n_cols, int64_t i0,
+                                          int64_t j0) {
+    if constexpr (MODE == kGate) {
+        // Four adjacent elements a thread and turn, from the partial sums of both matrices.
+        __syncwarp();
+        cluster_wait();
+        const int mine = n_cols - rank * per < per ? n_cols - rank * per : per;
+        for (int e = (int)threadIdx.x; e < mine * (kMI / 8); e += THREADS) {
+            const int col = e / (kMI / 8), quad = e % (kMI / 8);   // 16 quads a column: four of each 16 elements
+            const float4* from = reinterpret_cast<const float4*>(part) + col * (kMI / 4) + (quad >> 2) * 8 + (quad & 3);
+            float z[4] = {}, u[4] = {};
+            for (int p = 0; p < split; ++p) {   // in the CTAs' order
+                const float4 zp = from[p * per * (kMI / 4) + (second.g.swapped ? 4 : 0)], up = from[p * per * (kMI / 4) + (second.g.swapped ? 0 : 4)];
+                z[0] = __fadd_rn(z[0], zp.x);
+                z[1] = __fadd_rn(z[1], zp.y);
+                z[2] = __fadd_rn(z[2], zp.z);
+                z[3] = __fadd_rn(z[3], zp.w);
+                u[0] = __fadd_rn(u[0], up.x);
+                u[1] = __fadd_rn(u[1], up.y);
+                u[2] = __fadd_rn(u[2], up.z);
+                u[3] = __fadd_rn(u[3], up.w);
+            }
+            const int64_t oi = i0 + 4 * quad, oj = j0 + rank * per + col;
+            const bool words = a.pairs && oi + 4 <= a.n_i;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                if (oi + h >= a.n_i) break;
+                if (a.bias != nullptr) z[h] = __fadd_rn(z[h], bf16_to_f32(a.bias[oi + h]));
+                if (second.g.bias != nullptr) u[h] = __fadd_rn(u[h], bf16_to_f32(second.g.bias[oi + h]));
+            }
+            if (a.z != nullptr) store4(a.z + oj * a.ld_z + oi, z, words, a.n_i - oi);
+            if (second.g.u != nullptr) store4(second.g.u + oj * second.g.ld_u + oi, u, words, a.n_i - oi);
+            activate_all(z, a.act);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) z[h] = __fmul_rn(z[h], u[h]);
+            store4(a.out + oj * a.ld_out + oi, z, words, a.n_i - oi);
+        }
+        return;
+    }
+    // Four adjacent elements a thread and turn; the residual's are on their way while the partial sums come in.
+    constexpr int kTurns = 4;
+    const int mine = n_cols - rank * per < per ? n_cols - rank * per : per, quads = mine > 0 ? mine * (kMI / 4) : 0;
+    uint32_t r[kTurns][2];
+    const auto fetch = [&](int e0) {
+#pragma unroll
+        for (int u = 0; u < kTurns; ++u) {
+            const int e = e0 + u * THREADS;
+            const int64_t oi = i0 + 4 * (e % (kMI / 4)), oj = j0 + rank * per + e / (kMI / 4);
+            r[u][0] = r[u][1] = 0;
+            if (a.resid == nullptr || e >= quads || oi >= a.n_i) continue;
+            const uint16_t* p = a.resid + oj * a.ld_resid + oi;
+            if (a.pairs && oi + 4 <= a.n_i) {
+                r[u][0] = reinterpret_cast<const uint32_t*>(p)[0];
+                r[u][1] = reinterpret_cast<const uint32_t*>(p)[1];
+            } else {
+                r[u][0] = p[0] | (oi + 1 < a.n_i ? (uint32_t)p[1] << 16 : 0u);
+                r[u][1] = (oi + 2 < a.n_i ? (uint32_t)p[2] : 0u) | (oi + 3 < a.n_i ? (uint32_t)p[3] << 16 : 0u);
+            }
+        }
+    };
+    fetch((int)threadIdx.x);
+    __syncwarp();
+    cluster_wait();
+    for (int e0 = (int)threadIdx.x; e0 < quads; e0 += kTurns * THREADS) {
+        if (e0 != (int)threadIdx.x) fetch(e0);
+#pragma unroll
+        for (int u = 0; u < kTurns; ++u) {
+            const int e = e0 + u * THREADS;
+            if (e >= quads) break;
+            const float4* from = reinterpret_cast<const float4*>(part) + e;
+            const float4 first = *from;
+            float y[4] = {first.x, first.y, first.z, first.w};
+            for (int p = 1; p < split; ++p) {   // in the CTAs' order
+                const float4 more = from[p * per * (kMI / 4)];
+                y[0] = __fadd_rn(y[0], more.x);
+                y[1] = __fadd_rn(y[1], more.y);
+                y[2] = __fadd_rn(y[2], more.z);
+                y[3] = __fadd_rn(y[3], more.w);
+            }
+            const int64_t oi = i0 + 4 * (e % (kMI / 4)), oj = j0 + rank * per + e / (kMI / 4);
+            const bool words = a.pairs && oi + 4 <= a.n_i;
+            if (a.bias != nullptr) {
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    if (oi + h < a.n_i) y[h] = __fadd_rn(y[h], bf16_to_f32(a.bias[oi + h]));
+            }
+            if (a.z != nullptr) store4(a.z + oj * a.ld_z + oi, y, words, a.n_i - oi);
+            activate_all(y, a.act);
+            if (a.resid != nullptr) {
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    y[h] = __fadd_rn(y[h], __uint_as_float((h & 1) ? r[u][h / 2] & 0xFFFF0000u : r[u][h / 2] << 16));
+            }
+            store4(a.out + oj * a.ld_out + oi, y, words, a.n_i - oi);
+        }
+    }
+}
+
+// One output tile of kMI x BN per cluster; its contraction is split over the cluster's CTAs.  Each of them adds up and writes
+// an equal share of the tile's columns: the others push their partial sums of it into its shared memory (the stages, free
+// by then), and it adds them in the CTAs' order.  Bound by the loads of a tile's operands into one SM (about 110 GB/s an
+// SM for wide tiles) or, with few tokens, by the weights' stream: 37 tokens, 4096 outputs from 8807, 18.0 us against
+// 11.2 of the weights alone; 512 tokens, 4096 from 4096, 23 us.  One CTA an SM (its stages fill shared memory), so a CTA
+// never waits for tensor memory that another one of this kernel holds.
 template <bool A_MN, bool B_MN, int BN, int MODE>
 __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                                                        const __grid_constant__ MmArgs args, const __grid_constant__ Second<MODE> second) {
@@ -408,7 +542,6 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
     __syncwarp();
     const bool done = warp >= 2 && mbar_wait(&acc_full, 0u, err);
     tc_fence_after();
-    const int q = warp & 3;
     const int n_cols = (int)(a.n_j - j0 < BN ? (a.n_j > j0 ? a.n_j - j0 : 0) : BN);
     const int per = (n_cols + split - 1) / split;   // columns of the tile that a CTA of the cluster adds up and writes
     float* part = reinterpret_cast<float*>(ring);   // [split][per][kMI]: the cluster's partial sums of this CTA's columns
@@ -418,33 +551,7 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
         cluster_arrive();
         cluster_wait();
     }
-    if (done) {
-        constexpr int kChunk = BN < 32 ? 16 : 32, kSets = mm_warps(BN) / 4;   // warps of a quarter take chunks in turn
-        const float bias = lane_bias(a, second, i0 + q * (kTileI<MODE> / 4));
-#pragma unroll 1
-        for (int c0 = ((warp - kMRoles) >> 2) * kChunk; c0 < n_cols; c0 += kSets * kChunk) {
-            float v[kChunk];
-            tmem_load<kChunk>(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c0, v);
-            if (split > 1) {
-                int owner = c0 / per, at = c0 - owner * per;
-                uint32_t to = cluster_addr(part + ((size_t)rank * per + at) * kMI + q * 32 + lane, owner);
-#pragma unroll
-                for (int e = 0; e < kChunk; ++e) {
-                    if (c0 + e < n_cols) store_remote(to, v[e]);
-                    to += kMI * 4;
-                    if (++at == per) {
-                        at = 0;
-                        ++owner;
-                        to = cluster_addr(part + (size_t)rank * per * kMI + q * 32 + lane, owner < split ? owner : 0);
-                    }
-                }
-            } else {
-                if constexpr (MODE == kGate) gate_epilogue<kChunk>(a, second.g, v, bias, i0 + q * kGateRows, j0 + c0, n_cols - c0);
-                else epilogue<kChunk>(a, v, bias, i0 + q * 32, j0 + c0, n_cols - c0);
-                __syncwarp();
-            }
-        }
-    }
+    if (done) tile_out<BN, MODE, mm_warps(BN) / 4>(a, second, tmem, part, per, rank, split, n_cols, i0, j0);
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -465,100 +572,7 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
     if (split > 1) {
         __syncwarp();
         cluster_arrive();
-        if constexpr (MODE == kGate) {
-            // Four adjacent elements a thread and turn, from the partial sums of both matrices.
-            __syncwarp();
-            cluster_wait();
-            const int mine = n_cols - rank * per < per ? n_cols - rank * per : per;
-            for (int e = (int)threadIdx.x; e < mine * (kMI / 8); e += mm_threads(BN)) {
-                const int col = e / (kMI / 8), quad = e % (kMI / 8);   // 16 quads a column: four of each 16 elements
-                const float4* from = reinterpret_cast<const float4*>(part) + col * (kMI / 4) + (quad >> 2) * 8 + (quad & 3);
-                float z[4] = {}, u[4] = {};
-                for (int p = 0; p < split; ++p) {   // in the CTAs' order
-                    const float4 zp = from[p * per * (kMI / 4) + (second.g.swapped ? 4 : 0)], up = from[p * per * (kMI / 4) + (second.g.swapped ? 0 : 4)];
-                    z[0] = __fadd_rn(z[0], zp.x);
-                    z[1] = __fadd_rn(z[1], zp.y);
-                    z[2] = __fadd_rn(z[2], zp.z);
-                    z[3] = __fadd_rn(z[3], zp.w);
-                    u[0] = __fadd_rn(u[0], up.x);
-                    u[1] = __fadd_rn(u[1], up.y);
-                    u[2] = __fadd_rn(u[2], up.z);
-                    u[3] = __fadd_rn(u[3], up.w);
-                }
-                const int64_t oi = i0 + 4 * quad, oj = j0 + rank * per + col;
-                const bool words = a.pairs && oi + 4 <= a.n_i;
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    if (oi + h >= a.n_i) break;
-                    if (a.bias != nullptr) z[h] = __fadd_rn(z[h], bf16_to_f32(a.bias[oi + h]));
-                    if (second.g.bias != nullptr) u[h] = __fadd_rn(u[h], bf16_to_f32(second.g.bias[oi + h]));
-                }
-                if (a.z != nullptr) store4(a.z + oj * a.ld_z + oi, z, words, a.n_i - oi);
-                if (second.g.u != nullptr) store4(second.g.u + oj * second.g.ld_u + oi, u, words, a.n_i - oi);
-                activate_all(z, a.act);
-#pragma unroll
-                for (int h = 0; h < 4; ++h) z[h] = __fmul_rn(z[h], u[h]);
-                store4(a.out + oj * a.ld_out + oi, z, words, a.n_i - oi);
-            }
-            return;
-        }
-        // Four adjacent elements a thread and turn; the residual's are on their way while the partial sums come in.
-        constexpr int kTurns = 4;
-        const int mine = n_cols - rank * per < per ? n_cols - rank * per : per, quads = mine > 0 ? mine * (kMI / 4) : 0;
-        uint32_t r[kTurns][2];
-        const auto fetch = [&](int e0) {
-#pragma unroll
-            for (int u = 0; u < kTurns; ++u) {
-                const int e = e0 + u * mm_threads(BN);
-                const int64_t oi = i0 + 4 * (e % (kMI / 4)), oj = j0 + rank * per + e / (kMI / 4);
-                r[u][0] = r[u][1] = 0;
-                if (a.resid == nullptr || e >= quads || oi >= a.n_i) continue;
-                const uint16_t* p = a.resid + oj * a.ld_resid + oi;
-                if (a.pairs && oi + 4 <= a.n_i) {
-                    r[u][0] = reinterpret_cast<const uint32_t*>(p)[0];
-                    r[u][1] = reinterpret_cast<const uint32_t*>(p)[1];
-                } else {
-                    r[u][0] = p[0] | (oi + 1 < a.n_i ? (uint32_t)p[1] << 16 : 0u);
-                    r[u][1] = (oi + 2 < a.n_i ? (uint32_t)p[2] : 0u) | (oi + 3 < a.n_i ? (uint32_t)p[3] << 16 : 0u);
-                }
-            }
-        };
-        fetch((int)threadIdx.x);
-        __syncwarp();
-        cluster_wait();
-        for (int e0 = (int)threadIdx.x; e0 < quads; e0 += kTurns * mm_threads(BN)) {
-            if (e0 != (int)threadIdx.x) fetch(e0);
-#pragma unroll
-            for (int u = 0; u < kTurns; ++u) {
-                const int e = e0 + u * mm_threads(BN);
-                if (e >= quads) break;
-                const float4* from = reinterpret_cast<const float4*>(part) + e;
-                const float4 first = *from;
-                float y[4] = {first.x, first.y, first.z, first.w};
-                for (int p = 1; p < split; ++p) {   // in the CTAs' order
-                    const float4 more = from[p * per * (kMI / 4)];
-                    y[0] = __fadd_rn(y[0], more.x);
-                    y[1] = __fadd_rn(y[1], more.y);
-                    y[2] = __fadd_rn(y[2], more.z);
-                    y[3] = __fadd_rn(y[3], more.w);
-                }
-                const int64_t oi = i0 + 4 * (e % (kMI / 4)), oj = j0 + rank * per + e / (kMI / 4);
-                const bool words = a.pairs && oi + 4 <= a.n_i;
-                if (a.bias != nullptr) {
-#pragma unroll
-                    for (int h = 0; h < 4; ++h)
-                        if (oi + h < a.n_i) y[h] = __fadd_rn(y[h], bf16_to_f32(a.bias[oi + h]));
-                }
-                if (a.z != nullptr) store4(a.z + oj * a.ld_z + oi, y, words, a.n_i - oi);
-                activate_all(y, a.act);
-                if (a.resid != nullptr) {
-#pragma unroll
-                    for (int h = 0; h < 4; ++h)
-                        y[h] = __fadd_rn(y[h], __uint_as_float((h & 1) ? r[u][h / 2] & 0xFFFF0000u : r[u][h / 2] << 16));
-                }
-                store4(a.out + oj * a.ld_out + oi, y, words, a.n_i - oi);
-            }
-        }
+        tile_join<MODE, mm_threads(BN)>(a, second, part, per, rank, split, n_cols, i0, j0);
     }
 }
 

@@ -141,6 +141,18 @@ __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t desc_a, uint
         : "r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(0u), "r"(0u), "r"(0u), "r"(0u)
         : "memory");
 }
+// The same with A in tensor memory: a row a lane, two adjacent contraction steps a 32-bit column, 16 steps eight columns.
+__device__ __forceinline__ void umma_bf16_from_tmem(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n\t"
+        "}"
+        :
+        : "r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(0u), "r"(0u), "r"(0u), "r"(0u)
+        : "memory");
+}
 // The pair's product: issued by the first CTA, each CTA's shared memory holds its half of both operands.
 __device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -197,6 +209,19 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
+// 32 columns of this thread's lane of tensor memory; tmem_stored() waits until they are there.
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        :
+        : "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+          "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+          "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 #endif
 
@@ -235,17 +260,36 @@ inline bool encode_bf16(CUtensorMap* map, const void* p, int64_t rows, int64_t c
 
 // Two such matrices of one leading dimension, `other` at a higher address, as one: groups of `group` rows of the one and the
 // same rows of the other, in boxes of box_cols x (group of each) x box_groups.  Whole groups only (rows / group of them); what
-// lies outside is read as zero.
-inline bool encode_bf16_twins(CUtensorMap* map, const void* p, const void* other, int64_t rows, int64_t cols, int64_t ld, int group, int box_groups, int box_cols) {
+// lies outside is read as zero.  `bytes` of an element, ld and cols in elements.
+inline bool encode_twins(CUtensorMap* map, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, int64_t bytes, const void* p, const void* other, int64_t rows,
+                         int64_t cols, int64_t ld, int group, int box_groups, int box_cols) {
     EncodeTiledFn encode = encode_tiled();
     const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(other) - reinterpret_cast<uintptr_t>(p));
     if (encode == nullptr || rows < group || apart <= 0 || apart % 16 != 0 || apart >= ((int64_t)1 << 40)) return false;
     const cuuint64_t gdim[4] = {(cuuint64_t)cols, (cuuint64_t)group, 2u, (cuuint64_t)(rows / group)};
-    const cuuint64_t gstride[3] = {(cuuint64_t)ld * 2u, (cuuint64_t)apart, (cuuint64_t)ld * 2u * (cuuint64_t)group};
+    const cuuint64_t gstride[3] = {(cuuint64_t)(ld * bytes), (cuuint64_t)apart, (cuuint64_t)(ld * bytes * group)};
     const cuuint32_t box[4] = {(cuuint32_t)box_cols, (cuuint32_t)group, 2u, (cuuint32_t)box_groups};
     const cuuint32_t estride[4] = {1u, 1u, 1u, 1u};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4u, const_cast<void*>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encode(map, type, 4u, const_cast<void*>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+inline bool encode_bf16_twins(CUtensorMap* map, const void* p, const void* other, int64_t rows, int64_t cols, int64_t ld, int group, int box_groups, int box_cols) {
+    return encode_twins(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, 2, p, other, rows, cols, ld, group, box_groups, box_cols);
+}
+// Row-major bytes [rows, cols], ld a multiple of 16, in boxes of 64 x box_rows with the 64-byte swizzle (16-byte piece c of row
+// r lies at c ^ (r / 2) % 4); and two such matrices as one.
+inline bool encode_bytes(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+    EncodeTiledFn encode = encode_tiled();
+    if (encode == nullptr) return false;
+    const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t gstride[1] = {rows > 1 ? (cuuint64_t)ld : (cuuint64_t)align_up((size_t)cols, 16)};
+    const cuuint32_t box[2] = {64u, (cuuint32_t)box_rows};
+    const cuuint32_t estride[2] = {1u, 1u};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2u, const_cast<void*>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+inline bool encode_bytes_twins(CUtensorMap* map, const void* p, const void* other, int64_t rows, int64_t cols, int64_t ld, int group, int box_groups) {
+    return encode_twins(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_64B, 1, p, other, rows, cols, ld, group, box_groups, 64);
 }
 
 }  // namespace mosaic

@@ -307,6 +307,222 @@ __global__ void __launch_bounds__(32 * k4Warps) few4_kernel(const __grid_constan
     }
 }
 
+// ---------------------------------------------------------------- more tokens
+// The tensor cores' product with the weights' tile made on the way: mm_kernel's tile, cluster and epilogue (mm.cuh), but of A only
+// the codes are loaded, 128 rows x 128 columns a stage in 8 KB; eight warps make bf16 of them, a weight row a lane, and put
+// them into tensor memory, where the matrix instruction reads its first operand.  The weights so cross shared memory as codes,
+// once, instead of as bf16 twice: with them in shared memory its bandwidth would hold the stream to about half of what
+// memory gives.
+constexpr int kC4Cols = 128, kC4Warps = 8, kC4Threads = 32 * (kMRoles + kC4Warps);
+constexpr uint32_t kC4Bytes = kMI * kC4Cols / 2, kC4Box = kGateRows * kC4Cols / 2;   // of a stage's codes, of 16 rows of them
+template <int BN> constexpr int kC4Slots = BN <= 64 ? 6 : 5;                          // in shared memory, and of 64 columns each in tensor memory
+template <int BN> constexpr uint32_t kC4Slot = kC4Bytes + 2u * BN * kMC * 2u;
+template <int BN> constexpr uint32_t kC4Acc = BN < 32 ? 32 : BN;                      // tensor-memory columns of the accumulator
+// One CTA an SM: it takes all of the tensor memory, and one that waited for it could hold up its cluster.
+template <int BN> constexpr size_t kC4Smem = kC4Slots<BN> * kC4Slot<BN> + 1024 > 120 * 1024 ? kC4Slots<BN> * kC4Slot<BN> + 1024 : 120 * 1024;
+
+struct Scales4 {
+    const uint16_t *p, *p2;            // p2: the second matrix's (kGate)
+    int64_t ld, ld2;
+    int shift, shift2;
+    int groups, groups2;               // a row's
+    int wide, wide2;                   // a stage's scales of a row may be read as one word
+};
+
+// The scales of a row's 128 columns from `col` on, for each 32 of them, past the last group its own again.
+__device__ __forceinline__ uint2 scales_of(const uint16_t* row, int col, int shift, int groups, bool wide) {
+    const int at = col >> shift;
+    if (shift == 7) {
+        const uint32_t s = row[at];
+        return make_uint2(s | (s << 16), s | (s << 16));
+    }
+    if (shift == 6) {
+        const uint32_t w = wide && at + 2 <= groups ? *reinterpret_cast<const uint32_t*>(row + at)
+                                                    : (uint32_t)row[at] | ((uint32_t)row[min(at + 1, groups - 1)] << 16);
+        return make_uint2(__byte_perm(w, 0u, 0x1010), __byte_perm(w, 0u, 0x3232));
+    }
+    if (wide && at + 4 <= groups) return *reinterpret_cast<const uint2*>(row + at);
+    return make_uint2((uint32_t)row[at] | ((uint32_t)row[min(at + 1, groups - 1)] << 16),
+                      (uint32_t)row[min(at + 2, groups - 1)] | ((uint32_t)row[min(at + 3, groups - 1)] << 16));
+}
+// The eight weights of a word in their order: each byte's codes to bits 3..6 of the halves by one multiplication, then as in weights4.
+__device__ __forceinline__ void weights4_in_order(uint32_t word, uint32_t s2, uint32_t c2, uint32_t* w) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t at = __byte_perm(word, 0u, 0x4440 | j) * 0x8008u;
+        uint32_t sum;
+        asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(sum) : "r"(at), "r"(0x00780078u), "r"(0x41804180u));
+        w[j] = fma_bf16x2(sum, s2, c2);
+    }
+}
+
+template <int BN, int MODE>
+__global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap x_map,
+                                                         const __grid_constant__ MmArgs a, const __grid_constant__ Second<MODE> second,
+                                                         const __grid_constant__ Scales4 scales) {
+    constexpr int kSlots = kC4Slots<BN>;
+    constexpr uint32_t kDesc = instr_desc(false, false, kMI, BN);
+    extern __shared__ unsigned char mm4_smem_raw[];
+    __shared__ uint64_t full[kSlots], ready[kSlots], empty[kSlots], acc_full;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int err_word;
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(mm4_smem_raw) + 1023u) & ~(uintptr_t)1023u);
+    volatile int* err = &err_word;
+    const int split = a.split, rank = (int)(blockIdx.x % (unsigned)split);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tile = (int)(blockIdx.x / (unsigned)split);
+    const int64_t i0 = (int64_t)(tile % a.tiles_i) * kTileI<MODE>, j0 = (int64_t)(tile / a.tiles_i) * BN;
+    const int64_t steps = (a.n_c + kC4Cols - 1) / kC4Cols;
+    const int s0 = (int)(steps * rank / split), s1 = (int)(steps * (rank + 1) / split);   // split <= steps: never empty
+
+    if (threadIdx.x == 0) {
+        prefetch_map(&code_map);
+        prefetch_map(&x_map);
+        for (int s = 0; s < kSlots; ++s) {
+            mbar_init(&full[s], 1u);
+            mbar_init(&ready[s], 4u);   // the four warps that make a stage's weights
+            mbar_init(&empty[s], 1u);
+        }
+        mbar_init(&acc_full, 1u);
+        *err = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot, tmem_a = tmem + kC4Acc<BN>;
+    uint32_t issued = 0;
+    allow_next_kernel();   // not before this CTA has its tensor memory: the next kernel's CTAs wait for it with theirs in hand
+    await_previous_kernel();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            const bool whole = one_box(second, i0);
+            for (int s = s0; s < s1; ++s) {
+                const uint32_t it = (uint32_t)(s - s0), slot = it % kSlots, ph = (it / kSlots) & 1u;
+                if (!mbar_wait(&empty[slot], ph ^ 1u, err)) break;
+                mbar_expect_tx(&full[slot], kC4Slot<BN>);
+                unsigned char* codes = ring + (size_t)slot * kC4Slot<BN>;
+                const int c = s * (kC4Cols / 2);
+                if constexpr (MODE == kGate) {
+                    if (whole) tma_load_box4(codes, &second.both, &full[slot], c, (int)i0 / kGateRows);
+#pragma unroll
+                    for (int b = 0; b < kMI / (2 * kGateRows) && !whole; ++b) {
+                        tma_load_box(codes + (2 * b) * kC4Box, &code_map, &full[slot], c, (int)i0 + b * kGateRows);
+                        tma_load_box(codes + (2 * b + 1) * kC4Box, &second.a, &full[slot], c, (int)i0 + b * kGateRows);
+                    }
+                } else {
+                    tma_load_box(codes, &code_map, &full[slot], c, (int)i0);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) tma_load_box(codes + kC4Bytes + h * (BN * kMC * 2), &x_map, &full[slot], s * kC4Cols + h * kMC, (int)j0);
+                issued = it + 1u;
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            bool ok = true;
+            for (int s = s0; s < s1 && ok; ++s) {
+                const uint32_t it = (uint32_t)(s - s0), slot = it % kSlots, ph = (it / kSlots) & 1u;
+                ok = mbar_wait(&full[slot], ph, err) && mbar_wait(&ready[slot], ph, err);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t sb = smem_u32(ring + (size_t)slot * kC4Slot<BN>) + kC4Bytes;
+#pragma unroll
+                for (int k = 0; k < kC4Cols / 16; ++k) {
+                    const uint64_t db = operand_desc(sb + (uint32_t)(k / 4) * (BN * kMC * 2) + (uint32_t)(k % 4) * 32u, 16u);
+                    umma_bf16_from_tmem(tmem, tmem_a + slot * 64u + (uint32_t)k * 8u, db, kDesc, (it > 0 || k > 0) ? 1u : 0u);
+                }
+                umma_commit(&empty[slot]);
+            }
+            if (ok) umma_commit(&acc_full);
+        }
+    } else {
+        // a weight row a lane; the two sets of four warps take stages in turn
+        const int q = warp & 3, set = (warp - kMRoles) >> 2, r = q * 32 + lane;
+        int64_t row = i0 + r;
+        bool other = false;
+        if constexpr (MODE == kGate) {
+            other = (((r >> 4) & 1) != 0) != (second.g.swapped != 0);
+            row = i0 + (r >> 5) * kGateRows + (r & 15);
+        }
+        if (row >= a.n_i) row = a.n_i - 1;   // rows past the end: any numbers, not stored
+        const uint16_t* at = other ? scales.p2 + row * scales.ld2 : scales.p + row * scales.ld;
+        const int shift = other ? scales.shift2 : scales.shift, groups = other ? scales.groups2 : scales.groups;
+        const bool wide = (other ? scales.wide2 : scales.wide) != 0;
+        uint2 next = make_uint2(0u, 0u);
+        if (s0 + set < s1) next = scales_of(at, (s0 + set) * kC4Cols, shift, groups, wide);
+        for (int s = s0 + set; s < s1; s += 2) {
+            const uint32_t it = (uint32_t)(s - s0), slot = it % kSlots, ph = (it / kSlots) & 1u;
+            const uint2 sc = next;
+            if (s + 2 < s1) next = scales_of(at, (s + 2) * kC4Cols, shift, groups, wide);
+            // the codes have landed; the loader had waited for the products of the slot's last turn, so its tensor memory is free too
+            if (!mbar_wait(&full[slot], ph, err)) break;
+            __syncwarp();
+            tc_fence_after();
+            const unsigned char* codes = ring + (size_t)slot * kC4Slot<BN> + r * 64;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t w[32];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int c = h * 2 + e;
+                    const uint4 v = *reinterpret_cast<const uint4*>(codes + ((c ^ ((r >> 1) & 3)) << 4));
+                    const uint32_t both = h == 0 ? sc.x : sc.y, s2 = __byte_perm(both, 0u, e == 0 ? 0x1010 : 0x3232), c2 = minus24(s2);
+                    weights4_in_order(v.x, s2, c2, w + e * 16);
+                    weights4_in_order(v.y, s2, c2, w + e * 16 + 4);
+                    weights4_in_order(v.z, s2, c2, w + e * 16 + 8);
+                    weights4_in_order(v.w, s2, c2, w + e * 16 + 12);
+                }
+                tmem_store32(tmem_a + ((uint32_t)(q * 32) << 16) + slot * 64u + (uint32_t)h * 32u, w);
+            }
+            tmem_stored();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ready[slot]);
+        }
+    }
+    __syncwarp();
+    const bool done = warp >= kMRoles && mbar_wait(&acc_full, 0u, err);
+    tc_fence_after();
+    const int n_cols = (int)(a.n_j - j0 < BN ? a.n_j - j0 : BN);
+    const int per = (n_cols + split - 1) / split;
+    float* part = reinterpret_cast<float*>(ring);
+    if (split > 1) {
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (done) tile_out<BN, MODE, kC4Warps / 4>(a, second, tmem, part, per, rank, split, n_cols, i0, j0);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+    if (threadIdx.x == 0 && *err != 0) {
+        // a role gave up: let the loads of the last stages land before shared memory is reused or left (bounded)
+        for (uint32_t back = 1; back <= (uint32_t)kSlots && back <= issued; ++back) {
+            const uint32_t it = issued - back, slot = it % kSlots, ph = (it / kSlots) & 1u;
+            const long long t0 = clock64();
+            while (!mbar_try_wait(&full[slot], ph) && clock64() - t0 < kWaitCycles) {
+            }
+        }
+        if (a.status != nullptr) atomicExch(a.status, 1);
+    }
+    if (split > 1) {
+        __syncwarp();
+        cluster_arrive();
+        tile_join<MODE, kC4Threads>(a, second, part, per, rank, split, n_cols, i0, j0);
+    }
+}
+
 // ---------------------------------------------------------------- host side
 int64_t code_width(int64_t cols) { return (cols + 31) / 32 * 16; }
 int group_shift(int64_t group) { return group == 32 ? 5 : group == 64 ? 6 : group == 128 ? 7 : 0; }
@@ -365,10 +581,13 @@ int few4_warps(int64_t tokens, int64_t cols) {
 }
 bool is_few4(int64_t tokens, int64_t cols) { return few4_warps(tokens, cols) > 0; }
 
-// Scratch: few tokens need an aligned copy of X if it is not; many need the weights in bf16 as well.
+// Beyond, a bf16 copy of the weights and mm.cuh's products.
+constexpr int64_t kC4Tokens = 256;
+
+// Scratch: an aligned copy of X if it is not; many tokens need the weights in bf16 as well.
 size_t workspace4(const Matrix& x, int64_t outputs, int matrices) {
     size_t need = x.tma_ok() ? 0 : x.padded_bytes();
-    if (!is_few4(x.rows, x.cols)) need += (size_t)matrices * Matrix{nullptr, outputs, x.cols, x.cols}.padded_bytes();
+    if (x.rows > kC4Tokens) need += (size_t)matrices * Matrix{nullptr, outputs, x.cols, x.cols}.padded_bytes();
     return need;
 }
 
@@ -403,6 +622,86 @@ template <bool GATE> int launch_few4(Few4Args a, cudaStream_t st) {
     return MOSAIC_OK;
 }
 
+// Nanoseconds of 128 columns of a tile by its tokens, and the rest as in mm.cuh.
+constexpr int64_t k4Step = 230, k4WideStep = 330;
+
+template <int BN, int MODE>
+int launch_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& x, MmArgs a, const GateArgs& g, int split, cudaStream_t st) {
+    static_assert(kC4Slots<BN> * kC4Slot<BN> >= (BN + kMMaxSplit) * kMI * 4, "the partial sums lie where the stages were");
+    static DeviceCache opted;
+    if (opted.get([]() -> int {
+            if (cudaFuncSetAttribute(mm4_kernel<BN, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kC4Smem<BN>) == cudaSuccess) return 1;
+            (void)cudaGetLastError();
+            return -1;
+        }) < 0)
+        return MOSAIC_ERR_CUDA;
+    const int64_t width = code_width(a.n_c);
+    CUtensorMap code_map, x_map;
+    Second<MODE> second;
+    if (!encode_bytes(&code_map, W->codes, a.n_i, width, W->ldc, MODE == kGate ? kGateRows : kMI) || !encode_bf16(&x_map, x.p, x.rows, x.cols, x.ld, BN, kMC))
+        return MOSAIC_ERR_CUDA;
+    const auto wide = [](const mosaic_weight4* w) {
+        const int64_t n = kC4Cols / w->group;
+        return w->lds % n == 0 && (reinterpret_cast<uintptr_t>(w->scales) & (uintptr_t)(2 * n - 1)) == 0 ? 1 : 0;
+    };
+    const auto groups = [&](const mosaic_weight4* w) { return (int)((a.n_c + w->group - 1) / w->group); };
+    Scales4 s = {static_cast<const uint16_t*>(W->scales), nullptr, W->lds, 0, group_shift(W->group), 0, groups(W), 0, wide(W), 0};
+    if constexpr (MODE == kGate) {
+        second.g = g;
+        const bool one = W->ldc == W2->ldc && encode_bytes_twins(&second.both, W->codes, W2->codes, a.n_i, width, W->ldc, kGateRows, kMI / (2 * kGateRows));
+        if (!one) second.both = CUtensorMap{};
+        second.g.whole = one ? (int)(a.n_i / kGateRows * kGateRows) : 0;
+        if (!encode_bytes(&second.a, W2->codes, a.n_i, width, W2->ldc, kGateRows)) return MOSAIC_ERR_CUDA;
+        const Scales4 t = {static_cast<const uint16_t*>(W2->scales), nullptr, W2->lds, 0, group_shift(W2->group), 0, groups(W2), 0, wide(W2), 0};
+        if (g.swapped != 0) {   // the scales' first matrix is the gate's, wherever it lies
+            s.p2 = s.p; s.ld2 = s.ld; s.shift2 = s.shift; s.groups2 = s.groups; s.wide2 = s.wide;
+            s.p = t.p; s.ld = t.ld; s.shift = t.shift; s.groups = t.groups; s.wide = t.wide;
+        } else {
+            s.p2 = t.p; s.ld2 = t.ld; s.shift2 = t.shift; s.groups2 = t.groups; s.wide2 = t.wide;
+        }
+    }
+    a.tiles_i = (int)((a.n_i + kTileI<MODE> - 1) / kTileI<MODE>);
+    a.tiles_j = (int)((a.n_j + BN - 1) / BN);
+    a.split = split;
+    Launch l(dim3((unsigned)((int64_t)a.tiles_i * a.tiles_j * split)), kC4Threads, kC4Smem<BN>, st, split);
+    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, mm4_kernel<BN, MODE>, code_map, x_map, a, second, s));
+    return MOSAIC_OK;
+}
+
+template <int MODE> int run_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& x, MmArgs a, GateArgs g, cudaStream_t st) {
+    if (MODE == kGate && reinterpret_cast<uintptr_t>(W2->codes) < reinterpret_cast<uintptr_t>(W->codes)) {   // the lower one first
+        const mosaic_weight4* t = W;
+        W = W2;
+        W2 = t;
+        g.swapped = 1;
+    }
+    const auto even = [](const void* p, int64_t ld) { return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & 3u) == 0 && ld % 2 == 0); };
+    a.pairs = even(a.out, a.ld_out) && even(a.resid, a.ld_resid) ? 1 : 0;
+    a.first_pair = -1;
+    const int64_t ti = (a.n_i + kTileI<MODE> - 1) / kTileI<MODE>, steps = (a.n_c + kC4Cols - 1) / kC4Cols;
+    int64_t best = 0;
+    int bn = 16, split = 1;
+    for (int w = 16; w <= 128; w *= 2) {
+        const int64_t tiles = ti * ((a.n_j + w - 1) / w);
+        for (int p = 1; p <= kMMaxSplit && (p == 1 || steps >= 2 * p); ++p) {
+            const int64_t held = resident_clusters(p), waves = (tiles + held - 1) / held;
+            const int64_t c = waves * ((steps + p - 1) / p * (w > 64 ? k4WideStep : k4Step) + w * kTileColumn + kFixed + (p > 1 ? kSplitFixed + w * kSplitColumn : 0));
+            if (best == 0 || c < best) {
+                best = c;
+                bn = w;
+                split = p;
+            }
+        }
+        if (w >= a.n_j) break;
+    }
+    if (ti * ((a.n_j + bn - 1) / bn) * split > 0x7FFFFFFF) return MOSAIC_ERR_INVALID_ARG;
+    switch (bn) {
+        case 16: return launch_mm4<16, MODE>(W, W2, x, a, g, split, st);
+        case 32: return launch_mm4<32, MODE>(W, W2, x, a, g, split, st);
+        case 64: return launch_mm4<64, MODE>(W, W2, x, a, g, split, st);
+        default: return launch_mm4<128, MODE>(W, W2, x, a, g, split, st);
+    }
+}
 // The weights in bf16, in scratch.
 int widen4(const mosaic_weight4* w, int64_t rows, int64_t cols, char** ws, Matrix* out, cudaStream_t st) {
     *out = {nullptr, rows, cols, cols};
@@ -472,14 +771,15 @@ extern "C" int mosaic_linear4(const void* X, int64_t ldx, const mosaic_weight4* 
         a.y = static_cast<uint16_t*>(Y); a.ldy = ldy;
         return launch_few4<false>(a, st);
     }
-    Matrix w;
-    if ((rc = widen4(W, out_features, in_features, &scratch, &w, st)) != MOSAIC_OK) return rc;
     MmArgs a = {};
     a.n_i = out_features; a.n_j = tokens; a.n_c = in_features;
     a.out = static_cast<uint16_t*>(Y); a.ld_out = ldy;
     a.bias = static_cast<const uint16_t*>(bias);
     a.resid = static_cast<const uint16_t*>(residual); a.ld_resid = ldr;
     a.act = act; a.status = status_dev;
+    if (tokens <= kC4Tokens) return run_mm4<kPlain>(W, nullptr, x, a, GateArgs{}, st);
+    Matrix w;
+    if ((rc = widen4(W, out_features, in_features, &scratch, &w, st)) != MOSAIC_OK) return rc;
     return run_mm<false, false>(w, x, a, st);
 }
 
@@ -515,15 +815,16 @@ extern "C" int mosaic_gated_linear4(const void* X, int64_t ldx, const mosaic_wei
         a.y = static_cast<uint16_t*>(H); a.ldy = ldh;
         return launch_few4<true>(a, st);
     }
-    Matrix wg, wu;
-    if ((rc = widen4(W_gate, channels, in_features, &scratch, &wg, st)) != MOSAIC_OK || (rc = widen4(W_up, channels, in_features, &scratch, &wu, st)) != MOSAIC_OK) return rc;
     MmArgs a = {};
     a.n_i = channels; a.n_j = tokens; a.n_c = in_features;
     a.out = static_cast<uint16_t*>(H); a.ld_out = ldh;
     a.bias = static_cast<const uint16_t*>(bias_gate);
     a.act = act; a.status = status_dev;
     Also also = {};
-    also.A = wu;
     also.gate.bias = static_cast<const uint16_t*>(bias_up);
+    if (tokens <= kC4Tokens) return run_mm4<kGate>(W_gate, W_up, x, a, also.gate, st);
+    Matrix wg, wu;
+    if ((rc = widen4(W_gate, channels, in_features, &scratch, &wg, st)) != MOSAIC_OK || (rc = widen4(W_up, channels, in_features, &scratch, &wu, st)) != MOSAIC_OK) return rc;
+    also.A = wu;
     return run_mm<false, false, kGate>(wg, x, a, st, also);
 }

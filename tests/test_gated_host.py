@@ -151,7 +151,7 @@ def test_products4_refusals_need_no_device(lib, call):
     assert call(lib, W=w4(codes=2 * A + 8)) == MISALIGNED and call(lib, W=w4(ldc=40)) == MISALIGNED and call(lib, W=w4(scales=3 * A + 1)) == MISALIGNED
     assert call(lib, status=A + 2) == MISALIGNED and call(lib, Y=A) == ALIAS and call(lib, Y=2 * A) == ALIAS and call(lib, Y=3 * A) == ALIAS and call(lib, bias=4 * A) == ALIAS
     assert call(lib, X=A + 2) == NULL and call(lib, X=A + 2, ws=8 * A, ws_bytes=100) == WS and call(lib, X=A + 2, ws=8 * A + 8, ws_bytes=1 << 20) == MISALIGNED
-    assert call(lib, m=33) == NULL and call(lib, m=33, ws=8 * A, ws_bytes=32 * 64 * 2 - 1) == WS   # many tokens: the weights in bf16
+    assert call(lib, m=api.FEW4_TOKENS + 1) == NULL and call(lib, m=api.FEW4_TOKENS + 1, ws=8 * A, ws_bytes=32 * 64 * 2 - 1) == WS   # many tokens: the weights in bf16
     if call is linear4:
         assert call(lib, R=4 * A, ldr=40) == ALIAS and call(lib, R=4 * A + 32) == ALIAS
     else:

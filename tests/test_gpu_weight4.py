@@ -97,7 +97,7 @@ def weight4(n, k, g, group, scale):
     return w4, W
 
 
-TOKENS = [1, 2, 7, 8, 9, 16, 17, 24, 32, 33, 65, 200]
+TOKENS = [1, 2, 7, 8, 9, 16, 17, 24, 33, 65, 129, 256, 257]
 
 
 @pytest.mark.parametrize("m", TOKENS)
