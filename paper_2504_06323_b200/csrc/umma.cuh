@@ -51,6 +51,7 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t pa
 // Waits for the phase of the given parity to complete.  False if it gave up: after kWaitCycles
 // (then it raises *err) or because another role raised *err.
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* err, long long budget = kWaitCycles) {
+    if (mbar_try_wait(bar, parity)) return true;
     const long long t0 = clock64();
     while (!mbar_try_wait(bar, parity)) {
         if (*err != 0) return false;
@@ -141,16 +142,19 @@ __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t desc_a, uint
         : "r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(0u), "r"(0u), "r"(0u), "r"(0u)
         : "memory");
 }
-// The same with A in tensor memory: a row a lane, two adjacent contraction steps a 32-bit column, 16 steps eight columns.
-__device__ __forceinline__ void umma_bf16_from_tmem(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+// The same with A in tensor memory: a row a lane, two adjacent contraction steps a 32-bit column, 16 steps eight columns.  B's
+// descriptor in its halves: the issuing thread is alone, and every instruction it saves counts.
+__device__ __forceinline__ void umma_bf16_from_tmem(uint32_t tmem_d, uint32_t tmem_a, uint32_t desc_b_lo, uint32_t desc_b_hi, uint32_t idesc, bool accumulate) {
     asm volatile(
         "{\n\t"
         ".reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n\t"
+        ".reg .b64 b;\n\t"
+        "mov.b64 b, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t"
         "}"
         :
-        : "r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(0u), "r"(0u), "r"(0u), "r"(0u)
+        : "r"(tmem_d), "r"(tmem_a), "r"(desc_b_lo), "r"(desc_b_hi), "r"(idesc), "r"(accumulate ? 1u : 0u)
         : "memory");
 }
 // The pair's product: issued by the first CTA, each CTA's shared memory holds its half of both operands.
@@ -174,6 +178,20 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
 // The barrier gets one arrival when every MMA issued so far by this thread has completed.
 __device__ __forceinline__ void umma_commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// True in one lane of a converged warp.  The tensor-core instructions take their operands from the warp's uniform registers: a loop
+// that all lanes run alike, with only the instructions left to one of them, keeps its addresses there; in a branch of one lane
+// each operand is moved over every time.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t is;
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t"
+        "}"
+        : "=r"(is));
+    return is != 0u;
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -276,20 +294,20 @@ inline bool encode_twins(CUtensorMap* map, CUtensorMapDataType type, CUtensorMap
 inline bool encode_bf16_twins(CUtensorMap* map, const void* p, const void* other, int64_t rows, int64_t cols, int64_t ld, int group, int box_groups, int box_cols) {
     return encode_twins(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, 2, p, other, rows, cols, ld, group, box_groups, box_cols);
 }
-// Row-major bytes [rows, cols], ld a multiple of 16, in boxes of 64 x box_rows with the 64-byte swizzle (16-byte piece c of row
-// r lies at c ^ (r / 2) % 4); and two such matrices as one.
+// Row-major bytes [rows, cols], ld a multiple of 16, in boxes of 128 x box_rows with the 128-byte swizzle (16-byte piece c of row
+// r lies at c ^ r % 8); and two such matrices as one.
 inline bool encode_bytes(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
     EncodeTiledFn encode = encode_tiled();
     if (encode == nullptr) return false;
     const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     const cuuint64_t gstride[1] = {rows > 1 ? (cuuint64_t)ld : (cuuint64_t)align_up((size_t)cols, 16)};
-    const cuuint32_t box[2] = {64u, (cuuint32_t)box_rows};
+    const cuuint32_t box[2] = {128u, (cuuint32_t)box_rows};
     const cuuint32_t estride[2] = {1u, 1u};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2u, const_cast<void*>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 inline bool encode_bytes_twins(CUtensorMap* map, const void* p, const void* other, int64_t rows, int64_t cols, int64_t ld, int group, int box_groups) {
-    return encode_twins(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_64B, 1, p, other, rows, cols, ld, group, box_groups, 64);
+    return encode_twins(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, 1, p, other, rows, cols, ld, group, box_groups, 128);
 }
 
 }  // namespace mosaic

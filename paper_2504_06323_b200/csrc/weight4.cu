@@ -309,17 +309,22 @@ __global__ void __launch_bounds__(32 * k4Warps) few4_kernel(const __grid_constan
 
 // ---------------------------------------------------------------- more tokens
 // The tensor cores' product with the weights' tile made on the way: mm_kernel's tile, cluster and epilogue (mm.cuh), but of A only
-// the codes are loaded, 128 rows x 128 columns a stage in 8 KB; eight warps make bf16 of them, a weight row a lane, and put
+// the codes are loaded, 128 rows x 256 columns a stage in 16 KB; 16 warps make bf16 of them, a weight row a lane, and put
 // them into tensor memory, where the matrix instruction reads its first operand.  The weights so cross shared memory as codes,
 // once, instead of as bf16 twice: with them in shared memory its bandwidth would hold the stream to about half of what
 // memory gives.
-constexpr int kC4Cols = 128, kC4Warps = 8, kC4Threads = 32 * (kMRoles + kC4Warps);
+constexpr int kC4Cols = 256, kC4Unit = 128, kC4Warps = 16, kC4Threads = 32 * (kMRoles + kC4Warps);   // code loader, MMA issue; weight makers
 constexpr uint32_t kC4Bytes = kMI * kC4Cols / 2, kC4Box = kGateRows * kC4Cols / 2;   // of a stage's codes, of 16 rows of them
-template <int BN> constexpr int kC4Slots = BN <= 64 ? 6 : 5;                          // in shared memory, and of 64 columns each in tensor memory
-template <int BN> constexpr uint32_t kC4Slot = kC4Bytes + 2u * BN * kMC * 2u;
+// Rows of 128 bytes a box: the copy engine takes about four cycles a row, whatever its length.  X comes with the codes it meets: in a
+// ring of its own it waited behind the codes of stages to come.
+template <int BN> constexpr int kC4Slots = BN == 16 ? 8 : BN == 32 ? 6 : BN == 64 ? 4 : 2;
+template <int BN> constexpr uint32_t kC4Slot = kC4Bytes + (uint32_t)BN * kC4Cols * 2u;
+constexpr int kC4Made = 6;             // units of 128 columns in tensor memory, 64 of its columns each
 template <int BN> constexpr uint32_t kC4Acc = BN < 32 ? 32 : BN;                      // tensor-memory columns of the accumulator
+constexpr long long kLandCycles = 20000000ll;   // ten milliseconds: far more than a load takes
 // One CTA an SM: it takes all of the tensor memory, and one that waited for it could hold up its cluster.
-template <int BN> constexpr size_t kC4Smem = kC4Slots<BN> * kC4Slot<BN> + 1024 > 120 * 1024 ? kC4Slots<BN> * kC4Slot<BN> + 1024 : 120 * 1024;
+template <int BN> constexpr size_t kC4Smem = kC4Slots<BN> * (size_t)kC4Slot<BN> + 1024;
+static_assert(kC4Smem<16> > 115 * 1024 && kC4Smem<32> > 115 * 1024 && kC4Smem<64> > 115 * 1024 && kC4Smem<128> > 115 * 1024, "one CTA an SM");
 
 struct Scales4 {
     const uint16_t *p, *p2;            // p2: the second matrix's (kGate)
@@ -329,21 +334,23 @@ struct Scales4 {
     int wide, wide2;                   // a stage's scales of a row may be read as one word
 };
 
-// The scales of a row's 128 columns from `col` on, for each 32 of them, past the last group its own again.
+// The scales of a row's 128 columns from `col` on, past the last group that one's again; as they are loaded, and then for each
+// 32 columns (apart, so that nothing waits for the loads before their stage).
 __device__ __forceinline__ uint2 scales_of(const uint16_t* row, int col, int shift, int groups, bool wide) {
     const int at = col >> shift;
-    if (shift == 7) {
-        const uint32_t s = row[at];
-        return make_uint2(s | (s << 16), s | (s << 16));
-    }
+    if (shift == 7) return make_uint2(row[at], 0u);
     if (shift == 6) {
-        const uint32_t w = wide && at + 2 <= groups ? *reinterpret_cast<const uint32_t*>(row + at)
-                                                    : (uint32_t)row[at] | ((uint32_t)row[min(at + 1, groups - 1)] << 16);
-        return make_uint2(__byte_perm(w, 0u, 0x1010), __byte_perm(w, 0u, 0x3232));
+        if (wide && at + 2 <= groups) return make_uint2(*reinterpret_cast<const uint32_t*>(row + at), 0u);
+        return make_uint2((uint32_t)row[at] | ((uint32_t)row[min(at + 1, groups - 1)] << 16), 0u);
     }
     if (wide && at + 4 <= groups) return *reinterpret_cast<const uint2*>(row + at);
     return make_uint2((uint32_t)row[at] | ((uint32_t)row[min(at + 1, groups - 1)] << 16),
                       (uint32_t)row[min(at + 2, groups - 1)] | ((uint32_t)row[min(at + 3, groups - 1)] << 16));
+}
+__device__ __forceinline__ uint2 scales_spread(uint2 s, int shift) {
+    if (shift == 7) return make_uint2(__byte_perm(s.x, 0u, 0x1010), __byte_perm(s.x, 0u, 0x1010));
+    if (shift == 6) return make_uint2(__byte_perm(s.x, 0u, 0x1010), __byte_perm(s.x, 0u, 0x3232));
+    return s;
 }
 // The eight weights of a word in their order: each byte's codes to bits 3..6 of the halves by one multiplication, then as in weights4.
 __device__ __forceinline__ void weights4_in_order(uint32_t word, uint32_t s2, uint32_t c2, uint32_t* w) {
@@ -360,10 +367,10 @@ template <int BN, int MODE>
 __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap x_map,
                                                          const __grid_constant__ MmArgs a, const __grid_constant__ Second<MODE> second,
                                                          const __grid_constant__ Scales4 scales) {
-    constexpr int kSlots = kC4Slots<BN>;
+    constexpr int kSlots = kC4Slots<BN>, kSets = kC4Warps / 4, kSub = kC4Cols / kC4Unit;
     constexpr uint32_t kDesc = instr_desc(false, false, kMI, BN);
     extern __shared__ unsigned char mm4_smem_raw[];
-    __shared__ uint64_t full[kSlots], ready[kSlots], empty[kSlots], acc_full;
+    __shared__ uint64_t full[kSlots], empty[kSlots], ready[kC4Made], used[kC4Made], acc_full;
     __shared__ uint32_t tmem_slot;
     __shared__ int err_word;
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(mm4_smem_raw) + 1023u) & ~(uintptr_t)1023u);
@@ -372,16 +379,21 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int tile = (int)(blockIdx.x / (unsigned)split);
     const int64_t i0 = (int64_t)(tile % a.tiles_i) * kTileI<MODE>, j0 = (int64_t)(tile / a.tiles_i) * BN;
-    const int64_t steps = (a.n_c + kC4Cols - 1) / kC4Cols;
-    const int s0 = (int)(steps * rank / split), s1 = (int)(steps * (rank + 1) / split);   // split <= steps: never empty
+    const int64_t all_steps = (a.n_c + kC4Cols - 1) / kC4Cols;
+    const int s0 = (int)(all_steps * rank / split), steps = (int)(all_steps * (rank + 1) / split) - s0;   // split <= steps: never empty
+    const int u0 = s0 * kSub, all_units = (int)((a.n_c + kC4Unit - 1) / kC4Unit);                          // a last stage may be half a one
+    const int units = (all_units < u0 + steps * kSub ? all_units : u0 + steps * kSub) - u0;
 
     if (threadIdx.x == 0) {
         prefetch_map(&code_map);
         prefetch_map(&x_map);
         for (int s = 0; s < kSlots; ++s) {
             mbar_init(&full[s], 1u);
-            mbar_init(&ready[s], 4u);   // the four warps that make a stage's weights
-            mbar_init(&empty[s], 1u);
+            mbar_init(&empty[s], 1u);    // the products of its columns have completed, so its codes have been read
+        }
+        for (int s = 0; s < kC4Made; ++s) {
+            mbar_init(&ready[s], 4u);    // the four warps that make a unit's weights
+            mbar_init(&used[s], 1u);     // its products have completed
         }
         mbar_init(&acc_full, 1u);
         *err = 0;
@@ -396,19 +408,18 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot, tmem_a = tmem + kC4Acc<BN>;
-    uint32_t issued = 0;
     allow_next_kernel();   // not before this CTA has its tensor memory: the next kernel's CTAs wait for it with theirs in hand
     await_previous_kernel();
 
     if (warp == 0) {
         if (lane == 0) {
             const bool whole = one_box(second, i0);
-            for (int s = s0; s < s1; ++s) {
-                const uint32_t it = (uint32_t)(s - s0), slot = it % kSlots, ph = (it / kSlots) & 1u;
-                if (!mbar_wait(&empty[slot], ph ^ 1u, err)) break;
+            for (int s = 0; s < steps; ++s) {
+                const int slot = s % kSlots;
+                if (!mbar_wait(&empty[slot], ((uint32_t)(s / kSlots) & 1u) ^ 1u, err)) break;
                 mbar_expect_tx(&full[slot], kC4Slot<BN>);
-                unsigned char* codes = ring + (size_t)slot * kC4Slot<BN>;
-                const int c = s * (kC4Cols / 2);
+                unsigned char* codes = ring + slot * kC4Slot<BN>;
+                const int c = (s0 + s) * (kC4Cols / 2);
                 if constexpr (MODE == kGate) {
                     if (whole) tma_load_box4(codes, &second.both, &full[slot], c, (int)i0 / kGateRows);
 #pragma unroll
@@ -420,30 +431,56 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
                     tma_load_box(codes, &code_map, &full[slot], c, (int)i0);
                 }
 #pragma unroll
-                for (int h = 0; h < 2; ++h) tma_load_box(codes + kC4Bytes + h * (BN * kMC * 2), &x_map, &full[slot], s * kC4Cols + h * kMC, (int)j0);
-                issued = it + 1u;
+                for (int h = 0; h < kC4Cols / kMC; ++h)
+                    tma_load_box(codes + kC4Bytes + h * (BN * kMC * 2), &x_map, &full[slot], (s0 + s) * kC4Cols + h * kMC, (int)j0);
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            bool ok = true;
-            for (int s = s0; s < s1 && ok; ++s) {
-                const uint32_t it = (uint32_t)(s - s0), slot = it % kSlots, ph = (it / kSlots) & 1u;
-                ok = mbar_wait(&full[slot], ph, err) && mbar_wait(&ready[slot], ph, err);
+        // all lanes alike, one of them issues; its pace is the pipeline's
+        const bool issue = elect_one();
+        const uint32_t acc = __shfl_sync(0xFFFFFFFFu, tmem, 0), made0 = acc + kC4Acc<BN>;
+        const uint64_t d0 = operand_desc(smem_u32(ring) + kC4Bytes, 16u);
+        const uint32_t hi = (uint32_t)(d0 >> 32), lo0 = __shfl_sync(0xFFFFFFFFu, (uint32_t)d0, 0);
+        bool ok = true;
+        int u = 0, slot = 0, made = 0;
+        uint32_t slot_ph = 0, made_ph = 0, lo = lo0;
+        while (u < units) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[slot], slot_ph, err));
+            if (!ok) break;
+#pragma unroll
+            for (int h = 0; h < kSub; ++h) {
+                if (u == units) break;
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&ready[made], made_ph, err));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t sb = smem_u32(ring + (size_t)slot * kC4Slot<BN>) + kC4Bytes;
+                const uint32_t from = made0 + (uint32_t)made * 64u;
+                if (issue) {
 #pragma unroll
-                for (int k = 0; k < kC4Cols / 16; ++k) {
-                    const uint64_t db = operand_desc(sb + (uint32_t)(k / 4) * (BN * kMC * 2) + (uint32_t)(k % 4) * 32u, 16u);
-                    umma_bf16_from_tmem(tmem, tmem_a + slot * 64u + (uint32_t)k * 8u, db, kDesc, (it > 0 || k > 0) ? 1u : 0u);
+                    for (int k = 0; k < kC4Unit / 16; ++k)
+                        umma_bf16_from_tmem(acc, from + (uint32_t)k * 8u, lo + (uint32_t)((h * (kC4Unit / kMC) + k / 4) * (BN * kMC * 2) + (k % 4) * 32) / 16u, hi, kDesc,
+                                            h > 0 || k > 0 || u > 0);
+                    umma_commit(&used[made]);
                 }
-                umma_commit(&empty[slot]);
+                __syncwarp();
+                ++u;
+                if (++made == kC4Made) {
+                    made = 0;
+                    made_ph ^= 1u;
+                }
             }
-            if (ok) umma_commit(&acc_full);
+            if (!ok) break;
+            if (issue) umma_commit(&empty[slot]);
+            __syncwarp();
+            lo += kC4Slot<BN> / 16u;
+            if (++slot == kSlots) {
+                slot = 0;
+                slot_ph ^= 1u;
+                lo = lo0;
+            }
         }
+        if (ok && issue) umma_commit(&acc_full);
     } else {
-        // a weight row a lane; the two sets of four warps take stages in turn
+        // a weight row a lane; sets of four warps take units in turn
         const int q = warp & 3, set = (warp - kMRoles) >> 2, r = q * 32 + lane;
         int64_t row = i0 + r;
         bool other = false;
@@ -456,35 +493,34 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
         const int shift = other ? scales.shift2 : scales.shift, groups = other ? scales.groups2 : scales.groups;
         const bool wide = (other ? scales.wide2 : scales.wide) != 0;
         uint2 next = make_uint2(0u, 0u);
-        if (s0 + set < s1) next = scales_of(at, (s0 + set) * kC4Cols, shift, groups, wide);
-        for (int s = s0 + set; s < s1; s += 2) {
-            const uint32_t it = (uint32_t)(s - s0), slot = it % kSlots, ph = (it / kSlots) & 1u;
-            const uint2 sc = next;
-            if (s + 2 < s1) next = scales_of(at, (s + 2) * kC4Cols, shift, groups, wide);
-            // the codes have landed; the loader had waited for the products of the slot's last turn, so its tensor memory is free too
-            if (!mbar_wait(&full[slot], ph, err)) break;
+        if (set < units) next = scales_of(at, (u0 + set) * kC4Unit, shift, groups, wide);
+        for (int u = set; u < units; u += kSets) {
+            const int s = u / kSub, slot = s % kSlots, made = u % kC4Made;
+            const uint2 sc = scales_spread(next, shift);
+            if (u + kSets < units) next = scales_of(at, (u0 + u + kSets) * kC4Unit, shift, groups, wide);
+            if (!mbar_wait(&full[slot], (uint32_t)(s / kSlots) & 1u, err) || !mbar_wait(&used[made], ((uint32_t)(u / kC4Made) & 1u) ^ 1u, err)) break;
             __syncwarp();
             tc_fence_after();
-            const unsigned char* codes = ring + (size_t)slot * kC4Slot<BN> + r * 64;
+            const unsigned char* codes = ring + slot * kC4Slot<BN> + r * 128;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t w[32];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int c = h * 2 + e;
-                    const uint4 v = *reinterpret_cast<const uint4*>(codes + ((c ^ ((r >> 1) & 3)) << 4));
+                    const int c = (u % kSub) * 4 + h * 2 + e;
+                    const uint4 v = *reinterpret_cast<const uint4*>(codes + ((c ^ (r & 7)) << 4));
                     const uint32_t both = h == 0 ? sc.x : sc.y, s2 = __byte_perm(both, 0u, e == 0 ? 0x1010 : 0x3232), c2 = minus24(s2);
                     weights4_in_order(v.x, s2, c2, w + e * 16);
                     weights4_in_order(v.y, s2, c2, w + e * 16 + 4);
                     weights4_in_order(v.z, s2, c2, w + e * 16 + 8);
                     weights4_in_order(v.w, s2, c2, w + e * 16 + 12);
                 }
-                tmem_store32(tmem_a + ((uint32_t)(q * 32) << 16) + slot * 64u + (uint32_t)h * 32u, w);
+                tmem_store32(tmem_a + ((uint32_t)(q * 32) << 16) + (uint32_t)made * 64u + (uint32_t)h * 32u, w);
             }
             tmem_stored();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&ready[slot]);
+            if (lane == 0) mbar_arrive(&ready[made]);
         }
     }
     __syncwarp();
@@ -507,12 +543,9 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
     if (threadIdx.x == 0 && *err != 0) {
-        // a role gave up: let the loads of the last stages land before shared memory is reused or left (bounded)
-        for (uint32_t back = 1; back <= (uint32_t)kSlots && back <= issued; ++back) {
-            const uint32_t it = issued - back, slot = it % kSlots, ph = (it / kSlots) & 1u;
-            const long long t0 = clock64();
-            while (!mbar_try_wait(&full[slot], ph) && clock64() - t0 < kWaitCycles) {
-            }
+        // a role gave up: let loads on their way land before shared memory is reused or left (bounded)
+        const long long t0 = clock64();
+        while (clock64() - t0 < kLandCycles) {
         }
         if (a.status != nullptr) atomicExch(a.status, 1);
     }
@@ -622,8 +655,8 @@ template <bool GATE> int launch_few4(Few4Args a, cudaStream_t st) {
     return MOSAIC_OK;
 }
 
-// Nanoseconds of 128 columns of a tile by its tokens, and the rest as in mm.cuh.
-constexpr int64_t k4Step = 230, k4WideStep = 330;
+// Nanoseconds of 256 columns of a tile by its tokens, and the rest as in mm.cuh.
+constexpr int64_t k4Step = 600, k4WideStep = 700;
 
 template <int BN, int MODE>
 int launch_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& x, MmArgs a, const GateArgs& g, int split, cudaStream_t st) {
@@ -641,7 +674,7 @@ int launch_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& 
     if (!encode_bytes(&code_map, W->codes, a.n_i, width, W->ldc, MODE == kGate ? kGateRows : kMI) || !encode_bf16(&x_map, x.p, x.rows, x.cols, x.ld, BN, kMC))
         return MOSAIC_ERR_CUDA;
     const auto wide = [](const mosaic_weight4* w) {
-        const int64_t n = kC4Cols / w->group;
+        const int64_t n = kC4Unit / w->group;
         return w->lds % n == 0 && (reinterpret_cast<uintptr_t>(w->scales) & (uintptr_t)(2 * n - 1)) == 0 ? 1 : 0;
     };
     const auto groups = [&](const mosaic_weight4* w) { return (int)((a.n_c + w->group - 1) / w->group); };
