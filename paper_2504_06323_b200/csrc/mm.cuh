@@ -516,28 +516,34 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            bool ok = true;
-            for (int s = s0; s < s1; ++s) {
-                const uint32_t it = (uint32_t)(s - s0), slot = it % (uint32_t)a.stages, ph = (it / (uint32_t)a.stages) & 1u;
-                if (!mbar_wait(&full[slot], ph, err)) {
-                    ok = false;
-                    break;
-                }
-                tc_fence_after();
-                const uint32_t stage = smem_u32(ring + (size_t)slot * kStage);
+        // all lanes alike, one of them issues (umma.cuh, elect_one)
+        const bool issue = elect_one();
+        const uint32_t acc = __shfl_sync(0xFFFFFFFFu, tmem, 0), ring0 = __shfl_sync(0xFFFFFFFFu, smem_u32(ring), 0);
+        bool ok = true;
+        uint32_t slot = 0, ph = 0;
+        for (int s = s0; s < s1; ++s) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[slot], ph, err));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t stage = ring0 + slot * kStage;
+            if (issue) {
 #pragma unroll
                 for (int k = 0; k < kMSub * kMC / 16; ++k) {
                     // 16 contraction steps further: 16 swizzle rows (MN-major) or 32 bytes along one (K-major)
                     const uint32_t sa = stage + (uint32_t)(k / (kMC / 16)) * kHalf, sb = sa + kABytes, kk = (uint32_t)(k % (kMC / 16));
                     const uint64_t da = operand_desc(sa + kk * (A_MN ? 2048u : 32u), A_MN ? kMBox : 16u);
                     const uint64_t db = operand_desc(sb + kk * (B_MN ? 2048u : 32u), B_MN ? kMBox : 16u);
-                    umma_bf16(tmem, da, db, kDesc, (it > 0 || k > 0) ? 1u : 0u);
+                    umma_bf16(acc, da, db, kDesc, (s > s0 || k > 0) ? 1u : 0u);
                 }
                 umma_commit(&empty[slot]);
             }
-            if (ok) umma_commit(&acc_full);
+            __syncwarp();
+            if (++slot == (uint32_t)a.stages) {
+                slot = 0;
+                ph ^= 1u;
+            }
         }
+        if (ok && issue) umma_commit(&acc_full);
     }
     __syncwarp();
     const bool done = warp >= 2 && mbar_wait(&acc_full, 0u, err);
@@ -697,31 +703,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
             issued = it;
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
-            uint32_t it = 0, n = 0;
+        if (rank == 0) {   // all lanes alike, one of them issues
+            const bool issue = elect_one();
+            const uint32_t acc = __shfl_sync(0xFFFFFFFFu, tmem, 0), ring0 = __shfl_sync(0xFFFFFFFFu, smem_u32(ring), 0);
+            uint32_t slot = 0, ph = 0, n = 0;
             bool ok = true;
             for (int tile = pair; tile < tiles && ok; tile += pairs, ++n) {
                 const uint32_t buf = n & 1u;
-                if (!mbar_wait_cluster(&acc_empty[buf], ((n >> 1) & 1u) ^ 1u, err)) break;
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(&acc_empty[buf], ((n >> 1) & 1u) ^ 1u, err));
+                if (!ok) break;
                 tc_fence_after();
-                for (int s = 0; s < steps; ++s, ++it) {
-                    const uint32_t slot = it % kPStages, ph = (it / kPStages) & 1u;
-                    if (!mbar_wait_cluster(&full[slot], ph, err)) {
-                        ok = false;
-                        break;
-                    }
+                for (int s = 0; s < steps; ++s) {
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(&full[slot], ph, err));
+                    if (!ok) break;
                     tc_fence_after();
-                    const uint32_t stage = smem_u32(ring + (size_t)slot * kPStage);
+                    const uint32_t stage = ring0 + slot * kPStage;
+                    if (issue) {
 #pragma unroll
-                    for (int k = 0; k < kPSub * kMC / 16; ++k) {
-                        const uint32_t sa = stage + (uint32_t)(k / (kMC / 16)) * 2u * kPOperand, sb = sa + kPOperand, kk = (uint32_t)(k % (kMC / 16));
-                        const uint64_t da = operand_desc(sa + kk * (A_MN ? 2048u : 32u), A_MN ? kMBox : 16u);
-                        const uint64_t db = operand_desc(sb + kk * (B_MN ? 2048u : 32u), B_MN ? kMBox : 16u);
-                        umma_bf16_pair(tmem + buf * 256u, da, db, kDesc, (s > 0 || k > 0) ? 1u : 0u);
+                        for (int k = 0; k < kPSub * kMC / 16; ++k) {
+                            const uint32_t sa = stage + (uint32_t)(k / (kMC / 16)) * 2u * kPOperand, sb = sa + kPOperand, kk = (uint32_t)(k % (kMC / 16));
+                            const uint64_t da = operand_desc(sa + kk * (A_MN ? 2048u : 32u), A_MN ? kMBox : 16u);
+                            const uint64_t db = operand_desc(sb + kk * (B_MN ? 2048u : 32u), B_MN ? kMBox : 16u);
+                            umma_bf16_pair(acc + buf * 256u, da, db, kDesc, (s > 0 || k > 0) ? 1u : 0u);
+                        }
+                        umma_commit_pair(&empty[slot]);
                     }
-                    umma_commit_pair(&empty[slot]);
+                    __syncwarp();
+                    if (++slot == (uint32_t)kPStages) {
+                        slot = 0;
+                        ph ^= 1u;
+                    }
                 }
-                if (ok) umma_commit_pair(&acc_full[buf]);
+                if (ok && issue) umma_commit_pair(&acc_full[buf]);
+                __syncwarp();
             }
         }
     } else {

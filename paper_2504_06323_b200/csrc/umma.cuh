@@ -64,6 +64,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
 }
 
 __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* err, long long budget = kWaitCycles) {
+    if (mbar_try_wait_cluster(bar, parity)) return true;
     const long long t0 = clock64();
     while (!mbar_try_wait_cluster(bar, parity)) {
         if (*err != 0) return false;
