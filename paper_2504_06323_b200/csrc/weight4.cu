@@ -656,7 +656,7 @@ template <bool GATE> int launch_few4(Few4Args a, cudaStream_t st) {
 }
 
 // Nanoseconds of 256 columns of a tile by its tokens, and the rest as in mm.cuh.
-constexpr int64_t k4Step = 600, k4WideStep = 700;
+constexpr int64_t k4Step = 670, k4WideStep = 1000;
 
 template <int BN, int MODE>
 int launch_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& x, MmArgs a, const GateArgs& g, int split, cudaStream_t st) {
