@@ -27,11 +27,13 @@ __global__ void __launch_bounds__(32 * kSavedWarps) store_kernel(const uint16_t*
     }
 #pragma unroll
     for (int r = 0; r < kSavedRows; ++r) {
-        uint32_t largest = largest_finite8(w[r]);
+        uint32_t largest = largest8(w[r]);
+        const bool finite = largest < kNotFinite;
+        if (!finite) largest = largest_finite8(w[r]);
         largest = max(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, 1));
         if (r0 + r >= rows || c >= (cols + kSavedGroup - 1) / kSavedGroup * kSavedGroup) continue;
         const uint32_t E = saved_exponent(largest);
-        *reinterpret_cast<uint2*>(out.codes + (r0 + r) * out.ldc + c) = saved_codes8(w[r], E);
+        *reinterpret_cast<uint2*>(out.codes + (r0 + r) * out.ldc + c) = saved_codes8(w[r], E, finite);
         if ((lane & 1) == 0) out.exponents[(r0 + r) * out.lde + c / kSavedGroup] = (uint8_t)E;
     }
 }

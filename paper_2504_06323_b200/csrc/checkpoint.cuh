@@ -34,60 +34,69 @@ int store_saved(const void* X, int64_t ldx, int64_t rows, int64_t cols, const Sa
 int load_saved(const Saved& in, int64_t rows, int64_t cols, void* X, int64_t ldx, cudaStream_t st);
 
 #ifdef __CUDACC__
-// The largest magnitude's bits among eight values: of all, unless one is not finite, then of the finite ones.
-__device__ __forceinline__ uint32_t finite_bits(uint32_t half) { return (half & 0x7F80u) == 0x7F80u ? 0u : half & 0x7FFFu; }
-__device__ __forceinline__ uint32_t largest_finite8(const uint32_t (&w)[4]) {
+// The largest magnitude's bits among eight values, infinities and NaN above all numbers; and among the finite ones.
+__device__ __forceinline__ uint32_t largest8(const uint32_t (&w)[4]) {
     const uint32_t m = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
-    uint32_t largest = max(m & 0xFFFFu, m >> 16);
-    if (largest >= 0x7F80u) {
-        largest = 0;
+    return max(m & 0xFFFFu, m >> 16);
+}
+constexpr uint32_t kNotFinite = 0x7F80u;
+__device__ __forceinline__ uint32_t finite_bits(uint32_t half) { return (half & kNotFinite) == kNotFinite ? 0u : half & 0x7FFFu; }
+__device__ __forceinline__ uint32_t largest_finite8(const uint32_t (&w)[4]) {
+    uint32_t largest = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) largest = max(largest, max(finite_bits(w[e] & 0xFFFFu), finite_bits(w[e] >> 16)));
-    }
+    for (int e = 0; e < 4; ++e) largest = max(largest, max(finite_bits(w[e] & 0xFFFFu), finite_bits(w[e] >> 16)));
     return largest;
 }
 __device__ __forceinline__ uint32_t saved_exponent(uint32_t largest) { return largest >> 7 > 1u ? largest >> 7 : 1u; }
 
-// Eight values' codes.  Adding 3 2^22 rounds a small number to a whole one (ties to even) in the float's low bits; the eight
-// sums are packed by multiplying them into place and taking off what the exponents' bits add up to.  128 more in each keeps
-// borrows out, and comes off as the bytes' top bits.
-__device__ __forceinline__ uint2 saved_codes8(const uint32_t (&w)[4], uint32_t E) {
-    const float up = __uint_as_float((E >= 6u ? 260u - E : 254u) << 23);   // 2^(133 - E), or as much of it as a float holds
+// Eight values' codes.  One fma scales (exactly) and rounds: adding 3 2^22 leaves a small number's whole part in the float's low
+// bits, ties to even.  The eight sums are packed by multiplying them into place and taking off what the exponents' bits add
+// up to.  128 more in each keeps borrows out, and comes off as the bytes' top bits.  finite: all eight are.
+__device__ __forceinline__ uint2 saved_codes8(const uint32_t (&w)[4], uint32_t E, bool finite) {
     constexpr float kRound = 12582912.0f + 128.0f;
     constexpr uint32_t kBits = 0x4B400000u, kAll = kBits * 0x01010101u;
-    uint32_t q[2];
+    uint32_t q[2] = {0u, 0u};
+    const float up = __uint_as_float((E >= 6u ? 260u - E : 254u) << 23);   // 2^(133 - E), or as much of it as a float holds
+    if (E >= 6u) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        uint32_t sum = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float y = __fmul_rn(half_of(w, h * 4 + e), up);
-            if (E < 6u) y = __fmul_rn(y, __uint_as_float((133u - E) << 23));
-            y = __fadd_rn(fminf(fmaxf(y, -127.0f), 127.0f), kRound);   // +-127.5 is the one that would leave the range
-            sum += __float_as_uint(y) << (8 * e);
+        for (int e = 0; e < 8; ++e) {   // +-127.5 is the one that would leave the range
+            const float y = fminf(fmaxf(__fmaf_rn(half_of(w, e), up, kRound), kRound - 127.0f), kRound + 127.0f);
+            q[e >> 2] += __float_as_uint(y) << (8 * (e & 3));
         }
-        q[h] = (sum - kAll) ^ 0x80808080u;
+    } else {
+        const float more = __uint_as_float((133u - E) << 23);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float y = fminf(fmaxf(__fmaf_rn(__fmul_rn(half_of(w, e), up), more, kRound), kRound - 127.0f), kRound + 127.0f);
+            q[e >> 2] += __float_as_uint(y) << (8 * (e & 3));
+        }
     }
-    const uint32_t m = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
-    if (max(m & 0xFFFFu, m >> 16) >= 0x7F80u) {   // rare
+    q[0] = (q[0] - kAll) ^ 0x80808080u;
+    q[1] = (q[1] - kAll) ^ 0x80808080u;
+    if (!finite) {   // rare
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t half = (e & 1) ? w[e >> 1] >> 16 : w[e >> 1];
-            if ((half & 0x7F80u) == 0x7F80u) q[e >> 2] = (q[e >> 2] & ~(0xFFu << (8 * (e & 3)))) | (0x80u << (8 * (e & 3)));
+            if ((half & kNotFinite) == kNotFinite) q[e >> 2] = (q[e >> 2] & ~(0xFFu << (8 * (e & 3)))) | (0x80u << (8 * (e & 3)));
         }
     }
     return make_uint2(q[0], q[1]);
 }
 
-// Eight values from their codes, exactly: a byte under the exponent of 2^23 is 2^23 + code + 128.
+// Eight values from their codes, exactly: a byte in the middle of a float of exponent 2^15 makes it 2^15 + code + 128, and one fma
+// takes the 32896 off and scales.
 __device__ __forceinline__ void saved_values8(uint2 codes, uint32_t E, float (&v)[8]) {
-    // 2^(E - 133): a normal number from E = 7 on, below a subnormal one
-    const float step = __uint_as_float(E >= 7u ? (E - 6u) << 23 : (E == 0u ? 0u : 1u << (E + 16u)));
     const uint32_t u[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u};
+    if (E < 230u) {
+        // 2^(E - 133): a normal number from E = 7 on, below a subnormal one
+        const float step = __uint_as_float(E >= 7u ? (E - 6u) << 23 : (E == 0u ? 0u : 1u << (E + 16u))), less = __fmul_rn(step, -32896.0f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float f = __uint_as_float(__byte_perm(u[e >> 2], 0x4B000000u, 0x7440 | (e & 3)));
-        v[e] = __fmul_rn(__fsub_rn(f, 8388736.0f), step);
+        for (int e = 0; e < 8; ++e) v[e] = __fmaf_rn(__uint_as_float(__byte_perm(u[e >> 2], 0x47000000u, 0x7404 | ((e & 3) << 4))), step, less);
+    } else {   // what is taken off would leave a float's range
+        const float step = __uint_as_float((E - 6u) << 23);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = __fmul_rn(__fsub_rn(__uint_as_float(__byte_perm(u[e >> 2], 0x47000000u, 0x7404 | ((e & 3) << 4))), 32896.0f), step);
     }
     const auto no_zero = [](uint32_t x) { return ((x - 0x01010101u) & ~x & 0x80808080u) == 0u; };
     if (!no_zero(u[0]) || !no_zero(u[1])) {   // a zero byte is the code of what was not finite: rare

@@ -33,21 +33,27 @@ __device__ __forceinline__ float scale_of(float largest) {
 }
 
 // Eight codes, 8 added to each.  w / s is made correctly rounded from the correctly rounded reciprocal by one correction (Markstein's
-// division; every step but the last exact or harmless while nothing underflows, so tiny scales divide).  Adding 3 2^22 rounds
-// it to a whole number in the float's low bits; the eight are packed by multiplying them into place and taking off what
-// the exponents' bits add up to.
+// division; nothing underflows between the borders of the first branch, and w / s is below 7.3 there: s is within 2^-5 of a
+// seventh of the largest).  Adding 3 2^22 rounds it to a whole number in the float's low bits, ties to even; the eight are
+// packed by multiplying them into place and taking off what the exponents' bits add up to.
 __device__ __forceinline__ uint32_t codes_of8(const uint32_t (&w)[4], float s) {
-    const float r = __frcp_rn(s);
     constexpr float kRound = 12582912.0f + 8.0f;
     constexpr uint32_t kBits = 0x4B400000u, kAll = kBits * 0x11111111u;
     uint32_t sum = 0;
+    if (s > 7.8886091e-31f && s < 1.0e37f) {   // 2^-100
+        const float r = __frcp_rn(s);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float x = half_of(w, e);
-        float y = __fmul_rn(x, r);
-        y = __fmaf_rn(__fmaf_rn(-y, s, x), r, y);
-        if (s < 7.8886091e-31f) y = __fdiv_rn(x, s);   // 2^-100
-        sum += __float_as_uint(__fadd_rn(fminf(fmaxf(y, -7.0f), 7.0f), kRound)) << (4 * e);
+        for (int e = 0; e < 8; ++e) {
+            const float x = half_of(w, e), y = __fmul_rn(x, r);
+            sum += __float_as_uint(__fadd_rn(__fmaf_rn(__fmaf_rn(-y, s, x), r, y), kRound)) << (4 * e);
+        }
+    } else {
+#pragma unroll 1
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t pair = e < 4 ? (e < 2 ? w[0] : w[1]) : (e < 6 ? w[2] : w[3]);
+            const float x = __uint_as_float((e & 1) ? pair & 0xFFFF0000u : pair << 16);
+            sum += __float_as_uint(__fadd_rn(fminf(fmaxf(__fdiv_rn(x, s), -7.0f), 7.0f), kRound)) << (4 * e);
+        }
     }
     return sum - kAll;
 }
