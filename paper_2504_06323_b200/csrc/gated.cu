@@ -83,7 +83,7 @@ template <bool VEC, bool SAVED> struct SlopeRow {
 // A warp takes 256 columns, a lane eight of them, the CTA's eight warps every eighth row of its band, the next row on its way
 // while one is computed; with SUMS the warps' column sums meet in shared memory in their order.
 template <bool VEC, bool SAVED, bool SUMS>
-__global__ void __launch_bounds__(32 * 8) gated_slope_kernel(const __grid_constant__ GatedSlope a) {
+__global__ void __launch_bounds__(32 * 8, VEC && SUMS ? 2 : 4) gated_slope_kernel(const __grid_constant__ GatedSlope a) {
     constexpr int kWarps = 8;
     __shared__ float sums[SUMS ? kWarps : 1][kWarpCols];
     __shared__ uint4 turns[VEC ? 1 : kWarps][32];

@@ -315,17 +315,21 @@ __global__ void __launch_bounds__(32 * k4Warps) few4_kernel(const __grid_constan
 
 // ---------------------------------------------------------------- more tokens
 // The tensor cores' product with the weights' tile made on the way: mm_kernel's tile, cluster and epilogue (mm.cuh), but of A only
-// the codes are loaded, 128 rows x 256 columns a stage in 16 KB; 16 warps make bf16 of them, a weight row a lane, and put
+// the codes are loaded, 128 rows x 256 columns a stage in 16 KB; 8 or 12 warps make bf16 of them, a weight row a lane, and put
 // them into tensor memory, where the matrix instruction reads its first operand.  The weights so cross shared memory as codes,
 // once, instead of as bf16 twice: with them in shared memory its bandwidth would hold the stream to about half of what
 // memory gives.
-constexpr int kC4Cols = 256, kC4Unit = 128, kC4Warps = 16, kC4Threads = 32 * (kMRoles + kC4Warps);   // code loader, MMA issue; weight makers
+constexpr int kC4Cols = 256;
+// Sets of four warps make a stage's weights in turn.  No more sets than slots of either ring: a set waits for a slot's phase by its
+// parity alone, so that it must have seen the phase before.
+template <int BN> constexpr int kC4Sets = BN == 128 ? 2 : 3;
+template <int BN> constexpr int kC4Threads = 32 * (kMRoles + 4 * kC4Sets<BN>);   // code loader, MMA issue; weight makers
 constexpr uint32_t kC4Bytes = kMI * kC4Cols / 2, kC4Box = kGateRows * kC4Cols / 2;   // of a stage's codes, of 16 rows of them
 // Rows of 128 bytes a box: the copy engine takes about four cycles a row, whatever its length.  X comes with the codes it meets: in a
 // ring of its own it waited behind the codes of stages to come.
 template <int BN> constexpr int kC4Slots = BN == 16 ? 8 : BN == 32 ? 6 : BN == 64 ? 4 : 2;
 template <int BN> constexpr uint32_t kC4Slot = kC4Bytes + (uint32_t)BN * kC4Cols * 2u;
-constexpr int kC4Made = 6;             // units of 128 columns in tensor memory, 64 of its columns each
+constexpr int kC4Made = 3;             // stages made weights of, 128 columns of tensor memory each
 template <int BN> constexpr uint32_t kC4Acc = BN < 32 ? 32 : BN;                      // tensor-memory columns of the accumulator
 constexpr long long kLandCycles = 20000000ll;   // ten milliseconds: far more than a load takes
 // One CTA an SM: it takes all of the tensor memory, and one that waited for it could hold up its cluster.
@@ -340,22 +344,36 @@ struct Scales4 {
     int wide, wide2;                   // a stage's scales of a row may be read as one word
 };
 
-// The scales of a row's 128 columns from `col` on, past the last group that one's again; as they are loaded, and then for each
-// 32 columns (apart, so that nothing waits for the loads before their stage).
-__device__ __forceinline__ uint2 scales_of(const uint16_t* row, int col, int shift, int groups, bool wide) {
-    const int at = col >> shift;
-    if (shift == 7) return make_uint2(row[at], 0u);
-    if (shift == 6) {
-        if (wide && at + 2 <= groups) return make_uint2(*reinterpret_cast<const uint32_t*>(row + at), 0u);
-        return make_uint2((uint32_t)row[at] | ((uint32_t)row[min(at + 1, groups - 1)] << 16), 0u);
+// The scales of a row's 256 columns from `col` on, past the last group that one's again; as they are loaded, and then a word for each
+// 64 columns, a half for each 32 (apart, so that nothing waits for the loads before their stage).
+__device__ __forceinline__ uint4 scales_of(const uint16_t* row, int col, int shift, int groups, bool wide) {
+    const int at = col >> shift, n = kC4Cols >> shift;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (wide && at + n <= groups) {
+        if (shift == 7) v.x = *reinterpret_cast<const uint32_t*>(row + at);
+        else if (shift == 6) {
+            const uint2 w = *reinterpret_cast<const uint2*>(row + at);
+            v.x = w.x;
+            v.y = w.y;
+        } else {
+            v = *reinterpret_cast<const uint4*>(row + at);
+        }
+        return v;
     }
-    if (wide && at + 4 <= groups) return *reinterpret_cast<const uint2*>(row + at);
-    return make_uint2((uint32_t)row[at] | ((uint32_t)row[min(at + 1, groups - 1)] << 16),
-                      (uint32_t)row[min(at + 2, groups - 1)] | ((uint32_t)row[min(at + 3, groups - 1)] << 16));
+    const auto pair = [&](int k) { return (uint32_t)row[min(at + k, groups - 1)] | ((uint32_t)row[min(at + k + 1, groups - 1)] << 16); };
+    v.x = pair(0);
+    if (shift <= 6) v.y = pair(2);
+    if (shift == 5) {
+        v.z = pair(4);
+        v.w = pair(6);
+    }
+    return v;
 }
-__device__ __forceinline__ uint2 scales_spread(uint2 s, int shift) {
-    if (shift == 7) return make_uint2(__byte_perm(s.x, 0u, 0x1010), __byte_perm(s.x, 0u, 0x1010));
-    if (shift == 6) return make_uint2(__byte_perm(s.x, 0u, 0x1010), __byte_perm(s.x, 0u, 0x3232));
+__device__ __forceinline__ uint4 scales_spread(uint4 s, int shift) {
+    const auto lo = [](uint32_t w) { return __byte_perm(w, 0u, 0x1010); };
+    const auto hi = [](uint32_t w) { return __byte_perm(w, 0u, 0x3232); };
+    if (shift == 7) return make_uint4(lo(s.x), lo(s.x), hi(s.x), hi(s.x));
+    if (shift == 6) return make_uint4(lo(s.x), hi(s.x), lo(s.y), hi(s.y));
     return s;
 }
 // The eight weights of a word in their order: each byte's codes to bits 3..6 of the halves by one multiplication, then as in weights4.
@@ -370,10 +388,11 @@ __device__ __forceinline__ void weights4_in_order(uint32_t word, uint32_t s2, ui
 }
 
 template <int BN, int MODE>
-__global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap x_map,
+__global__ void __launch_bounds__(kC4Threads<BN>) mm4_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap x_map,
                                                          const __grid_constant__ MmArgs a, const __grid_constant__ Second<MODE> second,
                                                          const __grid_constant__ Scales4 scales) {
-    constexpr int kSlots = kC4Slots<BN>, kSets = kC4Warps / 4, kSub = kC4Cols / kC4Unit;
+    constexpr int kSlots = kC4Slots<BN>, kSets = kC4Sets<BN>;
+    static_assert(kSets <= kSlots && kSets <= kC4Made, "a parity tells two phases apart, no more");
     constexpr uint32_t kDesc = instr_desc(false, false, kMI, BN);
     extern __shared__ unsigned char mm4_smem_raw[];
     __shared__ uint64_t full[kSlots], empty[kSlots], ready[kC4Made], used[kC4Made], acc_full;
@@ -387,8 +406,6 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
     const int64_t i0 = (int64_t)(tile % a.tiles_i) * kTileI<MODE>, j0 = (int64_t)(tile / a.tiles_i) * BN;
     const int64_t all_steps = (a.n_c + kC4Cols - 1) / kC4Cols;
     const int s0 = (int)(all_steps * rank / split), steps = (int)(all_steps * (rank + 1) / split) - s0;   // split <= steps: never empty
-    const int u0 = s0 * kSub, all_units = (int)((a.n_c + kC4Unit - 1) / kC4Unit);                          // a last stage may be half a one
-    const int units = (all_units < u0 + steps * kSub ? all_units : u0 + steps * kSub) - u0;
 
     if (threadIdx.x == 0) {
         prefetch_map(&code_map);
@@ -398,7 +415,7 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
             mbar_init(&empty[s], 1u);    // the products of its columns have completed, so its codes have been read
         }
         for (int s = 0; s < kC4Made; ++s) {
-            mbar_init(&ready[s], 4u);    // the four warps that make a unit's weights
+            mbar_init(&ready[s], 4u);    // the four warps that make a stage's weights
             mbar_init(&used[s], 1u);     // its products have completed
         }
         mbar_init(&acc_full, 1u);
@@ -448,35 +465,25 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
         const uint64_t d0 = operand_desc(smem_u32(ring) + kC4Bytes, 16u);
         const uint32_t hi = (uint32_t)(d0 >> 32), lo0 = __shfl_sync(0xFFFFFFFFu, (uint32_t)d0, 0);
         bool ok = true;
-        int u = 0, slot = 0, made = 0;
+        int slot = 0, made = 0;
         uint32_t slot_ph = 0, made_ph = 0, lo = lo0;
-        while (u < units) {
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[slot], slot_ph, err));
+        for (int s = 0; s < steps; ++s) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[slot], slot_ph, err) && mbar_wait(&ready[made], made_ph, err));
             if (!ok) break;
+            tc_fence_after();
+            const uint32_t from = made0 + (uint32_t)made * 128u;
+            if (issue) {
 #pragma unroll
-            for (int h = 0; h < kSub; ++h) {
-                if (u == units) break;
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&ready[made], made_ph, err));
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t from = made0 + (uint32_t)made * 64u;
-                if (issue) {
-#pragma unroll
-                    for (int k = 0; k < kC4Unit / 16; ++k)
-                        umma_bf16_from_tmem(acc, from + (uint32_t)k * 8u, lo + (uint32_t)((h * (kC4Unit / kMC) + k / 4) * (BN * kMC * 2) + (k % 4) * 32) / 16u, hi, kDesc,
-                                            h > 0 || k > 0 || u > 0);
-                    umma_commit(&used[made]);
-                }
-                __syncwarp();
-                ++u;
-                if (++made == kC4Made) {
-                    made = 0;
-                    made_ph ^= 1u;
-                }
+                for (int k = 0; k < kC4Cols / 16; ++k)
+                    umma_bf16_from_tmem(acc, from + (uint32_t)k * 8u, lo + (uint32_t)((k / 4) * (BN * kMC * 2) + (k % 4) * 32) / 16u, hi, kDesc, k > 0 || s > 0);
+                umma_commit(&used[made]);
+                umma_commit(&empty[slot]);
             }
-            if (!ok) break;
-            if (issue) umma_commit(&empty[slot]);
             __syncwarp();
+            if (++made == kC4Made) {
+                made = 0;
+                made_ph ^= 1u;
+            }
             lo += kC4Slot<BN> / 16u;
             if (++slot == kSlots) {
                 slot = 0;
@@ -486,7 +493,7 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
         }
         if (ok && issue) umma_commit(&acc_full);
     } else {
-        // a weight row a lane; sets of four warps take units in turn
+        // a weight row a lane; sets of four warps take stages in turn
         const int q = warp & 3, set = (warp - kMRoles) >> 2, r = q * 32 + lane;
         int64_t row = i0 + r;
         bool other = false;
@@ -498,30 +505,30 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
         const uint16_t* at = other ? scales.p2 + row * scales.ld2 : scales.p + row * scales.ld;
         const int shift = other ? scales.shift2 : scales.shift, groups = other ? scales.groups2 : scales.groups;
         const bool wide = (other ? scales.wide2 : scales.wide) != 0;
-        uint2 next = make_uint2(0u, 0u);
-        if (set < units) next = scales_of(at, (u0 + set) * kC4Unit, shift, groups, wide);
-        for (int u = set; u < units; u += kSets) {
-            const int s = u / kSub, slot = s % kSlots, made = u % kC4Made;
-            const uint2 sc = scales_spread(next, shift);
-            if (u + kSets < units) next = scales_of(at, (u0 + u + kSets) * kC4Unit, shift, groups, wide);
-            if (!mbar_wait(&full[slot], (uint32_t)(s / kSlots) & 1u, err) || !mbar_wait(&used[made], ((uint32_t)(u / kC4Made) & 1u) ^ 1u, err)) break;
+        uint4 next = make_uint4(0u, 0u, 0u, 0u);
+        if (set < steps) next = scales_of(at, (s0 + set) * kC4Cols, shift, groups, wide);
+        for (int s = set; s < steps; s += kSets) {
+            const int slot = s % kSlots, made = s % kC4Made;
+            const uint4 sc = scales_spread(next, shift);
+            if (s + kSets < steps) next = scales_of(at, (s0 + s + kSets) * kC4Cols, shift, groups, wide);
+            if (!mbar_wait(&full[slot], (uint32_t)(s / kSlots) & 1u, err) || !mbar_wait(&used[made], ((uint32_t)(s / kC4Made) & 1u) ^ 1u, err)) break;
             __syncwarp();
             tc_fence_after();
             const unsigned char* codes = ring + slot * kC4Slot<BN> + r * 128;
+            const uint32_t to = tmem_a + ((uint32_t)(q * 32) << 16) + (uint32_t)made * 128u;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 4; ++h) {
                 uint32_t w[32];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int c = (u % kSub) * 4 + h * 2 + e;
-                    const uint4 v = *reinterpret_cast<const uint4*>(codes + ((c ^ (r & 7)) << 4));
-                    const uint32_t both = h == 0 ? sc.x : sc.y, s2 = __byte_perm(both, 0u, e == 0 ? 0x1010 : 0x3232), c2 = minus24(s2);
+                    const uint4 v = *reinterpret_cast<const uint4*>(codes + (((h * 2 + e) ^ (r & 7)) << 4));
+                    const uint32_t both = h == 0 ? sc.x : h == 1 ? sc.y : h == 2 ? sc.z : sc.w, s2 = __byte_perm(both, 0u, e == 0 ? 0x1010 : 0x3232), c2 = minus24(s2);
                     weights4_in_order(v.x, s2, c2, w + e * 16);
                     weights4_in_order(v.y, s2, c2, w + e * 16 + 4);
                     weights4_in_order(v.z, s2, c2, w + e * 16 + 8);
                     weights4_in_order(v.w, s2, c2, w + e * 16 + 12);
                 }
-                tmem_store32(tmem_a + ((uint32_t)(q * 32) << 16) + (uint32_t)made * 64u + (uint32_t)h * 32u, w);
+                tmem_store32(to + (uint32_t)h * 32u, w);
             }
             tmem_stored();
             tc_fence_before();
@@ -540,7 +547,7 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
         cluster_arrive();
         cluster_wait();
     }
-    if (done) tile_out<BN, MODE, kC4Warps / 4>(a, second, tmem, part, per, rank, split, n_cols, i0, j0);
+    if (done) tile_out<BN, MODE, kSets>(a, second, tmem, part, per, rank, split, n_cols, i0, j0);
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -558,7 +565,7 @@ __global__ void __launch_bounds__(kC4Threads) mm4_kernel(const __grid_constant__
     if (split > 1) {
         __syncwarp();
         cluster_arrive();
-        tile_join<MODE, kC4Threads>(a, second, part, per, rank, split, n_cols, i0, j0);
+        tile_join<MODE, kC4Threads<BN>>(a, second, part, per, rank, split, n_cols, i0, j0);
     }
 }
 
@@ -662,7 +669,7 @@ template <bool GATE> int launch_few4(Few4Args a, cudaStream_t st) {
 }
 
 // Nanoseconds of 256 columns of a tile by its tokens, and the rest as in mm.cuh.
-constexpr int64_t k4Step = 670, k4WideStep = 1000;
+constexpr int64_t k4Step = 590, k4WideStep = 1050;
 
 template <int BN, int MODE>
 int launch_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& x, MmArgs a, const GateArgs& g, int split, cudaStream_t st) {
@@ -680,7 +687,7 @@ int launch_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& 
     if (!encode_bytes(&code_map, W->codes, a.n_i, width, W->ldc, MODE == kGate ? kGateRows : kMI) || !encode_bf16(&x_map, x.p, x.rows, x.cols, x.ld, BN, kMC))
         return MOSAIC_ERR_CUDA;
     const auto wide = [](const mosaic_weight4* w) {
-        const int64_t n = kC4Unit / w->group;
+        const int64_t n = kC4Cols / w->group;
         return w->lds % n == 0 && (reinterpret_cast<uintptr_t>(w->scales) & (uintptr_t)(2 * n - 1)) == 0 ? 1 : 0;
     };
     const auto groups = [&](const mosaic_weight4* w) { return (int)((a.n_c + w->group - 1) / w->group); };
@@ -702,7 +709,7 @@ int launch_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& 
     a.tiles_i = (int)((a.n_i + kTileI<MODE> - 1) / kTileI<MODE>);
     a.tiles_j = (int)((a.n_j + BN - 1) / BN);
     a.split = split;
-    Launch l(dim3((unsigned)((int64_t)a.tiles_i * a.tiles_j * split)), kC4Threads, kC4Smem<BN>, st, split);
+    Launch l(dim3((unsigned)((int64_t)a.tiles_i * a.tiles_j * split)), kC4Threads<BN>, kC4Smem<BN>, st, split);
     MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, mm4_kernel<BN, MODE>, code_map, x_map, a, second, s));
     return MOSAIC_OK;
 }
