@@ -629,9 +629,10 @@ int mosaic_dequantize4(const mosaic_weight4 *in, int64_t rows, int64_t cols, voi
  *     Y = act(X W^T + bias) + residual,   H = act(X W_gate^T + bias_gate) * (X W_up^T + bias_up)
  * Arguments as there; the residual may be Y itself.  dtype is that of X, the biases, the
  * residual and the output: MOSAIC_BF16.
- *   ws        device scratch, >= the query for the same arguments: 0 for up to 32 tokens
+ *   ws        device scratch, >= the query for the same arguments: 0 for up to 256 tokens
  *             when X has a 16-byte aligned base and leading dimension; for more tokens
  *             it holds the weights in bf16
+ *   status_dev  as in mosaic_linear
  * Products are exact, sums in fp32, one rounding to bf16 for the output.
  * ------------------------------------------------------------------------- */
 size_t mosaic_linear4_workspace_bytes(const void *X, int64_t ldx, int64_t tokens, int64_t out_features,
