@@ -24,7 +24,11 @@ struct Weight4 {
 constexpr int kPackWarps = 8, kPackRows = 4;
 
 __device__ __forceinline__ float scale_of(float largest) {
-    const float ideal = __fdiv_rn(largest, 7.0f);
+    // a seventh, correctly rounded: a product and one correction (Markstein's division; below 2^-100, where the remainder
+    // could underflow, divided)
+    const float guess = __fmul_rn(largest, 0.142857149f);
+    float ideal = __fmaf_rn(__fmaf_rn(-7.0f, guess, largest), 0.142857149f, guess);
+    if (largest < 7.8886091e-31f) ideal = __fdiv_rn(largest, 7.0f);
     if (!(ideal <= 1.0633824e37f)) return ideal != ideal ? ideal : 1.0633824e37f;   // 2^123: 24 s below stays finite
     if (ideal < 1.17549435e-38f) return 0.0f;                                       // below bf16's normal numbers
     uint32_t u = __float_as_uint(ideal);
@@ -32,16 +36,19 @@ __device__ __forceinline__ float scale_of(float largest) {
     return __uint_as_float(u & 0xFFF80000u);
 }
 
-// Eight codes, 8 added to each.  w / s is made correctly rounded from the correctly rounded reciprocal by one correction (Markstein's
-// division; nothing underflows between the borders of the first branch, and w / s is below 7.3 there: s is within 2^-5 of a
-// seventh of the largest).  Adding 3 2^22 rounds it to a whole number in the float's low bits, ties to even; the eight are
-// packed by multiplying them into place and taking off what the exponents' bits add up to.
+// Eight codes, 8 added to each.  w / s from an approximate reciprocal and one correction (Markstein's division): off by a rounding at
+// most, and exact where w / s is half a whole number, because the correction's own error is the product of two small
+// ones; every other w / s, of eight bits over five, is 2^-11 or more from such a border.  Between the borders of the first
+// branch nothing underflows and w / s is below 7.3: s is within 2^-5 of a seventh of the largest.  Adding 3 2^22 rounds to a
+// whole number in the float's low bits, ties to even; the eight are packed by multiplying them into place and taking off
+// what the exponents' bits add up to.
 __device__ __forceinline__ uint32_t codes_of8(const uint32_t (&w)[4], float s) {
     constexpr float kRound = 12582912.0f + 8.0f;
     constexpr uint32_t kBits = 0x4B400000u, kAll = kBits * 0x11111111u;
     uint32_t sum = 0;
     if (s > 7.8886091e-31f && s < 1.0e37f) {   // 2^-100
-        const float r = __frcp_rn(s);
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float x = half_of(w, e), y = __fmul_rn(x, r);
@@ -58,7 +65,7 @@ __device__ __forceinline__ uint32_t codes_of8(const uint32_t (&w)[4], float s) {
     return sum - kAll;
 }
 
-template <bool VEC>
+template <bool VEC, int SHIFT>
 __global__ void __launch_bounds__(32 * kPackWarps) quantize4_kernel(const uint16_t* W, int64_t ldw, int64_t rows, int64_t cols, const __grid_constant__ Weight4 out,
                                                                     unsigned chunks) {
     __shared__ uint4 turns[VEC ? 1 : kPackWarps][32];
@@ -77,11 +84,12 @@ __global__ void __launch_bounds__(32 * kPackWarps) quantize4_kernel(const uint16
         // the largest magnitude's bits: infinities and NaN are above all numbers
         const uint32_t m = __vmaxu2(__vmaxu2(w[r][0] & 0x7FFF7FFFu, w[r][1] & 0x7FFF7FFFu), __vmaxu2(w[r][2] & 0x7FFF7FFFu, w[r][3] & 0x7FFF7FFFu));
         uint32_t bits = max(m & 0xFFFFu, m >> 16);
-        for (int o = 1; o < 1 << (out.shift - 3); o <<= 1) bits = max(bits, __shfl_xor_sync(0xFFFFFFFFu, bits, o));
+#pragma unroll
+        for (int o = 1; o < 1 << (SHIFT - 3); o <<= 1) bits = max(bits, __shfl_xor_sync(0xFFFFFFFFu, bits, o));
         const float s = bits >= 0x7F80u ? __uint_as_float(0x7FC00000u) : scale_of(bf16_to_f32((uint16_t)bits));
         if (r0 + r >= rows || c >= (cols + 31) / 32 * 32) continue;
         *reinterpret_cast<uint32_t*>(out.codes + (r0 + r) * out.ldc + c / 2) = s > 0.0f ? codes_of8(w[r], s) : 0x88888888u;
-        if ((c & ((1 << out.shift) - 1)) == 0 && c < cols) out.scales[(r0 + r) * out.lds + (c >> out.shift)] = (uint16_t)(__float_as_uint(s) >> 16);
+        if ((c & ((1 << SHIFT) - 1)) == 0 && c < cols) out.scales[(r0 + r) * out.lds + (c >> SHIFT)] = (uint16_t)(__float_as_uint(s) >> 16);
     }
 }
 
@@ -766,8 +774,11 @@ extern "C" int mosaic_quantize4(const void* W, int64_t rows, int64_t cols, int64
     const int rc = check_pack(W, rows, cols, ldw, dtype, out);
     if (rc != MOSAIC_OK || rows == 0) return rc;
     PackLaunch l(rows, cols, static_cast<cudaStream_t>(stream));
-    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, Matrix{W, rows, cols, ldw}.tma_ok() ? quantize4_kernel<true> : quantize4_kernel<false>,
-                                       static_cast<const uint16_t*>(W), ldw, rows, cols, as_weight4(out), l.chunks));
+    using Kernel = void (*)(const uint16_t*, int64_t, int64_t, int64_t, Weight4, unsigned);
+    static const Kernel kernels[2][3] = {{quantize4_kernel<false, 5>, quantize4_kernel<false, 6>, quantize4_kernel<false, 7>},
+                                         {quantize4_kernel<true, 5>, quantize4_kernel<true, 6>, quantize4_kernel<true, 7>}};
+    const Kernel kernel = kernels[Matrix{W, rows, cols, ldw}.tma_ok() ? 1 : 0][group_shift(out->group) - 5];
+    MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, kernel, static_cast<const uint16_t*>(W), ldw, rows, cols, as_weight4(out), l.chunks));
     return MOSAIC_OK;
 }
 

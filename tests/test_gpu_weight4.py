@@ -89,6 +89,20 @@ def test_packing_ties_and_extremes(group):
     check_pack(empty(0, 40), group)
 
 
+@pytest.mark.parametrize("power", [-120, -99, -12, 0, 60, 118])
+def test_every_value_under_every_scale(power):
+    """A group's largest is 7 s, so its scale is s: every bf16 number up to 7 s beside it, for all 16 significands of s."""
+    rows = []
+    for s in range(16, 32):
+        v = torch.arange(1, 1 << 15, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).double()
+        v = v[(v >= s * 0.2) & (v <= 7.0 * s)]
+        v = torch.nn.functional.pad(v, (0, -v.numel() % 31)).view(-1, 31)
+        rows.append(torch.cat([torch.full((v.shape[0], 1), 7.0 * s, dtype=torch.float64), v], 1))
+    W = (torch.cat(rows) * 2.0 ** power).to(torch.bfloat16)
+    W[1::2, 1:] *= -1
+    check_pack(W.to(DEV), 32)
+
+
 def weight4(n, k, g, group, scale):
     """(packed, the values it stands for)"""
     w4 = api.Weight4.of(matrix(n, k, g, scale=scale), group)
