@@ -189,10 +189,14 @@ int run_gated_slope(const GatedSlope& a, bool vec, bool saved, void* dbias_gate,
 size_t copy_bytes(const Matrix& m) { return m.tma_ok() ? 0 : m.padded_bytes(); }
 Matrix plain(const Matrix& m) { return {nullptr, m.rows, m.cols, m.padded_ld()}; }   // where a call keeps one of its own
 
+// Whether the kernel for few tokens takes a call.
+bool few_tokens(const Matrix& x, const Matrix& wg, const Matrix& wu) { return x.rows <= (x.tma_ok() && wg.tma_ok() && wu.tma_ok() ? kFewVector : kFewTokens); }
+
 size_t forward_workspace(const Matrix& x, const Matrix& wg, const Matrix& wu, bool saved) {
     size_t need = 0;
-    if (x.rows > kFewTokens) need += copy_bytes(x) + copy_bytes(wg) + copy_bytes(wu);
-    if (saved) need += 2 * Matrix{nullptr, x.rows, wg.rows, wg.rows}.padded_bytes();
+    const bool few = few_tokens(x, wg, wu);
+    if (!few) need += copy_bytes(x) + copy_bytes(wg) + copy_bytes(wu);
+    if (few && saved) need += 2 * Matrix{nullptr, x.rows, wg.rows, wg.rows}.padded_bytes();
     return need;
 }
 size_t backward_workspace(const Matrix& dh, const Matrix& x, bool x_saved, const Matrix& wg, const Matrix& wu, bool want_dx, bool want_dw, bool want_db) {
@@ -261,7 +265,8 @@ extern "C" int mosaic_gated_linear(const void* X, int64_t ldx, const void* W_gat
     if (status_dev != nullptr) MOSAIC_CUDA_TRY(cudaMemsetAsync(status_dev, 0, sizeof(int), st));
     if (tokens == 0) return MOSAIC_OK;
     char* scratch = static_cast<char*>(ws);
-    if (saved) {
+    const bool few = few_tokens(x, wg, wu), two_steps = few && saved;   // few tokens: through bf16, whose groups are other warps' too
+    if (two_steps) {
         z = u = plain(h);
         z.p = scratch;
         u.p = scratch + z.padded_bytes();
@@ -273,8 +278,15 @@ extern "C" int mosaic_gated_linear(const void* X, int64_t ldx, const void* W_gat
     a.bias = static_cast<const uint16_t*>(bias_gate);
     a.z = static_cast<uint16_t*>(const_cast<void*>(z.p)); a.ld_z = z.ld;
     a.act = act; a.status = status_dev;
-    const GateArgs g{static_cast<const uint16_t*>(W_up), ld_up, static_cast<const uint16_t*>(bias_up), static_cast<uint16_t*>(const_cast<void*>(u.p)), u.ld};
-    if (tokens <= (x.tma_ok() && wg.tma_ok() && wu.tma_ok() ? kFewVector : kFewTokens)) {
+    GateArgs g = {};
+    g.w = static_cast<const uint16_t*>(W_up); g.ld_w = ld_up;
+    g.bias = static_cast<const uint16_t*>(bias_up);
+    g.u = static_cast<uint16_t*>(const_cast<void*>(u.p)); g.ld_u = u.ld;
+    if (saved && !few) {
+        g.z8 = as_saved(z_saved);
+        g.u8 = as_saved(u_saved);
+    }
+    if (few) {
         if ((rc = launch_few<true>(x, wg, a, st, g)) != MOSAIC_OK) return rc;
     } else {
         if ((rc = readable(x, &scratch, st)) != MOSAIC_OK || (rc = readable(wg, &scratch, st)) != MOSAIC_OK || (rc = readable(wu, &scratch, st)) != MOSAIC_OK) return rc;
@@ -283,7 +295,7 @@ extern "C" int mosaic_gated_linear(const void* X, int64_t ldx, const void* W_gat
         also.gate = g;
         if ((rc = run_mm<false, false, kGate>(wg, x, a, st, also)) != MOSAIC_OK) return rc;
     }
-    if (saved) {
+    if (two_steps) {
         if ((rc = store_saved(z.p, z.ld, tokens, channels, as_saved(z_saved), st)) != MOSAIC_OK) return rc;
         if ((rc = store_saved(u.p, u.ld, tokens, channels, as_saved(u_saved), st)) != MOSAIC_OK) return rc;
     }

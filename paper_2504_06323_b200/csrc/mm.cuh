@@ -13,7 +13,7 @@
 #pragma once
 #include <cooperative_groups.h>
 
-#include "linear.cuh"
+#include "checkpoint.cuh"
 #include "umma.cuh"
 
 namespace cg = cooperative_groups;
@@ -58,6 +58,7 @@ struct GateArgs {
     const uint16_t* bias;              // [n_i] or null
     uint16_t* u;                       // [n_j, n_i] or null
     int64_t ld_u;
+    Saved z8, u8;                      // or, in 8 bits, both of them (codes null: not)
     int swapped;                       // a tile's rows begin with A2's: what lies lower in memory comes first
     int whole;                         // rows that one box loads of both; 0: box by box
 };
@@ -159,6 +160,61 @@ template <int N> __device__ __forceinline__ void epilogue(const MmArgs& a, float
     for (int e = 0; e < N; ++e, p += a.ld_out)
         if (e < n) *p = f32_to_bf16(v[e]);
 }
+// 16 accumulator columns of a warp whose 16 lower and 16 upper lanes each hold a group of channels, v[at + e] in column (token) e < n:
+// the groups in 8 bits, as store_saved would make them of the bf16 values.  Words of two tokens' magnitudes are maximised
+// over the group's lanes, each lane ending with the two of one word (so it has their exponents to write); four tokens' codes are
+// turned round among four lanes, so that a lane writes four channels of a token.
+template <int N> __device__ __forceinline__ void keep16(const Saved& to, const float (&v)[N], int at, int64_t i0, int64_t j, int n) {
+    const int lane = (int)threadIdx.x & 31, l = lane & 15;
+    uint32_t h[8], m[8], any = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        h[k] = pack2(v[at + 2 * k], v[at + 2 * k + 1]);
+        m[k] = h[k] & 0x7FFF7FFFu;
+        any = __vmaxu2(any, m[k]);
+    }
+    if (max(any & 0xFFFFu, any >> 16) >= kNotFinite) {   // rare
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m[k] = finite_bits(h[k] & 0xFFFFu) | (finite_bits(h[k] >> 16) << 16);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[k] = __vmaxu2(m[k], __shfl_xor_sync(0xFFFFFFFFu, m[k], 8));
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < o; ++k) {
+            const bool upper = (lane & o) != 0;
+            const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, upper ? m[k] : m[k + o], o);
+            m[k] = __vmaxu2(upper ? m[k + o] : m[k], other);
+        }
+    const uint32_t E2 = saved_exponent(m[0] & 0xFFFFu) | (saved_exponent(m[0] >> 16) << 16);   // of tokens 2 (l & 7) and the next
+    const int64_t group = i0 / kSavedGroup;
+    if (l < 8) {
+        if (2 * l < n) to.exponents[(j + 2 * l) * to.lde + group] = (uint8_t)E2;
+        if (2 * l + 1 < n) to.exponents[(j + 2 * l + 1) * to.lde + group] = (uint8_t)(E2 >> 16);
+    }
+    constexpr float kRound = 12582912.0f + 128.0f;
+#pragma unroll
+    for (int t = 0; t < 16; t += 4) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t pair = __shfl_sync(0xFFFFFFFFu, E2, (lane & 16) | ((t + e) >> 1)), E = (e & 1) ? pair >> 16 : pair & 0xFFFFu;
+            const uint32_t half = (e & 1) ? h[(t + e) >> 1] >> 16 : h[(t + e) >> 1] & 0xFFFFu;
+            const float up = __uint_as_float((E >= 6u ? 260u - E : 254u) << 23), more = E >= 6u ? 1.0f : __uint_as_float((133u - E) << 23);
+            const float y = fminf(fmaxf(__fmaf_rn(__fmul_rn(__uint_as_float(half << 16), more), up, kRound), kRound - 127.0f), kRound + 127.0f);
+            word |= ((half & kNotFinite) == kNotFinite ? 0u : __float_as_uint(y) & 0xFFu) << (8 * e);   // code + 128; 0: not finite
+        }
+        word ^= 0x80808080u;
+        const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, word, 2);
+        word = (lane & 2) ? __byte_perm(word, other, 0x3276) : __byte_perm(word, other, 0x5410);
+        const uint32_t next = __shfl_xor_sync(0xFFFFFFFFu, word, 1);
+        word = (lane & 1) ? __byte_perm(word, next, 0x3715) : __byte_perm(word, next, 0x6240);
+        const int token = t + (lane & 3);
+        if (token < n) *reinterpret_cast<uint32_t*>(to.codes + (j + token) * to.ldc + i0 + (l & 12)) = word;
+    }
+}
+
 // The same for kGate: lanes below 16 hold rows of A (element i0 + lane), the others of A2, or the other way round.  After the exchange a lane has both
 // values of its element for half of the columns.
 template <int N> __device__ __forceinline__ void gate_epilogue(const MmArgs& a, const GateArgs& g, float (&v)[N], float bias, int64_t i0, int64_t j, int n) {
@@ -184,6 +240,11 @@ template <int N> __device__ __forceinline__ void gate_epilogue(const MmArgs& a, 
             for (int e = 0; e < N; ++e, p += ld_kept)
                 if (e < n) *p = f32_to_bf16(v[e]);
         }
+    }
+    if (g.z8.codes != nullptr && i0 < a.n_i) {
+#pragma unroll
+        for (int at = 0; at < N; at += 16)
+            if (at < n) keep16(up ? g.u8 : g.z8, v, at, i0, j + at, n - at);
     }
     float z[N / 2], u[N / 2];
 #pragma unroll
@@ -312,6 +373,25 @@ __device__ __forceinline__ void tile_out(const MmArgs& a, const Second<MODE>& se
     }
 }
 
+// A group of 16 channels in 8 bits by four adjacent lanes, four channels each from oi on (all four lanes are there, or none).
+__device__ __forceinline__ void keep4(const Saved& to, const float (&x)[4], int64_t oi, int64_t oj, int64_t n_i) {
+    const int lane = (int)threadIdx.x & 31;
+    const uint32_t four = 0xFu << (lane & 28);
+    uint32_t half[4], largest = 0;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        half[h] = oi + h < n_i ? f32_to_bf16(x[h]) : 0u;
+        largest = max(largest, finite_bits(half[h]));
+    }
+    largest = max(largest, __shfl_xor_sync(four, largest, 1));
+    largest = max(largest, __shfl_xor_sync(four, largest, 2));
+    if (oi / kSavedGroup * kSavedGroup >= n_i) return;   // the group is not of the matrix
+    const uint32_t E = saved_exponent(largest), w[4] = {half[0] | (half[1] << 16), half[2] | (half[3] << 16), 0u, 0u};
+    const bool finite = max(max(half[0] & 0x7FFFu, half[1] & 0x7FFFu), max(half[2] & 0x7FFFu, half[3] & 0x7FFFu)) < kNotFinite;
+    *reinterpret_cast<uint32_t*>(to.codes + oj * to.ldc + oi) = saved_codes8(w, E, finite).x;
+    if ((oi & (kSavedGroup - 1)) == 0) to.exponents[oj * to.lde + oi / kSavedGroup] = (uint8_t)E;
+}
+
 // The sum of the CTAs' parts of this CTA's columns, and its epilogue.  Between it and tile_out the CTAs arrive at their barrier.
 template <int MODE, int THREADS>
 __device__ __forceinline__ void tile_join(const MmArgs& a, const Second<MODE>& second, const float* part, int per, int rank, int split, int n_cols, int64_t i0,
@@ -343,6 +423,10 @@ __device__ __forceinline__ void tile_join(const MmArgs& a, const Second<MODE>& s
                 if (oi + h >= a.n_i) break;
                 if (a.bias != nullptr) z[h] = __fadd_rn(z[h], bf16_to_f32(a.bias[oi + h]));
                 if (second.g.bias != nullptr) u[h] = __fadd_rn(u[h], bf16_to_f32(second.g.bias[oi + h]));
+            }
+            if (second.g.z8.codes != nullptr) {   // four lanes hold a group
+                keep4(second.g.z8, z, oi, oj, a.n_i);
+                keep4(second.g.u8, u, oi, oj, a.n_i);
             }
             if (a.z != nullptr) store4(a.z + oj * a.ld_z + oi, z, words, a.n_i - oi);
             if (second.g.u != nullptr) store4(second.g.u + oj * second.g.ld_u + oi, u, words, a.n_i - oi);

@@ -65,6 +65,8 @@ def test_gated_workspaces(lib):
     assert q(A + 2, 64, 2 * A, 64, 3 * A, 64, 8, 32, 64, 0) == 8 * 64 * 2
     assert q(A, 63, 2 * A, 63, 3 * A, 63, 8, 32, 63, 0) == 8 * 64 * 2 + 2 * 32 * 64 * 2
     assert q(A, 63, 2 * A, 63, 3 * A, 63, 4, 32, 63, 0) == 0               # few tokens are read as they are
+    assert q(A, 64, 2 * A, 64, 3 * A, 64, 8, 32, 64, 1) == 0               # checkpoints are written by the product itself,
+    assert q(A, 64, 2 * A, 64, 3 * A, 64, 2, 32, 64, 1) == 2 * 256         # but of few tokens
     b = lib.mosaic_gated_linear_backward_workspace_bytes
     assert b(A, 64, 0, 2 * A, 64, 3 * A, 64, 8, 32, 64, 1, 1, 0) == 2 * 8 * 32 * 2          # dZ and dU
     assert b(A, 64, 0, 2 * A, 64, 3 * A, 64, 8, 32, 64, 0, 0, 1) == 2 * 256                  # column sums
