@@ -499,8 +499,8 @@ __device__ __forceinline__ void tile_join(const MmArgs& a, const Second<MODE>& s
 // One output tile of kMI x BN per cluster; its contraction is split over the cluster's CTAs.  Each of them adds up and writes
 // an equal share of the tile's columns: the others push their partial sums of it into its shared memory (the stages, free
 // by then), and it adds them in the CTAs' order.  Bound by the loads of a tile's operands into one SM (about 110 GB/s an
-// SM for wide tiles) or, with few tokens, by the weights' stream: 37 tokens, 4096 outputs from 8807, 18.0 us against
-// 11.2 of the weights alone; 512 tokens, 4096 from 4096, 23 us.  One CTA an SM (its stages fill shared memory), so a CTA
+// SM for wide tiles) or, with few tokens, by the weights' stream: 37 tokens, 4096 outputs from 8807, 17 us against
+// 11.2 of the weights alone; 512 tokens, 4096 from 4096, 19 us.  One CTA an SM (its stages fill shared memory), so a CTA
 // never waits for tensor memory that another one of this kernel holds.
 template <bool A_MN, bool B_MN, int BN, int MODE>
 __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
@@ -671,8 +671,9 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
 // of both operands in shared memory (64 KB a stage for 256 x 256 x 128 products: half of what a CTA alone would have
 // to load for the same work) and 128 x 256 of the accumulator in its tensor memory, twice: the epilogue of a tile
 // runs under the products of the next.  Persistent: a pair takes tile after tile.  The tiles go band by band
-// (kPBand tiles of output rows), so that the tiles in flight share operands in L2.  Bound by the tensor pipe, 76 % busy at
-// 14336 outputs from 4096 and 2048 tokens with bias, silu and Z (179 us, of which 147 are the flop at the measured peak).
+// (kPBand tiles of output rows), so that the tiles in flight share operands in L2.  Bound by the tensor pipe, 86 % busy at
+// 14336 gated outputs from 4096 and 2048 tokens with Z and U (324 us, of which 289 are the flop at the measured peak; the plain
+// product of as many outputs 320).
 constexpr int kPTile = 256, kPHalf = 128;
 constexpr int kPSub = 2;   // 64 contraction steps each: eight instructions a barrier (with four, 1377 instead of 1505 Tflop/s at 4096 x 13824 x 5120)
 constexpr int kPStages = 3;

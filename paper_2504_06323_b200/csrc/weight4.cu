@@ -20,7 +20,8 @@ struct Weight4 {
 };
 
 // ---------------------------------------------------------------- packing
-// A warp takes 256 columns, a lane eight of them, 4 to 16 lanes a group; kPackRows rows in flight.
+// A warp takes 256 columns, a lane eight of them, 4 to 16 lanes a group; kPackRows rows in flight.  Packing is bound by
+// instructions: 11008 x 4096 in groups of 128 packed and unpacked in a row 49.5 us, of which 35 are the bytes.
 constexpr int kPackWarps = 8, kPackRows = 4;
 
 __device__ __forceinline__ float scale_of(float largest) {
@@ -156,7 +157,8 @@ __global__ void __launch_bounds__(32 * kPackWarps) dequantize4_kernel(const __gr
 // in flight; it reads them back itself, so no thread waits for another.  The matrix instruction (16 rows, 8 tokens, 16
 // columns) does not mind which columns it is given as long as both operands agree: a lane's own 32 columns, in the order in
 // which codes become weights, so that nothing moves between lanes; X lies in shared memory in that order.  Sums in fp32;
-// over a tile's warps in their order.
+// over a tile's warps in their order.  Bound by instructions, of which the integer pipe takes half at half rate: one token through
+// gate and up of 11008 x 4096 13.1 us warm, 17.3 cold, of which 7.1 are the bytes.
 constexpr int k4Warps = 24, k4Tokens = 8, k4Rows = 16, k4Block = 128, k4Ahead = 2;
 constexpr size_t k4Ring = 2 * k4Ahead * 1024;   // a warp's codes in flight
 
@@ -326,7 +328,9 @@ __global__ void __launch_bounds__(32 * k4Warps) few4_kernel(const __grid_constan
 // the codes are loaded, 128 rows x 256 columns a stage in 16 KB; 8 or 12 warps make bf16 of them, a weight row a lane, and put
 // them into tensor memory, where the matrix instruction reads its first operand.  The weights so cross shared memory as codes,
 // once, instead of as bf16 twice: with them in shared memory its bandwidth would hold the stream to about half of what
-// memory gives.
+// memory gives.  Bound by the widening's instructions, 0.29 us a tile and 128 columns whatever the tokens up to 64, and in small
+// calls by start and end (about 5 us with a cluster): 16 tokens, 4096 outputs from 8807, 10.9 us; 64 tokens, 11008 from
+// 4096, 13.3 (19 with bf16 weights).
 constexpr int kC4Cols = 256;
 // Sets of four warps make a stage's weights in turn.  No more sets than slots of either ring: a set waits for a slot's phase by its
 // parity alone, so that it must have seen the phase before.
