@@ -204,6 +204,17 @@ def test_gated_backward_shapes(m, n, k):
     check_gated_backward(dH, X, Wg, Wu, Z, U, act, *out.values())
 
 
+@pytest.mark.parametrize("m,n,k", [(2560, 1500, 2304), (3000, 1000, 2560), (4096, 700, 2200)])
+def test_gated_backward_last_wave_cut_up(m, n, k):
+    """dX and dW of more tiles than pairs of SMs, with few left over: their quarters share the contraction."""
+    g = torch.Generator(device=DEV).manual_seed(m)
+    X, Wg, Wu = matrix(m, k, g), matrix(n, k, g, scale=0.05), matrix(n, k, g, scale=0.05)
+    dH, Z, U = matrix(m, n, g), matrix(m, n, g, scale=2.0), matrix(m, n, g)
+    out = dict(dX=empty(m, k), dW_gate=empty(n, k), dW_up=empty(n, k))
+    run_back(dH, X, Wg, Wu, Z, U, act="silu", **out)
+    check_gated_backward(dH, X, Wg, Wu, Z, U, "silu", *out.values())
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("m", [1, 77])
 @pytest.mark.parametrize("off", [0, 1])

@@ -146,6 +146,48 @@ def test_gated_linear4(m, n, k, groups):
     check_gated(X, Wg, Wu, bg, bu, act, H, None, None)
 
 
+@pytest.mark.parametrize("m", [1, 8, 20, 70, 200])
+def test_gated_weights_lie_anywhere(m):
+    """Gate before up in memory or behind it, of equal or unequal pitch and group, or one and the same: the same bits."""
+    g = torch.Generator(device=DEV).manual_seed(m)
+    n, k = 200, 1200
+    Wg, Wu, X = matrix(n, k, g, scale=0.05), matrix(n, k, g, scale=0.05), matrix(m, k, g)
+    width, seen = 608, []
+    for gate_at, up_at, gate_w, up_w in ((0, 1, width, width), (1, 0, width, width), (0, 1, width + 16, width), (1, 0, width, width + 32)):
+        buf, scales = torch.full((2, n * (width + 32)), 0xA5, dtype=torch.uint8, device=DEV), torch.zeros(2, n, 40, dtype=torch.bfloat16, device=DEV)
+        pair = [api.Weight4(buf[at, :n * w].view(n, w), scales[at, :, :38], k, 32) for at, w in ((gate_at, gate_w), (up_at, up_w))]
+        for w4, W in zip(pair, (Wg, Wu)):
+            api.mosaic_quantize4(W, w4)
+        H = empty(m, n)
+        api.mosaic_gated_linear4(X, *pair, H)
+        seen.append(H)
+    assert all(torch.equal(seen[0], other) for other in seen[1:])
+    values = [empty(n, k), empty(n, k)]
+    for w4, v in zip(pair, values):
+        api.mosaic_dequantize4(w4, v)
+    check_gated(X, *values, None, None, "silu", seen[0], None, None)
+    api.mosaic_gated_linear4(X, pair[0], pair[0], H)
+    check_gated(X, values[0], values[0], None, None, "silu", H, None, None)
+
+
+@pytest.mark.parametrize("m", [1, 8, 16, 40, 128, 256])
+@pytest.mark.parametrize("n,k", [(300, 9000), (4096, 4096), (130, 300)])
+def test_calls_repeat_their_bits(m, n, k):
+    """Fifty calls in a row over contractions of one stage to many: no wait lets a stage of another turn through."""
+    g = torch.Generator(device=DEV).manual_seed(m + n)
+    w4, _ = weight4(n, k, g, 64, 0.02)
+    u4, _ = weight4(n, k, g, 128, 0.02)
+    X = matrix(m, k, g)
+    first = None
+    for _ in range(50):
+        Y, H = empty(m, n), empty(m, n)
+        api.mosaic_linear4(X, w4, Y)
+        api.mosaic_gated_linear4(X, w4, u4, H)
+        if first is None:
+            first = Y, H
+        assert torch.equal(Y, first[0]) and torch.equal(H, first[1])
+
+
 @pytest.mark.parametrize("m", [1, 20, 40])
 def test_nothing_behind_the_last_column_or_row_is_used(m):
     """Codes behind the last column hold anything, scales around the matrix NaN; outputs end where they should."""
