@@ -787,6 +787,10 @@ def _like(t, name: str, dtype, device: int, rows: int, cols: int):
     """(pointer, leading dimension) of an optional [rows, cols] matrix."""
     if t is None:
         return None, cols
+    if isinstance(t, _Tensor) and t.shape == (rows, cols) and t.dtype is dtype and t.get_device() == device:   # as it should be
+        ld, step = t.stride()
+        if step == 1 or cols <= 1:
+            return t.data_ptr(), (ld if rows > 1 else max(ld, cols))
     p, r, c, ld = _matrix(t, name, dtype, device)
     if r != rows or c != cols:
         raise ValueError(f"{name} must be [{rows}, {cols}], got [{r}, {c}]")
@@ -1007,8 +1011,9 @@ def mosaic_gated_linear_backward(dH, X, W_gate, W_up, Z, U, act="silu", dX=None,
     dbu = _dense_or_none(dbias_up, "dbias_up", bf16, dev, n)
     sp = _dense_or_none(status, "status", torch.int32, dev, 1)
     L = lib()
-    need = L.mosaic_gated_linear_backward_workspace_bytes(xp, ldx, x8 is not None, gp, ldg, up, ldu, tokens, n, n_in, dX is not None, want_dw,
-                                                          dbg is not None or dbu is not None)
+    # of the pointers the query looks at the alignment alone
+    need = _scratch("mosaic_gated_linear_backward_workspace_bytes", dev, (xp or 0) & 15, ldx, x8 is not None, (gp or 0) & 15, ldg, (up or 0) & 15, ldu,
+                    tokens, n, n_in, dX is not None, want_dw, dbg is not None or dbu is not None)
     sc, sn = _ws(ws, dev).get(need, st or 0) if need else (None, 0)
     _check(L.mosaic_gated_linear_backward(dhp, lddh, xp, ldx, x8, gp, ldg, up, ldu, zp, ldz, vp, ldv, z8, u8, tokens, n, n_in, BF16, _act_code(act),
                                           dxp, lddx, dgp, lddg, dup, lddu, dbg, dbu, hp, ldh, sp, sc, sn, st), "mosaic_gated_linear_backward")
