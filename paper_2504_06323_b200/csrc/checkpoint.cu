@@ -12,7 +12,7 @@ constexpr int kSavedWarps = 8, kSavedRows = 4;
 template <bool VEC>
 __global__ void __launch_bounds__(32 * kSavedWarps) store_kernel(const uint16_t* X, int64_t ldx, int64_t rows, int64_t cols, const __grid_constant__ Saved out,
                                                                  unsigned chunks) {
-    __shared__ uint4 turns[VEC ? 1 : kSavedWarps][32];
+    __shared__ uint4 turns[VEC ? 1 : kSavedWarps][kTurn];
     allow_next_kernel();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint4* turn = turns[VEC ? 0 : warp];
@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(32 * kSavedWarps) store_kernel(const uint16_t*
 template <bool VEC>
 __global__ void __launch_bounds__(32 * kSavedWarps) load_kernel(const __grid_constant__ Saved in, int64_t rows, int64_t cols, uint16_t* X, int64_t ldx,
                                                                 unsigned chunks) {
-    __shared__ uint4 turns[VEC ? 1 : kSavedWarps][32];
+    __shared__ uint4 turns[VEC ? 1 : kSavedWarps][kTurn];
     allow_next_kernel();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint4* turn = turns[VEC ? 0 : warp];

@@ -48,7 +48,7 @@ template <bool VEC, bool SAVED> struct SlopeRow {
     uint32_t dh[4], z[SAVED ? 2 : 4], u[SAVED ? 2 : 4], ze, ue;
     __device__ __forceinline__ void load(const GatedSlope& a, int64_t r, int64_t c0, uint4* turn) {
         const int64_t c = c0 + ((int)threadIdx.x & 31) * kLaneCols;
-        lane_load8<VEC>(a.dh + r * a.ld_dh, c0, a.cols, turn, dh);
+        lane_load8<VEC, true>(a.dh + r * a.ld_dh, c0, a.cols, turn, dh);
         if constexpr (SAVED) {
             z[0] = z[1] = u[0] = u[1] = 0u;
             ze = ue = 1u;
@@ -60,8 +60,8 @@ template <bool VEC, bool SAVED> struct SlopeRow {
                 ue = a.u8.exponents[r * a.u8.lde + c / kSavedGroup];
             }
         } else {
-            lane_load8<VEC>(a.z + r * a.ld_z, c0, a.cols, turn, z);
-            lane_load8<VEC>(a.u + r * a.ld_u, c0, a.cols, turn, u);
+            lane_load8<VEC, true>(a.z + r * a.ld_z, c0, a.cols, turn, z);
+            lane_load8<VEC, true>(a.u + r * a.ld_u, c0, a.cols, turn, u);
         }
     }
     __device__ __forceinline__ void values(float (&d)[8], float (&zv)[8], float (&uv)[8]) const {
@@ -82,14 +82,14 @@ template <bool VEC, bool SAVED> struct SlopeRow {
 
 // A warp takes 256 columns, a lane eight of them, the CTA's eight warps every eighth row of its band, the next row on its way
 // while one is computed; with SUMS the warps' column sums meet in shared memory in their order.  Bound by instructions (53 an
-// element, issue 79 %) next to memory (48 %): 2048 x 13824 from 8 bits with H 57 us, of which 44 are the bytes; of odd rows, two
-// bytes a lane and load, by the loads' latency: 1001 x 8807 with sums 40 us (14).  Four CTAs an SM, but where sums take the
+// element, issue 79 %) next to memory (48 %): 2048 x 13824 from 8 bits with H 57 us, of which 44 are the bytes; of odd rows by the
+// loads' latency: 1001 x 8807 with sums 33 us (14).  Four CTAs an SM, but where sums take the
 // registers of aligned rows: two there (44.7 with its product, 50.4 with four).
 template <bool VEC, bool SAVED, bool SUMS>
 __global__ void __launch_bounds__(32 * 8, VEC && SUMS ? 2 : 4) gated_slope_kernel(const __grid_constant__ GatedSlope a) {
     constexpr int kWarps = 8;
     __shared__ float sums[SUMS ? kWarps : 1][kWarpCols];
-    __shared__ uint4 turns[VEC ? 1 : kWarps][32];
+    __shared__ uint4 turns[VEC ? 1 : kWarps][kTurn];
     allow_next_kernel();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint4* turn = turns[VEC ? 0 : warp];
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(32 * 8, VEC && SUMS ? 2 : 4) gated_slope_kerne
             *reinterpret_cast<uint4*>(a.dz + r * a.ld_d + c) = make_uint4(pz[0], pz[1], pz[2], pz[3]);
             *reinterpret_cast<uint4*>(a.du + r * a.ld_d + c) = make_uint4(pu[0], pu[1], pu[2], pu[3]);
         }
-        if (a.h != nullptr) lane_store8<VEC>(a.h + r * a.ld_h, c0, a.cols, turn, ph);
+        if (a.h != nullptr) lane_store8<VEC, true>(a.h + r * a.ld_h, c0, a.cols, turn, ph);
     }
     if constexpr (SUMS) {
 #pragma unroll

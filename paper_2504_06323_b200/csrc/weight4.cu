@@ -69,7 +69,7 @@ __device__ __forceinline__ uint32_t codes_of8(const uint32_t (&w)[4], float s) {
 template <bool VEC, int SHIFT>
 __global__ void __launch_bounds__(32 * kPackWarps) quantize4_kernel(const uint16_t* W, int64_t ldw, int64_t rows, int64_t cols, const __grid_constant__ Weight4 out,
                                                                     unsigned chunks) {
-    __shared__ uint4 turns[VEC ? 1 : kPackWarps][32];
+    __shared__ uint4 turns[VEC ? 1 : kPackWarps][kTurn];
     allow_next_kernel();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint4* turn = turns[VEC ? 0 : warp];
@@ -113,7 +113,7 @@ __device__ __forceinline__ uint32_t weights4(uint32_t word, int i, uint32_t s2, 
 template <bool VEC>
 __global__ void __launch_bounds__(32 * kPackWarps) dequantize4_kernel(const __grid_constant__ Weight4 in, int64_t rows, int64_t cols, uint16_t* W, int64_t ldw,
                                                                       unsigned chunks) {
-    __shared__ uint4 turns[VEC ? 1 : kPackWarps][32];
+    __shared__ uint4 turns[VEC ? 1 : kPackWarps][kTurn];
     allow_next_kernel();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint4* turn = turns[VEC ? 0 : warp];
