@@ -545,7 +545,8 @@ int mosaic_checkpoint_load(const mosaic_checkpoint *in, int64_t rows, int64_t co
  *   status_dev      as in mosaic_gram_accumulate, or NULL
  *   ws              device scratch, >= the query for the same arguments (saved: whether
  *                   checkpoints are given); 0 when X and both W have 16-byte aligned
- *                   bases and leading dimensions and nothing is saved in 8 bits
+ *                   bases and leading dimensions, but for checkpoints of up to two
+ *                   tokens (four where they are not aligned), which need a bf16 copy
  * Sums in fp32 on the tensor cores; biases, activation and product in fp32 on the sums; one
  * rounding to bf16 for each of H, Z and U.  tokens = 0 is legal.  Outputs must not
  * overlap the inputs or each other.

@@ -164,12 +164,13 @@ template <int N> __device__ __forceinline__ void epilogue(const MmArgs& a, float
 // the groups in 8 bits, as store_saved would make them of the bf16 values.  Words of two tokens' magnitudes are maximised
 // over the group's lanes, each lane ending with the two of one word (so it has their exponents to write); four tokens' codes are
 // turned round among four lanes, so that a lane writes four channels of a token.
-template <int N> __device__ __forceinline__ void keep16(const Saved& to, const float (&v)[N], int at, int64_t i0, int64_t j, int n) {
+template <int N> __device__ __forceinline__ void keep16(const Saved& to, const float (&v)[N], int at, int64_t i0, int64_t n_i, int64_t j, int n) {
     const int lane = (int)threadIdx.x & 31, l = lane & 15;
+    const bool there = i0 + l < n_i;   // behind the last channel rows of zeros, whose sums are NaN where X is not finite
     uint32_t h[8], m[8], any = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        h[k] = pack2(v[at + 2 * k], v[at + 2 * k + 1]);
+        h[k] = there ? pack2(v[at + 2 * k], v[at + 2 * k + 1]) : 0u;
         m[k] = h[k] & 0x7FFF7FFFu;
         any = __vmaxu2(any, m[k]);
     }
@@ -244,7 +245,7 @@ template <int N> __device__ __forceinline__ void gate_epilogue(const MmArgs& a, 
     if (g.z8.codes != nullptr && i0 < a.n_i) {
 #pragma unroll
         for (int at = 0; at < N; at += 16)
-            if (at < n) keep16(up ? g.u8 : g.z8, v, at, i0, j + at, n - at);
+            if (at < n) keep16(up ? g.u8 : g.z8, v, at, i0, a.n_i, j + at, n - at);
     }
     float z[N / 2], u[N / 2];
 #pragma unroll

@@ -110,6 +110,25 @@ def test_gated_forward_keeps_8_bits(m, n, k):
         assert torch.equal(c.codes.cpu(), codes) and torch.equal(c.exponents.cpu(), E)
 
 
+@pytest.mark.parametrize("scale", [1.0, 3e-39, 1e37])
+@pytest.mark.parametrize("m,n,k", [(2, 40, 64), (16, 100, 64), (128, 688, 256), (64, 513, 777), (300, 1000, 2048), (2304, 1153, 64)])
+def test_gated_forward_keeps_what_is_not_finite_and_what_is_tiny(m, n, k, scale):
+    """Infinities and NaN on the way, sums that leave bf16's range and sums of subnormals: what the 8 bits keep is what they would keep of
+    the bf16 Z and U."""
+    g = torch.Generator(device=DEV).manual_seed(m + n + k)
+    X, Wg, Wu = matrix(m, k, g, -k % 8), matrix(n, k, g, -k % 8, scale=scale), matrix(n, k, g, -k % 8, scale=scale)
+    X[0, 3], X[1, 5] = float("inf"), float("nan")
+    Wg[n // 2, 7], Wu[n // 3, 9] = -float("inf"), float("nan")
+    H, H8, Z, U = (empty(m, n) for _ in range(4))
+    Z8, U8 = api.Checkpoint.empty(m, n), api.Checkpoint.empty(m, n)
+    run_gated(X, Wg, Wu, H, act="none", Z=Z, U=U)
+    run_gated(X, Wg, Wu, H8, act="none", Z=Z8, U=U8)
+    assert same(H, H8)
+    for c, t in ((Z8, Z), (U8, U)):
+        codes, E = reference(t)
+        assert torch.equal(c.codes.cpu(), codes) and torch.equal(c.exponents.cpu(), E)
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 1, 1), (3, 130, 65), (17, 127, 63), (64, 513, 777), (129, 65, 129), (1000, 1025, 96), (2304, 1153, 64)])
 @pytest.mark.parametrize("which", ["x", "zu", "xzu"])
 def test_gated_backward_reads_8_bits(m, n, k, which):
@@ -130,6 +149,29 @@ def test_gated_backward_reads_8_bits(m, n, k, which):
     run_back(dH, back(X8), Wg, Wu, back(Z8), back(U8), act=act, **b)
     for q in a:
         assert torch.equal(a[q], b[q]), q
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 130, 65), (129, 65, 129), (600, 1025, 96)])
+def test_gated_backward_of_what_is_not_finite(m, n, k):
+    """A NaN or infinity that 8 bits kept is a NaN in its token's gradients, and in the sums over tokens, as from the loaded matrices."""
+    g = torch.Generator(device=DEV).manual_seed(m)
+    X, Z, U, dH = matrix(m, k, g), matrix(m, n, g), matrix(m, n, g), matrix(m, n, g)
+    X[0, 0], Z[1, 1], U[2, n - 1] = float("inf"), float("nan"), -float("inf")
+    Wg, Wu = matrix(n, k, g, scale=0.05), matrix(n, k, g, scale=0.05)
+    kept = []
+    for t in (X, Z, U):
+        c = api.Checkpoint.empty(*t.shape)
+        api.mosaic_checkpoint_store(t, c)
+        kept.append(c)
+    out = lambda: dict(dX=empty(m, k), dW_gate=empty(n, k), dW_up=empty(n, k), dbias_gate=empty(n), dbias_up=empty(n), H=empty(m, n))  # noqa: E731
+    a, b = out(), out()
+    run_back(dH, kept[0], Wg, Wu, kept[1], kept[2], act="silu", **a)
+    run_back(dH, loaded(kept[0]), Wg, Wu, loaded(kept[1]), loaded(kept[2]), act="silu", **b)
+    for q in a:
+        assert same(a[q], b[q]), q
+    bad = torch.isnan(a["dX"]).all(1)
+    assert bad[1] and bad[2] and not bad[0] and not bad[3:].any()
+    assert torch.isnan(a["dW_gate"][:, 0]).all() and torch.isnan(a["dbias_gate"][1]) and torch.isnan(a["dbias_gate"][n - 1])
 
 
 def test_refusals():
