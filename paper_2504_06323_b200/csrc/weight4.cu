@@ -337,8 +337,8 @@ constexpr int kC4Cols = 256;
 template <int BN> constexpr int kC4Sets = BN == 128 ? 2 : 3;
 template <int BN> constexpr int kC4Threads = 32 * (kMRoles + 4 * kC4Sets<BN>);   // code loader, MMA issue; weight makers
 constexpr uint32_t kC4Bytes = kMI * kC4Cols / 2, kC4Box = kGateRows * kC4Cols / 2;   // of a stage's codes, of 16 rows of them
-// Rows of 128 bytes a box: the copy engine takes about four cycles a row, whatever its length.  X comes with the codes it meets: in a
-// ring of its own it waited behind the codes of stages to come.
+// X comes with the codes it meets: in a ring of its own it waited behind the codes of stages to come (17.3 us for 11.4, 16 tokens,
+// 4096 outputs from 8807).
 template <int BN> constexpr int kC4Slots = BN == 16 ? 8 : BN == 32 ? 6 : BN == 64 ? 4 : 2;
 template <int BN> constexpr uint32_t kC4Slot = kC4Bytes + (uint32_t)BN * kC4Cols * 2u;
 constexpr int kC4Made = 3;             // stages made weights of, 128 columns of tensor memory each
