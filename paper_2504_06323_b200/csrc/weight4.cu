@@ -332,8 +332,7 @@ __global__ void __launch_bounds__(32 * k4Warps) few4_kernel(const __grid_constan
 // calls by start and end (about 5 us with a cluster): 16 tokens, 4096 outputs from 8807, 10.9 us; 64 tokens, 11008 from
 // 4096, 13.3 (19 with bf16 weights).
 constexpr int kC4Cols = 256;
-// Sets of four warps make a stage's weights in turn.  No more sets than slots of either ring: a set waits for a slot's phase by its
-// parity alone, so that it must have seen the phase before.
+// Sets of four warps make a stage's weights in turn.
 template <int BN> constexpr int kC4Sets = BN == 128 ? 2 : 3;
 template <int BN> constexpr int kC4Threads = 32 * (kMRoles + 4 * kC4Sets<BN>);   // code loader, MMA issue; weight makers
 constexpr uint32_t kC4Bytes = kMI * kC4Cols / 2, kC4Box = kGateRows * kC4Cols / 2;   // of a stage's codes, of 16 rows of them
@@ -342,6 +341,17 @@ constexpr uint32_t kC4Bytes = kMI * kC4Cols / 2, kC4Box = kGateRows * kC4Cols / 
 template <int BN> constexpr int kC4Slots = BN == 16 ? 8 : BN == 32 ? 6 : BN == 64 ? 4 : 2;
 template <int BN> constexpr uint32_t kC4Slot = kC4Bytes + (uint32_t)BN * kC4Cols * 2u;
 constexpr int kC4Made = 3;             // stages made weights of, 128 columns of tensor memory each
+// A set waits twice a stage: for its codes (full), and for room, that is for the products of the stage kC4Made before it (used).  A
+// wait sees a phase's parity alone: it passes as well while the phase before that one has not completed, so the set must know that
+// it has.  Loads land in any order; that a later stage has landed proves nothing.  So the ring whose slots are each one
+// set's own comes first - there the set has waited for every phase itself - and its phase then proves the other ring's:
+//     room first: the products of stage s - kC4Made are complete, so were issued, so every stage up to it has landed, the one
+//         before in the slot of s among them if there are kC4Made slots or more
+//     codes first: the load of stage s was issued, so the products of s - slots are complete, so the weights of every stage up to
+//         it were made, by sets that had found the room that this set asks about if there are no more slots than kC4Made
+template <int BN> constexpr bool kC4RoomFirst = kC4Made % kC4Sets<BN> == 0;
+template <int BN> constexpr bool kC4Proved = kC4RoomFirst<BN> ? kC4Slots<BN> >= kC4Made : kC4Slots<BN> % kC4Sets<BN> == 0 && kC4Slots<BN> <= kC4Made;
+static_assert(kC4Proved<16> && kC4Proved<32> && kC4Proved<64> && kC4Proved<128>, "a wait's parity tells two phases apart, no more");
 template <int BN> constexpr uint32_t kC4Acc = BN < 32 ? 32 : BN;                      // tensor-memory columns of the accumulator
 constexpr long long kLandCycles = 20000000ll;   // ten milliseconds: far more than a load takes
 // One CTA an SM: it takes all of the tensor memory, and one that waited for it could hold up its cluster.
@@ -404,7 +414,6 @@ __global__ void __launch_bounds__(kC4Threads<BN>) mm4_kernel(const __grid_consta
                                                          const __grid_constant__ MmArgs a, const __grid_constant__ Second<MODE> second,
                                                          const __grid_constant__ Scales4 scales) {
     constexpr int kSlots = kC4Slots<BN>, kSets = kC4Sets<BN>;
-    static_assert(kSets <= kSlots && kSets <= kC4Made, "a parity tells two phases apart, no more");
     constexpr uint32_t kDesc = instr_desc(false, false, kMI, BN);
     extern __shared__ unsigned char mm4_smem_raw[];
     __shared__ uint64_t full[kSlots], empty[kSlots], ready[kC4Made], used[kC4Made], acc_full;
@@ -523,7 +532,10 @@ __global__ void __launch_bounds__(kC4Threads<BN>) mm4_kernel(const __grid_consta
             const int slot = s % kSlots, made = s % kC4Made;
             const uint4 sc = scales_spread(next, shift);
             if (s + kSets < steps) next = scales_of(at, (s0 + s + kSets) * kC4Cols, shift, groups, wide);
-            if (!mbar_wait(&full[slot], (uint32_t)(s / kSlots) & 1u, err) || !mbar_wait(&used[made], ((uint32_t)(s / kC4Made) & 1u) ^ 1u, err)) break;
+            const auto room = [&]() { return mbar_wait(&used[made], ((uint32_t)(s / kC4Made) & 1u) ^ 1u, err); };
+            if (kC4RoomFirst<BN> && !room()) break;
+            if (!mbar_wait(&full[slot], (uint32_t)(s / kSlots) & 1u, err)) break;
+            if (!kC4RoomFirst<BN> && !room()) break;
             __syncwarp();
             tc_fence_after();
             const unsigned char* codes = ring + slot * kC4Slot<BN> + r * 128;
