@@ -36,3 +36,31 @@ def test_many_stages(m, n, k):
         more = both()
         assert torch.equal(more[0], Y) and torch.equal(more[1], H)
     assert not bool(status.any())
+
+
+@pytest.mark.parametrize("m,n,k", [(2049, 2500, 136), (260, 5000, 4100), (4100, 4200, 264), (2304, 2305, 64), (2560, 2050, 1500), (300, 8807, 1001)])
+def test_prompts(m, n, k):
+    """Tokens of a whole prompt: tiles of pairs of CTAs, a last wave cut up, X off 16 bytes beside the unpacked weights."""
+    g = torch.Generator(device=DEV).manual_seed(m + n + k)
+    act, group = ACTS[(m + n) % 4], (32, 64, 128)[k % 3]
+    w4, W = weight4(n, k, g, group, 1.0 / math.sqrt(k))
+    X, R, Y = matrix(m, k, g, m % 3), matrix(m, n, g), matrix(m, n, g, 1)
+    bias = vector(n, g) if n % 2 else None
+    status = torch.full((1,), 7, device=DEV, dtype=torch.int32)
+    api.mosaic_linear4(X, w4, Y, bias=bias, residual=R if k % 2 == 0 else None, act=act, status=status)
+    assert int(status.item()) == 0
+    check_forward(X, W, bias, R if k % 2 == 0 else None, act, Y, None)
+
+
+@pytest.mark.parametrize("m,n,k", [(2049, 1250, 136), (260, 5000, 4100), (4100, 2100, 264), (2304, 1153, 64), (2560, 1050, 1500), (300, 4403, 1001)])
+def test_gated_prompts(m, n, k):
+    g = torch.Generator(device=DEV).manual_seed(m + n + k)
+    act = ACTS[(m + k) % 4]
+    g4, Wg = weight4(n, k, g, 128, 1.0 / math.sqrt(k))
+    u4, Wu = weight4(n, k, g, 32, 1.0 / math.sqrt(k))
+    X, H = matrix(m, k, g, m % 3), matrix(m, n, g, 1)
+    bg, bu = vector(n, g) if n % 2 else None, vector(n, g) if k % 2 else None
+    status = torch.full((1,), 7, device=DEV, dtype=torch.int32)
+    api.mosaic_gated_linear4(X, g4, u4, H, bias_gate=bg, bias_up=bu, act=act, status=status)
+    assert int(status.item()) == 0
+    check_gated(X, Wg, Wu, bg, bu, act, H, None, None)
