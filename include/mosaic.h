@@ -508,7 +508,9 @@ int mosaic_linear_backward(const void *dY, int64_t lddy, const void *X, int64_t 
  *     code  = x 2^(133 - E), rounded to the nearest whole number (ties to even) and
  *             kept within +-127; -128 for a NaN or an infinity
  *     value = code 2^(E - 133), a bf16 number again; -128 is read as NaN, -0 as +0
- * A value differs from what was stored by at most 2^-7 of the group's largest.
+ * A value differs from what was stored by at most half a code, 2^(E - 134).  That is 2^-7
+ * of the group's largest magnitude where this is a normal number; in a group without one
+ * it is 2^-133, and the smallest number, 2^-133, is kept as 0.
  *   codes       device, int8 [rows, cols], row pitch ldc: a multiple of 16, at least
  *               cols rounded up to it; 16-byte aligned.  Codes from cols on up to the
  *               next multiple of 16 are written as 0 and never used
