@@ -122,7 +122,8 @@ class Block:
     def packed(self, group: int = 128) -> "Served":
         """The block in 4 bits, `group` weights a scale."""
         four = {w: api.Weight4.of(getattr(self, w), group) for w in ("gate", "up", "down", "head") if getattr(self, w) is not None}
-        return Served(four["up"], four["down"], four["head"], self.bias, self.act, self.ws, four.get("gate"))
+        bias = None if self.bias is None else self.bias.clone()   # packed too: the block may go on learning
+        return Served(four["up"], four["down"], four["head"], bias, self.act, self.ws, four.get("gate"))
 
     def check(self) -> None:
         """Raise if a wait of the last products ran out (reads the status words from the device)."""
