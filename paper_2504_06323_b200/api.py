@@ -920,6 +920,8 @@ class Checkpoint:
 
 def _saved(c, name: str, device: int, rows: int, cols: int):
     """Pointer of a checkpoint of a [rows, cols] matrix."""
+    if not isinstance(c, Checkpoint):
+        raise TypeError(f"{name} must be a Checkpoint")
     if c.rows != rows or c.cols != cols:
         raise ValueError(f"{name} must keep [{rows}, {cols}], keeps [{c.rows}, {c.cols}]")
     if c.device != device:

@@ -3,7 +3,7 @@ place, arguments that are none, and a student that goes on learning."""
 import pytest
 import torch
 
-from paper_2504_06323_b200 import recovery
+from paper_2504_06323_b200 import api, recovery
 from test_gpu_recovery_fused import blocks
 
 pytestmark = pytest.mark.gpu
@@ -31,3 +31,11 @@ def test_the_fused_block_is_served_from_copies():
     before = served.forward(X).clone()
     student.down.zero_()
     assert torch.equal(served.forward(X), before)
+
+
+def test_no_checkpoint_is_refused():
+    X = torch.zeros(5, 96, device=DEV, dtype=torch.bfloat16)
+    for call in (lambda: api.mosaic_checkpoint_store(X, X), lambda: api.mosaic_checkpoint_store(X, None), lambda: api.mosaic_checkpoint_load(X, X),
+                 lambda: api.mosaic_checkpoint_load(None, X), lambda: api.mosaic_checkpoint_store(X, api.Weight4.empty(5, 96, 32))):
+        with pytest.raises(TypeError):
+            call()
