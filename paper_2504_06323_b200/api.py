@@ -895,10 +895,15 @@ class _CheckpointStruct(C.Structure):
 
 class Checkpoint:
     """A matrix of activations in 8 bits: `codes` int8 [rows, cols rounded up to 16 or more] and `exponents` uint8
-    [rows, ceil(cols / 16)], both with unit column stride.  The tensors are checked here and kept alive by the object."""
+    [rows, ceil(cols / 16)], both with unit column stride.  The tensors are checked here and kept alive by the object; where one
+    has been put in another place since, a call checks and reads what is there now."""
 
     def __init__(self, codes: torch.Tensor, exponents: torch.Tensor, cols: int):
-        cols = int(cols)
+        self.codes, self.exponents, self.cols = codes, exponents, int(cols)
+        self._lay_out()
+
+    def _lay_out(self) -> None:
+        codes, exponents, cols = self.codes, self.exponents, self.cols
         groups = -(-cols // 16)
         for t, name, dtype, least in ((codes, "codes", torch.int8, 16 * groups), (exponents, "exponents", torch.uint8, groups)):
             _, rows, width, _ = _matrix(t, name, dtype)
@@ -906,9 +911,9 @@ class Checkpoint:
                 raise ValueError(f"{name} must be [{codes.shape[0]}, {least}] or wider for {cols} columns, got {list(t.shape)}")
         if codes.device != exponents.device:
             raise ValueError("codes and exponents must be on one device")
-        self.codes, self.exponents, self.rows, self.cols, self.device = codes, exponents, codes.shape[0], cols, codes.get_device()
+        self.rows, self.device, self.at_codes, self.at_exponents = codes.shape[0], codes.get_device(), codes.data_ptr(), exponents.data_ptr()
         ldc = _matrix(codes, "codes", torch.int8)[3]
-        self._struct = _CheckpointStruct(codes.data_ptr(), -(-ldc // 16) * 16 if self.rows <= 1 else ldc, exponents.data_ptr(),
+        self._struct = _CheckpointStruct(self.at_codes, -(-ldc // 16) * 16 if self.rows <= 1 else ldc, self.at_exponents,
                                          _matrix(exponents, "exponents", torch.uint8)[3])
         self.ptr = C.addressof(self._struct)
 
@@ -922,6 +927,8 @@ def _saved(c, name: str, device: int, rows: int, cols: int):
     """Pointer of a checkpoint of a [rows, cols] matrix."""
     if not isinstance(c, Checkpoint):
         raise TypeError(f"{name} must be a Checkpoint")
+    if c.codes.data_ptr() != c.at_codes or c.exponents.data_ptr() != c.at_exponents:
+        c._lay_out()
     if c.rows != rows or c.cols != cols:
         raise ValueError(f"{name} must keep [{rows}, {cols}], keeps [{c.rows}, {c.cols}]")
     if c.device != device:
@@ -1029,21 +1036,25 @@ class _Weight4Struct(C.Structure):
 class Weight4:
     """A weight matrix in 4 bits: `codes` uint8 [rows, 16 for every 32 columns, or more] and `scales` bf16 [rows, ceil(cols /
     group)], both with unit column stride; `group` is 32, 64 or 128.  The tensors are checked here and kept alive by the
-    object."""
+    object; where one has been put in another place since, a call checks and reads what is there now."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, group: int):
-        cols, group = int(cols), int(group)
-        if group not in (32, 64, 128):
+        self.codes, self.scales, self.cols, self.group = codes, scales, int(cols), int(group)
+        if self.group not in (32, 64, 128):
             raise ValueError(f"group must be 32, 64 or 128, got {group}")
+        self._lay_out()
+
+    def _lay_out(self) -> None:
+        codes, scales, cols, group = self.codes, self.scales, self.cols, self.group
         for t, name, dtype, least in ((codes, "codes", torch.uint8, -(-cols // 32) * 16), (scales, "scales", torch.bfloat16, -(-cols // group))):
             _, rows, width, _ = _matrix(t, name, dtype)
             if cols <= 0 or width < least or rows != codes.shape[0]:
                 raise ValueError(f"{name} must be [{codes.shape[0]}, {least}] or wider for {cols} columns, got {list(t.shape)}")
         if codes.device != scales.device:
             raise ValueError("codes and scales must be on one device")
-        self.codes, self.scales, self.rows, self.cols, self.group, self.device = codes, scales, codes.shape[0], cols, group, codes.get_device()
+        self.rows, self.device, self.at_codes, self.at_scales = codes.shape[0], codes.get_device(), codes.data_ptr(), scales.data_ptr()
         ldc = _matrix(codes, "codes", torch.uint8)[3]
-        self._struct = _Weight4Struct(codes.data_ptr(), -(-ldc // 16) * 16 if self.rows <= 1 else ldc, scales.data_ptr(),
+        self._struct = _Weight4Struct(self.at_codes, -(-ldc // 16) * 16 if self.rows <= 1 else ldc, self.at_scales,
                                       _matrix(scales, "scales", torch.bfloat16)[3], group)
         self.ptr = C.addressof(self._struct)
 
@@ -1064,6 +1075,8 @@ def _weight4(w, name: str, device: int, rows: int | None, cols: int):
     """Pointer of a 4-bit [rows, cols] matrix (rows None: any number)."""
     if not isinstance(w, Weight4):
         raise TypeError(f"{name} must be a Weight4")
+    if w.codes.data_ptr() != w.at_codes or w.scales.data_ptr() != w.at_scales:
+        w._lay_out()
     if (rows is not None and w.rows != rows) or w.cols != cols:
         raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {cols}], is [{w.rows}, {w.cols}]")
     if w.device != device:

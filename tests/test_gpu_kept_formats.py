@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2504_06323_b200 import api, recovery
+from test_gpu_linear import matrix
 from test_gpu_recovery_fused import blocks
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,52 @@ def test_no_checkpoint_is_refused():
                  lambda: api.mosaic_checkpoint_load(None, X), lambda: api.mosaic_checkpoint_store(X, api.Weight4.empty(5, 96, 32))):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("how", ["attribute", "data"])
+def test_codes_put_in_another_place_are_read_there(how):
+    """The calls read the tensors that an object holds now, wherever they lie."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    W, X = matrix(40, 96, g, scale=0.2), matrix(5, 96, g)
+    w4, c = api.Weight4.of(W, 32), api.Checkpoint.empty(5, 96)
+    api.mosaic_checkpoint_store(X, c)
+    old = w4.codes, w4.scales, c.codes, c.exponents     # alive, and changed below: no call may still read them
+
+    def put(o, name):
+        t = getattr(o, name)
+        if how == "attribute":
+            setattr(o, name, t.clone())
+            t.zero_()
+        else:
+            first = t.detach()
+            t.data = t.clone()
+            first.zero_()
+            old_data.append(first)
+
+    old_data = []
+    want = {}
+    for state in ("before", "after"):
+        Y, back, x = torch.empty(5, 40, device=DEV, dtype=torch.bfloat16), torch.empty_like(W), torch.empty(5, 96, device=DEV, dtype=torch.bfloat16)
+        api.mosaic_linear4(X, w4, Y)
+        api.mosaic_dequantize4(w4, back)
+        api.mosaic_checkpoint_load(c, x)
+        if state == "before":
+            want = dict(Y=Y, back=back, x=x)
+            for o, name in ((w4, "codes"), (w4, "scales"), (c, "codes"), (c, "exponents")):
+                put(o, name)
+        else:
+            assert torch.equal(Y, want["Y"]) and torch.equal(back, want["back"]) and torch.equal(x, want["x"])
+    assert len(old) == 4
+
+
+def test_what_does_not_fit_any_more_is_refused():
+    w4, c = api.Weight4.empty(40, 96, 32), api.Checkpoint.empty(5, 96)
+    X, Y = torch.zeros(5, 96, device=DEV, dtype=torch.bfloat16), torch.zeros(5, 40, device=DEV, dtype=torch.bfloat16)
+    keep = w4.codes, c.exponents
+    w4.codes = w4.codes[:, :32].clone()
+    c.exponents = c.exponents.cpu()
+    with pytest.raises(ValueError):
+        api.mosaic_linear4(X, w4, Y)
+    with pytest.raises(TypeError):
+        api.mosaic_checkpoint_store(X, c)
+    assert len(keep) == 2
