@@ -238,7 +238,9 @@ class Workspace:
     A buffer belongs to its stream in the allocator's books as well: when the Workspace goes, it is handed on only behind
     the work that still uses it.  One that was outgrown is kept as long as the Workspace, for a captured graph may go on
     using it; each is at least twice the one before, so all that were outgrown are together smaller than the last.
-    Graphs captured on one stream share its buffer: to replay two of them at once, give each a Workspace."""
+    Graphs captured on one stream share its buffer: to replay two of them at once, give each a Workspace.  A graph uses the
+    buffers of the Workspace that it was captured with, as it uses the tensors of its calls: all must live as long as it is
+    replayed (the default one, used where none is given, always does)."""
 
     def __init__(self, device="cuda"):
         self.device = torch.device(device)

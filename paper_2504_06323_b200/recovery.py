@@ -26,7 +26,8 @@ class Block:
     [vocab, hidden] and bias [channels] or None:
         mlp(X) = act(gate(X) + bias) * up(X)      the gated MLP of the LLaMA-shaped models
         mlp(X) = act(up(X) + bias)                without a gate
-    Buffers are kept for the last number of tokens; a block serves one stream at a time.
+    Buffers are kept for the last number of tokens; a block serves one stream at a time.  A graph captured over its calls uses
+    its buffers and its workspace: as long as it is replayed, the block must live and get no other number of tokens.
     `fused` (needs a gate): gate, up and the product as one operator, whose values are not rounded before the product.
     `saved8` (needs fused): X and the values before activation and product are kept in 8 bits, H is computed again."""
 
