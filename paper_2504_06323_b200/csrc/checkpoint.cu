@@ -6,7 +6,7 @@ namespace {
 
 // A warp takes 256 columns, a lane eight of them (two lanes a group), kSavedRows rows in flight.  A pass reads two bytes an
 // element and writes 1 1/16, or the other way round.  Bound by memory with issue close behind (85 % storing, 69 % loading):
-// 4096 x 13824 stored and loaded in a row 61 us, 5.6 TB/s, of which 53 are the bytes at the measured peak.
+// 4096 x 13824 stored and loaded in a row 61 to 64 us, 5.4 to 5.6 TB/s, of which 53 are the bytes at the measured peak.
 constexpr int kSavedWarps = 8, kSavedRows = 4;
 
 template <bool VEC>
