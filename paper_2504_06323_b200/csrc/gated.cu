@@ -5,8 +5,8 @@
 //     backward   dZ = dH * U * act'(Z),  dU = dH * act(Z);   dX = dZ Wg + dU Wu
 //                dWg = dZ^T X,  dWu = dU^T X,  db = sums over tokens of dZ and dU
 //
-// Forward: one launch of mm.cuh's kernels over both weight matrices, whose rows alternate within a tile, so that an accumulator
-// of each is in the same warp and neither Z nor U needs to reach memory.  Backward: one elementwise pass makes dZ and dU (and H
+// Forward: one launch of mm.cuh's kernels over both weight matrices, half of a tile's rows of either, so that the accumulators of
+// both are in the same CTA and neither Z nor U needs to reach memory.  Backward: one elementwise pass makes dZ and dU (and H
 // again), dX is one product over both contractions, dWg and dWu are one launch over both outputs.
 #include "checkpoint.cuh"
 #include "mm.cuh"

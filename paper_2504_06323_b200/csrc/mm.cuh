@@ -45,10 +45,10 @@ struct MmArgs {
 
 // What a product is made of:
 //   kPlain  out = A B
-//   kGate   out = act(A B + bias) * (A2 B + bias2) with z and u, the two before the activation.  A tile's rows are 16 of A, the
-//           same 16 of A2, the next 16 of A and so on: n_i counts output elements, of which a tile of the matrix instruction
-//           then has half as many.  A warp's 32 accumulator lanes hold 16 elements of both, so the product needs one
-//           exchange between lanes, and the loads, the instructions and their rate are those of the plain product.
+//   kGate   out = act(A B + bias) * (A2 B + bias2) with z and u, the two before the activation.  A tile's rows are 64 of A and the
+//           same 64 of A2: n_i counts output elements, of which a tile of the matrix instruction then has half as many.
+//           Two warps hold 32 elements of z and of u, exchange half of their columns through shared memory and make half
+//           of the output each; the loads, the instructions and their rate are those of the plain product.
 //   kSum    out = A B + A2 B2: one contraction after the other into the same accumulator
 //   kTwin   out = A B, out2 = A B2 of the same extents in one launch: the tiles' second half
 enum Mode { kPlain = 0, kGate, kSum, kTwin };
@@ -59,12 +59,10 @@ struct GateArgs {
     uint16_t* u;                       // [n_j, n_i] or null
     int64_t ld_u;
     Saved z8, u8;                      // or, in 8 bits, both of them (codes null: not)
-    int swapped;                       // a tile's rows begin with A2's: what lies lower in memory comes first
-    int whole;                         // rows that one box loads of both; 0: box by box
 };
 template <int MODE> struct Second {};
 template <> struct Second<kGate> {
-    CUtensorMap a, both;
+    CUtensorMap a;
     GateArgs g;
 };
 template <> struct Second<kSum> {
@@ -160,12 +158,13 @@ template <int N> __device__ __forceinline__ void epilogue(const MmArgs& a, float
     for (int e = 0; e < N; ++e, p += a.ld_out)
         if (e < n) *p = f32_to_bf16(v[e]);
 }
-// 16 accumulator columns of a warp whose 16 lower and 16 upper lanes each hold a group of channels, v[at + e] in column (token) e < n:
+// 16 accumulator columns of a warp whose lanes hold 32 adjacent channels, two groups, from i0 on, v[at + e] in column (token) e < n:
 // the groups in 8 bits, as store_saved would make them of the bf16 values.  Words of two tokens' magnitudes are maximised
 // over the group's lanes, each lane ending with the two of one word (so it has their exponents to write); four tokens' codes are
 // turned round among four lanes, so that a lane writes four channels of a token.
 template <int N> __device__ __forceinline__ void keep16(const Saved& to, const float (&v)[N], int at, int64_t i0, int64_t n_i, int64_t j, int n) {
     const int lane = (int)threadIdx.x & 31, l = lane & 15;
+    i0 += lane & 16;                   // the lane's group
     const bool there = i0 + l < n_i;   // behind the last channel rows of zeros, whose sums are NaN where X is not finite
     uint32_t h[8], m[8], any = 0;
 #pragma unroll
@@ -190,7 +189,7 @@ template <int N> __device__ __forceinline__ void keep16(const Saved& to, const f
         }
     const uint32_t E2 = saved_exponent(m[0] & 0xFFFFu) | (saved_exponent(m[0] >> 16) << 16);   // of tokens 2 (l & 7) and the next
     const int64_t group = i0 / kSavedGroup;
-    if (l < 8) {
+    if (l < 8 && i0 < n_i) {
         if (2 * l < n) to.exponents[(j + 2 * l) * to.lde + group] = (uint8_t)E2;
         if (2 * l + 1 < n) to.exponents[(j + 2 * l + 1) * to.lde + group] = (uint8_t)(E2 >> 16);
     }
@@ -212,30 +211,32 @@ template <int N> __device__ __forceinline__ void keep16(const Saved& to, const f
         const uint32_t next = __shfl_xor_sync(0xFFFFFFFFu, word, 1);
         word = (lane & 1) ? __byte_perm(word, next, 0x3715) : __byte_perm(word, next, 0x6240);
         const int token = t + (lane & 3);
-        if (token < n) *reinterpret_cast<uint32_t*>(to.codes + (j + token) * to.ldc + i0 + (l & 12)) = word;
+        if (token < n && i0 < n_i) *reinterpret_cast<uint32_t*>(to.codes + (j + token) * to.ldc + i0 + (l & 12)) = word;
     }
 }
 
-// The same for kGate: lanes below 16 hold rows of A (element i0 + lane), the others of A2, or the other way round.  After the exchange a lane has both
-// values of its element for half of the columns.
-template <int N> __device__ __forceinline__ void gate_epilogue(const MmArgs& a, const GateArgs& g, float (&v)[N], float bias, int64_t i0, int64_t j, int n) {
-    const int lane = (int)threadIdx.x & 31, c = lane & 15;
-    const bool up = (lane >= 16) != (g.swapped != 0);
-    const int64_t i = i0 + c;
+// The same for kGate, by two warps: one holds z of 32 elements from i0 on, the other (`up`) u of the same.  Each keeps what it holds,
+// then they exchange halves of the columns through `swap` (kSwap floats of shared memory, theirs alone), and each makes the output
+// of a half.  Both warps call with the same columns; `id` is their barrier.
+constexpr int kSwap = 2 * 32 * 16;   // 16 columns of either warp
+template <int N> __device__ __forceinline__ void gate_epilogue(const MmArgs& a, const GateArgs& g, float (&v)[N], float bias, int64_t i0, int64_t j, int n, bool up,
+                                                               float4* swap, int id) {
+    const int lane = (int)threadIdx.x & 31;
+    const int64_t i = i0 + lane;
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = __fadd_rn(v[e], bias);
-    const bool odd = (lane & 1) != 0, words = a.pairs && i0 + 16 <= a.n_i;
+    const bool odd = (lane & 1) != 0, words = a.pairs && i0 + 32 <= a.n_i;
     uint16_t* kept = up ? g.u : a.z;
     const int64_t ld_kept = up ? g.ld_u : a.ld_z;
-    if (a.z != nullptr || g.u != nullptr) {
+    if (kept != nullptr) {
         if (words) {
             uint16_t* p = kept + (j + (lane & 1)) * ld_kept + (i & ~(int64_t)1);
 #pragma unroll
             for (int e = 0; e < N; e += 2, p += 2 * ld_kept) {
                 const uint32_t w = exchange(pack2(v[e], v[e + 1]), odd);
-                if (e + (lane & 1) < n && kept != nullptr) *reinterpret_cast<uint32_t*>(p) = w;
+                if (e + (lane & 1) < n) *reinterpret_cast<uint32_t*>(p) = w;
             }
-        } else if (kept != nullptr && i < a.n_i) {
+        } else if (i < a.n_i) {
             uint16_t* p = kept + j * ld_kept + i;
 #pragma unroll
             for (int e = 0; e < N; ++e, p += ld_kept)
@@ -243,21 +244,37 @@ template <int N> __device__ __forceinline__ void gate_epilogue(const MmArgs& a, 
         }
     }
     if (g.z8.codes != nullptr && i0 < a.n_i) {
+        __syncwarp();
 #pragma unroll
         for (int at = 0; at < N; at += 16)
             if (at < n) keep16(up ? g.u8 : g.z8, v, at, i0, a.n_i, j + at, n - at);
     }
+    float4 *mine = swap + (up ? kSwap / 8 : 0) + lane, *theirs = swap + (up ? 0 : kSwap / 8) + lane;
+    float x[N / 2];                    // this warp's values of the columns that it goes on with
+#pragma unroll
+    for (int e = 0; e < N / 2; e += 4) {
+        mine[e * 8] = up ? make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]) : make_float4(v[N / 2 + e], v[N / 2 + e + 1], v[N / 2 + e + 2], v[N / 2 + e + 3]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[e + k] = up ? v[N / 2 + e + k] : v[e + k];
+    }
+    __syncwarp();
+    two_warps_meet(id);
     float z[N / 2], u[N / 2];
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) {
-        const float other = __shfl_xor_sync(0xFFFFFFFFu, up ? v[e] : v[e + N / 2], 16);
-        z[e] = up ? other : v[e];
-        u[e] = up ? v[e + N / 2] : other;
+    for (int e = 0; e < N / 2; e += 4) {
+        const float4 f = theirs[e * 8];
+        const float other[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            z[e + k] = up ? other[k] : x[e + k];
+            u[e + k] = up ? x[e + k] : other[k];
+        }
     }
+    two_warps_meet(id);                // read, before the next columns are written there
     activate_all(z, a.act);
 #pragma unroll
     for (int e = 0; e < N / 2; ++e) z[e] = __fmul_rn(z[e], u[e]);
-    const int first = up ? N / 2 : 0;   // this lane's first column
+    const int first = up ? N / 2 : 0;  // this warp's first column
     if (words) {
         uint16_t* p = a.out + (j + first + (lane & 1)) * a.ld_out + (i & ~(int64_t)1);
 #pragma unroll
@@ -272,6 +289,10 @@ template <int N> __device__ __forceinline__ void gate_epilogue(const MmArgs& a, 
             if (first + e < n) *p = f32_to_bf16(z[e]);
     }
 }
+// Of the 128 lanes of tensor memory, a warp's quarter q: its first output element from the tile's, for kGate whether it holds u.
+template <int MODE> __device__ __forceinline__ int quarter_first(int q) { return MODE == kGate ? (q & 1) * 32 : q * 32; }
+template <int MODE> __device__ __forceinline__ bool quarter_up(int q) { return MODE == kGate && q >= 2; }
+__device__ __forceinline__ int quarter_barrier(int set, int q) { return 1 + set * 2 + (q & 1); }
 template <int N> __device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[N]) {
     if constexpr (N == 16) tmem_load16(addr, v);
     else tmem_load32(addr, v);
@@ -290,15 +311,13 @@ template <int MODE> __device__ __forceinline__ decltype(auto) twin_args(const Mm
         return (args);
     }
 }
-// The bias of a lane's accumulator row; i0 is the warp's first element.
-template <int MODE> __device__ __forceinline__ float lane_bias(const MmArgs& a, const Second<MODE>& second, int64_t i0) {
-    const int lane = (int)threadIdx.x & 31;
+// The bias of a lane's accumulator row; i0 is the first element of the warp, quarter q of the lanes.
+template <int MODE> __device__ __forceinline__ float lane_bias(const MmArgs& a, const Second<MODE>& second, int64_t i0, int q) {
     const uint16_t* bias = a.bias;
-    int64_t i = i0 + lane;
     if constexpr (MODE == kGate) {
-        if ((lane >= 16) != (second.g.swapped != 0)) bias = second.g.bias;
-        i = i0 + (lane & 15);
+        if (quarter_up<MODE>(q)) bias = second.g.bias;
     }
+    const int64_t i = i0 + ((int)threadIdx.x & 31);
     return bias != nullptr && i < a.n_i ? bf16_to_f32(bias[i]) : 0.0f;
 }
 // The map of B (and for kSum of A) that a step reads.
@@ -309,12 +328,6 @@ template <int MODE> __device__ __forceinline__ const CUtensorMap* map_a(const CU
 template <int MODE> __device__ __forceinline__ const CUtensorMap* map_b(const CUtensorMap& b_map, const Second<MODE>& second, bool other) {
     if constexpr (MODE == kSum || MODE == kTwin) return other ? &second.b : &b_map;
     return &b_map;
-}
-// Whether a tile's rows of A and A2 are loaded as one box (kGate): eight boxes instead of one a step, and the pair kernel took 403
-// instead of 320 us for 14336 outputs of 2048 tokens.
-template <int MODE> __device__ __forceinline__ bool one_box(const Second<MODE>& second, int64_t i0) {
-    if constexpr (MODE == kGate) return i0 + kMI / 2 <= second.g.whole;
-    return false;
 }
 template <int MODE> __device__ __forceinline__ void prefetch_second(const Second<MODE>& second) {
     if constexpr (MODE == kGate || MODE == kSum) prefetch_map(&second.a);
@@ -332,7 +345,7 @@ __device__ __forceinline__ void store4(uint16_t* p, const float (&y)[4], bool wo
     }
 }
 
-constexpr int kGateRows = 16;   // rows of A, then of A2, in kGate's tiles
+constexpr int kGateRows = kMI / 2;   // rows of A, then of A2, in kGate's tiles
 constexpr uint32_t kGateBox = kGateRows * kMC * 2;
 template <int MODE> constexpr int kTileI = MODE == kGate ? kMI / 2 : kMI;   // output elements of a tile's 128 rows
 constexpr int kMSub = 2;     // 64 contraction steps each a stage: eight instructions a barrier
@@ -348,9 +361,11 @@ __device__ __forceinline__ void tile_out(const MmArgs& a, const Second<MODE>& se
                                          int64_t i0, int64_t j0) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3;
     constexpr int kChunk = BN < 32 ? 16 : 32;   // warps of a quarter take chunks in turn
-    const float bias = lane_bias(a, second, i0 + q * (kTileI<MODE> / 4));
+    const int set = (warp - kMRoles) >> 2;
+    const int64_t iw = i0 + quarter_first<MODE>(q);
+    const float bias = lane_bias(a, second, iw, q);
 #pragma unroll 1
-    for (int c0 = ((warp - kMRoles) >> 2) * kChunk; c0 < n_cols; c0 += SETS * kChunk) {
+    for (int c0 = set * kChunk; c0 < n_cols; c0 += SETS * kChunk) {
         float v[kChunk];
         tmem_load<kChunk>(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c0, v);
         if (split > 1) {
@@ -367,11 +382,22 @@ __device__ __forceinline__ void tile_out(const MmArgs& a, const Second<MODE>& se
                 }
             }
         } else {
-            if constexpr (MODE == kGate) gate_epilogue<kChunk>(a, second.g, v, bias, i0 + q * kGateRows, j0 + c0, n_cols - c0);
-            else epilogue<kChunk>(a, v, bias, i0 + q * 32, j0 + c0, n_cols - c0);
+            if constexpr (MODE == kGate)   // the stages are free, and no partial sums come
+                gate_epilogue<kChunk>(a, second.g, v, bias, iw, j0 + c0, n_cols - c0, quarter_up<MODE>(q),
+                                      reinterpret_cast<float4*>(part) + (set * 2 + (q & 1)) * (kSwap / 4), quarter_barrier(set, q));
+            else epilogue<kChunk>(a, v, bias, iw, j0 + c0, n_cols - c0);
             __syncwarp();
         }
     }
+}
+// Whether a warp's accumulator is there (`done`), and for kGate that of the warp beside it: they meet within the epilogue.
+template <int MODE> __device__ __forceinline__ bool tile_done(bool done) {
+    if constexpr (MODE == kGate) {
+        const int warp = threadIdx.x >> 5;
+        __syncwarp();
+        if (warp >= kMRoles) done = two_warps_agree(quarter_barrier((warp - kMRoles) >> 2, warp & 3), done);
+    }
+    return done;
 }
 
 // A group of 16 channels in 8 bits by four adjacent lanes, four channels each from oi on (all four lanes are there, or none).
@@ -403,11 +429,11 @@ __device__ __forceinline__ void tile_join(const MmArgs& a, const Second<MODE>& s
         cluster_wait();
         const int mine = n_cols - rank * per < per ? n_cols - rank * per : per;
         for (int e = (int)threadIdx.x; e < mine * (kMI / 8); e += THREADS) {
-            const int col = e / (kMI / 8), quad = e % (kMI / 8);   // 16 quads a column: four of each 16 elements
-            const float4* from = reinterpret_cast<const float4*>(part) + col * (kMI / 4) + (quad >> 2) * 8 + (quad & 3);
+            const int col = e / (kMI / 8), quad = e % (kMI / 8);   // 16 quads of either matrix a column
+            const float4* from = reinterpret_cast<const float4*>(part) + col * (kMI / 4) + quad;
             float z[4] = {}, u[4] = {};
             for (int p = 0; p < split; ++p) {   // in the CTAs' order
-                const float4 zp = from[p * per * (kMI / 4) + (second.g.swapped ? 4 : 0)], up = from[p * per * (kMI / 4) + (second.g.swapped ? 0 : 4)];
+                const float4 zp = from[p * per * (kMI / 4)], up = from[p * per * (kMI / 4) + kMI / 8];
                 z[0] = __fadd_rn(z[0], zp.x);
                 z[1] = __fadd_rn(z[1], zp.y);
                 z[2] = __fadd_rn(z[2], zp.z);
@@ -565,7 +591,6 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
 
     if (warp == 0) {
         if (lane == 0) {
-            const bool whole = one_box(second, i0);
             for (int s = s0; s < s1; ++s) {
                 const uint32_t it = (uint32_t)(s - s0), slot = it % (uint32_t)a.stages, ph = (it / (uint32_t)a.stages) & 1u;
                 if (!mbar_wait(&empty[slot], ph ^ 1u, err)) break;
@@ -578,12 +603,8 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
                     unsigned char* sb = sa + kABytes;
                     const int c = ((later ? s - (int)part_steps : s) * kMSub + h) * kMC;
                     if constexpr (MODE == kGate) {
-                        if (whole) tma_load_box4(sa, &second.both, &full[slot], c, (int)i0 / kGateRows);
-#pragma unroll
-                        for (int b = 0; b < kMI / (2 * kGateRows) && !whole; ++b) {
-                            tma_load_box(sa + (size_t)(2 * b) * kGateBox, am, &full[slot], c, (int)i0 + b * kGateRows);
-                            tma_load_box(sa + (size_t)(2 * b + 1) * kGateBox, &second.a, &full[slot], c, (int)i0 + b * kGateRows);
-                        }
+                        tma_load_box(sa, am, &full[slot], c, (int)i0);
+                        tma_load_box(sa + kGateBox, &second.a, &full[slot], c, (int)i0);
                     } else if (A_MN) {
 #pragma unroll
                         for (int b = 0; b < kMI / 64; ++b) tma_load_box(sa + (size_t)b * kMBox, am, &full[slot], (int)i0 + b * 64, c);
@@ -631,7 +652,7 @@ __global__ void __launch_bounds__(mm_threads(BN)) mm_kernel(const __grid_constan
         if (ok && issue) umma_commit(&acc_full);
     }
     __syncwarp();
-    const bool done = warp >= 2 && mbar_wait(&acc_full, 0u, err);
+    const bool done = tile_done<MODE>(warp >= kMRoles && mbar_wait(&acc_full, 0u, err));
     tc_fence_after();
     const int n_cols = (int)(a.n_j - j0 < BN ? (a.n_j > j0 ? a.n_j - j0 : 0) : BN);
     const int per = (n_cols + split - 1) / split;   // columns of the tile that a CTA of the cluster adds up and writes
@@ -682,7 +703,7 @@ constexpr uint32_t kPOperand = kPHalf * kMC * 2, kPStage = kPSub * 2 * kPOperand
 constexpr int kPEpiWarps = 16;   // four per quarter of the lanes
 constexpr int kPThreads = 64 + 32 * kPEpiWarps;
 constexpr int kPBand = 8;
-constexpr size_t kPSmem = (size_t)kPStages * kPStage + 1024;
+template <int MODE> constexpr size_t kPSmem = (size_t)kPStages * kPStage + 1024 + (MODE == kGate ? kPEpiWarps / 2 * kSwap * 4 : 0);
 
 __device__ __forceinline__ void pair_tile(int tile, int tiles_i, int tiles_j, int* ti, int* tj) {
     const int band = tile / (kPBand * tiles_i), in = tile - band * kPBand * tiles_i;
@@ -748,7 +769,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
                 pair_tile(tile, a.tiles_i, all_j, &ti, &tj);
                 const bool twin = MODE == kTwin && tj >= a.tiles_j;
                 const int i0 = ti * (2 * kOwn) + rank * kOwn, j0 = (twin ? tj - a.tiles_j : tj) * kPTile + rank * kPHalf;
-                const bool whole = one_box(second, i0);
                 for (int s = 0; s < steps; ++s, ++it) {
                     const uint32_t slot = it % kPStages, ph = (it / kPStages) & 1u;
                     if (!mbar_wait(&empty[slot], ph ^ 1u, err)) {
@@ -765,12 +785,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
                         unsigned char* sb = sa + kPOperand;
                         const int c = ((later ? s - part_steps : s) * kPSub + h) * kMC;
                         if constexpr (MODE == kGate) {
-                            if (whole) tma_load_box4_pair(sa, &second.both, bar, c, i0 / kGateRows);
-#pragma unroll
-                            for (int b = 0; b < kMI / (2 * kGateRows) && !whole; ++b) {
-                                tma_load_box_pair(sa + (size_t)(2 * b) * kGateBox, am, bar, c, i0 + b * kGateRows);
-                                tma_load_box_pair(sa + (size_t)(2 * b + 1) * kGateBox, &second.a, bar, c, i0 + b * kGateRows);
-                            }
+                            tma_load_box_pair(sa, am, bar, c, i0);
+                            tma_load_box_pair(sa + kGateBox, &second.a, bar, c, i0);
                         } else if (A_MN) {
                             tma_load_box_pair(sa, am, bar, i0, c);
                             tma_load_box_pair(sa + kMBox, am, bar, i0 + 64, c);
@@ -834,16 +850,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
             if (twin) tj -= a.tiles_j;
             const auto& o = twin_args(a, second, twin);
             const uint32_t buf = n & 1u;
-            const int64_t i0 = (int64_t)ti * (2 * kOwn) + rank * kOwn + q * (kOwn / 4), j0 = (int64_t)tj * kPTile;
+            const int64_t i0 = (int64_t)ti * (2 * kOwn) + rank * kOwn + quarter_first<MODE>(q), j0 = (int64_t)tj * kPTile;
             const int n_cols = (int)(a.n_j - j0 < kPTile ? a.n_j - j0 : kPTile);
-            const float bias = lane_bias(a, second, i0);
-            if (!mbar_wait(&acc_full[buf], (n >> 1) & 1u, err)) break;
+            const float bias = lane_bias(a, second, i0, q);
+            if (!tile_done<MODE>(mbar_wait(&acc_full[buf], (n >> 1) & 1u, err))) break;
             tc_fence_after();
 #pragma unroll 1
             for (int c0 = set * 64; c0 < set * 64 + 64 && c0 < n_cols; c0 += 32) {
                 float v[32];
                 tmem_load32(tmem + ((uint32_t)(q * 32) << 16) + buf * 256u + (uint32_t)c0, v);
-                if constexpr (MODE == kGate) gate_epilogue<32>(o, second.g, v, bias, i0, j0 + c0, n_cols - c0);
+                if constexpr (MODE == kGate)
+                    gate_epilogue<32>(o, second.g, v, bias, i0, j0 + c0, n_cols - c0, quarter_up<MODE>(q),
+                                      reinterpret_cast<float4*>(ring + kPStages * kPStage) + (set * 2 + (q & 1)) * (kSwap / 4), quarter_barrier(set, q));
                 else epilogue<32>(o, v, bias, i0, j0 + c0, n_cols - c0);
                 __syncwarp();
             }
@@ -1183,11 +1201,7 @@ struct Also {
 };
 template <bool A_MN, bool B_MN, int MODE> int encode_second(Second<MODE>* second, const Matrix& A, const Also& also, int rows_a, int rows_b) {
     if constexpr (MODE == kGate) {
-        // A is the one at the lower address (run_mm): both as one matrix of four dimensions, if their rows are equally far apart
         second->g = also.gate;
-        const bool one = also.A.ld == A.ld && encode_bf16_twins(&second->both, A.p, also.A.p, A.rows, A.cols, A.ld, kGateRows, kMI / (2 * kGateRows), kMC);
-        if (!one) second->both = CUtensorMap{};
-        second->g.whole = one ? (int)(A.rows / kGateRows * kGateRows) : 0;
         return encode_bf16(&second->a, also.A.p, also.A.rows, also.A.cols, also.A.ld, kGateRows, kMC) ? MOSAIC_OK : MOSAIC_ERR_CUDA;
     } else if constexpr (MODE == kSum) {
         return encode_operands<A_MN, B_MN>(&second->a, &second->b, also.A, also.B, rows_a, rows_b);
@@ -1229,7 +1243,7 @@ template <bool A_MN, bool B_MN, int MODE> int launch_pair(const Matrix& A, const
     a.tiles_j = a.pair_j;
     static DeviceCache opted;
     const int ok = opted.get([&]() -> int {
-        if (cudaFuncSetAttribute(mm_pair_kernel<A_MN, B_MN, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPSmem) != cudaSuccess) {
+        if (cudaFuncSetAttribute(mm_pair_kernel<A_MN, B_MN, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPSmem<MODE>) != cudaSuccess) {
             (void)cudaGetLastError();
             return -1;
         }
@@ -1237,21 +1251,13 @@ template <bool A_MN, bool B_MN, int MODE> int launch_pair(const Matrix& A, const
     });
     if (ok < 0) return MOSAIC_ERR_CUDA;
     const int64_t pairs = sm_count() / 2;
-    Launch l(dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), kPThreads, kPSmem, st);   // the cluster is the kernel's own
+    Launch l(dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), kPThreads, kPSmem<MODE>, st);   // the cluster is the kernel's own
     MOSAIC_CUDA_TRY(cudaLaunchKernelEx(&l.cfg, mm_pair_kernel<A_MN, B_MN, MODE>, a_map, b_map, a, second, (int)tiles));
     return MOSAIC_OK;
 }
 
 // out[j, i] = sum_c A B; A: [n_i, n_c] (or [n_c, n_i] if A_MN), B likewise; the other modes as `also` says.
 template <bool A_MN, bool B_MN, int MODE = kPlain> int run_mm(const Matrix& A, const Matrix& B, MmArgs a, cudaStream_t st, const Also& also = {}) {
-    if constexpr (MODE == kGate) {
-        if (also.gate.swapped == 0 && reinterpret_cast<uintptr_t>(also.A.p) < reinterpret_cast<uintptr_t>(A.p)) {
-            Also turned = also;
-            turned.A = A;
-            turned.gate.swapped = 1;
-            return run_mm<A_MN, B_MN, MODE>(also.A, B, a, st, turned);
-        }
-    }
     const int64_t steps = (MODE == kSum ? 2 : 1) * ((a.n_c + kMC - 1) / kMC), sms = sm_count(), halves = MODE == kTwin ? 2 : 1;
     const auto even = [](const void* p, int64_t ld) { return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & 3u) == 0 && ld % 2 == 0); };
     a.pairs = even(a.out, a.ld_out) && even(a.resid, a.ld_resid) && even(a.z, a.ld_z) && even(also.gate.u, also.gate.ld_u) && even(also.out, also.ld_out) ? 1 : 0;

@@ -99,17 +99,21 @@ __device__ __forceinline__ void tma_load_box_pair(void* dst, const CUtensorMap* 
                  "l"(map), "r"(bar), "r"(col), "r"(row)
                  : "memory");
 }
-// The same two for a box of four dimensions, its rows' place given by the last coordinate.
-__device__ __forceinline__ void tma_load_box4(void* dst, const CUtensorMap* map, uint64_t* bar, int col, int group) {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %5, %5, %4}], [%2];" ::"r"(smem_u32(dst)),
-                 "l"(map), "r"(smem_u32(bar)), "r"(col), "r"(group), "r"(0)
-                 : "memory");
-}
-__device__ __forceinline__ void tma_load_box4_pair(void* dst, const CUtensorMap* map, uint32_t bar, int col, int group) {
-    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %5, %5, %4}], [%2];" ::"r"(
-                     smem_u32(dst)),
-                 "l"(map), "r"(bar), "r"(col), "r"(group), "r"(0)
-                 : "memory");
+// Two warps that work on one thing meet (id 1 to 15), and whether all of their lanes agree.
+__device__ __forceinline__ void two_warps_meet(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool two_warps_agree(int id, bool yes) {
+    uint32_t all;
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %2, 0;\n\t"
+        "bar.red.and.pred q, %1, 64, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t"
+        "}"
+        : "=r"(all)
+        : "r"(id), "r"(yes ? 1u : 0u)
+        : "memory");
+    return all != 0u;
 }
 __device__ __forceinline__ void mbar_arrive_at(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -277,26 +281,8 @@ inline bool encode_bf16(CUtensorMap* map, const void* p, int64_t rows, int64_t c
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Two such matrices of one leading dimension, `other` at a higher address, as one: groups of `group` rows of the one and the
-// same rows of the other, in boxes of box_cols x (group of each) x box_groups.  Whole groups only (rows / group of them); what
-// lies outside is read as zero.  `bytes` of an element, ld and cols in elements.
-inline bool encode_twins(CUtensorMap* map, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, int64_t bytes, const void* p, const void* other, int64_t rows,
-                         int64_t cols, int64_t ld, int group, int box_groups, int box_cols) {
-    EncodeTiledFn encode = encode_tiled();
-    const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(other) - reinterpret_cast<uintptr_t>(p));
-    if (encode == nullptr || rows < group || apart <= 0 || apart % 16 != 0 || apart >= ((int64_t)1 << 40)) return false;
-    const cuuint64_t gdim[4] = {(cuuint64_t)cols, (cuuint64_t)group, 2u, (cuuint64_t)(rows / group)};
-    const cuuint64_t gstride[3] = {(cuuint64_t)(ld * bytes), (cuuint64_t)apart, (cuuint64_t)(ld * bytes * group)};
-    const cuuint32_t box[4] = {(cuuint32_t)box_cols, (cuuint32_t)group, 2u, (cuuint32_t)box_groups};
-    const cuuint32_t estride[4] = {1u, 1u, 1u, 1u};
-    return encode(map, type, 4u, const_cast<void*>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-inline bool encode_bf16_twins(CUtensorMap* map, const void* p, const void* other, int64_t rows, int64_t cols, int64_t ld, int group, int box_groups, int box_cols) {
-    return encode_twins(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, 2, p, other, rows, cols, ld, group, box_groups, box_cols);
-}
 // Row-major bytes [rows, cols], ld a multiple of 16, in boxes of 128 x box_rows with the 128-byte swizzle (16-byte piece c of row
-// r lies at c ^ r % 8); and two such matrices as one.
+// r lies at c ^ r % 8).
 inline bool encode_bytes(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
     EncodeTiledFn encode = encode_tiled();
     if (encode == nullptr) return false;
@@ -306,9 +292,6 @@ inline bool encode_bytes(CUtensorMap* map, const void* p, int64_t rows, int64_t 
     const cuuint32_t estride[2] = {1u, 1u};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2u, const_cast<void*>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-inline bool encode_bytes_twins(CUtensorMap* map, const void* p, const void* other, int64_t rows, int64_t cols, int64_t ld, int group, int box_groups) {
-    return encode_twins(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, 1, p, other, rows, cols, ld, group, box_groups, 128);
 }
 
 }  // namespace mosaic

@@ -335,7 +335,7 @@ constexpr int kC4Cols = 256;
 // Sets of four warps make a stage's weights in turn.
 template <int BN> constexpr int kC4Sets = BN == 128 ? 2 : 3;
 template <int BN> constexpr int kC4Threads = 32 * (kMRoles + 4 * kC4Sets<BN>);   // code loader, MMA issue; weight makers
-constexpr uint32_t kC4Bytes = kMI * kC4Cols / 2, kC4Box = kGateRows * kC4Cols / 2;   // of a stage's codes, of 16 rows of them
+constexpr uint32_t kC4Bytes = kMI * kC4Cols / 2, kC4Box = kGateRows * kC4Cols / 2;   // of a stage's codes, of kGate's rows of one matrix
 // X comes with the codes it meets: in a ring of its own it waited behind the codes of stages to come (17.3 us for 11.4, 16 tokens,
 // 4096 outputs from 8807).
 template <int BN> constexpr int kC4Slots = BN == 16 ? 8 : BN == 32 ? 6 : BN == 64 ? 4 : 2;
@@ -457,7 +457,6 @@ __global__ void __launch_bounds__(kC4Threads<BN>) mm4_kernel(const __grid_consta
 
     if (warp == 0) {
         if (lane == 0) {
-            const bool whole = one_box(second, i0);
             for (int s = 0; s < steps; ++s) {
                 const int slot = s % kSlots;
                 if (!mbar_wait(&empty[slot], ((uint32_t)(s / kSlots) & 1u) ^ 1u, err)) break;
@@ -465,12 +464,8 @@ __global__ void __launch_bounds__(kC4Threads<BN>) mm4_kernel(const __grid_consta
                 unsigned char* codes = ring + slot * kC4Slot<BN>;
                 const int c = (s0 + s) * (kC4Cols / 2);
                 if constexpr (MODE == kGate) {
-                    if (whole) tma_load_box4(codes, &second.both, &full[slot], c, (int)i0 / kGateRows);
-#pragma unroll
-                    for (int b = 0; b < kMI / (2 * kGateRows) && !whole; ++b) {
-                        tma_load_box(codes + (2 * b) * kC4Box, &code_map, &full[slot], c, (int)i0 + b * kGateRows);
-                        tma_load_box(codes + (2 * b + 1) * kC4Box, &second.a, &full[slot], c, (int)i0 + b * kGateRows);
-                    }
+                    tma_load_box(codes, &code_map, &full[slot], c, (int)i0);
+                    tma_load_box(codes + kC4Box, &second.a, &full[slot], c, (int)i0);
                 } else {
                     tma_load_box(codes, &code_map, &full[slot], c, (int)i0);
                 }
@@ -519,8 +514,8 @@ __global__ void __launch_bounds__(kC4Threads<BN>) mm4_kernel(const __grid_consta
         int64_t row = i0 + r;
         bool other = false;
         if constexpr (MODE == kGate) {
-            other = (((r >> 4) & 1) != 0) != (second.g.swapped != 0);
-            row = i0 + (r >> 5) * kGateRows + (r & 15);
+            other = r >= kGateRows;
+            row = i0 + (r & (kGateRows - 1));
         }
         if (row >= a.n_i) row = a.n_i - 1;   // rows past the end: any numbers, not stored
         const uint16_t* at = other ? scales.p2 + row * scales.ld2 : scales.p + row * scales.ld;
@@ -561,7 +556,7 @@ __global__ void __launch_bounds__(kC4Threads<BN>) mm4_kernel(const __grid_consta
         }
     }
     __syncwarp();
-    const bool done = warp >= kMRoles && mbar_wait(&acc_full, 0u, err);
+    const bool done = tile_done<MODE>(warp >= kMRoles && mbar_wait(&acc_full, 0u, err));
     tc_fence_after();
     const int n_cols = (int)(a.n_j - j0 < BN ? a.n_j - j0 : BN);
     const int per = (n_cols + split - 1) / split;
@@ -713,17 +708,8 @@ int launch_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& 
     Scales4 s = {static_cast<const uint16_t*>(W->scales), nullptr, W->lds, 0, group_shift(W->group), 0, groups(W), 0, wide(W), 0};
     if constexpr (MODE == kGate) {
         second.g = g;
-        const bool one = W->ldc == W2->ldc && encode_bytes_twins(&second.both, W->codes, W2->codes, a.n_i, width, W->ldc, kGateRows, kMI / (2 * kGateRows));
-        if (!one) second.both = CUtensorMap{};
-        second.g.whole = one ? (int)(a.n_i / kGateRows * kGateRows) : 0;
         if (!encode_bytes(&second.a, W2->codes, a.n_i, width, W2->ldc, kGateRows)) return MOSAIC_ERR_CUDA;
-        const Scales4 t = {static_cast<const uint16_t*>(W2->scales), nullptr, W2->lds, 0, group_shift(W2->group), 0, groups(W2), 0, wide(W2), 0};
-        if (g.swapped != 0) {   // the scales' first matrix is the gate's, wherever it lies
-            s.p2 = s.p; s.ld2 = s.ld; s.shift2 = s.shift; s.groups2 = s.groups; s.wide2 = s.wide;
-            s.p = t.p; s.ld = t.ld; s.shift = t.shift; s.groups = t.groups; s.wide = t.wide;
-        } else {
-            s.p2 = t.p; s.ld2 = t.ld; s.shift2 = t.shift; s.groups2 = t.groups; s.wide2 = t.wide;
-        }
+        s.p2 = static_cast<const uint16_t*>(W2->scales); s.ld2 = W2->lds; s.shift2 = group_shift(W2->group); s.groups2 = groups(W2); s.wide2 = wide(W2);
     }
     a.tiles_i = (int)((a.n_i + kTileI<MODE> - 1) / kTileI<MODE>);
     a.tiles_j = (int)((a.n_j + BN - 1) / BN);
@@ -733,13 +719,7 @@ int launch_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& 
     return MOSAIC_OK;
 }
 
-template <int MODE> int run_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& x, MmArgs a, GateArgs g, cudaStream_t st) {
-    if (MODE == kGate && reinterpret_cast<uintptr_t>(W2->codes) < reinterpret_cast<uintptr_t>(W->codes)) {   // the lower one first
-        const mosaic_weight4* t = W;
-        W = W2;
-        W2 = t;
-        g.swapped = 1;
-    }
+template <int MODE> int run_mm4(const mosaic_weight4* W, const mosaic_weight4* W2, const Matrix& x, MmArgs a, const GateArgs& g, cudaStream_t st) {
     const auto even = [](const void* p, int64_t ld) { return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & 3u) == 0 && ld % 2 == 0); };
     a.pairs = even(a.out, a.ld_out) && even(a.resid, a.ld_resid) ? 1 : 0;
     a.first_pair = -1;
